@@ -58,7 +58,8 @@
 extern "C" {
 #endif
 
-/* 2: adds prcr_select_topk_cached (1: every other entry point) */
+/* 2: adds prcr_select_topk_cached (1: the entry points before it). Entry points added
+ * since change nothing of these and are found by their names. */
 #define PRCR_VERSION 2
 
 #if defined(__GNUC__)
@@ -84,8 +85,10 @@ extern "C" {
                                   or a position or query position has magnitude 2^31
                                   or more (beyond the exact fixed-point angle
                                   reduction): the rebind skips that token's rows;
-                                  decode and cached selection treat that sequence as
-                                  having no readable slot                             */
+                                  decode, cached selection and accumulated weights
+                                  treat that sequence as having no readable slot      */
+#define PRCR_ST_TIMEOUT   32u  /* chunk attention: a wait inside a kernel ran out (two
+                                  seconds); the outputs of the call are not valid     */
 
 /* Position rules (Sec. 3.2; Table 2) */
 #define PRCR_MODE_PCR      0  /* Position-Consistent Reinsertion (the method)        */
@@ -391,6 +394,122 @@ PRCR_API int prcr_select_topk_cached(const prcr_rope_cfg* cfg, const prcr_cache_
                                      int32_t* seq_rev_off, int32_t* rev_tok_off, float* score_out,
                                      uint32_t* status, void* workspace, size_t workspace_bytes,
                                      void* stream);
+
+/* Longest max_len of the four entry points below. */
+#define PRCR_CACHE_MAX_LEN (1 << 30)
+
+/* prcr_append_kv - the K/V rows of new tokens that have no raw store (text
+ * tokens of a prompt or a decode step) into the decoder cache, a packed batch of
+ * sequences at once: token i of sequence b, tok_off[b] + i of the call, goes to
+ * slot cache_len_in[b] + i with its key rotated at (t, h, w) = coords[tok_off[b] + i]
+ * as prcr_prefill_capture rotates (Eq. "historical_position_bound_kv") and its
+ * value bit for bit, at layers layer_begin .. layer_begin+n_layers-1.
+ *   source key of (layer i, token j, head h, dim d):
+ *     k_src[i*src_layer_stride + j*src_token_stride + h*D + d]   (device, bf16)
+ *   coords      device int32 [total][3]
+ *   tok_off     device int32 [n_seqs+1]: [0] = 0, not decreasing, [n_seqs] <= total
+ *               (rows behind it are padding); otherwise PRCR_ST_CSR, and nothing
+ *               is appended
+ *   cache_len_out device int32 [n_seqs]: cache_len_in + the sequence's tokens (must
+ *               not alias cache_len_in)
+ * A slot beyond the capacity or in an unmapped block sets PRCR_ST_CAPACITY /
+ * PRCR_ST_NO_BLOCK and its rows are skipped. Source and cache must not overlap. */
+PRCR_API int prcr_append_kv(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, int32_t n_seqs,
+                            int32_t layer_begin, int32_t n_layers, const void* k_src,
+                            const void* v_src, int64_t src_layer_stride, int64_t src_token_stride,
+                            const int32_t* coords, const int32_t* tok_off, int32_t total,
+                            const int32_t* cache_len_in, int32_t* cache_len_out, uint32_t* status,
+                            void* stream);
+
+/* prcr_chunk_attention - attention of a packed batch's new tokens over the active
+ * cache at one layer (Eq. "decode_with_active_cache" for several tokens): a whole
+ * prompt, the next piece of one, drafted tokens, or a single token per sequence.
+ * The rows of the new tokens are in the cache already (prcr_append_kv,
+ * prcr_prefill_capture): sequence b holds seq_len[b] slots, the last n_b =
+ * q_off[b+1] - q_off[b] of them its new tokens', and query i of them sees slots
+ * [0, seq_len[b] - n_b + i] (causal):
+ *   out[t][h] = softmax(RoPE(q[t][h], coords[t]) K^T / sqrt(D)) V,  t = q_off[b] + i.
+ * Query head h reads KV head h / (n_q_heads / n_kv_heads).
+ *   q        device bf16: query of (t, h) at q[t*q_token_stride + h*D], raw (pre-rotation)
+ *   coords   device int32 [total_q][3] (t, h, w); (p, p, p) for a text token
+ *   q_off    device int32 [n_seqs+1]: [0] = 0, not decreasing, [n_seqs] <= total_q;
+ *            otherwise PRCR_ST_CSR and nothing is written
+ *   seq_len  device int32 [n_seqs]; max_len >= every seq_len is a host bound
+ *   out      device bf16: out[t*out_token_stride + h*D]; rows behind q_off[n_seqs]
+ *            are left as they were. out may not overlap q
+ * q and out are 16-byte aligned, their strides multiples of 8. Limits: D in {64,
+ * 128, 256}, at most 8 query heads per KV head, n_q_heads * D <= PRCR_DECODE_MAX_Q_ELEMS.
+ * The rotated query and the probabilities are rounded to bf16 for the tensor
+ * cores; sums, maxima and the output's accumulator are float32.
+ * workspace: device, >= prcr_chunk_workspace_size(...) bytes (0 where the call
+ * needs none), 16-byte aligned, not shared with a concurrent call.
+ * A seq_len that is negative, beyond the capacity or above max_len sets
+ * PRCR_ST_CAPACITY (slots past either are left out); an unmapped block in
+ * range sets PRCR_ST_NO_BLOCK and its slots are left out. A query that sees no
+ * slot gets zeros. Slots that a query does not see have no influence on its
+ * output, whatever they hold (infinities and NaN included).                   */
+PRCR_API size_t prcr_chunk_workspace_size(const prcr_rope_cfg* cfg, int32_t n_seqs,
+                                          int32_t n_q_heads, int32_t total_q, int64_t max_len);
+PRCR_API int prcr_chunk_attention(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache,
+                                  int32_t n_seqs, int32_t layer, int32_t n_q_heads, const void* q,
+                                  int64_t q_token_stride, const int32_t* coords,
+                                  const int32_t* q_off, int32_t total_q, const int32_t* seq_len,
+                                  int64_t max_len, void* out, int64_t out_token_stride,
+                                  uint32_t* status, void* workspace, size_t workspace_bytes,
+                                  void* stream);
+
+/* prcr_accumulate_weights - how much attention one decode step gives to each slot,
+ * added to the slots' scores: for every sequence b, layer l and KV head h
+ *   score[b][l][h][s] = decay * score[b][l][h][s]
+ *       + sum over the query heads g of KV head h of
+ *         softmax_s(RoPE(q[b][l][g], (p, p, p)) K^T / sqrt(D)),   s < seq_len[b],
+ * p = q_pos[b]. q, q_pos, seq_len and max_len are those of prcr_decode_attention
+ * (q 16-byte aligned). decay 1 adds up every step's weights, below 1 forgets older
+ * steps, 0 keeps this step's alone and does not read the scores.
+ *   score    device float32, row of (b, l, h) at score[((b*n_layers + l)*n_kv_heads + h)
+ *            * score_stride], score_stride >= max_len; entries from seq_len[b] on
+ *            are left as they were
+ * Limits, a seq_len beyond the capacity or max_len, a q_pos of magnitude 2^31 or
+ * more, and unmapped blocks are prcr_decode_attention's (such slots get weight 0).
+ * workspace: device, >= prcr_weights_workspace_size(...) bytes, 16-byte aligned,
+ * not shared with a concurrent call.                                          */
+PRCR_API size_t prcr_weights_workspace_size(const prcr_rope_cfg* cfg, int32_t n_seqs,
+                                            int32_t n_q_heads, int64_t max_len);
+PRCR_API int prcr_accumulate_weights(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache,
+                                     int32_t n_seqs, int32_t n_q_heads, const void* q,
+                                     const int64_t* q_pos, const int32_t* seq_len, int64_t max_len,
+                                     float* score, int64_t score_stride, float decay,
+                                     uint32_t* status, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+
+/* prcr_evict - cut every sequence's cache to `budget` slots by the slots' scores
+ * (e.g. prcr_accumulate_weights'). A sequence with seq_len[b] > budget keeps, for
+ * every layer and KV head by itself, its first n_sink and its last n_recent slots
+ * and of those between the budget - n_sink - n_recent of the highest score (equal
+ * scores: lower slot first; NaN lowest). The kept K/V rows move, in ascending
+ * order of their slots, to slots 0 .. budget-1; the scores move with them. A
+ * sequence of at most budget slots keeps them all. Keys stay as they were rotated,
+ * so positions and the next text position do not change.
+ *   dst         NULL: in place. Otherwise the cache that the kept rows are written to
+ *               (other blocks of the same pool under their own table, or other
+ *               memory); the rows read must not be among those written
+ *   seq_len     device int32 [n_seqs]; max_len >= every seq_len is a host bound
+ *   score       device float32 as for prcr_accumulate_weights (score_stride >= max_len)
+ *   score_out   device, same layout; may be score itself. Entries from the new
+ *               length to score_stride become 0
+ *   keep_out    device int32 [n_seqs][n_layers][n_kv_heads][budget]: the slots kept,
+ *               ascending; -1 behind the new length
+ *   seq_len_out device int32 [n_seqs]: min(seq_len, budget) (must not alias seq_len)
+ * Any head_dim. A block must not be mapped twice. A seq_len that is negative,
+ * beyond the capacity or max_len, a new length beyond dst's capacity, or an unmapped
+ * block in either sets PRCR_ST_CAPACITY / PRCR_ST_NO_BLOCK, and that sequence is left as it was: its
+ * keep_out is -1, seq_len_out is seq_len in place and 0 otherwise, rows and
+ * scores are not written.                                                     */
+PRCR_API int prcr_evict(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache,
+                        const prcr_cache_desc* dst, int32_t n_seqs, const int32_t* seq_len,
+                        int64_t max_len, int32_t budget, int32_t n_sink, int32_t n_recent,
+                        const float* score, float* score_out, int64_t score_stride,
+                        int32_t* keep_out, int32_t* seq_len_out, uint32_t* status, void* stream);
 
 /* prcr_next_text_pos - host helper: the position the next text token takes
  * after a revisit appended k_seq tokens to a sequence whose latest text token

@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(_PKG, "libprcr.so")
 
 # return codes / status bits / modes / flags / layouts / cache kinds (mirror include/prcr.h)
 OK, EINVAL, EALIGN, EWORKSPACE, ECUDA = 0, -1, -2, -3, -4
-ST_IDX_RANGE, ST_NO_BLOCK, ST_CAPACITY, ST_CSR, ST_POS_RANGE = 1, 2, 4, 8, 16
+ST_IDX_RANGE, ST_NO_BLOCK, ST_CAPACITY, ST_CSR, ST_POS_RANGE, ST_TIMEOUT = 1, 2, 4, 8, 16, 32
 MODE_PCR, MODE_ORIGINAL, MODE_UIR, MODE_LPA = 0, 1, 2, 3
 FLAG_DEGENERATE_CENTER = 1
 LAYOUT_SECTIONED, LAYOUT_INTERLEAVED = 0, 1
@@ -28,7 +28,9 @@ EXPORTS = ("prcr_workspace_size", "prcr_rebind_inject", "prcr_plan", "prcr_rebin
            "prcr_store_raw", "prcr_next_text_pos", "prcr_error_string", "prcr_version",
            "prcr_rebind_inject_static", "prcr_prefill_capture", "prcr_decode_workspace_size",
            "prcr_decode_attention", "prcr_select_workspace_size", "prcr_select_topk",
-           "prcr_select_topk_cached")
+           "prcr_select_topk_cached", "prcr_append_kv", "prcr_chunk_workspace_size",
+           "prcr_chunk_attention", "prcr_weights_workspace_size", "prcr_accumulate_weights",
+           "prcr_evict")
 STATIC_MAX_TOKENS = 65536
 
 
@@ -113,6 +115,29 @@ def lib():
                                           C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                           C.c_size_t, C.c_void_p]
     L.prcr_select_topk_cached.restype = C.c_int
+    L.prcr_append_kv.argtypes = [P(RopeCfg), P(CacheDesc), C.c_int32, C.c_int32, C.c_int32,
+                                 C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p,
+                                 C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                 C.c_void_p]
+    L.prcr_append_kv.restype = C.c_int
+    L.prcr_chunk_workspace_size.argtypes = [P(RopeCfg), C.c_int32, C.c_int32, C.c_int32, C.c_int64]
+    L.prcr_chunk_workspace_size.restype = C.c_size_t
+    L.prcr_chunk_attention.argtypes = [P(RopeCfg), P(CacheDesc), C.c_int32, C.c_int32, C.c_int32,
+                                       C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32,
+                                       C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                       C.c_void_p, C.c_size_t, C.c_void_p]
+    L.prcr_chunk_attention.restype = C.c_int
+    L.prcr_weights_workspace_size.argtypes = [P(RopeCfg), C.c_int32, C.c_int32, C.c_int64]
+    L.prcr_weights_workspace_size.restype = C.c_size_t
+    L.prcr_accumulate_weights.argtypes = [P(RopeCfg), P(CacheDesc), C.c_int32, C.c_int32,
+                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
+                                          C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_void_p,
+                                          C.c_size_t, C.c_void_p]
+    L.prcr_accumulate_weights.restype = C.c_int
+    L.prcr_evict.argtypes = [P(RopeCfg), P(CacheDesc), P(CacheDesc), C.c_int32, C.c_void_p,
+                             C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                             C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+    L.prcr_evict.restype = C.c_int
     L.prcr_next_text_pos.argtypes = [C.c_int64, C.c_int64, C.c_int32]
     L.prcr_next_text_pos.restype = C.c_int64
     L.prcr_error_string.argtypes = [C.c_int]
@@ -397,6 +422,136 @@ def select_topk_cached(cfg, cache, layer: int, q: torch.Tensor, q_pos: torch.Ten
                                        _ptr(score_out), status.data_ptr(), workspace.data_ptr(),
                                        workspace.numel() * workspace.element_size(), _stream(stream))
     return _check(rc, "prcr_select_topk_cached")
+
+
+def _small(name: str, t: torch.Tensor, dtype, numel: int):
+    """A contiguous index or length tensor of at least `numel` entries."""
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < numel:
+        raise TypeError(f"{name} must be a contiguous {dtype} tensor of at least {numel} entries")
+
+
+def _same_device(first: torch.Tensor, *others):
+    """The library works on the current device: tensors of another one are refused."""
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("all tensors must be on one device")
+    if first.device.type != "cuda":
+        raise ValueError("tensors must be on a CUDA device")
+    if first.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {first.device}, which is not the current CUDA device")
+
+
+def append_kv(cfg, cache, layer_begin: int, k_src: torch.Tensor, v_src: torch.Tensor,
+              coords: torch.Tensor, tok_off: torch.Tensor, cache_len_in: torch.Tensor,
+              cache_len_out: torch.Tensor, status: torch.Tensor, stream=None):
+    """prcr_append_kv: k_src / v_src are the new tokens' pre-rotation rows [n_layers, total, H, D]
+    bf16 (row-contiguous), coords int32 [total, 3], tok_off int32 [B + 1], cache_len_in /
+    cache_len_out int32 [B]."""
+    _bf16(k_src, "k_src"); _bf16(v_src, "v_src")
+    stride, shape = k_src.stride(), k_src.shape
+    if stride != v_src.stride() or shape != v_src.shape or len(shape) != 4:
+        raise ValueError("k_src and v_src must be [n_layers, total, H, D] with the same strides")
+    if shape[2] != cfg.n_kv_heads or shape[3] != cfg.head_dim:
+        raise ValueError("k_src rows must be [n_kv_heads, head_dim]")
+    n_seqs, total = cache_len_in.numel(), shape[1]
+    _small("coords", coords, torch.int32, 3 * total)
+    _small("tok_off", tok_off, torch.int32, n_seqs + 1)
+    _small("cache_len_in", cache_len_in, torch.int32, 0)
+    _small("cache_len_out", cache_len_out, torch.int32, n_seqs)
+    _same_device(cache._keep[0], k_src, v_src, coords, tok_off, cache_len_in, cache_len_out, status)
+    rc = lib().prcr_append_kv(C.byref(cfg), C.byref(cache), n_seqs, int(layer_begin), shape[0],
+                              k_src.data_ptr(), v_src.data_ptr(), stride[0], stride[1],
+                              coords.data_ptr(), tok_off.data_ptr(), total,
+                              cache_len_in.data_ptr(), cache_len_out.data_ptr(), status.data_ptr(),
+                              _stream(stream))
+    return _check(rc, "prcr_append_kv")
+
+
+def chunk_workspace_size(cfg, n_seqs: int, n_q_heads: int, total_q: int, max_len: int) -> int:
+    return int(lib().prcr_chunk_workspace_size(C.byref(cfg), int(n_seqs), int(n_q_heads),
+                                               int(total_q), int(max_len)))
+
+
+def chunk_attention(cfg, cache, layer: int, q: torch.Tensor, coords: torch.Tensor,
+                    q_off: torch.Tensor, seq_len: torch.Tensor, max_len: int, out: torch.Tensor,
+                    status: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None):
+    """prcr_chunk_attention: q and out [total_q, Hq, D] bf16 (a token's [Hq, D] contiguous, any
+    token stride), coords int32 [total_q, 3], q_off int32 [B + 1], seq_len int32 [B]."""
+    _bf16(q, "q"); _bf16(out, "out")
+    if q.shape != out.shape or q.dim() != 3 or q.shape[2] != cfg.head_dim:
+        raise ValueError("q and out must be [total_q, Hq, head_dim]")
+    n_seqs, total = seq_len.numel(), q.shape[0]
+    _small("coords", coords, torch.int32, 3 * total)
+    _small("q_off", q_off, torch.int32, n_seqs + 1)
+    _small("seq_len", seq_len, torch.int32, 0)
+    _same_device(cache._keep[0], q, coords, q_off, seq_len, out, status, workspace)
+    ws = None if workspace is None else workspace.data_ptr()
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = lib().prcr_chunk_attention(C.byref(cfg), C.byref(cache), n_seqs, int(layer), q.shape[1],
+                                    q.data_ptr(), q.stride(0), coords.data_ptr(), q_off.data_ptr(),
+                                    total, seq_len.data_ptr(), int(max_len), out.data_ptr(),
+                                    out.stride(0), status.data_ptr(), ws, nbytes, _stream(stream))
+    return _check(rc, "prcr_chunk_attention")
+
+
+def weights_workspace_size(cfg, n_seqs: int, n_q_heads: int, max_len: int) -> int:
+    return int(lib().prcr_weights_workspace_size(C.byref(cfg), int(n_seqs), int(n_q_heads),
+                                                 int(max_len)))
+
+
+def _score_rows(cfg, n_seqs: int, name: str, t: torch.Tensor):
+    if (t.dtype != torch.float32 or not t.is_contiguous() or t.dim() != 4
+            or t.shape[0] < n_seqs or t.shape[1:3] != (cfg.n_layers, cfg.n_kv_heads)):
+        raise TypeError(f"{name} must be a contiguous float32 [B, n_layers, n_kv_heads, S] tensor")
+
+
+def accumulate_weights(cfg, cache, q: torch.Tensor, q_pos: torch.Tensor, seq_len: torch.Tensor,
+                       max_len: int, score: torch.Tensor, status: torch.Tensor, decay: float = 1.0,
+                       workspace: Optional[torch.Tensor] = None, stream=None):
+    """prcr_accumulate_weights: q [B, n_layers, Hq, D] bf16 (contiguous), q_pos int64 [B], seq_len
+    int32 [B], score float32 [B, n_layers, n_kv_heads, S] with S >= max_len."""
+    if q.dtype != torch.bfloat16 or not q.is_contiguous() or q.dim() != 4:
+        raise TypeError("q must be a contiguous bfloat16 [B, n_layers, Hq, D] tensor")
+    if q.shape[1] != cfg.n_layers or q.shape[3] != cfg.head_dim:
+        raise ValueError("q must be [B, n_layers, Hq, head_dim]")
+    n_seqs = q.shape[0]
+    _small("q_pos", q_pos, torch.int64, n_seqs)
+    _small("seq_len", seq_len, torch.int32, n_seqs)
+    _score_rows(cfg, n_seqs, "score", score)
+    _same_device(cache._keep[0], q, q_pos, seq_len, score, status, workspace)
+    ws = None if workspace is None else workspace.data_ptr()
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = lib().prcr_accumulate_weights(C.byref(cfg), C.byref(cache), n_seqs, q.shape[2],
+                                       q.data_ptr(), q_pos.data_ptr(), seq_len.data_ptr(),
+                                       int(max_len), score.data_ptr(), score.shape[3],
+                                       float(decay), status.data_ptr(), ws, nbytes, _stream(stream))
+    return _check(rc, "prcr_accumulate_weights")
+
+
+def evict(cfg, cache, seq_len: torch.Tensor, max_len: int, budget: int, n_sink: int, n_recent: int,
+          score: torch.Tensor, keep_out: torch.Tensor, seq_len_out: torch.Tensor,
+          status: torch.Tensor, dst: Optional[CacheDesc] = None,
+          score_out: Optional[torch.Tensor] = None, stream=None):
+    """prcr_evict: in place, or into the cache `dst`; seq_len / seq_len_out int32 [B], score and
+    score_out (default: score itself) float32 [B, n_layers, n_kv_heads, S], keep_out int32
+    [B, n_layers, n_kv_heads, budget]."""
+    n_seqs = seq_len.numel()
+    score_out = score if score_out is None else score_out
+    _small("seq_len", seq_len, torch.int32, 0)
+    _small("seq_len_out", seq_len_out, torch.int32, n_seqs)
+    _score_rows(cfg, n_seqs, "score", score)
+    _score_rows(cfg, n_seqs, "score_out", score_out)
+    if score.shape[3] != score_out.shape[3]:
+        raise ValueError("score and score_out must have rows of the same length")
+    _small("keep_out", keep_out, torch.int32, n_seqs * cfg.n_layers * cfg.n_kv_heads * int(budget))
+    _same_device(cache._keep[0], seq_len, seq_len_out, score, score_out, keep_out, status,
+                 None if dst is None else dst._keep[0])
+    rc = lib().prcr_evict(C.byref(cfg), C.byref(cache), None if dst is None else C.byref(dst),
+                          n_seqs, seq_len.data_ptr(), int(max_len), int(budget), int(n_sink),
+                          int(n_recent), score.data_ptr(), score_out.data_ptr(), score.shape[3],
+                          keep_out.data_ptr(), seq_len_out.data_ptr(), status.data_ptr(),
+                          _stream(stream))
+    return _check(rc, "prcr_evict")
 
 
 def next_text_pos(p_txt: int, k_seq: int, mode: int = MODE_PCR) -> int:

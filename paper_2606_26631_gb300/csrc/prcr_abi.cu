@@ -12,7 +12,6 @@
 #include "prcr_internal.h"
 
 namespace prcr {
-namespace {
 
 // Turn rates of a (theta, head_dim) pair, computed once (long double pow is
 // slow where long double is a software type) and kept for the process.
@@ -32,11 +31,6 @@ void copy_turn_freq(const prcr_rope_cfg* cfg, uint64_t* out) {
     std::memcpy(out, it->second.data(), sizeof(uint64_t) * size_t(cfg->head_dim / 2));
 }
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-inline bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
-inline bool mult8(int64_t s) { return s >= 0 && (s & 7) == 0; }
-
 int check_cfg(const prcr_rope_cfg* c) {
     if (!c) return PRCR_EINVAL;
     const int D = c->head_dim;
@@ -53,6 +47,8 @@ int check_cfg(const prcr_rope_cfg* c) {
     return PRCR_OK;
 }
 
+namespace {
+
 int check_store(const prcr_rope_cfg* c, const prcr_store_desc* s) {
     if (!s || !s->k || !s->v || !s->coords) return PRCR_EINVAL;
     const int64_t row = int64_t(c->n_kv_heads) * c->head_dim;
@@ -64,6 +60,8 @@ int check_store(const prcr_rope_cfg* c, const prcr_store_desc* s) {
         return PRCR_EALIGN;
     return PRCR_OK;
 }
+
+}  // namespace
 
 int check_cache(const prcr_rope_cfg* c, const prcr_cache_desc* k) {
     if (!k || !k->k || !k->v) return PRCR_EINVAL;
@@ -85,8 +83,6 @@ int check_cache(const prcr_rope_cfg* c, const prcr_cache_desc* k) {
     }
     return PRCR_OK;
 }
-
-}  // namespace
 
 cudaError_t raise_smem_limit(const void* kernel, size_t smem) {
     static std::mutex mu;
@@ -183,10 +179,10 @@ PlanArgs make_plan_args(const prcr_store_desc* store, const prcr_cache_desc* cac
     return a;
 }
 
-enum KernelId { kRebind = 0, kCapture = 1, kFused = 2 };
+}  // namespace
 
 // Resident CTAs per SM of a kernel per (device, kernel, block, smem), cached.
-int blocks_per_sm(int dev, int block, size_t smem, int kernel = kRebind) {
+int blocks_per_sm(int dev, int block, size_t smem, int kernel) {
     static std::mutex mu;
     static std::map<std::tuple<int, int, int, size_t>, int> cache;
     const auto key = std::make_tuple(dev, kernel, block, smem);
@@ -198,6 +194,7 @@ int blocks_per_sm(int dev, int block, size_t smem, int kernel = kRebind) {
     int n = 0;
     const cudaError_t e = kernel == kRebind    ? rebind_blocks_per_sm(block, smem, &n)
                           : kernel == kCapture ? capture_blocks_per_sm(block, smem, &n)
+                          : kernel == kAppend  ? append_blocks_per_sm(block, smem, &n)
                                                : fused_blocks_per_sm(block, smem, &n);
     if (e != cudaSuccess || n < 1) n = 1;
     std::lock_guard<std::mutex> g(mu);
@@ -220,6 +217,8 @@ int sm_count(int dev) {
     cache[dev] = n;
     return n;
 }
+
+namespace {
 
 // Layers each CTA of the fused kernel walks. Every CTA of a grid does the same work, so
 // the grid runs in ceil(waves) rounds of `slots` resident CTAs: pick the
@@ -257,6 +256,8 @@ int layers_per_cta(int64_t tiles, int n_layers, int64_t slots) {
 // 33, of 11 22 us, with eight of 128 x 22 x 1344 of 4 42.6, of 11 43.5. Capture (few 6
 // / heads, two at least; a wave is all resident CTAs): one head of 128 x 18 layers x
 // 3410 tokens 90 us at 2, 71 at 6; eight x 36 x 768 x 3 images 158 at 2, 161 at 4.
+}  // namespace
+
 int stream_layers_per_cta(int64_t tiles, int n_layers, int64_t wave, int few) {
     if (n_layers > 65535) return layers_per_cta(tiles, n_layers, wave);  // grid y
     auto even = [&](int g) {
@@ -267,6 +268,8 @@ int stream_layers_per_cta(int64_t tiles, int n_layers, int64_t wave, int few) {
         if (tiles * ((n_layers + g - 1) / g) <= wave) return even(g);
     return even(few);
 }
+
+namespace {
 
 // Arguments and launch shape of the row-moving kernel (rebind or fused).
 // after_plan: this call's own plan kernel precedes it, which releases it only

@@ -1,0 +1,246 @@
+// extern "C" entry points that append to the decoder cache, attend over it with
+// chunks of new tokens, add up its slots' attention weights and evict from it:
+// argument checks and launch planning.
+#include <algorithm>
+#include <cmath>
+
+#include "prcr_internal.h"
+
+namespace prcr {
+namespace {
+
+int64_t cache_capacity(const prcr_cache_desc* c) {
+    return c->kind == PRCR_CACHE_CONTIGUOUS ? int64_t(c->max_slots) : int64_t(c->bt_stride) * c->block_size;
+}
+
+CacheView cache_view(const prcr_cache_desc* c, int layer) {
+    CacheView v = {};
+    v.k = static_cast<uint16_t*>(c->k) + int64_t(layer) * c->layer_stride;
+    v.v = static_cast<uint16_t*>(c->v) + int64_t(layer) * c->layer_stride;
+    v.seq_stride = c->seq_stride;
+    v.layer_stride = c->layer_stride;
+    v.block_stride = c->block_stride;
+    v.slot_stride = c->slot_stride;
+    v.capacity = cache_capacity(c);
+    v.block_table = c->block_table;
+    v.bt_stride = c->bt_stride;
+    v.block_size = c->kind == PRCR_CACHE_PAGED ? c->block_size : 1;
+    v.n_blocks = c->n_blocks;
+    v.kind = c->kind;
+    return v;
+}
+
+// query heads that the attention kernels take
+bool heads_ok(const prcr_rope_cfg* cfg, int32_t n_q_heads) {
+    const int D = cfg->head_dim;
+    return (D == 64 || D == 128 || D == 256) && n_q_heads >= cfg->n_kv_heads &&
+           n_q_heads % cfg->n_kv_heads == 0 && n_q_heads / cfg->n_kv_heads <= 8 &&
+           int64_t(n_q_heads) * D <= PRCR_DECODE_MAX_Q_ELEMS;
+}
+
+size_t weights_bytes(const prcr_rope_cfg* cfg, int64_t n_seqs, int64_t n_q_heads, int64_t max_len) {
+    return size_t(n_seqs) * cfg->n_layers * n_q_heads * max_len * sizeof(float);
+}
+
+int status_of(cudaError_t e) { return e == cudaSuccess ? PRCR_OK : PRCR_ECUDA; }
+
+}  // namespace
+}  // namespace prcr
+
+using namespace prcr;
+
+extern "C" {
+
+int prcr_append_kv(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, int32_t n_seqs, int32_t layer_begin,
+                   int32_t n_layers, const void* k_src, const void* v_src, int64_t src_layer_stride,
+                   int64_t src_token_stride, const int32_t* coords, const int32_t* tok_off, int32_t total,
+                   const int32_t* cache_len_in, int32_t* cache_len_out, uint32_t* status, void* stream) {
+    int rc = check_cfg(cfg);
+    if (rc) return rc;
+    if ((rc = check_cache(cfg, cache))) return rc;
+    if (n_seqs < 0 || n_seqs > cache->n_seqs || layer_begin < 0 || n_layers < 1 ||
+        layer_begin + int64_t(n_layers) > cfg->n_layers || total < 0)
+        return PRCR_EINVAL;
+    if (n_seqs == 0) return PRCR_OK;
+    const int64_t row = int64_t(cfg->n_kv_heads) * cfg->head_dim;
+    if (!tok_off || !cache_len_in || !cache_len_out || !status || cache_len_in == cache_len_out) return PRCR_EINVAL;
+    if (total > 0 && (!k_src || !v_src || !coords || src_token_stride < row || src_layer_stride < 0))
+        return PRCR_EINVAL;
+    if (!aligned4(tok_off) || !aligned4(cache_len_in) || !aligned4(cache_len_out) || !aligned4(status))
+        return PRCR_EALIGN;
+    if (total > 0 && (!aligned16(k_src) || !aligned16(v_src) || !mult8(src_layer_stride) ||
+                      !mult8(src_token_stride) || !aligned4(coords)))
+        return PRCR_EALIGN;
+    AppendArgs a = {};
+    a.cache = cache_view(cache, layer_begin);
+    a.src_k = static_cast<const uint16_t*>(k_src);
+    a.src_v = static_cast<const uint16_t*>(v_src);
+    a.src_layer_stride = src_layer_stride;
+    a.src_token_stride = src_token_stride;
+    a.coords = coords;
+    a.tok_off = tok_off;
+    a.len_in = cache_len_in;
+    a.len_out = cache_len_out;
+    a.status = status;
+    a.n_seqs = n_seqs;
+    a.total = total;
+    a.n_layers = n_layers;
+    a.head_dim = cfg->head_dim;
+    a.layout = cfg->layout;
+    a.sec_t = cfg->sections[0];
+    a.sec_h = cfg->sections[1];
+    a.sec_w = cfg->sections[2];
+    copy_turn_freq(cfg, a.turn_freq);
+    const int lanes = cfg->n_kv_heads * (cfg->head_dim / 16);
+    const int T = std::max(1, kRebindTargetThreads / lanes);
+    const int block = T * lanes;
+    const size_t smem = size_t(T) * (cfg->head_dim * sizeof(float) + sizeof(int64_t));
+    a.lanes = lanes;
+    a.tok_per_cta = T;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return PRCR_ECUDA;
+    const int64_t tiles = std::max<int64_t>(1, (int64_t(total) + T - 1) / T);
+    const int64_t slots = int64_t(sm_count(dev)) * blocks_per_sm(dev, block, smem, kAppend);
+    const int G = stream_layers_per_cta(tiles, n_layers, slots, std::max(2, 6 / cfg->n_kv_heads));
+    a.layers_per_cta = G;
+    const dim3 grid(unsigned(tiles), unsigned((n_layers + G - 1) / G), 1);
+    return status_of(launch_append(a, grid, block, smem, static_cast<cudaStream_t>(stream)));
+}
+
+size_t prcr_chunk_workspace_size(const prcr_rope_cfg* cfg, int32_t n_seqs, int32_t n_q_heads, int32_t total_q,
+                                 int64_t max_len) {
+    if (check_cfg(cfg) || n_seqs < 1 || total_q < 1 || max_len < 1 || !heads_ok(cfg, n_q_heads)) return 0;
+    return 0;
+}
+
+int prcr_chunk_attention(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, int32_t n_seqs, int32_t layer,
+                         int32_t n_q_heads, const void* q, int64_t q_token_stride, const int32_t* coords,
+                         const int32_t* q_off, int32_t total_q, const int32_t* seq_len, int64_t max_len, void* out,
+                         int64_t out_token_stride, uint32_t* status, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+    int rc = check_cfg(cfg);
+    if (rc) return rc;
+    if ((rc = check_cache(cfg, cache))) return rc;
+    if (!heads_ok(cfg, n_q_heads) || n_seqs < 0 || n_seqs > cache->n_seqs || layer < 0 || layer >= cfg->n_layers ||
+        total_q < 0 || max_len < 0 || max_len > PRCR_CACHE_MAX_LEN || max_len > cache_capacity(cache))
+        return PRCR_EINVAL;
+    if (n_seqs == 0 || total_q == 0) return PRCR_OK;
+    const int64_t row = int64_t(n_q_heads) * cfg->head_dim;
+    if (!q || !coords || !q_off || !seq_len || !out || !status || q_token_stride < row || out_token_stride < row)
+        return PRCR_EINVAL;
+    if (!aligned16(q) || !aligned16(out) || !mult8(q_token_stride) || !mult8(out_token_stride) || !aligned4(coords) ||
+        !aligned4(q_off) || !aligned4(seq_len) || !aligned4(status))
+        return PRCR_EALIGN;
+    (void)workspace;
+    (void)workspace_bytes;
+    ChunkArgs a = {};
+    a.cache = cache_view(cache, layer);
+    a.q = static_cast<const uint16_t*>(q);
+    a.q_stride = q_token_stride;
+    a.coords = coords;
+    a.q_off = q_off;
+    a.seq_len = seq_len;
+    a.out = static_cast<uint16_t*>(out);
+    a.out_stride = out_token_stride;
+    a.status = status;
+    a.max_len = max_len;
+    a.n_seqs = n_seqs;
+    a.total_q = total_q;
+    a.n_kv_heads = cfg->n_kv_heads;
+    a.group = n_q_heads / cfg->n_kv_heads;
+    a.head_dim = cfg->head_dim;
+    a.layout = cfg->layout;
+    a.sec_t = cfg->sections[0];
+    a.sec_h = cfg->sections[1];
+    a.sec_w = cfg->sections[2];
+    a.scale_log2 = float(1.4426950408889634 / std::sqrt(double(cfg->head_dim)));
+    copy_turn_freq(cfg, a.turn_freq);
+    return status_of(launch_chunk(a, static_cast<cudaStream_t>(stream)));
+}
+
+size_t prcr_weights_workspace_size(const prcr_rope_cfg* cfg, int32_t n_seqs, int32_t n_q_heads, int64_t max_len) {
+    if (check_cfg(cfg) || n_seqs < 1 || max_len < 1 || !heads_ok(cfg, n_q_heads)) return 0;
+    return weights_bytes(cfg, n_seqs, n_q_heads, max_len);
+}
+
+int prcr_accumulate_weights(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, int32_t n_seqs, int32_t n_q_heads,
+                            const void* q, const int64_t* q_pos, const int32_t* seq_len, int64_t max_len,
+                            float* score, int64_t score_stride, float decay, uint32_t* status, void* workspace,
+                            size_t workspace_size, void* stream) {
+    int rc = check_cfg(cfg);
+    if (rc) return rc;
+    if ((rc = check_cache(cfg, cache))) return rc;
+    if (!heads_ok(cfg, n_q_heads) || n_seqs < 0 || n_seqs > cache->n_seqs || max_len < 0 ||
+        max_len > PRCR_CACHE_MAX_LEN || max_len > cache_capacity(cache) || score_stride < max_len ||
+        !std::isfinite(decay))
+        return PRCR_EINVAL;
+    if (n_seqs == 0 || max_len == 0) return PRCR_OK;
+    if (n_seqs > 65535 || int64_t(cfg->n_layers) * cfg->n_kv_heads > 65535) return PRCR_EINVAL;  // grid z and y
+    if (!q || !q_pos || !seq_len || !score || !status) return PRCR_EINVAL;
+    if (!aligned16(q) || !aligned8(q_pos) || !aligned4(seq_len) || !aligned4(score) || !aligned4(status))
+        return PRCR_EALIGN;
+    if (!workspace || workspace_size < weights_bytes(cfg, n_seqs, n_q_heads, max_len)) return PRCR_EWORKSPACE;
+    if (!aligned16(workspace)) return PRCR_EALIGN;
+    WeightsArgs a = {};
+    a.cache = cache_view(cache, 0);
+    a.q = static_cast<const uint16_t*>(q);
+    a.q_pos = q_pos;
+    a.seq_len = seq_len;
+    a.score = score;
+    a.logits = static_cast<float*>(workspace);
+    a.status = status;
+    a.max_len = max_len;
+    a.score_stride = score_stride;
+    a.decay = decay;
+    a.n_seqs = n_seqs;
+    a.n_layers = cfg->n_layers;
+    a.n_kv_heads = cfg->n_kv_heads;
+    a.group = n_q_heads / cfg->n_kv_heads;
+    a.head_dim = cfg->head_dim;
+    a.scale_log2 = float(1.4426950408889634 / std::sqrt(double(cfg->head_dim)));
+    copy_turn_freq(cfg, a.turn_freq);
+    return status_of(launch_weights(a, static_cast<cudaStream_t>(stream)));
+}
+
+int prcr_evict(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, const prcr_cache_desc* dst, int32_t n_seqs,
+               const int32_t* seq_len, int64_t max_len, int32_t budget, int32_t n_sink, int32_t n_recent,
+               const float* score, float* score_out, int64_t score_stride, int32_t* keep_out, int32_t* seq_len_out,
+               uint32_t* status, void* stream) {
+    int rc = check_cfg(cfg);
+    if (rc) return rc;
+    if ((rc = check_cache(cfg, cache))) return rc;
+    if (dst && (rc = check_cache(cfg, dst))) return rc;
+    if (n_seqs < 0 || n_seqs > cache->n_seqs || (dst && n_seqs > dst->n_seqs) || max_len < 0 ||
+        max_len > PRCR_CACHE_MAX_LEN || max_len > cache_capacity(cache) || score_stride < max_len || budget < 1 ||
+        budget > PRCR_CACHE_MAX_LEN || n_sink < 0 || n_recent < 0 || int64_t(n_sink) + n_recent > budget)
+        return PRCR_EINVAL;
+    if (dst && dst->kind == PRCR_CACHE_CONTIGUOUS && (dst->k == cache->k || dst->v == cache->v)) return PRCR_EINVAL;
+    if (n_seqs == 0) return PRCR_OK;
+    if (n_seqs > 65535 || cfg->n_layers > 65535) return PRCR_EINVAL;  // grid z and y
+    if (!seq_len || !score || !score_out || !keep_out || !seq_len_out || !status || seq_len == seq_len_out)
+        return PRCR_EINVAL;
+    if (!aligned4(seq_len) || !aligned4(score) || !aligned4(score_out) || !aligned4(keep_out) ||
+        !aligned4(seq_len_out) || !aligned4(status))
+        return PRCR_EALIGN;
+    EvictArgs a = {};
+    a.src = cache_view(cache, 0);
+    a.dst = dst ? cache_view(dst, 0) : a.src;
+    a.seq_len = seq_len;
+    a.len_out = seq_len_out;
+    a.score = score;
+    a.score_out = score_out;
+    a.keep = keep_out;
+    a.status = status;
+    a.max_len = max_len;
+    a.score_stride = score_stride;
+    a.budget = budget;
+    a.n_sink = n_sink;
+    a.n_recent = n_recent;
+    a.n_layers = cfg->n_layers;
+    a.n_kv_heads = cfg->n_kv_heads;
+    a.head_dim = cfg->head_dim;
+    a.in_place = dst == nullptr;
+    return status_of(launch_evict(a, n_seqs, static_cast<cudaStream_t>(stream)));
+}
+
+}  // extern "C"

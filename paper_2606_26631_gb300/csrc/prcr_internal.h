@@ -343,6 +343,118 @@ struct SelectArgs {
     uint64_t turn_freq[kMaxPairs];  // pair i: round(inv_freq_i / (2 pi) * 2^64)
 };
 
+// A cache as the kernels of prcr_append_kv, prcr_chunk_attention,
+// prcr_accumulate_weights and prcr_evict see it.
+struct CacheView {
+    uint16_t* k;
+    uint16_t* v;
+    int64_t seq_stride;         // contiguous
+    int64_t layer_stride;
+    int64_t block_stride;       // paged
+    int64_t slot_stride;
+    int64_t capacity;           // slots per sequence
+    const int32_t* block_table;
+    int32_t bt_stride;
+    int32_t block_size;         // 1 for a contiguous cache
+    int32_t n_blocks;
+    int32_t kind;
+};
+
+struct AppendArgs {
+    CacheView cache;            // k, v shifted to layer_begin
+    const uint16_t* src_k;
+    const uint16_t* src_v;
+    int64_t src_layer_stride;
+    int64_t src_token_stride;
+    const int32_t* coords;      // [total][3]
+    const int32_t* tok_off;     // [n_seqs + 1]
+    const int32_t* len_in;      // [n_seqs]
+    int32_t* len_out;           // [n_seqs]
+    uint32_t* status;
+    int32_t n_seqs;
+    int32_t total;
+    int32_t n_layers;
+    int32_t head_dim;
+    int32_t lanes;              // threads per token: n_kv_heads * head_dim / 16
+    int32_t tok_per_cta;
+    int32_t layers_per_cta;
+    int32_t layout;
+    int32_t sec_t;
+    int32_t sec_h;
+    int32_t sec_w;
+    uint64_t turn_freq[kMaxPairs];  // pair i: round(inv_freq_i / (2 pi) * 2^64)
+};
+
+struct ChunkArgs {
+    CacheView cache;            // k, v shifted to the layer
+    const uint16_t* q;
+    int64_t q_stride;           // elements between tokens
+    const int32_t* coords;      // [total_q][3]
+    const int32_t* q_off;       // [n_seqs + 1]
+    const int32_t* seq_len;     // [n_seqs]
+    uint16_t* out;
+    int64_t out_stride;
+    uint32_t* status;
+    int64_t max_len;
+    int32_t n_seqs;
+    int32_t total_q;
+    int32_t n_kv_heads;
+    int32_t group;
+    int32_t head_dim;
+    int32_t layout;
+    int32_t sec_t;
+    int32_t sec_h;
+    int32_t sec_w;
+    float scale_log2;           // log2(e) / sqrt(head_dim)
+    uint64_t turn_freq[kMaxPairs];
+};
+
+struct WeightsArgs {
+    CacheView cache;
+    const uint16_t* q;          // [B][n_layers][n_q_heads][D]
+    const int64_t* q_pos;       // [B]
+    const int32_t* seq_len;     // [B]
+    float* score;               // [B][n_layers][n_kv_heads][score_stride]
+    float* logits;              // workspace [B][n_layers][n_q_heads][max_len]
+    uint32_t* status;
+    int64_t max_len;
+    int64_t score_stride;
+    float decay;
+    int32_t n_seqs;
+    int32_t n_layers;
+    int32_t n_kv_heads;
+    int32_t group;
+    int32_t head_dim;
+    float scale_log2;
+    uint64_t turn_freq[kMaxPairs];
+};
+
+struct EvictArgs {
+    CacheView src;
+    CacheView dst;              // == src in place
+    const int32_t* seq_len;     // [B]
+    int32_t* len_out;           // [B]
+    const float* score;         // [B][n_layers][n_kv_heads][score_stride]
+    float* score_out;
+    int32_t* keep;              // [B][n_layers][n_kv_heads][budget]
+    uint32_t* status;
+    int64_t max_len;
+    int64_t score_stride;
+    int32_t budget;
+    int32_t n_sink;
+    int32_t n_recent;
+    int32_t n_layers;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t in_place;
+};
+
+cudaError_t append_blocks_per_sm(int block, size_t smem, int* out);
+cudaError_t launch_append(const AppendArgs& a, dim3 grid, int block, size_t smem, cudaStream_t stream);
+cudaError_t launch_chunk(const ChunkArgs& a, cudaStream_t stream);
+cudaError_t launch_weights(const WeightsArgs& a, cudaStream_t stream);
+cudaError_t launch_evict(const EvictArgs& a, int n_seqs, cudaStream_t stream);
+
 // Every argument check of prcr_rebind_inject except the workspace's: PRCR_OK
 // or the negative code that call would return.
 int check_revisit_args(const prcr_rope_cfg* cfg, const prcr_store_desc* store,
@@ -361,6 +473,19 @@ cudaError_t launch_select_cached_logits(const SelectArgs& a, int n_seqs, int sms
 // the steps after the logits: normalisers, relevances, top-k (fine: logits of
 // float32's accuracy)
 cudaError_t launch_select_tail(const SelectArgs& a, int n_seqs, bool fine, cudaStream_t stream);
+
+// Argument checks, launch rules and per-device facts that the entry points share.
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+inline bool mult8(int64_t s) { return s >= 0 && (s & 7) == 0; }
+int check_cfg(const prcr_rope_cfg* c);
+int check_cache(const prcr_rope_cfg* c, const prcr_cache_desc* k);
+void copy_turn_freq(const prcr_rope_cfg* cfg, uint64_t* out);
+int sm_count(int dev);
+enum KernelId { kRebind = 0, kCapture = 1, kFused = 2, kAppend = 3 };
+int blocks_per_sm(int dev, int block, size_t smem, int kernel = kRebind);
+int stream_layers_per_cta(int64_t tiles, int n_layers, int64_t wave, int few);
 
 // The dynamic shared-memory limit of a kernel on the current device, raised to
 // `smem` where it is lower. It belongs to the kernel, not to a launch, so it is

@@ -1,0 +1,136 @@
+"""CPU checks of append_kv, chunk_attention, accumulate_weights and evict: what the
+host refuses, before any CUDA call (the addresses below are never read)."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2606_26631_gb300 as prcr
+from paper_2606_26631_gb300 import _binding as B
+
+FAKE = 1 << 40
+
+
+def _cfg(D=64, H=2, L=2):
+    return prcr.rope_cfg(L, H, D, (D // 2, 0, 0))
+
+
+def _flat(**o):
+    return B.CacheDesc(**{**dict(kind=0, block_size=1, k=FAKE, v=FAKE + 2 ** 20, seq_stride=2 * 256 * 128, layer_stride=256 * 128, block_stride=0,
+                                 slot_stride=128, block_table=None, bt_stride=0, n_blocks=0, max_slots=256, n_seqs=3), **o})
+
+
+def _paged(**o):
+    return B.CacheDesc(**{**dict(kind=1, block_size=16, k=FAKE, v=FAKE + 2 ** 20, seq_stride=0, layer_stride=2048 * 64, block_stride=2048,
+                                 slot_stride=128, block_table=FAKE, bt_stride=16, n_blocks=64, max_slots=0, n_seqs=3), **o})
+
+
+APPEND = dict(cfg=_cfg(), cache=_flat(), n_seqs=3, l0=0, nl=2, k=FAKE, v=FAKE, ls=40 * 128, ts=128, coords=FAKE, off=FAKE, total=40,
+              len_in=FAKE, len_out=FAKE + 64, status=FAKE)
+CHUNK = dict(cfg=_cfg(), cache=_flat(), n_seqs=3, layer=0, hq=8, q=FAKE, qs=512, coords=FAKE, off=FAKE, total=40, len=FAKE, max_len=200,
+             out=FAKE, os=512, status=FAKE, ws=FAKE, ws_bytes=1 << 40)
+WEIGHTS = dict(cfg=_cfg(), cache=_flat(), n_seqs=3, hq=8, q=FAKE, pos=FAKE, len=FAKE, max_len=200, score=FAKE, ss=200, decay=1.0, status=FAKE,
+               ws=FAKE, ws_bytes=1 << 40)
+EVICT = dict(cfg=_cfg(), cache=_flat(), dst=None, n_seqs=3, len=FAKE, max_len=200, budget=50, sink=4, recent=10, score=FAKE, score_out=FAKE,
+             ss=200, keep=FAKE, len_out=FAKE + 64, status=FAKE)
+ENTRY = {"prcr_append_kv": APPEND, "prcr_chunk_attention": CHUNK, "prcr_accumulate_weights": WEIGHTS, "prcr_evict": EVICT}
+
+
+def call(name, **over):
+    a = {**ENTRY[name], **over}
+    args = [C.byref(x) if isinstance(x, C.Structure) else x for x in a.values()]
+    return getattr(prcr.lib(), name)(*args, None)
+
+
+COMMON = [
+    (dict(cfg=_cfg(D=40)), B.EINVAL), (dict(cfg=None), B.EINVAL), (dict(cache=None), B.EINVAL), (dict(n_seqs=-1), B.EINVAL),
+    (dict(n_seqs=4), B.EINVAL), (dict(cache=_flat(k=None)), B.EINVAL), (dict(cache=_flat(v=FAKE + 8)), B.EALIGN),
+    (dict(cache=_flat(slot_stride=64)), B.EINVAL), (dict(cache=_paged(block_table=None)), B.EINVAL),
+    (dict(cache=_paged(block_size=0)), B.EINVAL), (dict(status=None), B.EINVAL), (dict(status=FAKE + 2), B.EALIGN),
+]
+BAD = {
+    "prcr_append_kv": [
+        (dict(l0=-1), B.EINVAL), (dict(l0=1), B.EINVAL), (dict(nl=0), B.EINVAL), (dict(total=-1), B.EINVAL), (dict(k=None), B.EINVAL),
+        (dict(v=None), B.EINVAL), (dict(ts=64), B.EINVAL), (dict(ls=-8), B.EINVAL), (dict(coords=None), B.EINVAL), (dict(off=None), B.EINVAL),
+        (dict(len_in=None), B.EINVAL), (dict(len_out=None), B.EINVAL), (dict(len_out=FAKE), B.EINVAL), (dict(k=FAKE + 8), B.EALIGN),
+        (dict(ts=132), B.EALIGN), (dict(ls=4), B.EALIGN), (dict(off=FAKE + 2), B.EALIGN), (dict(coords=FAKE + 1), B.EALIGN)],
+    "prcr_chunk_attention": [
+        (dict(cfg=_cfg(D=96)), B.EINVAL), (dict(hq=9), B.EINVAL), (dict(hq=1), B.EINVAL), (dict(hq=18), B.EINVAL), (dict(layer=-1), B.EINVAL),
+        (dict(layer=2), B.EINVAL), (dict(total=-1), B.EINVAL), (dict(max_len=-1), B.EINVAL), (dict(max_len=257), B.EINVAL),
+        (dict(cache=_paged(bt_stride=2 ** 30), max_len=2 ** 30 + 1), B.EINVAL), (dict(q=None), B.EINVAL), (dict(out=None), B.EINVAL),
+        (dict(qs=504), B.EINVAL), (dict(os=504), B.EINVAL), (dict(coords=None), B.EINVAL), (dict(off=None), B.EINVAL), (dict(len=None), B.EINVAL),
+        (dict(q=FAKE + 8), B.EALIGN), (dict(out=FAKE + 8), B.EALIGN), (dict(qs=516), B.EALIGN), (dict(os=516), B.EALIGN),
+        (dict(len=FAKE + 2), B.EALIGN), (dict(cfg=_cfg(D=256, H=8), cache=_flat(slot_stride=2048), hq=64), B.EINVAL)],
+    "prcr_accumulate_weights": [
+        (dict(cfg=_cfg(D=96)), B.EINVAL), (dict(hq=9), B.EINVAL), (dict(max_len=257), B.EINVAL), (dict(ss=199), B.EINVAL),
+        (dict(decay=float("nan")), B.EINVAL), (dict(decay=float("inf")), B.EINVAL), (dict(q=None), B.EINVAL), (dict(pos=None), B.EINVAL),
+        (dict(score=None), B.EINVAL), (dict(q=FAKE + 4), B.EALIGN), (dict(pos=FAKE + 4), B.EALIGN), (dict(score=FAKE + 2), B.EALIGN)],
+    "prcr_evict": [
+        (dict(max_len=257), B.EINVAL), (dict(ss=199), B.EINVAL), (dict(budget=0), B.EINVAL), (dict(sink=-1), B.EINVAL),
+        (dict(recent=-1), B.EINVAL), (dict(sink=41), B.EINVAL), (dict(score=None), B.EINVAL), (dict(score_out=None), B.EINVAL),
+        (dict(keep=None), B.EINVAL), (dict(len=None), B.EINVAL), (dict(len_out=FAKE), B.EINVAL), (dict(keep=FAKE + 2), B.EALIGN),
+        (dict(dst=_flat()), B.EINVAL), (dict(dst=_flat(k=FAKE + 2 ** 22, v=FAKE + 2 ** 23, n_seqs=2)), B.EINVAL),
+        (dict(dst=_flat(k=FAKE + 8)), B.EALIGN), (dict(sink=2 ** 31 - 1, recent=2 ** 31 - 1), B.EINVAL)],
+}
+
+
+@pytest.mark.parametrize("name,over,code", [(n, o, c) for n in ENTRY for o, c in COMMON + BAD[n]],
+                         ids=lambda v: ",".join(v) if isinstance(v, dict) else str(v))
+def test_refusals(name, over, code):
+    assert call(name, **over) == code
+
+
+def test_empty_calls():
+    for name in ENTRY:
+        assert call(name, n_seqs=0) == B.OK
+    assert call("prcr_chunk_attention", total=0) == B.OK
+    assert call("prcr_accumulate_weights", max_len=0) == B.OK
+
+
+def test_workspaces():
+    c = _cfg(D=128, H=8, L=36)
+    assert prcr.weights_workspace_size(_cfg(D=96), 1, 8, 100) == 0
+    assert prcr.chunk_workspace_size(_cfg(D=96), 1, 8, 100, 100) == 0
+    need = prcr.weights_workspace_size(c, 3, 32, 1000)
+    cache = _flat(slot_stride=1024, layer_stride=256 * 1024, max_slots=1000)
+    if need:
+        assert call("prcr_accumulate_weights", cfg=c, cache=cache, hq=32, max_len=1000, ss=1000, ws_bytes=need - 1) == B.EWORKSPACE
+        assert call("prcr_accumulate_weights", cfg=c, cache=cache, hq=32, max_len=1000, ss=1000, ws=None) == B.EWORKSPACE
+        assert call("prcr_accumulate_weights", cfg=c, cache=cache, hq=32, max_len=1000, ss=1000, ws=FAKE + 8) == B.EALIGN
+
+
+def _t(shape, dtype=torch.bfloat16):
+    return torch.zeros(shape, dtype=dtype)
+
+
+def test_binding_refuses():
+    """Wrong types, shapes and layouts raise before the library is called; so do tensors that are not on the current GPU."""
+    c, i32 = _cfg(), torch.int32
+    cache = prcr.cache_contiguous(_t((3, 2, 9, 2, 64)), _t((3, 2, 9, 2, 64)))
+    off, ln, st = _t(4, i32), _t(3, i32), _t(1, i32)
+    rows = _t((2, 5, 2, 64))
+    q, out, pos = _t((5, 8, 64)), _t((5, 8, 64)), _t((5, 3), i32)
+    score, keep = _t((3, 2, 2, 9), torch.float32), _t((3, 2, 2, 4), i32)
+    qw, p = _t((3, 2, 8, 64)), _t(3, torch.int64)
+    good = {
+        "append_kv": [c, cache, 0, rows, rows, pos, off, ln, ln.clone(), st],
+        "chunk_attention": [c, cache, 0, q, pos, off, ln, 9, out, st],
+        "accumulate_weights": [c, cache, qw, p, ln, 9, score, st],
+        "evict": [c, cache, ln, 9, 4, 1, 1, score, keep, ln.clone(), st],
+    }
+    for name, args in good.items():
+        with pytest.raises(ValueError, match="CUDA device"):
+            getattr(prcr, name)(*args)
+    wrong = {
+        "append_kv": {3: [rows.float(), rows[:, :, :1], rows.transpose(2, 3)], 4: [rows[:, :4]], 5: [pos.long(), pos[:4]], 6: [off[:3], off.long()],
+                      8: [ln[:2]]},
+        "chunk_attention": {3: [q.float(), q[:, :, :32], q.transpose(0, 1)], 4: [pos[:2], pos.float()], 5: [off[:2]], 8: [out[:4], out.float()]},
+        "accumulate_weights": {2: [qw.float(), qw[:, :1], qw.transpose(1, 2)], 3: [p.int(), p[:2]], 6: [score.double(), score[:2], score[..., :5]]},
+        "evict": {7: [score.half(), score[:, :1]], 8: [keep[:2], keep.float()], 9: [ln[:1]], 2: [ln.long()]},
+    }
+    for name, at in wrong.items():
+        for i, values in at.items():
+            for v in values:
+                with pytest.raises((TypeError, ValueError)) as e:
+                    getattr(prcr, name)(*good[name][:i], v, *good[name][i + 1:])
+                assert "CUDA device" not in str(e.value), (name, i)

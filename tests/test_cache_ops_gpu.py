@@ -1,0 +1,698 @@
+"""GPU parity of append_kv, chunk_attention, accumulate_weights and evict against
+64-bit references (cache_ops_util).
+
+chunk_attention is held to two bars. Element by element to the sum of its
+roundings' bounds (cache_ops_util.chunk64). And as a whole, as the 2-norm of the
+difference over that of the result: an unbiased rounding to bf16 is off by
+2^-8 / sqrt(3) of the step's binade, 1.6e-3 of the value in the mean square; the query's,
+the probabilities' and the output's are independent and, for N(0, 1) inputs, move the output
+by that much each, 2.9e-3 together; the bar is 5e-3."""
+import numpy as np
+import pytest
+import torch
+
+import cache_ops_util as U
+import paper_2606_26631_gb300 as prcr
+from cache_ops_util import DEV, Cache, i32, normal
+
+pytestmark = pytest.mark.gpu
+NORM = 5e-3
+
+
+def status_word():
+    return torch.zeros(1, dtype=torch.int32, device=DEV)
+
+
+def positions(n, p, rng):
+    """Half an image of rows of 7, then text."""
+    i = np.arange(n)
+    img = np.stack([np.full(n, p), p + i // 7, p + i % 7], 1)
+    txt = np.stack([p + 9 + i] * 3, 1)
+    return np.where((i < n // 2)[:, None], img, txt).astype(np.int32)
+
+
+# ----------------------------------------------------------------------------
+# append
+# ----------------------------------------------------------------------------
+def run_append(c, desc, layer0, ks, vs, pos, lens, len_in, pad=0):
+    off, li = U.offsets(lens), i32(len_in)
+    lo, st = torch.full_like(li, -7), status_word()
+    prcr.append_kv(c, desc, layer0, ks, vs, i32(pos), off, li, lo, st)
+    torch.cuda.synchronize()
+    return lo.cpu().numpy(), int(st.item())
+
+
+@pytest.mark.parametrize("L,l0,nl,H,D,block,layout,lens,strided", [
+    (3, 0, 3, 8, 128, 16, prcr.LAYOUT_SECTIONED, [1, 0, 40], False),
+    (5, 1, 3, 2, 64, 0, prcr.LAYOUT_INTERLEAVED, [7, 1, 3], True),
+    (2, 0, 2, 4, 256, 7, prcr.LAYOUT_SECTIONED, [1, 1, 1], True),
+    (2, 1, 1, 1, 16, 1, prcr.LAYOUT_SECTIONED, [0, 0, 9], False),
+    (36, 0, 36, 8, 128, 16, prcr.LAYOUT_SECTIONED, [1] * 5, False),
+    (2, 0, 2, 5, 80, 16, prcr.LAYOUT_INTERLEAVED, [300, 2, 0, 77], False),
+])
+def test_append(L, l0, nl, H, D, block, layout, lens, strided):
+    rng = np.random.default_rng(3)
+    B, T, pad = len(lens), sum(lens), 3
+    len_in = rng.integers(0, 40, B)
+    cache = Cache(L, H, D, [int(a + b + 2) for a, b in zip(len_in, lens)], block, fill=U.CANARY, gap=8 if strided else 0)
+    src = normal((nl, T + pad, 3 if strided else 2, H, D), 11)
+    ks, vs = src[:, :, 0], src[:, :, 1]
+    pos = rng.integers(-2 ** 31, 2 ** 31, (T + pad, 3)).astype(np.int32) if D == 80 else rng.integers(0, 40000, (T + pad, 3))
+    before_k, before_v = cache.k_all.clone(), cache.v_all.clone()
+    lo, st = run_append(U.cfg_of(L, H, D, layout), cache.desc(), l0, ks, vs, pos, lens, len_in)
+    assert st == 0 and np.array_equal(lo, len_in + lens)
+    at = 0
+    for b, n in enumerate(lens):
+        w = cache.where(b, np.arange(len_in[b], len_in[b] + n))
+        got_k, got_v = cache.k[w][l0:l0 + nl], cache.v[w][l0:l0 + nl]
+        assert torch.equal(got_v, vs[:, at:at + n])
+        x = U.f64(ks[:, at:at + n])
+        ref = U.rope64(x, pos[at:at + n], D, layout)
+        # half a bf16 step, and float32 sums and cos/sin on the pair's norm
+        pair = np.sqrt(x[..., :D // 2] ** 2 + x[..., D // 2:] ** 2)
+        bar = 2.0 ** -8 * np.abs(ref) + 2.0 ** -21 * np.concatenate([pair, pair], -1) + 1e-38
+        assert (np.abs(U.f64(got_k) - ref) <= bar).all()
+        for x_ in (cache.k, cache.v):  # back to what they were: nothing else may differ
+            rows = x_[w]
+            rows[l0:l0 + nl] = U.CANARY
+            x_[w] = rows
+        at += n
+    assert torch.equal(cache.k_all, before_k) and torch.equal(cache.v_all, before_v)
+
+
+def test_append_errors():
+    """Full cache, unmapped block, negative length: those rows are skipped and reported; malformed
+    offsets: nothing is written and lengths stay."""
+    L, H, D = 2, 2, 64
+    c = U.cfg_of(L, H, D)
+    ks, vs = normal((L, 12, H, D), 1), normal((L, 12, H, D), 2)
+    pos = np.zeros((12, 3))
+    cache = Cache(L, H, D, [32, 32, 32], 8, fill=U.CANARY, unmapped=[(1, 2)])
+    lo, st = run_append(c, cache.desc(), 0, ks, vs, pos, [4, 4, 4], [30, 14, -1])
+    assert st == prcr.ST_CAPACITY | prcr.ST_NO_BLOCK and list(lo) == [34, 18, 3]
+    # the last block, 16..23, of sequence 1 is unmapped; block -1 of the table reads as the last pool block: untouched
+    got = cache.v.clone()
+    for b, slots, n in ((0, [30, 31], 0), (1, [14, 15], 4)):
+        assert torch.equal(got[cache.where(b, slots)], vs[:, n:n + 2])
+        got[cache.where(b, slots)] = U.CANARY
+    assert bool((got == torch.tensor(U.CANARY, dtype=torch.bfloat16)).all())
+    for off in ([1, 4, 8, 12], [0, 8, 4, 12], [0, 4, 8, 13], [0, -3, 8, 12], [0, 2 ** 30, 8, 12]):
+        cache = Cache(L, H, D, [32, 32, 32], 8, fill=U.CANARY)
+        st, li = status_word(), i32([3, 4, 5])
+        lo = torch.full_like(li, -7)
+        prcr.append_kv(c, cache.desc(), 0, ks, vs, i32(pos), i32(off), li, lo, st)
+        torch.cuda.synchronize()
+        assert int(st.item()) == prcr.ST_CSR and torch.equal(lo, li)
+        assert bool((cache.k == torch.tensor(U.CANARY, dtype=torch.bfloat16)).all())
+
+
+# ----------------------------------------------------------------------------
+# chunk attention
+# ----------------------------------------------------------------------------
+class Chunk:
+    """A packed batch: new[b] queries over lens[b] slots of a cache."""
+
+    def __init__(self, H, g, D, new, lens, block, L=2, layer=1, layout=prcr.LAYOUT_SECTIONED, seed=0, pad=3, strided=False,
+                 q_scale=1.0, caps=None, **cache):
+        self.H, self.g, self.D, self.new, self.lens, self.layer, self.layout = H, g, D, list(new), list(lens), layer, layout
+        self.cache = Cache(L, H, D, caps or [max(n, 1) + 3 for n in lens], block, seed=seed, **cache)
+        T, Hq = sum(new) + pad, H * g
+        self.T, rng = T, np.random.default_rng(seed + 9)
+        big = normal((T, Hq + (2 * H if strided else 0), D), seed + 3, q_scale)
+        self.q = big[:, :Hq]
+        self.out_all = torch.full((T, Hq + (1 if strided else 0), D), U.CANARY, dtype=torch.bfloat16, device=DEV)
+        self.out = self.out_all[:, :Hq]
+        self.pos = np.concatenate([positions(n, int(rng.integers(0, 60000)), rng) for n in new] + [np.zeros((pad, 3), np.int32)])
+        self.cfg = U.cfg_of(L, H, D, layout)
+        self.args = (i32(self.pos), U.offsets(new), i32(lens))
+        self.max_len = max(self.lens + [0])
+        self.status = status_word()
+        self.ws = self.workspace(self.max_len)
+
+    def workspace(self, max_len):
+        n = prcr.chunk_workspace_size(self.cfg, len(self.new), self.H * self.g, self.T, max_len)
+        return torch.full((max(n, 16),), 0xff, dtype=torch.uint8, device=DEV)
+
+    def run(self, max_len=None, q_off=None, seq_len=None, ws=None, stream=None):
+        m = self.max_len if max_len is None else max_len
+        prcr.chunk_attention(self.cfg, self.cache.desc(), self.layer, self.q, self.args[0], self.args[1] if q_off is None else q_off,
+                             self.args[2] if seq_len is None else seq_len, m, self.out, self.status,
+                             (self.ws if m == self.max_len else self.workspace(m)) if ws is None else ws, stream=stream)
+        return self
+
+    def done(self):
+        torch.cuda.synchronize()
+        return int(self.status.item())
+
+    def check(self, seqs=None, drop=None, top=None, rows=None):
+        """Every query (or `rows` of them) of the sequences against the reference; drop(b): slots left out."""
+        at, whole = 0, [0.0, 0.0]
+        q, got = U.f64(self.q), U.f64(self.out)
+        for b, (n, length) in enumerate(zip(self.new, self.lens)):
+            if n and (seqs is None or b in seqs):
+                S = max(1, min(length, top if top is not None else length))
+                K, V = (U.f64(self.cache.rows(x, b, S)[self.layer]) for x in (self.cache.k, self.cache.v))
+                i = np.arange(n) if rows is None else np.unique(np.linspace(0, n - 1, rows).astype(int))
+                sees = U.causal(n, length, S)[i]
+                if drop is not None:
+                    sees[:, drop(b, np.arange(S))] = False
+                live = sees.any(0)
+                ref, bar = U.chunk64(q[at + i], self.pos[at + i], np.where(live[:, None, None], K, 0.0), np.where(live[:, None, None], V, 0.0),
+                                     sees, self.layout)
+                d = np.abs(got[at + i] - ref)
+                assert (d <= bar).all(), (b, np.unravel_index((d - bar).argmax(), d.shape), (d / bar).max())
+                whole[0] += (d ** 2).sum()
+                whole[1] += (ref ** 2).sum()
+            at += n
+        if whole[1]:
+            assert np.sqrt(whole[0] / whole[1]) <= NORM, np.sqrt(whole[0] / whole[1])
+        tail = self.out_all.clone()
+        tail[:at, :self.H * self.g] = U.CANARY
+        assert bool((tail == torch.tensor(U.CANARY, dtype=torch.bfloat16)).all()), "rows or gaps that are not the call's"
+
+
+SHAPES = [  # H, g, D, block
+    (8, 4, 128, 16), (4, 7, 128, 0), (2, 1, 128, 7), (1, 8, 128, 64), (3, 3, 64, 16), (2, 8, 64, 0), (2, 4, 256, 16), (4, 8, 256, 0),
+    (1, 1, 256, 1), (5, 6, 128, 128), (1, 5, 64, 8),
+]
+
+
+@pytest.mark.parametrize("H,g,D,block", SHAPES, ids=lambda v: str(v))
+@pytest.mark.parametrize("kind", ["token", "few", "prompt", "extend", "ragged"])
+def test_chunk(H, g, D, block, kind):
+    new, lens = {"token": ([1, 1, 1], [1, 2, 300]), "few": ([6, 0, 3, 1], [700, 40, 3, 129]), "prompt": ([130, 1, 65], [130, 1, 65]),
+                 "extend": ([70, 33], [400, 127 + 33]), "ragged": ([1, 128, 0, 40, 17], [257, 128, 0, 168, 1000])}[kind]
+    c = Chunk(H, g, D, new, lens, block, strided=kind in ("few", "extend"), gap=16 if kind == "few" else 0,
+              layout=prcr.LAYOUT_INTERLEAVED if kind == "extend" else prcr.LAYOUT_SECTIONED, seed=H * 100 + g)
+    assert c.run().done() == 0
+    c.check()
+
+
+@pytest.mark.parametrize("H,g,D,block,new,lens", [
+    (8, 4, 128, 16, [1], [9000]), (1, 1, 128, 16, [2], [40000]), (2, 7, 128, 0, [5, 1], [20011, 3]), (4, 4, 64, 32, [3], [12345]),
+    (2, 8, 256, 16, [4, 2], [5000, 6001]), (2, 4, 128, 16, [300], [20000]), (1, 8, 128, 0, [1024], [1024]), (2, 2, 64, 16, [2500], [2500]),
+    (1, 2, 256, 16, [1500], [1700]),
+], ids=lambda v: str(v))
+def test_chunk_long(H, g, D, block, new, lens):
+    c = Chunk(H, g, D, new, lens, block, seed=5)
+    assert c.run().done() == 0
+    c.check(rows=9)
+
+
+def test_chunk_first_slot_is_exact():
+    """A query that sees one slot gets its value, bit for bit (its weight is exactly 1)."""
+    for D, g, block in ((128, 4, 16), (64, 7, 0), (256, 2, 7)):
+        c = Chunk(2, g, D, [5, 1], [5, 1], block)
+        assert c.run().done() == 0
+        for b, t in ((0, 0), (1, 5)):
+            v = c.cache.rows(c.cache.v, b, 1)[1, 0]
+            assert torch.equal(c.out[t], v.repeat_interleave(g, 0))
+
+
+@pytest.mark.parametrize("D,block", [(128, 16), (64, 0), (256, 7), (128, 0)])
+def test_chunk_rows_that_see_nothing(D, block):
+    """More new tokens than slots: the first ones see no slot and get zeros; a sequence of no slots."""
+    c = Chunk(2, 4, D, [9, 3, 140], [4, 0, 2], block)
+    assert c.run().done() == 0
+    assert bool((c.out[:5] == 0).all()) and bool((c.out[9:12] == 0).all()) and bool((c.out[12:150] == 0).all())
+    c.check()
+    c = Chunk(2, 4, D, [9, 3], [0, 0], block)  # max_len 0
+    assert c.run().done() == 0
+    assert bool((c.out[:12] == 0).all())
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("H,g,D,block", [(2, 4, 128, 16), (1, 8, 64, 0), (2, 2, 256, 7)])
+def test_chunk_hidden_slots_do_not_matter(H, g, D, block, bad):
+    """Slots behind the length, and slots of later tokens, have no influence whatever they hold; queries that see them do
+    get what the formula gives."""
+    new, lens = [40, 150, 1], [300, 150, 17]
+    c = Chunk(H, g, D, new, lens, block, seed=2)
+    for b, n in enumerate(lens):  # rows behind the length
+        w = c.cache.where(b, np.arange(n, n + 3))
+        c.cache.k[w], c.cache.v[w] = bad, bad
+    hidden = {0: 290, 1: 100}  # a slot that later queries see
+    for b, s in hidden.items():
+        w = c.cache.where(b, [s])
+        c.cache.v[w] = bad
+    assert c.run().done() == 0
+    at = 0
+    for b, (n, length) in enumerate(zip(new, lens)):
+        K, V = (U.f64(c.cache.rows(x, b, length)[1]) for x in (c.cache.k, c.cache.v))
+        free = n if b not in hidden else hidden[b] - (length - n)
+        i = np.arange(free)
+        S = length if b not in hidden else hidden[b]
+        ref, bar = U.chunk64(U.f64(c.q[at:at + free]), c.pos[at:at + free], K[:S], V[:S], U.causal(n, length, S)[i])
+        got = U.f64(c.out[at:at + free])
+        assert (np.abs(got - ref) <= bar).all()
+        seeing = U.f64(c.out[at + free:at + n])
+        assert not np.isfinite(seeing).any()
+        at += n
+
+
+def test_chunk_nan_key_reaches_those_that_see_it():
+    c = Chunk(2, 4, 128, [100], [400], 16, seed=4)
+    c.cache.k[c.cache.where(0, [350])] = float("nan")
+    assert c.run().done() == 0
+    out = U.f64(c.out[:100])
+    assert np.isfinite(out[:50]).all() and np.isnan(out[50:]).all()
+    c.new = [50]  # the first fifty see slots up to 349
+    c.lens = [350]
+    q, pos = U.f64(c.q[:50]), c.pos[:50]
+    K, V = (U.f64(c.cache.rows(x, 0, 350)[1]) for x in (c.cache.k, c.cache.v))
+    ref, bar = U.chunk64(q, pos, K, V, U.causal(100, 400, 350)[:50])
+    assert (np.abs(out[:50] - ref) <= bar).all()
+
+
+@pytest.mark.parametrize("scale", [0.0, 30.0, 1000.0])
+def test_chunk_logits_of_any_size(scale):
+    """Equal logits (a plain mean of the values) and logits so far apart that one slot takes all."""
+    for D, new, lens in ((128, [60, 1], [500, 2000]), (64, [9], [300]), (256, [30], [200])):
+        c = Chunk(2, 4, D, new, lens, 16, q_scale=scale, seed=8)
+        assert c.run().done() == 0
+        got = U.f64(c.out[:sum(new)])
+        assert np.isfinite(got).all()
+        if scale < 100:
+            at = 0
+            for b, (n, length) in enumerate(zip(new, lens)):
+                K, V = (U.f64(c.cache.rows(x, b, length)[1]) for x in (c.cache.k, c.cache.v))
+                ref, bar = U.chunk64(U.f64(c.q[at:at + n]), c.pos[at:at + n], K, V, U.causal(n, length, length))
+                assert (np.abs(got[at:at + n] - ref) <= bar).all()
+                at += n
+
+
+def test_chunk_rising_maxima():
+    """Keys that grow along the sequence: every tile raises the running maximum."""
+    for D in (64, 128, 256):
+        c = Chunk(1, 4, D, [20], [1500], 16, seed=12)
+        grow = torch.linspace(0.1, 12.0, 1500, device=DEV).view(1, 1500, 1, 1)
+        w = c.cache.where(0, np.arange(1500))
+        c.cache.k[w] = (c.cache.k[w].float() * grow).bfloat16()
+        assert c.run().done() == 0
+        K, V = (U.f64(c.cache.rows(x, 0, 1500)[1]) for x in (c.cache.k, c.cache.v))
+        ref, bar = U.chunk64(U.f64(c.q[:20]), c.pos[:20], K, V, U.causal(20, 1500, 1500))
+        assert (np.abs(U.f64(c.out[:20]) - ref) <= bar).all()
+
+
+def test_chunk_device_errors():
+    """Unmapped blocks are left out, lengths beyond the capacity or max_len clamped, malformed offsets refused."""
+    c = Chunk(2, 4, 128, [20, 3], [200, 90], 16, unmapped=[(0, 3), (0, 4), (1, 0)])
+    assert c.run().done() == prcr.ST_NO_BLOCK
+    c.check(drop=lambda b, s: np.isin(s // 16, [3, 4]) if b == 0 else s // 16 == 0)
+    c = Chunk(2, 4, 128, [2], [16], 16, unmapped=[(0, 0)], caps=[16])  # no readable slot at all
+    assert c.run().done() == prcr.ST_NO_BLOCK and bool((c.out[:2] == 0).all())
+    # a length above max_len: queries see slots by their place behind the length, those past max_len are left out
+    c = Chunk(2, 4, 64, [20, 3], [200, 90], 0)
+    assert c.run(max_len=150).done() == prcr.ST_CAPACITY
+    c.check(top=150)
+    c = Chunk(2, 4, 64, [20, 3], [200, 90], 0)
+    c.lens[0] = 260  # capacity 203
+    assert c.run(max_len=203, seq_len=i32(c.lens)).done() == prcr.ST_CAPACITY
+    c.check(top=203)
+    c = Chunk(2, 4, 64, [20, 3], [200, 90], 0)
+    assert c.run(seq_len=i32([-5, 90])).done() == prcr.ST_CAPACITY
+    assert bool((c.out[:20] == 0).all())
+    c.check(seqs=[1])
+    for off in ([1, 20, 23], [0, 23, 20], [0, 20, 27], [0, -1, 23], [0, 2 ** 31 - 1, 23]):
+        c = Chunk(2, 4, 64, [20, 3], [200, 90], 16)
+        assert c.run(q_off=i32(off)).done() == prcr.ST_CSR
+        assert bool((c.out_all == torch.tensor(U.CANARY, dtype=torch.bfloat16)).all())
+
+
+def test_chunk_far_positions():
+    """Angles of positions near the ends of int32."""
+    c = Chunk(2, 4, 128, [12], [60], 16, seed=3)
+    c.pos = np.random.default_rng(1).integers(-2 ** 31, 2 ** 31, c.pos.shape).astype(np.int32)
+    c.args = (i32(c.pos),) + c.args[1:]
+    assert c.run().done() == 0
+    c.check()
+
+
+def test_chunk_many_sequences():
+    rng = np.random.default_rng(4)
+    new = rng.integers(0, 4, 300)
+    lens = new + rng.integers(0, 60, 300)
+    c = Chunk(2, 2, 64, [int(x) for x in new], [int(x) for x in lens], 8, seed=6)
+    assert c.run().done() == 0
+    c.check()
+
+
+def test_chunk_agrees_with_decode_attention():
+    """A single new token per sequence is decode_attention's step (its output is float32)."""
+    H, g, D = 8, 4, 128
+    c = Chunk(H, g, D, [1, 1, 1], [500, 33, 1200], 16, L=1, layer=0, pad=0)
+    c.pos[:] = c.pos[:, :1]
+    c.args = (i32(c.pos),) + c.args[1:]
+    assert c.run().done() == 0
+    q = c.q.contiguous().view(3, 1, H * g, D)
+    out = torch.empty(q.shape, dtype=torch.float32, device=DEV)
+    ws = torch.empty(max(16, prcr.decode_workspace_size(c.cfg, 3, H * g, 1200)), dtype=torch.uint8, device=DEV)
+    prcr.decode_attention(c.cfg, c.cache.desc(), q, torch.from_numpy(c.pos[:, 0].astype(np.int64)).to(DEV), c.args[2], 1200, out,
+                          c.status, ws)
+    assert c.done() == 0
+    c.check()
+    d = (c.out.float() - out[:, 0]).norm() / out.norm()
+    assert float(d) <= NORM
+
+
+def test_chunk_streams_and_graphs():
+    """Two calls at once on two streams with a workspace each; one call captured and replayed with new contents."""
+    a = Chunk(4, 4, 128, [3, 200], [3000, 900], 16, seed=1)
+    b = Chunk(4, 4, 128, [3, 200], [2500, 1100], 16, seed=2)
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        a.run(stream=s1)
+        b.run(stream=s2)
+    assert a.done() == 0 and b.done() == 0
+    a.check(rows=20)
+    b.check(rows=20)
+    g, want = torch.cuda.CUDAGraph(), a.out.clone()
+    with torch.cuda.graph(g):
+        a.run()
+    a.out.fill_(U.CANARY)
+    a.ws.fill_(0xff)
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(a.out, want)
+    a.q.copy_(b.q)
+    g.replay()
+    torch.cuda.synchronize()
+    a.check(rows=20)
+
+
+def test_chunk_is_repeatable():
+    c = Chunk(2, 7, 128, [5, 300], [9000, 700], 16, seed=1)
+    c.run().done()
+    want = c.out.clone()
+    for _ in range(3):
+        c.run()
+    c.done()
+    assert torch.equal(c.out, want)
+
+
+# ----------------------------------------------------------------------------
+# accumulated weights
+# ----------------------------------------------------------------------------
+def weights64(q, p, K, D, layout):
+    """sum over the group of softmax weights [H, S] and a bound on their error: float32 dots and rotations move a logit by at
+    most e = 2^-24 (D + 8) sum |q k| / sqrt(D), exp and the sums add 2^-20."""
+    Hq, H = q.shape[0], K.shape[1]
+    g = Hq // H
+    qr = U.rope64(q[None], np.full((1, 3), float(p)), D, layout)[0]
+    w, bar = np.zeros((H, K.shape[0])), np.zeros((H, K.shape[0]))
+    for h in range(Hq):
+        k = K[:, h // g]
+        x = U.softmax64(k @ qr[h] / np.sqrt(D))
+        e = 2.0 ** -24 * (D + 8) * (np.abs(k) @ np.abs(qr[h])).max() / np.sqrt(D)
+        w[h // g] += x
+        bar[h // g] += x * (np.expm1(2 * e) + 2.0 ** -20)
+    return w, bar
+
+
+class Weights:
+    def __init__(self, H, g, D, L, lens, block, seed=0, layout=prcr.LAYOUT_SECTIONED, caps=None, extra=5, **cache):
+        self.H, self.g, self.D, self.L, self.lens, self.layout = H, g, D, L, list(lens), layout
+        B, rng = len(lens), np.random.default_rng(seed)
+        self.cache = Cache(L, H, D, caps or [n + 3 for n in lens], block, seed=seed, **cache)
+        self.cfg = U.cfg_of(L, H, D, layout)
+        self.q = normal((B, L, H * g, D), seed + 3)
+        self.pos = rng.integers(0, 60000, B)
+        self.max_len = max(lens)
+        self.score = torch.rand((B, L, H, self.max_len + extra), generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV)
+        self.before = self.score.cpu().numpy().astype(np.float64)
+        self.status = status_word()
+
+    def run(self, decay=1.0, max_len=None, seq_len=None, pos=None):
+        m = self.max_len if max_len is None else max_len
+        n = prcr.weights_workspace_size(self.cfg, len(self.lens), self.H * self.g, m)
+        ws = torch.full((max(n, 16),), 0xff, dtype=torch.uint8, device=DEV)
+        prcr.accumulate_weights(self.cfg, self.cache.desc(), self.q, torch.as_tensor(self.pos if pos is None else pos).to(DEV),
+                                i32(self.lens) if seq_len is None else seq_len, m, self.score, self.status, decay, ws)
+        torch.cuda.synchronize()
+        return int(self.status.item())
+
+    def check(self, decay=1.0, drop=None, top=None, steps=1):
+        got = self.score.cpu().numpy().astype(np.float64)
+        for b, n in enumerate(self.lens):
+            n = n if top is None else min(n, top)
+            assert np.array_equal(got[b, :, :, n:], self.before[b, :, :, n:], equal_nan=True)
+            for l in range(self.L):
+                if not n:
+                    continue
+                K = U.f64(self.cache.rows(self.cache.k, b, n)[l])
+                keep = np.ones(n, bool) if drop is None else ~drop(b, np.arange(n))
+                w, bar = np.zeros((self.H, n)), np.zeros((self.H, n))
+                if keep.any():
+                    w[:, keep], bar[:, keep] = weights64(U.f64(self.q[b, l]), self.pos[b], K[keep], self.D, self.layout)
+                old = 0.0 if decay == 0 else decay * self.before[b, l, :, :n]
+                ref = old + w
+                assert (np.abs(got[b, l, :, :n] - ref) <= bar + 2.0 ** -22 * (np.abs(old) + w) + 1e-37).all(), (b, l)
+
+
+@pytest.mark.parametrize("H,g,D,L,lens,block", [
+    (8, 4, 128, 2, [1, 0, 300], 16), (4, 7, 128, 1, [933, 17], 0), (2, 1, 64, 3, [129, 128], 7), (1, 8, 128, 2, [2500], 64),
+    (2, 4, 256, 2, [65, 700], 16), (3, 8, 64, 1, [5000, 3], 0), (1, 1, 256, 1, [16, 15, 17, 1], 1), (2, 4, 128, 1, [40000], 16),
+    (8, 4, 128, 36, [200], 16), (2, 3, 128, 1, [20000, 9], 16), (1, 8, 256, 1, [17000], 16),
+], ids=lambda v: str(v))
+def test_weights(H, g, D, L, lens, block):
+    w = Weights(H, g, D, L, lens, block, seed=H + g, gap=8 if block == 7 else 0,
+                layout=prcr.LAYOUT_INTERLEAVED if L == 3 else prcr.LAYOUT_SECTIONED)
+    assert w.run() == 0
+    w.check()
+
+
+def test_weights_decay():
+    w = Weights(2, 4, 128, 1, [300, 20], 16)
+    w.score[0, :, :, :300] = float("nan")  # not read at decay 0
+    w.before = w.score.cpu().numpy().astype(np.float64)
+    assert w.run(decay=0.0) == 0
+    w.check(decay=0.0)
+    w = Weights(2, 4, 64, 2, [300, 20], 0)
+    assert w.run(decay=0.75) == 0
+    w.check(decay=0.75)
+
+
+def test_weights_errors():
+    w = Weights(2, 4, 128, 2, [100, 64], 16, unmapped=[(0, 2), (1, 0), (1, 1), (1, 2), (1, 3)], caps=[112, 64])
+    assert w.run() == prcr.ST_NO_BLOCK
+    w.check(drop=lambda b, s: s // 16 == 2 if b == 0 else s >= 0)
+    w = Weights(2, 4, 128, 1, [100, 64], 16)
+    assert w.run(max_len=70) == prcr.ST_CAPACITY
+    w.check(top=70)
+    w = Weights(2, 4, 64, 1, [100, 64], 0)
+    assert w.run(seq_len=i32([-1, 64])) == prcr.ST_CAPACITY
+    w.lens[0] = 0
+    w.check()
+    for p in (2 ** 31, -2 ** 31):
+        w = Weights(2, 4, 256, 1, [100, 64], 16)
+        assert w.run(pos=np.array([p, w.pos[1]])) == prcr.ST_POS_RANGE
+        w.lens[0] = 0
+        w.check()
+
+
+def test_weights_hidden_slots_do_not_matter():
+    w = Weights(2, 4, 128, 1, [100, 33], 16)
+    for b, n in enumerate(w.lens):
+        w.cache.k[w.cache.where(b, [n, n + 1])] = float("nan")
+    w.cache.v[:] = float("nan")
+    assert w.run() == 0
+    w.check()
+
+
+# ----------------------------------------------------------------------------
+# eviction
+# ----------------------------------------------------------------------------
+class Evict:
+    def __init__(self, H, D, L, lens, block, budget, sink, recent, in_place, seed=0, dst_block=None, caps=None, dst_caps=None, **cache):
+        self.H, self.D, self.L, self.lens = H, D, L, list(lens)
+        self.budget, self.sink, self.recent = budget, sink, recent
+        B = len(lens)
+        self.cfg = U.cfg_of(L, H, D)
+        self.src = Cache(L, H, D, caps or [n + 2 for n in lens], block, seed=seed, **cache)
+        self.dst = self.src if in_place else Cache(L, H, D, dst_caps or [budget] * B, block if dst_block is None else dst_block, fill=U.CANARY)
+        self.in_place, self.max_len = in_place, max(lens)
+        self.score = torch.rand((B, L, H, self.max_len + 4), generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV)
+        self.status = status_word()
+
+    def run(self, max_len=None, seq_len=None, score_in_place=False):
+        B = len(self.lens)
+        self.k0, self.v0, self.s0 = self.src.k.clone(), self.src.v.clone(), self.score.cpu().numpy()
+        self.dk0, self.dv0 = self.dst.k_all.clone(), self.dst.v_all.clone()
+        self.keep = torch.full((B, self.L, self.H, self.budget), -99, dtype=torch.int32, device=DEV)
+        self.len_out = torch.full((B,), -99, dtype=torch.int32, device=DEV)
+        self.out = self.score if score_in_place else torch.full_like(self.score, U.CANARY)
+        prcr.evict(self.cfg, self.src.desc(), i32(self.lens) if seq_len is None else seq_len, self.max_len if max_len is None else max_len,
+                   self.budget, self.sink, self.recent, self.score, self.keep, self.len_out, self.status,
+                   dst=None if self.in_place else self.dst.desc(), score_out=self.out)
+        torch.cuda.synchronize()
+        return int(self.status.item())
+
+    def check(self, broken=()):
+        keep, out = self.keep.cpu().numpy(), self.out.cpu().numpy()
+        want_k, want_v = self.dk0.clone(), self.dv0.clone()
+        row = self.H * self.D
+        wk, wv = (x[..., :row].unflatten(-1, (self.H, self.D)) for x in (want_k, want_v))
+        for b, n in enumerate(self.lens):
+            if b in broken:
+                assert (keep[b] == -1).all() and int(self.len_out[b]) == (n if self.in_place else 0)
+                assert np.array_equal(out[b], self.s0[b] if self.out is self.score else np.full_like(out[b], U.CANARY))
+                continue
+            m = min(n, self.budget)
+            assert int(self.len_out[b]) == m
+            for l in range(self.L):
+                for h in range(self.H):
+                    ref = U.evict64(self.s0[b, l, h], n, self.budget, self.sink, self.recent)
+                    assert list(keep[b, l, h]) == ref + [-1] * (self.budget - m), (b, l, h)
+                    s = np.zeros_like(out[b, l, h])
+                    s[:m] = self.s0[b, l, h][ref]
+                    assert np.array_equal(out[b, l, h], s, equal_nan=True)
+            if m:
+                idx = self.keep[b, :, :, :m].long()  # [L, H, m]
+                for x0, w in ((self.k0, wk), (self.v0, wv)):
+                    rows = x0[self.src.where(b, np.arange(n))]  # [L, n, H, D]
+                    rows = rows.gather(1, idx.transpose(1, 2).unsqueeze(-1).expand(-1, -1, -1, self.D))
+                    w[self.dst.where(b, np.arange(m))] = rows
+        assert torch.equal(self.dst.k_all, want_k) and torch.equal(self.dst.v_all, want_v)
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("H,D,L,lens,block,budget,sink,recent", [
+    (8, 128, 2, [300, 64, 0, 65], 16, 64, 4, 16), (2, 64, 3, [700, 1], 0, 100, 0, 0), (1, 256, 1, [50], 7, 1, 0, 0),
+    (3, 128, 2, [513, 512, 511], 1, 200, 100, 100), (2, 48, 1, [1000, 90], 32, 333, 7, 50), (1, 16, 1, [5000], 0, 4999, 2, 9),
+    (4, 128, 28, [130, 40], 16, 33, 1, 0), (1, 128, 1, [40000], 16, 3001, 5, 700), (2, 128, 1, [2000], 16, 1, 0, 1),
+], ids=lambda v: str(v))
+def test_evict(H, D, L, lens, block, budget, sink, recent, in_place):
+    e = Evict(H, D, L, lens, block, budget, sink, recent, in_place, seed=H + D, gap=8 if block == 32 else 0)
+    assert e.run(score_in_place=in_place) == 0
+    e.check()
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_evict_ties_and_odd_scores(in_place):
+    """Equal scores, zeros of both signs, infinities and NaN."""
+    e = Evict(2, 64, 2, [400, 300], 16, 120, 3, 10, in_place, seed=2)
+    rng = np.random.default_rng(0)
+    s = rng.choice([0.0, -0.0, 0.25, 0.5, np.inf, -np.inf, np.nan, -1.0, 1e-40, -1e-40], size=tuple(e.score.shape)).astype(np.float32)
+    s[1] = 0.25  # all equal
+    s[0, 1] = np.nan
+    e.score.copy_(torch.from_numpy(s))
+    assert e.run() == 0
+    e.check()
+
+
+def test_evict_into_another_kind_of_cache():
+    e = Evict(2, 128, 2, [400, 90], 16, 120, 3, 10, False, dst_block=0)
+    assert e.run() == 0
+    e.check()
+    e = Evict(2, 128, 2, [400, 90], 0, 120, 3, 10, False, dst_block=5)
+    assert e.run() == 0
+    e.check()
+
+
+def test_evict_errors():
+    """A sequence with a fault is left as it was, the others are cut."""
+    for in_place in (True, False):
+        e = Evict(2, 64, 2, [200, 150, 90], 16, 60, 2, 8, in_place, unmapped=[(1, 3)])
+        assert e.run(score_in_place=in_place) == prcr.ST_NO_BLOCK
+        e.check(broken=[1])
+        e = Evict(2, 64, 2, [200, 150, 90], 0, 60, 2, 8, in_place)
+        assert e.run(max_len=180, score_in_place=in_place) == prcr.ST_CAPACITY
+        e.check(broken=[0])
+        e = Evict(2, 64, 2, [200, 150, 90], 0, 60, 2, 8, in_place)
+        e.lens[2] = -4
+        assert e.run(seq_len=i32(e.lens)) == prcr.ST_CAPACITY
+        e.check(broken=[2])
+    e = Evict(2, 64, 2, [200, 150], 16, 60, 2, 8, False, dst_caps=[64, 48])  # the second's table has a fourth block unmapped
+    assert e.run() == prcr.ST_NO_BLOCK
+    e.check(broken=[1])
+    e = Evict(2, 64, 2, [200, 150], 0, 60, 2, 8, False, dst_caps=[59, 59])
+    assert e.run() == prcr.ST_CAPACITY
+    e.check(broken=[0, 1])
+
+
+# ----------------------------------------------------------------------------
+# together
+# ----------------------------------------------------------------------------
+@pytest.mark.parametrize("H,g,D,block", [(4, 4, 128, 16), (2, 7, 64, 0), (1, 8, 256, 7)])
+def test_a_dialogue(H, g, D, block):
+    """Prompts appended and attended over, decode steps with weights added up, an eviction, and more tokens over what is
+    left: every attention against the 64-bit formula on rows that the test follows by itself."""
+    L, prompts, steps, budget = 2, [90, 41], 3, 48
+    B, Hq = len(prompts), H * g
+    c = U.cfg_of(L, H, D)
+    cache = Cache(L, H, D, [120, 120], block, fill=0.0)
+    st = status_word()
+    length, nxt = i32([0, 0]), [0, 0]
+    rows = [[[[] for _ in range(H)] for _ in range(L)] for _ in range(B)]  # (key, value) of each slot, 64 bits
+    score = torch.zeros((B, L, H, 120), device=DEV)
+    ref_score = [[[[] for _ in range(H)] for _ in range(L)] for _ in range(B)]
+    sizes = [prompts] + [[1, 1]] * steps + ["evict", [5, 1]]
+    for turn, new in enumerate(sizes):
+        if new == "evict":
+            keep = torch.zeros((B, L, H, budget), dtype=torch.int32, device=DEV)
+            out = torch.zeros_like(length)
+            top = int(length.max())
+            prcr.evict(c, cache.desc(), length, top, budget, 2, 6, score, keep, out, st)
+            for b in range(B):
+                n = int(length[b])
+                for l in range(L):
+                    for h in range(H):
+                        got = [int(i) for i in keep[b, l, h] if i >= 0]
+                        s = score_before = np.array(ref_score[b][l][h])
+                        assert len(got) == min(n, budget) and got == sorted(set(got))
+                        if n > budget:  # the kept ones are the best but for scores closer than float32 tells apart
+                            free = [i for i in got if 2 <= i < n - 6]
+                            lost = [i for i in range(2, n - 6) if i not in got]
+                            assert set(range(2)) <= set(got) and set(range(n - 6, n)) <= set(got)
+                            assert s[free].min() >= s[lost].max() * (1 - 1e-4)
+                        rows[b][l][h] = [rows[b][l][h][i] for i in got]
+                        ref_score[b][l][h] = [score_before[i] for i in got]
+            length = out
+            continue
+        T, off = sum(new), U.offsets(new)
+        pos = np.concatenate([positions(n, nxt[b], None) if n > 1 else np.full((1, 3), nxt[b]) for b, n in enumerate(new)]).astype(np.int32)
+        for b, n in enumerate(new):
+            nxt[b] += n + 12
+        ks, vs = normal((L, T, H, D), 50 + turn), normal((L, T, H, D), 70 + turn)
+        out_len = torch.zeros_like(length)
+        prcr.append_kv(c, cache.desc(), 0, ks, vs, i32(pos), off, length, out_len, st)
+        length = out_len
+        kr = U.rope64(U.f64(ks), pos, D)
+        at = 0
+        for b, n in enumerate(new):
+            for l in range(L):
+                for h in range(H):
+                    rows[b][l][h] += [(kr[l, at + i, h], U.f64(vs[l, at + i, h])) for i in range(n)]
+                    ref_score[b][l][h] += [0.0] * n
+            at += n
+        top = int(length.max())
+        q = normal((L, T, Hq, D), 90 + turn)
+        out = torch.zeros((L, T, Hq, D), dtype=torch.bfloat16, device=DEV)
+        for l in range(L):
+            ws = torch.empty(max(16, prcr.chunk_workspace_size(c, B, Hq, T, top)), dtype=torch.uint8, device=DEV)
+            prcr.chunk_attention(c, cache.desc(), l, q[l], i32(pos), off, length, top, out[l], st, ws)
+        if turn:  # a decode step: its weights too
+            ql = torch.stack([q[:, int(off[b + 1]) - 1] for b in range(B)])
+            p = torch.tensor([int(pos[int(off[b + 1]) - 1, 0]) for b in range(B)], device=DEV)
+            ws = torch.empty(prcr.weights_workspace_size(c, B, Hq, top), dtype=torch.uint8, device=DEV)
+            prcr.accumulate_weights(c, cache.desc(), ql.contiguous(), p, length, top, score, st, 1.0, ws)
+        torch.cuda.synchronize()
+        assert int(st.item()) == 0
+        at = 0
+        for b, n in enumerate(new):
+            for l in range(L):
+                # the cache's keys are the rotated ones rounded to bf16
+                K = np.stack([np.stack([r[0] for r in rows[b][l][h]]) for h in range(H)], 1)
+                K = U.f64(torch.from_numpy(K).float().bfloat16())
+                V = np.stack([np.stack([r[1] for r in rows[b][l][h]]) for h in range(H)], 1)
+                S = K.shape[0]
+                assert S == int(length[b])
+                ref, bar = U.chunk64(U.f64(q[l, at:at + n]), pos[at:at + n], K, V, U.causal(n, S, S))
+                d = np.abs(U.f64(out[l, at:at + n]) - ref)
+                assert (d <= bar).all(), (turn, b, l, (d / bar).max())
+                if turn:
+                    w, _ = weights64(U.f64(ql[b, l]), int(p[b]), K, D, prcr.LAYOUT_SECTIONED)
+                    for h in range(H):
+                        ref_score[b][l][h] = list(np.array(ref_score[b][l][h]) + w[h])
+            at += n
