@@ -38,6 +38,24 @@ bool heads_ok(const prcr_rope_cfg* cfg, int32_t n_q_heads) {
            int64_t(n_q_heads) * D <= PRCR_DECODE_MAX_Q_ELEMS;
 }
 
+// How a chunk call splits the slot axis: where its tiles of rows are fewer than
+// the SMs, into parts of whole 128-slot tiles.
+struct ChunkSplit {
+    int64_t items, splits, len;
+    size_t bytes;  // of the partials of this call, and of any shorter max_len
+};
+ChunkSplit chunk_split(const prcr_rope_cfg* cfg, int64_t n_seqs, int64_t n_q_heads, int64_t total_q, int64_t max_len, int sms) {
+    const int64_t group = n_q_heads / cfg->n_kv_heads;
+    ChunkSplit c;
+    c.items = total_q * group / chunk_rows(cfg->head_dim) + std::min(n_seqs, total_q);
+    const int64_t units = c.items * cfg->n_kv_heads, tiles = std::max<int64_t>(1, (max_len + 127) / 128);
+    const int64_t most = std::max<int64_t>(1, std::min(tiles, sms / units));
+    c.len = (tiles + most - 1) / most * 128;
+    c.splits = (tiles * 128 + c.len - 1) / c.len;
+    c.bytes = most > 1 ? size_t(total_q) * n_q_heads * most * (cfg->head_dim + 2) * sizeof(float) : 0;
+    return c;
+}
+
 size_t weights_bytes(const prcr_rope_cfg* cfg, int64_t n_seqs, int64_t n_q_heads, int64_t max_len) {
     return size_t(n_seqs) * cfg->n_layers * n_q_heads * max_len * sizeof(float);
 }
@@ -110,7 +128,9 @@ int prcr_append_kv(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, int32
 size_t prcr_chunk_workspace_size(const prcr_rope_cfg* cfg, int32_t n_seqs, int32_t n_q_heads, int32_t total_q,
                                  int64_t max_len) {
     if (check_cfg(cfg) || n_seqs < 1 || total_q < 1 || max_len < 1 || !heads_ok(cfg, n_q_heads)) return 0;
-    return 0;
+    int dev = 0, sms = 1;
+    if (cudaGetDevice(&dev) == cudaSuccess) sms = sm_count(dev);
+    return chunk_split(cfg, n_seqs, n_q_heads, total_q, max_len, sms).bytes;
 }
 
 int prcr_chunk_attention(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, int32_t n_seqs, int32_t layer,
@@ -131,9 +151,22 @@ int prcr_chunk_attention(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache,
     if (!aligned16(q) || !aligned16(out) || !mult8(q_token_stride) || !mult8(out_token_stride) || !aligned4(coords) ||
         !aligned4(q_off) || !aligned4(seq_len) || !aligned4(status))
         return PRCR_EALIGN;
-    (void)workspace;
-    (void)workspace_bytes;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return PRCR_ECUDA;
+    const ChunkSplit split = chunk_split(cfg, n_seqs, n_q_heads, total_q, max_len, sm_count(dev));
+    if (int64_t(total_q) * n_q_heads > INT32_MAX || split.items * cfg->n_kv_heads * split.splits > INT32_MAX)
+        return PRCR_EINVAL;  // rows, grid x
     ChunkArgs a = {};
+    if (split.splits > 1) {
+        const size_t rows = size_t(total_q) * n_q_heads * split.splits;
+        if (!workspace || workspace_bytes < rows * (cfg->head_dim + 2) * sizeof(float)) return PRCR_EWORKSPACE;
+        if (!aligned16(workspace)) return PRCR_EALIGN;
+        a.partial = static_cast<float*>(workspace);
+        a.partial_ml = reinterpret_cast<float2*>(a.partial + rows * cfg->head_dim);
+    }
+    a.items = int32_t(split.items);
+    a.splits = int32_t(split.splits);
+    a.split_len = split.len;
     a.cache = cache_view(cache, layer);
     a.q = static_cast<const uint16_t*>(q);
     a.q_stride = q_token_stride;

@@ -1,20 +1,65 @@
 // Attention of a packed batch's new tokens over the decoder cache, one layer:
 // query i of the n_b new tokens of sequence b sees the slots up to its own,
 //   out = softmax(RoPE(q, (t, h, w)) K^T / sqrt(D)) V over slots [0, len_b - n_b + i].
+//
+// The query heads of a KV head's group share its keys, so a sequence's rows for
+// one KV head are (token, head of the group) pairs, tokens first: row r is token
+// r / group. A CTA takes 128 NQ consecutive rows of one sequence and KV head
+// and walks the slots in tiles of 128:
+//   S = Q K^T and O += P V on the tensor cores (tcgen05, 128 x 128 x 16 steps,
+//   bf16 in, float32 out), the accumulators in tensor memory;
+//   P = exp2(S scale - m) by one thread per row, written back over S as bf16.
+// Roles: 4 warps of softmax per 128 rows, 4 warps that copy K and V rows, and one
+// thread that issues the matrix instructions.
+//  - head_dim 64 and 128 (NQ = 2): while the tensor cores work for one half of the
+//    rows, the other half's softmax runs.
+//  - head_dim 256 (NQ = 1, its accumulator is 256 columns): two S buffers; the next
+//    tile's S is made before this tile's O.
+// The running maximum m is only raised when it grows by more than 8 (in log2
+// units): P then holds values up to 2^8, which bf16 represents as exactly as
+// values up to 1, the sums are float32, and the accumulator is rarely read back
+// to be scaled.
+// Roundings to bf16: the rotated query and P are tensor-core operands. Each is
+// off by at most 2^-8 of its value, unbiased, as much as the output's own.
+//
+// Slots that a row does not see are masked before the exponential, so P is 0
+// there; 0 times an infinity or NaN of a hidden value row would still reach O.
+// Rows behind the sequence's length are never loaded (zeros are); a row of
+// later tokens can only matter if its value is not finite, and then the row's
+// result is not finite: such rows are computed again, in float32, from their
+// own slots alone. The same path serves a tile with an unmapped block.
 #include "prcr_cache.cuh"
 #include "prcr_pdl.cuh"
+#include "prcr_tc.cuh"
 
 namespace prcr {
 namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
+constexpr int kTile = 128;  // slots a tile
+constexpr float kRaise = 8.0f;
+
+template <int D, int NQ>
+struct ChunkShape {
+    static constexpr int kDims = D < 128 ? D : 128;      // dims of a ring entry
+    static constexpr int kParts = D / kDims;             // entries of a K (or V) tile
+    static constexpr int kPanel = kTile * 128;           // bytes: 64 dims of 128 rows
+    static constexpr int kEntry = kTile * kDims * 2;
+    static constexpr int kQTile = 128 * D * 2;
+    static constexpr int kStages = D == 64 ? 6 : 5;
+    static constexpr int kLag = 3;                       // entries in flight per loading warp
+    static constexpr int kSoftWarps = 4 * NQ;
+    static constexpr int kThreads = (kSoftWarps + 8) * 32;
+    static constexpr int kRows = 128 * NQ;
+    static constexpr size_t kSmem = 1024 + size_t(NQ) * kQTile + size_t(kStages) * kEntry;
+};
 
 // One query row by one warp in float32: online softmax over slots
 // [lo, hi), E dims a lane (dims lane * E ..). m is in units of log2.
 template <int D>
-__device__ __forceinline__ void row_attention(const ChunkArgs& a, int b, int t, int hq, int64_t lo, int64_t hi,
-                                              float& m, float& l, float (&o)[D / 32], uint32_t& err) {
-    constexpr int E = D / 32, P = D / 2;
+__device__ __noinline__ void row_attention(const ChunkArgs& a, int b, int t, int hq, int64_t lo, int64_t hi,
+                                           float& m, float& l, float (&o)[D / 32], uint32_t& err) {
+    constexpr int E = D / 32;
     const int lane = threadIdx.x & 31;
     const int kh = hq / a.group;
     const uint16_t* qr = a.q + int64_t(t) * a.q_stride + int64_t(hq) * D + lane * E;
@@ -52,47 +97,588 @@ __device__ __forceinline__ void row_attention(const ChunkArgs& a, int b, int t, 
     }
 }
 
-// The slots that token t of sequence b sees (at most the capacity and max_len).
-__device__ __forceinline__ int64_t visible(const ChunkArgs& a, int b, int t, uint32_t& err) {
-    const int64_t len = a.seq_len[b], top = min(a.cache.capacity, a.max_len);
-    if (len < 0 || len > top) err |= PRCR_ST_CAPACITY;
-    return max(int64_t(0), min(top, len - (a.q_off[b + 1] - 1 - t)));
+// What a CTA works on, and the barriers of its roles.
+struct ChunkWork {
+    int b, row0, rows, t0;        // sequence, first row, rows, the sequence's first token
+    int64_t first;                // slots that the sequence's token 0 sees - 1 (may be negative)
+    int64_t lo, hi;               // slots of this CTA
+    int tiles[2];                 // tiles of each 128 rows
+    uint32_t tmem;
+    int fail, unmapped;
+};
+struct ChunkBars {
+    uint64_t full[6], empty[6], q, s[2], p[2], o[2];
+};
+
+template <int D, int NQ>
+__global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(const __grid_constant__ ChunkArgs a) {
+    using Sh = ChunkShape<D, NQ>;
+    constexpr int P = D / 2, ST = Sh::kStages, PARTS = Sh::kParts, DIMS = Sh::kDims;
+    constexpr int kSoft = Sh::kSoftWarps;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ ChunkWork w;
+    __shared__ __align__(8) ChunkBars bars;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    // 1024-byte aligned: the swizzle goes by address bits
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t q_s = base, ring = base + NQ * Sh::kQTile;
+    const int G = a.group, H = a.n_kv_heads;
+    const int kh = int(blockIdx.x % unsigned(H));
+    const int rest = int(blockIdx.x / unsigned(H));
+    const int split = rest % a.splits;
+    int item = rest / a.splits;
+
+    pdl_allow();
+    if (tid == 0) {
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(smem_u32(&bars.full[i]), 4);
+            mbar_init(smem_u32(&bars.empty[i]), 1);
+        }
+        mbar_init(smem_u32(&bars.q), kSoft);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&bars.s[i]), 1);
+            mbar_init(smem_u32(&bars.p[i]), 4);
+            mbar_init(smem_u32(&bars.o[i]), 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        w.fail = 0;
+        w.unmapped = 0;
+    }
+    if (warp == kSoft + 4) tmem_alloc(smem_u32(&w.tmem), 512);
+    pdl_wait();
+
+    // this CTA's rows: items are tiles of 128 NQ rows, a sequence's last one
+    // (which sees the most slots) first
+    if (warp == 0) {
+        int before = 0, b = -1, cnt = 0, local = 0;
+        for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
+            int c = 0;
+            if (b0 + lane < a.n_seqs) {
+                const int64_t n = int64_t(a.q_off[b0 + lane + 1]) - a.q_off[b0 + lane];
+                c = n > 0 ? int((min(n, int64_t(a.total_q)) * G + Sh::kRows - 1) / Sh::kRows) : 0;
+            }
+            int upto = c;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(kFull, upto, d);
+                if (lane >= d) upto += o;
+            }
+            const bool here = item >= before + upto - c && item < before + upto;
+            const uint32_t who = __ballot_sync(kFull, here);
+            if (who) {
+                const int src = __ffs(int(who)) - 1;
+                b = b0 + src;
+                cnt = __shfl_sync(kFull, c, src);
+                local = item - before - __shfl_sync(kFull, upto - c, src);
+                break;
+            }
+            before += __shfl_sync(kFull, upto, 31);
+        }
+        if (lane == 0) {
+            w.b = b;
+            if (b >= 0) {
+                const int t0 = a.q_off[b], n = a.q_off[b + 1] - t0;
+                const int64_t len = a.seq_len[b], top = min(a.cache.capacity, a.max_len);
+                if (len < 0 || len > top) atomicOr(a.status, PRCR_ST_CAPACITY);
+                w.t0 = t0;
+                w.row0 = (cnt - 1 - local) * Sh::kRows;
+                w.rows = min(Sh::kRows, n * G - w.row0);
+                w.first = len - n;
+                w.lo = int64_t(split) * a.split_len;
+                int64_t hi = 0;
+                for (int q = 0; q < 2; ++q) {
+                    w.tiles[q] = 0;
+                    if (q < NQ && q * 128 < w.rows) {
+                        const int last = (w.row0 + min(w.rows, q * 128 + 128) - 1) / G;
+                        hi = min(min(top, w.first + last + 1), w.lo + a.split_len);
+                        w.tiles[q] = hi > w.lo ? int((hi - w.lo + kTile - 1) / kTile) : 0;
+                    }
+                }
+                w.hi = hi;
+            }
+        }
+    }
+    tc_fence_before();
+    const bool bad = __syncthreads_or(bad_offsets(a.q_off, a.n_seqs, a.total_q));
+    tc_fence_after();
+    if (bad && blockIdx.x == 0 && tid == 0) atomicOr(a.status, PRCR_ST_CSR);
+    const int nt = max(w.tiles[0], w.tiles[1]);
+    const uint32_t tmem = w.tmem;
+    const bool work = !bad && w.b >= 0 && w.rows > 0;
+    uint16_t* const out = a.out + int64_t(w.t0) * a.out_stride + int64_t(kh) * G * D;
+    bool failed = false;
+    float m_run = -INFINITY, l_run = 0.0f;
+
+    // Registers: 2 x 4 warps of 192 and 8 of 64 are the 16 of 128 that the CTA was
+    // launched with (NQ = 1: 4 of 232 and 8 of 136 are the 12 of 168).
+    // (Each role ends at the same two barriers, on its own way.)
+    if (work) {
+        if (warp < kSoft) {
+            if constexpr (NQ == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+            else asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+          if (nt > 0) {
+            // queries: rotated, rounded to bf16, into 128-byte rows of swizzled panels. A
+            // thread takes eight pairs of a token for all heads of the group. The
+            // angle is exact modulo one turn in integers; sin and cos are the fast
+            // ones (2^-20, where bf16 keeps 2^-9).
+            {
+                const int tok0 = w.row0 / G, n_tok = (w.row0 + w.rows - 1) / G - tok0 + 1;
+                constexpr int CH = P / 8;
+                for (int it = tid; it < n_tok * CH; it += kSoft * 32) {
+                    const int tok = tok0 + it / CH, pc = it % CH;
+                    const int64_t t = int64_t(w.t0) + tok;
+                    float c[8], s[8];
+                    int pos[3];
+#pragma unroll
+                    for (int x = 0; x < 3; ++x) pos[x] = a.coords[3 * t + x];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const int i = pc * 8 + u;
+                        const int ax = pair_axis(i, a.layout, a.sec_t, a.sec_h, a.sec_w);
+                        const int p = ax == 0 ? pos[0] : ax == 1 ? pos[1] : pos[2];
+                        const int frac = int(uint32_t((uint64_t(int64_t(p)) * a.turn_freq[i]) >> 32));
+                        __sincosf(float(frac) * 1.46291807926715968e-09f, &s[u], &c[u]);
+                    }
+                    const uint16_t* src = a.q + t * a.q_stride + int64_t(kh) * G * D + pc * 8;
+                    for (int g = 0; g < G; ++g) {
+                        const int r = tok * G + g - w.row0;
+                        if (r < 0 || r >= w.rows) continue;
+                        const uint4 x = ld_stream(src + g * D), y = ld_stream(src + g * D + P);
+                        uint4 xo, yo;
+                        rotate_vec(x, y, c, s, xo, yo);
+                        const uint32_t row = q_s + uint32_t(r >> 7) * Sh::kQTile + uint32_t(r & 127) * 128;
+                        const int cx = pc, cy = pc + CH, sw = r & 7;
+                        const uint32_t ax_ = row + uint32_t(cx >> 3) * Sh::kPanel + uint32_t(((cx & 7) ^ sw) * 16);
+                        const uint32_t ay_ = row + uint32_t(cy >> 3) * Sh::kPanel + uint32_t(((cy & 7) ^ sw) * 16);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ax_), "r"(xo.x), "r"(xo.y),
+                                     "r"(xo.z), "r"(xo.w)
+                                     : "memory");
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ay_), "r"(yo.x), "r"(yo.y),
+                                     "r"(yo.z), "r"(yo.w)
+                                     : "memory");
+                    }
+                }
+                // rows behind the last one: zeros
+                for (int it = w.rows * (D / 8) + tid; it < Sh::kRows * (D / 8); it += kSoft * 32) {
+                    const int r = it / (D / 8), c = it % (D / 8);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(
+                                     q_s + uint32_t(r >> 7) * Sh::kQTile + uint32_t(c >> 3) * Sh::kPanel +
+                                     uint32_t(r & 127) * 128 + uint32_t((c & 7) * 16)),
+                                 "r"(0)
+                                 : "memory");
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars.q));
+            }
+
+            // softmax of row `tid & 127` of the 128 rows that this warp belongs to
+            const int qi = warp >> 2;
+            const int r = tid;  // row of the CTA
+            const int64_t lim = min(w.hi, w.first + (w.row0 + min(r, w.rows - 1)) / G + 1);  // slots that the row sees
+            const int64_t lim_lo = __shfl_sync(kFull, lim, 0);                    // the warp's least
+            const uint32_t lanes = uint32_t(warp & 3) << 21;                      // TMEM lanes of this warp
+            const uint32_t o_t = tmem + 256 + uint32_t(qi) * D + lanes;
+            const float scale = a.scale_log2;
+            for (int j = 0; j < w.tiles[qi]; ++j) {
+                const int buf = NQ == 2 ? qi : (j & 1);
+                const uint32_t ph = NQ == 2 ? uint32_t(j & 1) : uint32_t((j >> 1) & 1);
+                const uint32_t s_t = tmem + uint32_t(buf) * 128 + lanes;
+                if (!mbar_wait(smem_u32(&bars.s[buf]), ph)) {
+                    failed = true;
+                    break;
+                }
+                tc_fence_after();
+                uint32_t s[128];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tmem_ld32(s_t + 32 * i, s + 32 * i);
+                tmem_wait_ld();
+                const int64_t at = w.lo + int64_t(j) * kTile;
+                if (at + kTile > lim_lo) {  // some row of the warp does not see all of the tile
+                    const int n = int(max(int64_t(0), min(int64_t(kTile), lim - at)));
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (i >= n) s[i] = 0xff800000u;
+                }
+                float x0 = __uint_as_float(s[0]), x1 = __uint_as_float(s[1]), x2 = __uint_as_float(s[2]),
+                      x3 = __uint_as_float(s[3]);
+#pragma unroll
+                for (int i = 4; i < 128; i += 4) {
+                    x0 = fmaxf(x0, __uint_as_float(s[i]));
+                    x1 = fmaxf(x1, __uint_as_float(s[i + 1]));
+                    x2 = fmaxf(x2, __uint_as_float(s[i + 2]));
+                    x3 = fmaxf(x3, __uint_as_float(s[i + 3]));
+                }
+                const float mt = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3)) * scale;
+                const bool raise = mt > m_run + kRaise || m_run == -INFINITY;
+                if (j == 0) {
+                    m_run = mt;
+                } else if (__any_sync(kFull, raise && mt > m_run)) {
+                    if (NQ == 1 && !mbar_wait(smem_u32(&bars.o[0]), uint32_t((j - 1) & 1))) {
+                        failed = true;
+                        break;
+                    }
+                    tc_fence_after();
+                    float f = 1.0f;
+                    if (raise && mt > m_run) {
+                        f = exp2_fast(m_run - mt);
+                        m_run = mt;
+                    }
+                    l_run *= f;
+                    const uint64_t f2 = pair64(f, f);
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(o_t + c, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            const uint64_t y = mul2(uint64_t(o[i]) | (uint64_t(o[i + 1]) << 32), f2);
+                            o[i] = uint32_t(y);
+                            o[i + 1] = uint32_t(y >> 32);
+                        }
+                        tmem_st32(o_t + c, o);
+                    }
+                }
+                const float mu = m_run == -INFINITY ? 0.0f : m_run;
+                const uint64_t c2 = pair64(scale, scale), m2 = pair64(-mu, -mu);
+                uint64_t sum0 = 0, sum1 = 0;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const int k = half * 64 + 2 * i;
+                        const uint64_t x = fma2(uint64_t(s[k]) | (uint64_t(s[k + 1]) << 32), c2, m2);
+                        const float e0 = exp2_fast(lo32(x)), e1 = exp2_fast(hi32(x));
+                        const uint64_t e = pair64(e0, e1);
+                        if (i & 1) sum1 = add2(sum1, e);
+                        else sum0 = add2(sum0, e);
+                        p[i] = pack_bf16x2(e0, e1);
+                    }
+                    tmem_st32(s_t + 32 * half, p);
+                }
+                const uint64_t sum = add2(sum0, sum1);
+                l_run += lo32(sum) + hi32(sum);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars.p[buf]));
+            }
+            // all of this half's products are done
+            if (!failed && w.tiles[qi] > 0) {
+                const uint32_t ph = NQ == 2 ? 0u : uint32_t((w.tiles[0] - 1) & 1);
+                if (!mbar_wait(smem_u32(&bars.o[qi]), ph)) failed = true;
+                tc_fence_after();
+            }
+          }
+            if (failed) w.fail = 1;
+            __syncthreads();
+            if (w.fail) {
+                if (tid == 0) atomicOr(a.status, PRCR_ST_TIMEOUT);
+            } else {
+        // results: a thread per row
+        const int qi = warp >> 2, r = tid;
+        const bool row_ok = r < w.rows;
+        const int rr = w.row0 + min(r, w.rows - 1);
+        const int tok = rr / G, g = rr - tok * G;
+        const int64_t lim = min(w.first + tok + 1, w.hi);  // (rows of the other half see no more than w.hi)
+        const uint32_t o_t = tmem + 256 + uint32_t(qi) * D + (uint32_t(warp & 3) << 21);
+        const bool any = w.tiles[qi] > 0;  // this half's accumulator holds something
+        uint16_t* dst = out + int64_t(tok) * a.out_stride + int64_t(g) * D;
+        const int64_t prow = (int64_t(w.t0 + tok) * H + kh) * G + g;  // row of the partials
+        float* po = a.splits > 1 ? a.partial + (prow * a.splits + split) * D : nullptr;
+        const bool live = row_ok && lim > w.lo;
+        const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
+        float odd = l_run * 0.0f;
+        if (any) {
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+                uint32_t o[32];
+                tmem_ld32(o_t + c, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) odd = fmaf(__uint_as_float(o[i]), 0.0f, odd);
+                if (a.splits == 1) {
+                    if (row_ok) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            uint4 v;
+                            v.x = pack_bf16x2(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
+                            v.y = pack_bf16x2(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
+                            v.z = pack_bf16x2(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
+                            v.w = pack_bf16x2(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
+                            st_row(dst + c + i, v);
+                        }
+                    }
+                } else if (live) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4)
+                        *reinterpret_cast<uint4*>(po + c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                }
+            }
+        } else if (row_ok && a.splits == 1) {  // sees no slot
+            for (int c = 0; c < D; c += 8) st_row(dst + c, make_uint4(0, 0, 0, 0));
+        }
+        if (a.splits > 1 && live) a.partial_ml[prow * a.splits + split] = make_float2(m_run, l_run);
+        // rows to be computed again from their own slots
+        uint32_t again = __ballot_sync(kFull, live && any && (odd != 0.0f || w.unmapped));
+        if (w.unmapped && tid == 0) atomicOr(a.status, PRCR_ST_NO_BLOCK);
+        while (again) {
+            const int src = __ffs(int(again)) - 1;
+            again &= again - 1;
+            const int tk = __shfl_sync(kFull, tok, src), gg = __shfl_sync(kFull, g, src);
+            const int64_t lm = __shfl_sync(kFull, lim, src);
+            float m, l, o[D / 32];
+            uint32_t err = 0;
+            row_attention<D>(a, w.b, w.t0 + tk, kh * G + gg, w.lo, lm, m, l, o, err);
+            __syncwarp();
+            constexpr int E = D / 32;
+            if (a.splits == 1) {
+                const float iv = l == 0.0f ? 0.0f : 1.0f / l;
+                uint16_t* d = out + int64_t(tk) * a.out_stride + int64_t(gg) * D + lane * E;
+#pragma unroll
+                for (int i = 0; i < E; i += 2) *reinterpret_cast<uint32_t*>(d + i) = pack_bf16x2(o[i] * iv, o[i + 1] * iv);
+            } else {
+                const int64_t pr = (int64_t(w.t0 + tk) * H + kh) * G + gg;
+                float* d = a.partial + (pr * a.splits + split) * D + lane * E;
+#pragma unroll
+                for (int i = 0; i < E; ++i) d[i] = o[i];
+                if (lane == 0) a.partial_ml[pr * a.splits + split] = make_float2(m, l);
+            }
+        }
+            }
+        } else if (warp < kSoft + 4) {
+            if constexpr (NQ == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+            else asm volatile("setmaxnreg.dec.sync.aligned.u32 136;");
+          if (nt > 0) {
+            // rows of K and V: warp lw copies slots 32 lw .. 32 lw + 31 of every tile,
+            // 16 bytes a lane; slots without a row are zeros
+            const int lw = warp - kSoft;
+            const uint16_t* ck = a.cache.k + int64_t(kh) * D;
+            const uint16_t* cv = a.cache.v + int64_t(kh) * D;
+            constexpr int CPR = DIMS / 8, RPI = 32 / CPR;  // chunks a row, rows an instruction
+            const int c = lane % CPR, rsub = lane / CPR;
+            int e = 0;          // entries issued
+            bool missing = false;
+            auto row_of = [&](int j) -> int64_t {
+                const int64_t slot = w.lo + int64_t(j) * kTile + lw * 32 + lane;
+                if (j >= nt || slot >= w.hi) return -1;
+                uint32_t er = 0;
+                const int64_t row = slot_row(a.cache, w.b, slot, er);
+                missing |= row < 0;
+                return row;
+            };
+            auto put = [&](const uint16_t* src, int64_t row, int part) -> bool {
+                const int st = e % ST;
+                if (e >= ST && !mbar_wait(smem_u32(&bars.empty[st]), uint32_t((e / ST - 1) & 1))) return false;
+                const uint32_t dst = ring + uint32_t(st) * Sh::kEntry + uint32_t(c >> 3) * Sh::kPanel + uint32_t(lw * 32) * 128;
+#pragma unroll
+                for (int i = 0; i < 32 / RPI; ++i) {
+                    const int r = i * RPI + rsub;
+                    const int64_t rr = __shfl_sync(kFull, row, r);
+                    const uint16_t* from = rr >= 0 ? src + rr + part * DIMS + c * 8 : src;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                     dst + uint32_t(r) * 128 + uint32_t(((c & 7) ^ (r & 7)) * 16)),
+                                 "l"(from), "r"(rr >= 0 ? 16 : 0)
+                                 : "memory");
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                if (e >= Sh::kLag) {
+                    asm volatile("cp.async.wait_group %0;" ::"n"(Sh::kLag) : "memory");
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&bars.full[(e - Sh::kLag) % ST]));
+                }
+                ++e;
+                return true;
+            };
+            // in the order of use: K0 V0 K1 V1 .., or with two S buffers K0 K1 V0 K2 V1 ..
+            bool ok = true;
+            int64_t row = row_of(0), next = row_of(1);
+            for (int p = 0; ok && p < PARTS; ++p) ok = put(ck, row, p);
+            for (int j = 0; ok && j < nt; ++j) {
+                if (NQ == 1 && j + 1 < nt)
+                    for (int p = 0; ok && p < PARTS; ++p) ok = put(ck, next, p);
+                for (int p = 0; ok && p < PARTS; ++p) ok = put(cv, row, p);
+                if (NQ == 2 && j + 1 < nt)
+                    for (int p = 0; ok && p < PARTS; ++p) ok = put(ck, next, p);
+                row = next;
+                next = row_of(j + 2);
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0 && ok)
+                for (int i = max(0, e - Sh::kLag); i < e; ++i) mbar_arrive(smem_u32(&bars.full[i % ST]));
+            if (missing) w.unmapped = 1;
+            if (!ok) w.fail = 1;
+          }
+            __syncthreads();
+        } else {
+            if constexpr (NQ == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+            else asm volatile("setmaxnreg.dec.sync.aligned.u32 136;");
+            if (warp == kSoft + 4 && lane == 0 && nt > 0) {
+                constexpr uint32_t id_qk = tc_idesc(kTile, false), id_pv = tc_idesc(DIMS, true);
+                int e = 0;  // entries consumed
+                auto full = [&](int i) { return mbar_wait(smem_u32(&bars.full[i % ST]), uint32_t((i / ST) & 1)); };
+                auto entry = [&](int i) { return ring + uint32_t(i % ST) * Sh::kEntry; };
+                // S of 128 rows: entries e0 .. hold the tile's keys
+                auto qk = [&](int q, int buf, int e0) {
+                    tc_fence_after();
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                        for (int k = 0; k < DIMS / 16; ++k) {
+                            const uint32_t step = uint32_t(k >> 2) * Sh::kPanel + uint32_t(k & 3) * 32;
+                            const uint32_t qa = q_s + uint32_t(q) * Sh::kQTile + uint32_t(part) * (DIMS / 64) * Sh::kPanel + step;
+                            tc_mma_ss(tmem + uint32_t(buf) * 128, tc_desc(qa, 16, 1024),
+                                      tc_desc(entry(e0 + part) + step, 16, 1024), id_qk, part + k > 0);
+                        }
+                };
+                auto pv = [&](int q, int buf, int e0, bool add) {
+                    tc_fence_after();
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                        for (int k = 0; k < kTile / 16; ++k)
+                            tc_mma_ts(tmem + 256 + uint32_t(q) * D + uint32_t(part) * DIMS, tmem + uint32_t(buf) * 128 + uint32_t(k) * 8,
+                                      tc_desc(entry(e0 + part) + uint32_t(k) * 2048, Sh::kPanel, 1024), id_pv, add || k > 0);
+                };
+                auto release = [&](int e0) {
+                    for (int part = 0; part < PARTS; ++part) tc_commit(smem_u32(&bars.empty[(e0 + part) % ST]));
+                };
+                auto ready = [&](int e0) {
+                    bool ok = true;
+                    for (int part = 0; part < PARTS; ++part) ok = ok && full(e0 + part);
+                    return ok;
+                };
+                bool ok = mbar_wait(smem_u32(&bars.q), 0) && ready(0);
+                if (ok) {
+                    for (int q = 0; q < NQ; ++q)
+                        if (w.tiles[q] > 0) {
+                            qk(q, q, 0);
+                            tc_commit(smem_u32(&bars.s[q]));
+                        }
+                    release(0);
+                    e = PARTS;
+                }
+                if constexpr (NQ == 2) {
+                    for (int j = 0; ok && j < nt; ++j) {
+                        const int ev = e, ek = e + PARTS;
+                        ok = ready(ev);
+                        bool have = false;
+                        for (int q = 0; ok && q < 2; ++q) {
+                            if (j >= w.tiles[q]) continue;
+                            ok = mbar_wait(smem_u32(&bars.p[q]), uint32_t(j & 1));
+                            if (!ok) break;
+                            pv(q, q, ev, j > 0);
+                            if (j + 1 < w.tiles[q]) {
+                                if (!have && !(ok = ready(ek))) break;
+                                have = true;
+                                qk(q, q, ek);
+                                tc_commit(smem_u32(&bars.s[q]));
+                            } else {
+                                tc_commit(smem_u32(&bars.o[q]));
+                            }
+                        }
+                        if (ok && j + 1 < nt) {
+                            release(ev);
+                            release(ek);
+                        }
+                        e += 2 * PARTS;
+                    }
+                } else {
+                    for (int j = 0; ok && j < nt; ++j) {
+                        if (j + 1 < nt) {
+                            ok = ready(e);
+                            if (!ok) break;
+                            qk(0, (j + 1) & 1, e);
+                            tc_commit(smem_u32(&bars.s[(j + 1) & 1]));
+                            release(e);
+                            e += PARTS;
+                        }
+                        ok = ready(e) && mbar_wait(smem_u32(&bars.p[j & 1]), uint32_t((j >> 1) & 1));
+                        if (!ok) break;
+                        pv(0, j & 1, e, j > 0);
+                        if (j + 1 < nt) release(e);
+                        tc_commit(smem_u32(&bars.o[0]));
+                        e += PARTS;
+                    }
+                }
+                if (!ok) {  // what was issued ends before the tensor memory is given back
+                    w.fail = 1;
+                    mbar_init(smem_u32(&bars.q), 1);
+                    tc_commit(smem_u32(&bars.q));
+                    mbar_wait(smem_u32(&bars.q), 0);
+                }
+            }
+            __syncwarp();
+            __syncthreads();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == kSoft + 4) tmem_free(tmem, 512);
 }
 
+// Joins the splits of a row: (max, sum, accumulator) of the splits that it sees.
 template <int D>
-__global__ void __launch_bounds__(256) chunk_rows_kernel(const __grid_constant__ ChunkArgs a) {
+__global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant__ ChunkArgs a) {
     constexpr int E = D / 32;
-    const int lane = threadIdx.x & 31;
-    const int Hq = a.n_kv_heads * a.group;
+    const int lane = threadIdx.x & 31, Hq = a.n_kv_heads * a.group;
     const int64_t row = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
     pdl_allow();
     pdl_wait();
-    if (__syncthreads_or(bad_offsets(a.q_off, a.n_seqs, a.total_q))) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.status, PRCR_ST_CSR);
-        return;
-    }
+    if (__syncthreads_or(bad_offsets(a.q_off, a.n_seqs, a.total_q))) return;
     if (row >= int64_t(a.total_q) * Hq) return;
     const int t = int(row / Hq), hq = int(row - int64_t(t) * Hq);
     const int b = sequence_of(a.q_off, a.n_seqs, t);
     if (t >= a.q_off[b + 1]) return;  // behind the last sequence
-    uint32_t err = 0;
-    float m, l, o[E];
-    row_attention<D>(a, b, t, hq, 0, visible(a, b, t, err), m, l, o, err);
+    const int64_t lim = min(min(a.cache.capacity, a.max_len), int64_t(a.seq_len[b]) - (a.q_off[b + 1] - 1 - t));
+    const int n = lim > 0 ? int((lim + a.split_len - 1) / a.split_len) : 0;
+    float m = -INFINITY, l = 0.0f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.0f;
+    for (int s = lane; s < n; s += 32) m = fmaxf(m, a.partial_ml[row * a.splits + s].x);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, d));
+    const float mu = m == -INFINITY ? 0.0f : m;
+    for (int s = 0; s < n; ++s) {
+        const float2 ml = a.partial_ml[row * a.splits + s];
+        const float f = exp2f(ml.x - mu);
+        l = fmaf(f, ml.y, l);
+        const float* p = a.partial + (row * a.splits + s) * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = fmaf(f, p[e], o[e]);
+    }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     uint16_t* out = a.out + int64_t(t) * a.out_stride + int64_t(hq) * D + lane * E;
 #pragma unroll
     for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t*>(out + e) = pack_bf16x2(o[e] * inv, o[e + 1] * inv);
-    if (err && lane == 0) atomicOr(a.status, err);
+}
+
+template <int D, int NQ>
+cudaError_t launch_shape(const ChunkArgs& a, cudaStream_t stream) {
+    using Sh = ChunkShape<D, NQ>;
+    const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(chunk_kernel<D, NQ>), Sh::kSmem);
+    if (e != cudaSuccess) return e;
+    const dim3 grid(unsigned(int64_t(a.items) * a.n_kv_heads * a.splits));
+    const cudaError_t r = launch_pdl(chunk_kernel<D, NQ>, grid, dim3(Sh::kThreads), Sh::kSmem, stream, a);
+    if (r != cudaSuccess || a.splits == 1) return r;
+    const int64_t rows = int64_t(a.total_q) * a.n_kv_heads * a.group;
+    return launch_pdl(chunk_merge_kernel<D>, dim3(unsigned((rows + 7) / 8)), dim3(256), 0, stream, a);
 }
 
 }  // namespace
 
+int chunk_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
+
 cudaError_t launch_chunk(const ChunkArgs& a, cudaStream_t stream) {
-    const int64_t rows = int64_t(a.total_q) * a.n_kv_heads * a.group;
-    const dim3 grid(unsigned((rows + 7) / 8));
-    if (a.head_dim == 64) return launch_pdl(chunk_rows_kernel<64>, grid, dim3(256), 0, stream, a);
-    if (a.head_dim == 128) return launch_pdl(chunk_rows_kernel<128>, grid, dim3(256), 0, stream, a);
-    return launch_pdl(chunk_rows_kernel<256>, grid, dim3(256), 0, stream, a);
+    if (a.head_dim == 64) return launch_shape<64, 2>(a, stream);
+    if (a.head_dim == 128) return launch_shape<128, 2>(a, stream);
+    return launch_shape<256, 1>(a, stream);
 }
 
 }  // namespace prcr
