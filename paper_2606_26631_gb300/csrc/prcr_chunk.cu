@@ -47,7 +47,6 @@ struct ChunkShape {
     static constexpr int kEntry = kTile * kDims * 2;
     static constexpr int kQTile = 128 * D * 2;
     static constexpr int kStages = D == 64 ? 6 : 5;
-    static constexpr int kLag = 3;                       // entries in flight per loading warp
     static constexpr int kSoftWarps = 4 * NQ;
     static constexpr int kThreads = (kSoftWarps + 8) * 32;
     static constexpr int kRows = 128 * NQ;
@@ -97,6 +96,23 @@ __device__ __noinline__ void row_attention(const ChunkArgs& a, int b, int t, int
     }
 }
 
+template <int N>
+__device__ __forceinline__ void store_row(void* p, const uint32_t* v, bool wide) {
+    char* c = static_cast<char*>(p);
+    if (wide) {
+#pragma unroll
+        for (int i = 0; i < N; i += 8)
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(c + 4 * i), "r"(v[i]),
+                         "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]),
+                         "r"(v[i + 7])
+                         : "memory");
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            *reinterpret_cast<uint4*>(c + 4 * i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    }
+}
+
 // What a CTA works on, and the barriers of its roles.
 struct ChunkWork {
     int b, row0, rows, t0;        // sequence, first row, rows, the sequence's first token
@@ -107,7 +123,7 @@ struct ChunkWork {
     int fail, unmapped;
 };
 struct ChunkBars {
-    uint64_t full[6], empty[6], q, s[2], p[2], o[2];
+    uint64_t full[6], empty[6], q, s[2], p[2], o[2], drain;
 };
 
 template <int D, int NQ>
@@ -118,6 +134,7 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
     extern __shared__ unsigned char smem_raw[];
     __shared__ ChunkWork w;
     __shared__ __align__(8) ChunkBars bars;
+    __shared__ uint64_t s_freq[P];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     // 1024-byte aligned: the swizzle goes by address bits
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -126,12 +143,12 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
     const int kh = int(blockIdx.x % unsigned(H));
     const int rest = int(blockIdx.x / unsigned(H));
     const int split = rest % a.splits;
-    int item = rest / a.splits;
+    const int item = rest / a.splits;
 
     pdl_allow();
     if (tid == 0) {
         for (int i = 0; i < ST; ++i) {
-            mbar_init(smem_u32(&bars.full[i]), 4);
+            mbar_init(smem_u32(&bars.full[i]), 128);  // every loading thread's copies
             mbar_init(smem_u32(&bars.empty[i]), 1);
         }
         mbar_init(smem_u32(&bars.q), kSoft);
@@ -145,16 +162,20 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
         w.unmapped = 0;
     }
     if (warp == kSoft + 4) tmem_alloc(smem_u32(&w.tmem), 512);
+    if (tid < P) s_freq[tid] = a.turn_freq[tid];
     pdl_wait();
 
     // this CTA's rows: items are tiles of 128 NQ rows, a sequence's last one
     // (which sees the most slots) first
     if (warp == 0) {
-        int before = 0, b = -1, cnt = 0, local = 0;
+        int before = 0, b = -1, cnt = 0, local = 0, off = 0, end = 0, len = 0;
         for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
             int c = 0;
             if (b0 + lane < a.n_seqs) {
-                const int64_t n = int64_t(a.q_off[b0 + lane + 1]) - a.q_off[b0 + lane];
+                off = a.q_off[b0 + lane];
+                end = a.q_off[b0 + lane + 1];
+                len = a.seq_len[b0 + lane];
+                const int64_t n = int64_t(end) - off;
                 c = n > 0 ? int((min(n, int64_t(a.total_q)) * G + Sh::kRows - 1) / Sh::kRows) : 0;
             }
             int upto = c;
@@ -170,6 +191,9 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                 b = b0 + src;
                 cnt = __shfl_sync(kFull, c, src);
                 local = item - before - __shfl_sync(kFull, upto - c, src);
+                off = __shfl_sync(kFull, off, src);
+                end = __shfl_sync(kFull, end, src);
+                len = __shfl_sync(kFull, len, src);
                 break;
             }
             before += __shfl_sync(kFull, upto, 31);
@@ -177,13 +201,13 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
         if (lane == 0) {
             w.b = b;
             if (b >= 0) {
-                const int t0 = a.q_off[b], n = a.q_off[b + 1] - t0;
-                const int64_t len = a.seq_len[b], top = min(a.cache.capacity, a.max_len);
+                const int t0 = off, n = end - off;
+                const int64_t top = min(a.cache.capacity, a.max_len);
                 if (len < 0 || len > top) atomicOr(a.status, PRCR_ST_CAPACITY);
                 w.t0 = t0;
                 w.row0 = (cnt - 1 - local) * Sh::kRows;
                 w.rows = min(Sh::kRows, n * G - w.row0);
-                w.first = len - n;
+                w.first = int64_t(len) - n;
                 w.lo = int64_t(split) * a.split_len;
                 int64_t hi = 0;
                 for (int q = 0; q < 2; ++q) {
@@ -223,39 +247,52 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
             // ones (2^-20, where bf16 keeps 2^-9).
             {
                 const int tok0 = w.row0 / G, n_tok = (w.row0 + w.rows - 1) / G - tok0 + 1;
-                constexpr int CH = P / 8;
+                constexpr int CH = P / 8, BATCH = 4;  // heads whose loads are in flight together
                 for (int it = tid; it < n_tok * CH; it += kSoft * 32) {
                     const int tok = tok0 + it / CH, pc = it % CH;
                     const int64_t t = int64_t(w.t0) + tok;
-                    float c[8], s[8];
+                    const uint16_t* src = a.q + t * a.q_stride + int64_t(kh) * G * D + pc * 8;
                     int pos[3];
 #pragma unroll
                     for (int x = 0; x < 3; ++x) pos[x] = a.coords[3 * t + x];
+                    float c[8], s[8];
+                    for (int g0 = 0; g0 < G; g0 += BATCH) {
+                        uint4 x[BATCH], y[BATCH];
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        const int i = pc * 8 + u;
-                        const int ax = pair_axis(i, a.layout, a.sec_t, a.sec_h, a.sec_w);
-                        const int p = ax == 0 ? pos[0] : ax == 1 ? pos[1] : pos[2];
-                        const int frac = int(uint32_t((uint64_t(int64_t(p)) * a.turn_freq[i]) >> 32));
-                        __sincosf(float(frac) * 1.46291807926715968e-09f, &s[u], &c[u]);
-                    }
-                    const uint16_t* src = a.q + t * a.q_stride + int64_t(kh) * G * D + pc * 8;
-                    for (int g = 0; g < G; ++g) {
-                        const int r = tok * G + g - w.row0;
-                        if (r < 0 || r >= w.rows) continue;
-                        const uint4 x = ld_stream(src + g * D), y = ld_stream(src + g * D + P);
-                        uint4 xo, yo;
-                        rotate_vec(x, y, c, s, xo, yo);
-                        const uint32_t row = q_s + uint32_t(r >> 7) * Sh::kQTile + uint32_t(r & 127) * 128;
-                        const int cx = pc, cy = pc + CH, sw = r & 7;
-                        const uint32_t ax_ = row + uint32_t(cx >> 3) * Sh::kPanel + uint32_t(((cx & 7) ^ sw) * 16);
-                        const uint32_t ay_ = row + uint32_t(cy >> 3) * Sh::kPanel + uint32_t(((cy & 7) ^ sw) * 16);
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ax_), "r"(xo.x), "r"(xo.y),
-                                     "r"(xo.z), "r"(xo.w)
-                                     : "memory");
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ay_), "r"(yo.x), "r"(yo.y),
-                                     "r"(yo.z), "r"(yo.w)
-                                     : "memory");
+                        for (int g = 0; g < BATCH; ++g) {
+                            const int r = tok * G + g0 + g - w.row0;
+                            if (g0 + g < G && r >= 0 && r < w.rows) {
+                                x[g] = ld_stream(src + (g0 + g) * D);
+                                y[g] = ld_stream(src + (g0 + g) * D + P);
+                            }
+                        }
+                        if (g0 == 0) {
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) {
+                                const int i = pc * 8 + u;
+                                const int ax = pair_axis(i, a.layout, a.sec_t, a.sec_h, a.sec_w);
+                                const int p = ax == 0 ? pos[0] : ax == 1 ? pos[1] : pos[2];
+                                const int frac = int(uint32_t((uint64_t(int64_t(p)) * s_freq[i]) >> 32));
+                                __sincosf(float(frac) * 1.46291807926715968e-09f, &s[u], &c[u]);
+                            }
+                        }
+#pragma unroll
+                        for (int g = 0; g < BATCH; ++g) {
+                            const int r = tok * G + g0 + g - w.row0;
+                            if (g0 + g >= G || r < 0 || r >= w.rows) continue;
+                            uint4 xo, yo;
+                            rotate_vec(x[g], y[g], c, s, xo, yo);
+                            const uint32_t row = q_s + uint32_t(r >> 7) * Sh::kQTile + uint32_t(r & 127) * 128;
+                            const int cx = pc, cy = pc + CH, sw = r & 7;
+                            const uint32_t ax_ = row + uint32_t(cx >> 3) * Sh::kPanel + uint32_t(((cx & 7) ^ sw) * 16);
+                            const uint32_t ay_ = row + uint32_t(cy >> 3) * Sh::kPanel + uint32_t(((cy & 7) ^ sw) * 16);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ax_), "r"(xo.x), "r"(xo.y),
+                                         "r"(xo.z), "r"(xo.w)
+                                         : "memory");
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ay_), "r"(yo.x), "r"(yo.y),
+                                         "r"(yo.z), "r"(yo.w)
+                                         : "memory");
+                        }
                     }
                 }
                 // rows behind the last one: zeros
@@ -391,6 +428,9 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
         const bool live = row_ok && lim > w.lo;
         const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
         float odd = l_run * 0.0f;
+        // a thread's row goes out in whole 32-byte sectors where it is so aligned
+        const bool wide = a.splits > 1 ? (reinterpret_cast<uintptr_t>(a.partial) & 31) == 0
+                                       : ((reinterpret_cast<uintptr_t>(a.out) | uintptr_t(a.out_stride * 2)) & 31) == 0;
         if (any) {
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
@@ -400,21 +440,15 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
 #pragma unroll
                 for (int i = 0; i < 32; ++i) odd = fmaf(__uint_as_float(o[i]), 0.0f, odd);
                 if (a.splits == 1) {
-                    if (row_ok) {
+                    uint32_t v[16];
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
-                            uint4 v;
-                            v.x = pack_bf16x2(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
-                            v.y = pack_bf16x2(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
-                            v.z = pack_bf16x2(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
-                            v.w = pack_bf16x2(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
-                            st_row(dst + c + i, v);
-                        }
+                    for (int i = 0; i < 16; ++i)
+                        v[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+                    if (row_ok) {
+                        store_row<16>(dst + c, v, wide);
                     }
                 } else if (live) {
-#pragma unroll
-                    for (int i = 0; i < 32; i += 4)
-                        *reinterpret_cast<uint4*>(po + c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    store_row<32>(po + c, o, wide);
                 }
             }
         } else if (row_ok && a.splits == 1) {  // sees no slot
@@ -461,13 +495,22 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
             const int c = lane % CPR, rsub = lane / CPR;
             int e = 0;          // entries issued
             bool missing = false;
-            auto row_of = [&](int j) -> int64_t {
+            // the block of this lane's slot of tile j, asked for a tile before it is needed
+            const int32_t* bt = a.cache.block_table + int64_t(w.b) * a.cache.bt_stride;
+            auto block_of_tile = [&](int j) -> int32_t {
+                const int64_t slot = w.lo + int64_t(j) * kTile + lw * 32 + lane;
+                if (a.cache.kind != PRCR_CACHE_PAGED || j >= nt || slot >= w.hi) return 0;
+                return bt[uint32_t(slot) / uint32_t(a.cache.block_size)];
+            };
+            auto row_of = [&](int j, int32_t blk) -> int64_t {
                 const int64_t slot = w.lo + int64_t(j) * kTile + lw * 32 + lane;
                 if (j >= nt || slot >= w.hi) return -1;
-                uint32_t er = 0;
-                const int64_t row = slot_row(a.cache, w.b, slot, er);
-                missing |= row < 0;
-                return row;
+                if (a.cache.kind == PRCR_CACHE_CONTIGUOUS) return int64_t(w.b) * a.cache.seq_stride + slot * a.cache.slot_stride;
+                if (blk < 0 || blk >= a.cache.n_blocks) {
+                    missing = true;
+                    return -1;
+                }
+                return int64_t(blk) * a.cache.block_stride + int64_t(uint32_t(slot) % uint32_t(a.cache.block_size)) * a.cache.slot_stride;
             };
             auto put = [&](const uint16_t* src, int64_t row, int part) -> bool {
                 const int st = e % ST;
@@ -483,34 +526,26 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                                  "l"(from), "r"(rr >= 0 ? 16 : 0)
                                  : "memory");
                 }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                if (e >= Sh::kLag) {
-                    asm volatile("cp.async.wait_group %0;" ::"n"(Sh::kLag) : "memory");
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&bars.full[(e - Sh::kLag) % ST]));
-                }
+                mbar_arrive_copies(smem_u32(&bars.full[st]));
                 ++e;
                 return true;
             };
             // in the order of use: K0 V0 K1 V1 .., or with two S buffers K0 K1 V0 K2 V1 ..
             bool ok = true;
-            int64_t row = row_of(0), next = row_of(1);
+            int32_t blk = block_of_tile(1);
+            int64_t row = row_of(0, block_of_tile(0)), next = 0;
             for (int p = 0; ok && p < PARTS; ++p) ok = put(ck, row, p);
             for (int j = 0; ok && j < nt; ++j) {
+                next = row_of(j + 1, blk);
+                blk = block_of_tile(j + 2);
                 if (NQ == 1 && j + 1 < nt)
                     for (int p = 0; ok && p < PARTS; ++p) ok = put(ck, next, p);
                 for (int p = 0; ok && p < PARTS; ++p) ok = put(cv, row, p);
                 if (NQ == 2 && j + 1 < nt)
                     for (int p = 0; ok && p < PARTS; ++p) ok = put(ck, next, p);
                 row = next;
-                next = row_of(j + 2);
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0 && ok)
-                for (int i = max(0, e - Sh::kLag); i < e; ++i) mbar_arrive(smem_u32(&bars.full[i % ST]));
             if (missing) w.unmapped = 1;
             if (!ok) w.fail = 1;
           }
@@ -518,68 +553,78 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
         } else {
             if constexpr (NQ == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
             else asm volatile("setmaxnreg.dec.sync.aligned.u32 136;");
-            if (warp == kSoft + 4 && lane == 0 && nt > 0) {
+            if (warp == kSoft + 4 && nt > 0) {
                 constexpr uint32_t id_qk = tc_idesc(kTile, false), id_pv = tc_idesc(DIMS, true);
+                const uint32_t on = elect_lane();
+                const uint64_t dq = tc_desc(q_s, 16, 1024), dk = tc_desc(ring, 16, 1024), dv = tc_desc(ring, Sh::kPanel, 1024);
                 int e = 0;  // entries consumed
-                auto full = [&](int i) { return mbar_wait(smem_u32(&bars.full[i % ST]), uint32_t((i / ST) & 1)); };
-                auto entry = [&](int i) { return ring + uint32_t(i % ST) * Sh::kEntry; };
+                // the entries' copies are in place, and visible to the tensor cores
+                auto ready = [&](int e0) {
+                    bool ok = true;
+                    for (int i = e0; i < e0 + PARTS; ++i)
+                        ok = ok && mbar_wait(smem_u32(&bars.full[i % ST]), uint32_t((i / ST) & 1));
+                    fence_async_smem();
+                    return ok;
+                };
                 // S of 128 rows: entries e0 .. hold the tile's keys
                 auto qk = [&](int q, int buf, int e0) {
                     tc_fence_after();
 #pragma unroll
-                    for (int part = 0; part < PARTS; ++part)
+                    for (int part = 0; part < PARTS; ++part) {
+                        const uint64_t da = dq + uint32_t(q) * (Sh::kQTile >> 4) + uint32_t(part) * ((DIMS / 64) * Sh::kPanel >> 4);
+                        const uint64_t db = dk + uint32_t((e0 + part) % ST) * (Sh::kEntry >> 4);
 #pragma unroll
                         for (int k = 0; k < DIMS / 16; ++k) {
-                            const uint32_t step = uint32_t(k >> 2) * Sh::kPanel + uint32_t(k & 3) * 32;
-                            const uint32_t qa = q_s + uint32_t(q) * Sh::kQTile + uint32_t(part) * (DIMS / 64) * Sh::kPanel + step;
-                            tc_mma_ss(tmem + uint32_t(buf) * 128, tc_desc(qa, 16, 1024),
-                                      tc_desc(entry(e0 + part) + step, 16, 1024), id_qk, part + k > 0);
+                            const uint32_t step = (uint32_t(k >> 2) * Sh::kPanel + uint32_t(k & 3) * 32) >> 4;
+                            tc_mma_ss(tmem + uint32_t(buf) * 128, da + step, db + step, id_qk, part + k > 0, on);
                         }
+                    }
                 };
                 auto pv = [&](int q, int buf, int e0, bool add) {
                     tc_fence_after();
 #pragma unroll
-                    for (int part = 0; part < PARTS; ++part)
+                    for (int part = 0; part < PARTS; ++part) {
+                        const uint64_t db = dv + uint32_t((e0 + part) % ST) * (Sh::kEntry >> 4);
 #pragma unroll
                         for (int k = 0; k < kTile / 16; ++k)
                             tc_mma_ts(tmem + 256 + uint32_t(q) * D + uint32_t(part) * DIMS, tmem + uint32_t(buf) * 128 + uint32_t(k) * 8,
-                                      tc_desc(entry(e0 + part) + uint32_t(k) * 2048, Sh::kPanel, 1024), id_pv, add || k > 0);
+                                      db + uint32_t(k) * (2048 >> 4), id_pv, add || k > 0, on);
+                    }
                 };
                 auto release = [&](int e0) {
-                    for (int part = 0; part < PARTS; ++part) tc_commit(smem_u32(&bars.empty[(e0 + part) % ST]));
-                };
-                auto ready = [&](int e0) {
-                    bool ok = true;
-                    for (int part = 0; part < PARTS; ++part) ok = ok && full(e0 + part);
-                    return ok;
+                    for (int part = 0; part < PARTS; ++part) tc_commit(smem_u32(&bars.empty[(e0 + part) % ST]), on);
                 };
                 bool ok = mbar_wait(smem_u32(&bars.q), 0) && ready(0);
                 if (ok) {
                     for (int q = 0; q < NQ; ++q)
                         if (w.tiles[q] > 0) {
                             qk(q, q, 0);
-                            tc_commit(smem_u32(&bars.s[q]));
+                            tc_commit(smem_u32(&bars.s[q]), on);
                         }
                     release(0);
                     e = PARTS;
                 }
                 if constexpr (NQ == 2) {
+                    const int n0 = w.tiles[0], n1 = w.tiles[1];
                     for (int j = 0; ok && j < nt; ++j) {
                         const int ev = e, ek = e + PARTS;
                         ok = ready(ev);
                         bool have = false;
-                        for (int q = 0; ok && q < 2; ++q) {
-                            if (j >= w.tiles[q]) continue;
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const int n = q ? n1 : n0;
+                            if (!ok || j >= n) continue;
                             ok = mbar_wait(smem_u32(&bars.p[q]), uint32_t(j & 1));
-                            if (!ok) break;
+                            if (!ok) continue;
                             pv(q, q, ev, j > 0);
-                            if (j + 1 < w.tiles[q]) {
-                                if (!have && !(ok = ready(ek))) break;
+                            if (j + 1 < n) {
+                                if (!have) ok = ready(ek);
                                 have = true;
+                                if (!ok) continue;
                                 qk(q, q, ek);
-                                tc_commit(smem_u32(&bars.s[q]));
+                                tc_commit(smem_u32(&bars.s[q]), on);
                             } else {
-                                tc_commit(smem_u32(&bars.o[q]));
+                                tc_commit(smem_u32(&bars.o[q]), on);
                             }
                         }
                         if (ok && j + 1 < nt) {
@@ -594,7 +639,7 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                             ok = ready(e);
                             if (!ok) break;
                             qk(0, (j + 1) & 1, e);
-                            tc_commit(smem_u32(&bars.s[(j + 1) & 1]));
+                            tc_commit(smem_u32(&bars.s[(j + 1) & 1]), on);
                             release(e);
                             e += PARTS;
                         }
@@ -602,15 +647,18 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                         if (!ok) break;
                         pv(0, j & 1, e, j > 0);
                         if (j + 1 < nt) release(e);
-                        tc_commit(smem_u32(&bars.o[0]));
+                        tc_commit(smem_u32(&bars.o[0]), on);
                         e += PARTS;
                     }
                 }
                 if (!ok) {  // what was issued ends before the tensor memory is given back
-                    w.fail = 1;
-                    mbar_init(smem_u32(&bars.q), 1);
-                    tc_commit(smem_u32(&bars.q));
-                    mbar_wait(smem_u32(&bars.q), 0);
+                    if (lane == 0) {
+                        w.fail = 1;
+                        mbar_init(smem_u32(&bars.drain), 1);
+                    }
+                    __syncwarp();
+                    tc_commit(smem_u32(&bars.drain), on);
+                    mbar_wait(smem_u32(&bars.drain), 0);
                 }
             }
             __syncwarp();
