@@ -53,6 +53,26 @@ struct ChunkShape {
     static constexpr size_t kSmem = 1024 + size_t(NQ) * kQTile + size_t(kStages) * kEntry;
 };
 
+// Byte offset of a row's 16-byte chunk in the CTA's query tiles: panels of 64
+// dims, 128 bytes a row, chunks swizzled by the row.
+template <class Sh>
+__device__ __forceinline__ uint32_t chunk_at(int r, int c) {
+    return uint32_t(r >> 7) * Sh::kQTile + uint32_t(c >> 3) * Sh::kPanel + uint32_t(r & 127) * 128 +
+           uint32_t(((c & 7) ^ (r & 7)) * 16);
+}
+__device__ __forceinline__ void st_shared(uint32_t p, const uint4& v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
+                 : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared(uint32_t p) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "r"(p)
+                 : "memory");
+    return v;
+}
+
 // One query row by one warp in float32: online softmax over slots
 // [lo, hi), E dims a lane (dims lane * E ..). m is in units of log2.
 template <int D>
@@ -123,7 +143,7 @@ struct ChunkWork {
     int fail, unmapped;
 };
 struct ChunkBars {
-    uint64_t full[6], empty[6], q, s[2], p[2], o[2], drain;
+    uint64_t full[6], empty[6], q, s[2], p[2][2], o[2], drain;  // p: halves of 64 slots
 };
 
 template <int D, int NQ>
@@ -154,7 +174,8 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
         mbar_init(smem_u32(&bars.q), kSoft);
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&bars.s[i]), 1);
-            mbar_init(smem_u32(&bars.p[i]), 4);
+            mbar_init(smem_u32(&bars.p[i][0]), 4);
+            mbar_init(smem_u32(&bars.p[i][1]), 4);
             mbar_init(smem_u32(&bars.o[i]), 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -248,62 +269,65 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
             {
                 const int tok0 = w.row0 / G, n_tok = (w.row0 + w.rows - 1) / G - tok0 + 1;
                 constexpr int CH = P / 8, BATCH = 4;  // heads whose loads are in flight together
-                for (int it = tid; it < n_tok * CH; it += kSoft * 32) {
-                    const int tok = tok0 + it / CH, pc = it % CH;
-                    const int64_t t = int64_t(w.t0) + tok;
-                    const uint16_t* src = a.q + t * a.q_stride + int64_t(kh) * G * D + pc * 8;
-                    int pos[3];
+                struct Item {
+                    int tok, pc, pos[3];
+                    uint4 x[BATCH], y[BATCH];
+                };
+                auto load = [&](Item& m, int g0) {
+                    const uint16_t* src = a.q + (int64_t(w.t0) + m.tok) * a.q_stride + (int64_t(kh) * G + g0) * D + m.pc * 8;
 #pragma unroll
-                    for (int x = 0; x < 3; ++x) pos[x] = a.coords[3 * t + x];
-                    float c[8], s[8];
-                    for (int g0 = 0; g0 < G; g0 += BATCH) {
-                        uint4 x[BATCH], y[BATCH];
-#pragma unroll
-                        for (int g = 0; g < BATCH; ++g) {
-                            const int r = tok * G + g0 + g - w.row0;
-                            if (g0 + g < G && r >= 0 && r < w.rows) {
-                                x[g] = ld_stream(src + (g0 + g) * D);
-                                y[g] = ld_stream(src + (g0 + g) * D + P);
-                            }
-                        }
-                        if (g0 == 0) {
-#pragma unroll
-                            for (int u = 0; u < 8; ++u) {
-                                const int i = pc * 8 + u;
-                                const int ax = pair_axis(i, a.layout, a.sec_t, a.sec_h, a.sec_w);
-                                const int p = ax == 0 ? pos[0] : ax == 1 ? pos[1] : pos[2];
-                                const int frac = int(uint32_t((uint64_t(int64_t(p)) * s_freq[i]) >> 32));
-                                __sincosf(float(frac) * 1.46291807926715968e-09f, &s[u], &c[u]);
-                            }
-                        }
-#pragma unroll
-                        for (int g = 0; g < BATCH; ++g) {
-                            const int r = tok * G + g0 + g - w.row0;
-                            if (g0 + g >= G || r < 0 || r >= w.rows) continue;
-                            uint4 xo, yo;
-                            rotate_vec(x[g], y[g], c, s, xo, yo);
-                            const uint32_t row = q_s + uint32_t(r >> 7) * Sh::kQTile + uint32_t(r & 127) * 128;
-                            const int cx = pc, cy = pc + CH, sw = r & 7;
-                            const uint32_t ax_ = row + uint32_t(cx >> 3) * Sh::kPanel + uint32_t(((cx & 7) ^ sw) * 16);
-                            const uint32_t ay_ = row + uint32_t(cy >> 3) * Sh::kPanel + uint32_t(((cy & 7) ^ sw) * 16);
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ax_), "r"(xo.x), "r"(xo.y),
-                                         "r"(xo.z), "r"(xo.w)
-                                         : "memory");
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ay_), "r"(yo.x), "r"(yo.y),
-                                         "r"(yo.z), "r"(yo.w)
-                                         : "memory");
+                    for (int g = 0; g < BATCH; ++g) {
+                        const int r = m.tok * G + g0 + g - w.row0;
+                        if (g0 + g < G && r >= 0 && r < w.rows) {
+                            m.x[g] = ld_stream(src + g * D);
+                            m.y[g] = ld_stream(src + g * D + P);
                         }
                     }
+                };
+                auto begin = [&](Item& m, int it) {
+                    m.tok = tok0 + it / CH;
+                    m.pc = it % CH;
+                    const int32_t* c = a.coords + 3 * (int64_t(w.t0) + m.tok);
+                    if (it < n_tok * CH) {
+#pragma unroll
+                        for (int x = 0; x < 3; ++x) m.pos[x] = c[x];
+                        load(m, 0);
+                    }
+                };
+                auto finish = [&](Item& m, int it) {
+                    if (it >= n_tok * CH) return;
+                    float c[8], s[8];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const int i = m.pc * 8 + u;
+                        const int ax = pair_axis(i, a.layout, a.sec_t, a.sec_h, a.sec_w);
+                        const int p = ax == 0 ? m.pos[0] : ax == 1 ? m.pos[1] : m.pos[2];
+                        const int frac = int(uint32_t((uint64_t(int64_t(p)) * s_freq[i]) >> 32));
+                        __sincosf(float(frac) * 1.46291807926715968e-09f, &s[u], &c[u]);
+                    }
+                    for (int g0 = 0; g0 < G; g0 += BATCH) {
+                        if (g0) load(m, g0);
+#pragma unroll
+                        for (int g = 0; g < BATCH; ++g) {
+                            const int r = m.tok * G + g0 + g - w.row0;
+                            if (g0 + g >= G || r < 0 || r >= w.rows) continue;
+                            uint4 xo, yo;
+                            rotate_vec(m.x[g], m.y[g], c, s, xo, yo);
+                            st_shared(q_s + chunk_at<Sh>(r, m.pc), xo);
+                            st_shared(q_s + chunk_at<Sh>(r, m.pc + CH), yo);
+                        }
+                    }
+                };
+                Item m0, m1;
+                for (int it = tid; it < n_tok * CH; it += 2 * kSoft * 32) {
+                    begin(m0, it);
+                    begin(m1, it + kSoft * 32);
+                    finish(m0, it);
+                    finish(m1, it + kSoft * 32);
                 }
                 // rows behind the last one: zeros
-                for (int it = w.rows * (D / 8) + tid; it < Sh::kRows * (D / 8); it += kSoft * 32) {
-                    const int r = it / (D / 8), c = it % (D / 8);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(
-                                     q_s + uint32_t(r >> 7) * Sh::kQTile + uint32_t(c >> 3) * Sh::kPanel +
-                                     uint32_t(r & 127) * 128 + uint32_t((c & 7) * 16)),
-                                 "r"(0)
-                                 : "memory");
-                }
+                for (int it = w.rows * (D / 8) + tid; it < Sh::kRows * (D / 8); it += kSoft * 32)
+                    st_shared(q_s + chunk_at<Sh>(it / (D / 8), it % (D / 8)), make_uint4(0, 0, 0, 0));
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&bars.q));
@@ -327,26 +351,24 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                 }
                 tc_fence_after();
                 uint32_t s[128];
+                float x[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) tmem_ld32(s_t + 32 * i, s + 32 * i);
+                for (int i = 0; i < 4; ++i) x[i] = tmem_ld32_max(s_t + 32 * i, s + 32 * i);
                 tmem_wait_ld();
                 const int64_t at = w.lo + int64_t(j) * kTile;
                 if (at + kTile > lim_lo) {  // some row of the warp does not see all of the tile
                     const int n = int(max(int64_t(0), min(int64_t(kTile), lim - at)));
 #pragma unroll
-                    for (int i = 0; i < 128; ++i)
-                        if (i >= n) s[i] = 0xff800000u;
-                }
-                float x0 = __uint_as_float(s[0]), x1 = __uint_as_float(s[1]), x2 = __uint_as_float(s[2]),
-                      x3 = __uint_as_float(s[3]);
+                    for (int k = 0; k < 4; ++k) {
+                        x[k] = -INFINITY;
 #pragma unroll
-                for (int i = 4; i < 128; i += 4) {
-                    x0 = fmaxf(x0, __uint_as_float(s[i]));
-                    x1 = fmaxf(x1, __uint_as_float(s[i + 1]));
-                    x2 = fmaxf(x2, __uint_as_float(s[i + 2]));
-                    x3 = fmaxf(x3, __uint_as_float(s[i + 3]));
+                        for (int i = 32 * k; i < 32 * k + 32; ++i) {
+                            if (i >= n) s[i] = 0xff800000u;
+                            x[k] = fmaxf(x[k], __uint_as_float(s[i]));
+                        }
+                    }
                 }
-                const float mt = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3)) * scale;
+                const float mt = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * scale;
                 const bool raise = mt > m_run + kRaise || m_run == -INFINITY;
                 if (j == 0) {
                     m_run = mt;
@@ -394,13 +416,13 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                         p[i] = pack_bf16x2(e0, e1);
                     }
                     tmem_st32(s_t + 32 * half, p);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&bars.p[buf][half]));
                 }
                 const uint64_t sum = add2(sum0, sum1);
                 l_run += lo32(sum) + hi32(sum);
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bars.p[buf]));
             }
             // all of this half's products are done
             if (!failed && w.tiles[qi] > 0) {
@@ -422,15 +444,13 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
         const int64_t lim = min(w.first + tok + 1, w.hi);  // (rows of the other half see no more than w.hi)
         const uint32_t o_t = tmem + 256 + uint32_t(qi) * D + (uint32_t(warp & 3) << 21);
         const bool any = w.tiles[qi] > 0;  // this half's accumulator holds something
-        uint16_t* dst = out + int64_t(tok) * a.out_stride + int64_t(g) * D;
+        const int64_t dst = int64_t(w.t0 + tok) * a.out_stride + (int64_t(kh) * G + g) * D;
         const int64_t prow = (int64_t(w.t0 + tok) * H + kh) * G + g;  // row of the partials
         float* po = a.splits > 1 ? a.partial + (prow * a.splits + split) * D : nullptr;
         const bool live = row_ok && lim > w.lo;
+        const bool wide = (reinterpret_cast<uintptr_t>(a.partial) & 31) == 0;
         const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
-        float odd = l_run * 0.0f;
-        // a thread's row goes out in whole 32-byte sectors where it is so aligned
-        const bool wide = a.splits > 1 ? (reinterpret_cast<uintptr_t>(a.partial) & 31) == 0
-                                       : ((reinterpret_cast<uintptr_t>(a.out) | uintptr_t(a.out_stride * 2)) & 31) == 0;
+        float odd[4] = {l_run * 0.0f, 0.0f, 0.0f, 0.0f};
         if (any) {
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
@@ -438,25 +458,40 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                 tmem_ld32(o_t + c, o);
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) odd = fmaf(__uint_as_float(o[i]), 0.0f, odd);
+                for (int i = 0; i < 32; ++i) odd[i & 3] = fmaf(__uint_as_float(o[i]), 0.0f, odd[i & 3]);
                 if (a.splits == 1) {
-                    uint32_t v[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        v[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
-                    if (row_ok) {
-                        store_row<16>(dst + c, v, wide);
+                    for (int i = 0; i < 32; i += 8) {
+                        uint4 v;
+                        v.x = pack_bf16x2(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
+                        v.y = pack_bf16x2(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
+                        v.z = pack_bf16x2(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
+                        v.w = pack_bf16x2(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
+                        st_shared(q_s + chunk_at<Sh>(r, (c + i) / 8), v);
                     }
                 } else if (live) {
                     store_row<32>(po + c, o, wide);
                 }
             }
-        } else if (row_ok && a.splits == 1) {  // sees no slot
-            for (int c = 0; c < D; c += 8) st_row(dst + c, make_uint4(0, 0, 0, 0));
+        }
+        if (a.splits == 1) {
+            // the queries' place now holds the results (this half's products with
+            // them are done): whole rows go out, 16 bytes a lane
+            constexpr int CPR = D / 8, RPI = 32 / CPR;
+            __syncwarp();
+#pragma unroll 4
+            for (int i = 0; i < 32 / RPI; ++i) {
+                const int src = i * RPI + lane / CPR;
+                const int64_t to = __shfl_sync(kFull, row_ok ? dst : int64_t(-1), src);
+                if (to >= 0)
+                    st_row(a.out + to + (lane % CPR) * 8,
+                           any ? ld_shared(q_s + chunk_at<Sh>((r & ~31) + src, lane % CPR)) : make_uint4(0, 0, 0, 0));
+            }
+            __syncwarp();
         }
         if (a.splits > 1 && live) a.partial_ml[prow * a.splits + split] = make_float2(m_run, l_run);
         // rows to be computed again from their own slots
-        uint32_t again = __ballot_sync(kFull, live && any && (odd != 0.0f || w.unmapped));
+        uint32_t again = __ballot_sync(kFull, live && any && (odd[0] + odd[1] + (odd[2] + odd[3]) != 0.0f || w.unmapped));
         if (w.unmapped && tid == 0) atomicOr(a.status, PRCR_ST_NO_BLOCK);
         while (again) {
             const int src = __ffs(int(again)) - 1;
@@ -580,16 +615,22 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                         }
                     }
                 };
-                auto pv = [&](int q, int buf, int e0, bool add) {
-                    tc_fence_after();
+                // O += P V of 128 rows, each half of the slots as soon as its P is there
+                auto pv = [&](int q, int buf, int e0, uint32_t ph, bool add) -> bool {
 #pragma unroll
-                    for (int part = 0; part < PARTS; ++part) {
-                        const uint64_t db = dv + uint32_t((e0 + part) % ST) * (Sh::kEntry >> 4);
+                    for (int half = 0; half < 2; ++half) {
+                        if (!mbar_wait(smem_u32(&bars.p[buf][half]), ph)) return false;
+                        tc_fence_after();
 #pragma unroll
-                        for (int k = 0; k < kTile / 16; ++k)
-                            tc_mma_ts(tmem + 256 + uint32_t(q) * D + uint32_t(part) * DIMS, tmem + uint32_t(buf) * 128 + uint32_t(k) * 8,
-                                      db + uint32_t(k) * (2048 >> 4), id_pv, add || k > 0, on);
+                        for (int part = 0; part < PARTS; ++part) {
+                            const uint64_t db = dv + uint32_t((e0 + part) % ST) * (Sh::kEntry >> 4);
+#pragma unroll
+                            for (int k = half * 4; k < half * 4 + 4; ++k)
+                                tc_mma_ts(tmem + 256 + uint32_t(q) * D + uint32_t(part) * DIMS, tmem + uint32_t(buf) * 128 + uint32_t(k) * 8,
+                                          db + uint32_t(k) * (2048 >> 4), id_pv, add || k > 0, on);
+                        }
                     }
+                    return true;
                 };
                 auto release = [&](int e0) {
                     for (int part = 0; part < PARTS; ++part) tc_commit(smem_u32(&bars.empty[(e0 + part) % ST]), on);
@@ -614,9 +655,8 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                         for (int q = 0; q < 2; ++q) {
                             const int n = q ? n1 : n0;
                             if (!ok || j >= n) continue;
-                            ok = mbar_wait(smem_u32(&bars.p[q]), uint32_t(j & 1));
+                            ok = pv(q, q, ev, uint32_t(j & 1), j > 0);
                             if (!ok) continue;
-                            pv(q, q, ev, j > 0);
                             if (j + 1 < n) {
                                 if (!have) ok = ready(ek);
                                 have = true;
@@ -643,9 +683,8 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                             release(e);
                             e += PARTS;
                         }
-                        ok = ready(e) && mbar_wait(smem_u32(&bars.p[j & 1]), uint32_t((j >> 1) & 1));
+                        ok = ready(e) && pv(0, j & 1, e, uint32_t((j >> 1) & 1), j > 0);
                         if (!ok) break;
-                        pv(0, j & 1, e, j > 0);
                         if (j + 1 < nt) release(e);
                         tc_commit(smem_u32(&bars.o[0]), on);
                         e += PARTS;

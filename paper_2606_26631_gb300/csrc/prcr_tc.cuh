@@ -134,6 +134,23 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* r) {
           "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(addr));
 }
+// and the largest of them (NaN left out)
+__device__ __forceinline__ float tmem_ld32_max(uint32_t addr, uint32_t* r) {
+    float f[32], m;
+    asm volatile(
+        "tcgen05.ld.red.sync.aligned.32x32b.x32.max.f32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, %32, [%33];"
+        : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]),
+          "=f"(f[8]), "=f"(f[9]), "=f"(f[10]), "=f"(f[11]), "=f"(f[12]), "=f"(f[13]), "=f"(f[14]),
+          "=f"(f[15]), "=f"(f[16]), "=f"(f[17]), "=f"(f[18]), "=f"(f[19]), "=f"(f[20]), "=f"(f[21]),
+          "=f"(f[22]), "=f"(f[23]), "=f"(f[24]), "=f"(f[25]), "=f"(f[26]), "=f"(f[27]), "=f"(f[28]),
+          "=f"(f[29]), "=f"(f[30]), "=f"(f[31]), "=f"(m)
+        : "r"(addr));
+#pragma unroll
+    for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(f[i]);
+    return m;
+}
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
