@@ -56,7 +56,28 @@ ChunkSplit chunk_split(const prcr_rope_cfg* cfg, int64_t n_seqs, int64_t n_q_hea
     return c;
 }
 
+// CTAs of a cluster that takes one (sequence, layer, KV head), and its slots per
+// CTA: the fewest whose logits leave room for two CTAs per SM (or, for long
+// sequences, for one); more where there are SMs left for them and each keeps a tile of 16
+// slots for every warp. 0 where no cluster's shared memory holds them.
+int weights_cluster(const prcr_rope_cfg* cfg, int64_t n_seqs, int64_t n_q_heads, int64_t max_len, int sms, int* slots) {
+    const int64_t units = n_seqs * cfg->n_layers * cfg->n_kv_heads;
+    const int group = int(n_q_heads / cfg->n_kv_heads);
+    auto per = [&](int c) { return ((max_len + 15) / 16 + c - 1) / c * 16; };
+    for (const size_t room : {size_t(104) * 1024, size_t(208) * 1024}) {
+        for (int c = 1; c <= 8; c *= 2) {
+            if (max_len > (int64_t(1) << 20) || weights_smem(cfg->head_dim, group, int(per(c))) > room) continue;
+            while (c < 8 && units * c * 2 <= 2 * int64_t(sms) && per(2 * c) >= 128) c *= 2;
+            *slots = int(per(c));
+            return c;
+        }
+    }
+    return 0;
+}
+
 size_t weights_bytes(const prcr_rope_cfg* cfg, int64_t n_seqs, int64_t n_q_heads, int64_t max_len) {
+    int slots;
+    if (weights_cluster(cfg, n_seqs, n_q_heads, max_len, 1, &slots)) return 0;
     return size_t(n_seqs) * cfg->n_layers * n_q_heads * max_len * sizeof(float);
 }
 
@@ -212,9 +233,14 @@ int prcr_accumulate_weights(const prcr_rope_cfg* cfg, const prcr_cache_desc* cac
     if (!q || !q_pos || !seq_len || !score || !status) return PRCR_EINVAL;
     if (!aligned16(q) || !aligned8(q_pos) || !aligned4(seq_len) || !aligned4(score) || !aligned4(status))
         return PRCR_EALIGN;
-    if (!workspace || workspace_size < weights_bytes(cfg, n_seqs, n_q_heads, max_len)) return PRCR_EWORKSPACE;
-    if (!aligned16(workspace)) return PRCR_EALIGN;
+    const size_t need = weights_bytes(cfg, n_seqs, n_q_heads, max_len);
+    if (need > 0 && (!workspace || workspace_size < need)) return PRCR_EWORKSPACE;
+    if (need > 0 && !aligned16(workspace)) return PRCR_EALIGN;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return PRCR_ECUDA;
     WeightsArgs a = {};
+    a.cluster = weights_cluster(cfg, n_seqs, n_q_heads, max_len, sm_count(dev), &a.slots_per_cta);
+    if (a.cluster * int64_t(n_seqs) * cfg->n_layers * cfg->n_kv_heads > INT32_MAX) return PRCR_EINVAL;  // grid x
     a.cache = cache_view(cache, 0);
     a.q = static_cast<const uint16_t*>(q);
     a.q_pos = q_pos;

@@ -420,7 +420,9 @@ struct WeightsArgs {
     const int64_t* q_pos;       // [B]
     const int32_t* seq_len;     // [B]
     float* score;               // [B][n_layers][n_kv_heads][score_stride]
-    float* logits;              // workspace [B][n_layers][n_q_heads][max_len]
+    float* logits;              // workspace [B][n_layers][n_q_heads][max_len] when cluster is 0
+    int32_t cluster;            // CTAs of a (sequence, layer, KV head), or 0: logits through the workspace
+    int32_t slots_per_cta;
     uint32_t* status;
     int64_t max_len;
     int64_t score_stride;
@@ -458,6 +460,7 @@ cudaError_t append_blocks_per_sm(int block, size_t smem, int* out);
 cudaError_t launch_append(const AppendArgs& a, dim3 grid, int block, size_t smem, cudaStream_t stream);
 cudaError_t launch_chunk(const ChunkArgs& a, cudaStream_t stream);
 int chunk_rows(int head_dim);  // rows (token, query head of a group) that a CTA takes
+size_t weights_smem(int head_dim, int group, int slots);  // of a CTA with so many slots
 cudaError_t launch_weights(const WeightsArgs& a, cudaStream_t stream);
 cudaError_t launch_evict(const EvictArgs& a, int n_seqs, cudaStream_t stream);
 

@@ -2,10 +2,28 @@
 //   score[b][l][h][s] = decay score[b][l][h][s] + sum over the query heads g of
 //   KV head h of softmax_s(RoPE(q[b][l][g], (p, p, p)) . K[b][l][s][h] / sqrt(D)).
 //
-// Two kernels: the logits to the workspace, then per (sequence, layer, KV head)
-// the normalisers and the sums.
+// A cluster of 1 to 8 CTAs takes one (sequence, layer, KV head) and reads its keys
+// once (weights_kernel):
+//  1. Warps stream tiles of 16 slots from global memory straight into the A
+//     fragments of mma.sync m16n8k16 (the dot product does not depend on the
+//     order of the dims, so a lane's 16-byte chunks of its two slots' rows are
+//     fragments as they are), the next tile's loads in flight during this one's
+//     products; columns are the group's query heads. bf16 operands hold 8
+//     bits, so the float32 query is split into three of them: products with
+//     the bf16 keys are exact to float32's accuracy. The logits stay in shared memory, [head][slot].
+//  2. Maxima, then exp and sums, of each head over all slots; a cluster's CTAs write theirs into
+//     one another's shared memory.
+//  3. The slot's weights, normalised, are added to its score.
+// Memory-bound: keys and scores are touched once. A warp keeps two tiles (8 KB at head_dim 128) in
+// flight, two CTAs of 8 warps fit an SM.
+// Where the logits of a sequence do not fit a cluster's shared memory (above
+// 400,000 / group slots), they go through the workspace instead (weights_logits_kernel,
+// weights_sum_kernel).
+#include <algorithm>
+
 #include "prcr_cache.cuh"
 #include "prcr_pdl.cuh"
+#include "prcr_tc.cuh"
 
 namespace prcr {
 namespace {
@@ -123,9 +141,289 @@ __global__ void __launch_bounds__(kWeightsThreads) weights_sum_kernel(const __gr
     }
 }
 
+// ---- one cluster per (sequence, layer, KV head) ----------------------------------------
+
+constexpr int kWarps = 8;
+constexpr int kMaxRanks = 8;
+
+// floats between the logits of two heads: 4 mod 32, so that a fragment's lanes
+// (8 slots x 4 pairs of heads) write to different banks
+__host__ __device__ inline int logit_stride(int slots) { return (slots + 31) / 32 * 32 + 4; }
+
+template <int D>
+struct WeightsShape {
+    static constexpr int kDims = D < 128 ? D : 128;  // dims of a load stage
+    static constexpr int kParts = D / kDims;
+    static constexpr int kLoads = kDims / 32;        // 16-byte chunks a lane reads of each of its two rows
+    static constexpr int kSteps = D / 16;
+    static constexpr size_t kFragBytes = size_t(3) * kSteps * 32 * sizeof(uint2);
+};
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void st_peer(const float* p, int rank, float x) {
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.f32 [a], %2;\n\t}" ::"r"(smem_u32(p)),
+                 "r"(rank), "f"(x)
+                 : "memory");
+}
+
+template <int D>
+__global__ void __launch_bounds__(kWarps * 32, 2) weights_kernel(const __grid_constant__ WeightsArgs a) {
+    using Sh = WeightsShape<D>;
+    constexpr int P = D / 2, KS = Sh::kSteps, LV = Sh::kLoads, PARTS = Sh::kParts;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float s_part[kWarps][8], s_peer[2][kMaxRanks][8];
+    uint2* const frag = reinterpret_cast<uint2*>(smem);  // [3][KS][32]: the query's B fragments
+    float* const logit = reinterpret_cast<float*>(smem + Sh::kFragBytes);
+    const int C = a.cluster, rank = int(blockIdx.x) % C;
+    const int unit = int(blockIdx.x) / C;
+    const int h = unit % a.n_kv_heads, l = unit / a.n_kv_heads % a.n_layers, b = unit / (a.n_kv_heads * a.n_layers);
+    const int g = a.group, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, t = lane & 3;
+    const int stride = logit_stride(a.slots_per_cta);
+    if (C > 1) cluster_arrive();
+    pdl_allow();
+    pdl_wait();
+    uint32_t err = 0;
+    const int len = int(weights_len(a, b, err));
+    const int64_t pos = a.q_pos[b];
+    const int per = ((len + 15) / 16 + C - 1) / C * 16;  // slots of a CTA, at most slots_per_cta
+    const int s0 = min(len, rank * per), n = min(len, s0 + per) - s0;
+    const int n_tiles = (n + 15) / 16;
+
+    // keys: this lane's two rows of a tile, slots gid and gid + 8
+    const uint16_t* const kbase = a.cache.k + int64_t(l) * a.cache.layer_stride + int64_t(h) * D + t * 8;
+    const int32_t* const bt = a.cache.block_table + int64_t(b) * a.cache.bt_stride;
+    const bool paged = a.cache.kind == PRCR_CACHE_PAGED;
+    auto block_of = [&](int i, int half) -> int32_t {
+        const int s = i * 16 + half * 8 + gid;
+        return paged && s < n ? bt[uint32_t(s0 + s) / uint32_t(a.cache.block_size)] : 0;
+    };
+    auto row_of = [&](int i, int half, int32_t blk) -> int64_t {
+        const int s = i * 16 + half * 8 + gid;
+        if (s >= n) return -1;
+        if (!paged) return int64_t(b) * a.cache.seq_stride + int64_t(s0 + s) * a.cache.slot_stride;
+        if (blk < 0 || blk >= a.cache.n_blocks) {
+            err |= PRCR_ST_NO_BLOCK;
+            return -1;
+        }
+        return int64_t(blk) * a.cache.block_stride + int64_t(uint32_t(s0 + s) % uint32_t(a.cache.block_size)) * a.cache.slot_stride;
+    };
+    struct Stage {
+        uint4 w0[LV], w1[LV];
+    };
+    auto load = [&](Stage& s, int64_t r0, int64_t r1, int part) {
+#pragma unroll
+        for (int u = 0; u < LV; ++u) {
+            s.w0[u] = r0 >= 0 ? ld_stream(kbase + r0 + part * Sh::kDims + 32 * u) : make_uint4(0, 0, 0, 0);
+            s.w1[u] = r1 >= 0 ? ld_stream(kbase + r1 + part * Sh::kDims + 32 * u) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    // (stages in the order of use: the parts of tile `warp`, of tile warp + 8, ..)
+    int tile = warp;
+    int32_t nb0 = block_of(tile + kWarps, 0), nb1 = block_of(tile + kWarps, 1);
+    int64_t r0 = row_of(tile, 0, block_of(tile, 0)), r1 = row_of(tile, 1, block_of(tile, 1));
+    Stage sa, sb;
+    if (tile < n_tiles) load(sa, r0, r1, 0);
+
+    // the group's queries, rotated and scaled, as fragments of three bf16 terms:
+    // k-step j of lane group t covers dims 8 (t + 4 (j / 2)) + 4 (j % 2) + 0..3, as
+    // the key chunks that the lane reads
+    const uint16_t* q = a.q + ((int64_t(b) * a.n_layers + l) * a.n_kv_heads + h) * g * D;
+    float* const q_s = logit;  // [8][D] until the fragments are made
+    for (int i = tid; i < 8 * P; i += kWarps * 32) {
+        const int j = i / P, d = i % P;
+        float x = 0.0f, y = 0.0f;
+        if (j < g) {
+            float s, c;
+            sincos_turns(double(pos), a.turn_freq[d], &s, &c);
+            const float u = lo_f32(q[j * D + d]), v = lo_f32(q[j * D + d + P]);
+            x = fmaf(u, c, -v * s) * a.scale_log2;
+            y = fmaf(v, c, u * s) * a.scale_log2;
+        }
+        q_s[j * D + d] = x;
+        q_s[j * D + d + P] = y;
+    }
+    __syncthreads();
+    for (int i = tid; i < KS * 32; i += kWarps * 32) {
+        const int j = i / 32, ln = i % 32;
+        const float* x = q_s + (ln >> 2) * D + 8 * ((ln & 3) + 4 * (j >> 1)) + 4 * (j & 1);
+        float v[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+        for (int term = 0; term < 3; ++term) {
+            const uint2 f = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+            frag[(term * KS + j) * 32 + ln] = f;
+            v[0] -= lo_f32(f.x);
+            v[1] -= hi_f32(f.x);
+            v[2] -= lo_f32(f.y);
+            v[3] -= hi_f32(f.y);
+        }
+    }
+    __syncthreads();
+
+    float mx[2] = {-INFINITY, -INFINITY};  // of heads 2t, 2t + 1
+    float acc[3][4];
+    auto products = [&](const Stage& s, int part) {
+        if (part == 0) {
+#pragma unroll
+            for (int i = 0; i < 12; ++i) acc[i / 4][i % 4] = 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < LV; ++u) {
+            const int j = (part * Sh::kDims / 16) + 2 * u;
+#pragma unroll
+            for (int term = 0; term < 3; ++term) {
+                const uint2 f0 = frag[(term * KS + j) * 32 + lane], f1 = frag[(term * KS + j + 1) * 32 + lane];
+                mma_16816(acc[term], s.w0[u].x, s.w1[u].x, s.w0[u].y, s.w1[u].y, f0.x, f0.y);
+                mma_16816(acc[term], s.w0[u].z, s.w1[u].z, s.w0[u].w, s.w1[u].w, f1.x, f1.y);
+            }
+        }
+    };
+    // the next stage is asked for, then this one's products are made; after a
+    // tile's last part its logits are kept
+    int part = 0;
+    auto step = [&](Stage& now, Stage& next) {
+        const bool last = part == PARTS - 1;
+        const int64_t c0 = r0, c1 = r1;
+        const int i = tile;
+        if (last) {
+            tile += kWarps;
+            r0 = row_of(tile, 0, nb0);
+            r1 = row_of(tile, 1, nb1);
+            nb0 = block_of(tile + kWarps, 0);
+            nb1 = block_of(tile + kWarps, 1);
+        }
+        if (tile < n_tiles) load(next, r0, r1, last ? 0 : part + 1);
+        products(now, part);
+        if (last) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int head = 2 * t + (e & 1), s = i * 16 + (e >> 1) * 8 + gid;
+                const float x = (e < 2 ? c0 : c1) >= 0 ? acc[0][e] + (acc[1][e] + acc[2][e]) : -INFINITY;
+                if (head < g) logit[head * stride + s] = x;
+                mx[e & 1] = fmaxf(mx[e & 1], x);
+            }
+        }
+        part = last ? 0 : part + 1;
+    };
+    while (tile < n_tiles) {
+        step(sa, sb);
+        if (tile >= n_tiles) break;
+        step(sb, sa);
+    }
+
+    // each head's maximum over the cluster
+    auto join = [&](float v0, float v1, int which, auto op, float init, float (&out)[8]) {
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) {
+            v0 = op(v0, __shfl_xor_sync(kFull, v0, d));
+            v1 = op(v1, __shfl_xor_sync(kFull, v1, d));
+        }
+        if (gid == 0) {
+            s_part[warp][2 * t] = v0;
+            s_part[warp][2 * t + 1] = v1;
+        }
+        __syncthreads();
+        if (C > 1) {
+            if (which == 0) cluster_wait();  // every CTA has begun
+            if (tid < 8 * C) {
+                float x = init;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) x = op(x, s_part[w][tid & 7]);
+                st_peer(&s_peer[which][rank][tid & 7], tid >> 3, x);
+            }
+            cluster_arrive();
+            cluster_wait();
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float x = init;
+            if (C > 1) {
+                for (int r = 0; r < C; ++r) x = op(x, s_peer[which][r][j]);
+            } else {
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) x = op(x, s_part[w][j]);
+            }
+            out[j] = x;
+        }
+        __syncthreads();
+    };
+    float m[8], inv[8];
+    join(mx[0], mx[1], 0, [](float x, float y) { return fmaxf(x, y); }, -INFINITY, m);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (m[j] == -INFINITY) m[j] = 0.0f;  // no readable slot: weights of zero
+
+    // exponentials in place of the logits, and their sums
+    float sum[8] = {};
+    for (int s = tid; s < n; s += kWarps * 32) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < g) {
+                const float e = exp2_fast(logit[j * stride + s] - m[j]);
+                logit[j * stride + s] = e;
+                sum[j] += e;
+            }
+    }
+    // (a lane ends with the warp's sums of heads 2t, 2t + 1 for `join`)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        sum[j] += __shfl_xor_sync(kFull, sum[j], 1);
+        sum[j] += __shfl_xor_sync(kFull, sum[j], 2);
+    }
+    const float v0 = t == 0 ? sum[0] : t == 1 ? sum[2] : t == 2 ? sum[4] : sum[6];
+    const float v1 = t == 0 ? sum[1] : t == 1 ? sum[3] : t == 2 ? sum[5] : sum[7];
+    join(v0, v1, 1, [](float x, float y) { return x + y; }, 0.0f, inv);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) inv[j] = inv[j] == 0.0f ? 0.0f : 1.0f / inv[j];
+
+    float* const score = a.score + int64_t(unit) * a.score_stride + s0;
+#pragma unroll 4
+    for (int s = tid; s < n; s += kWarps * 32) {
+        float w = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < g) w = fmaf(logit[j * stride + s], inv[j], w);
+        score[s] = a.decay == 0.0f ? w : fmaf(a.decay, score[s], w);
+    }
+    if (err && (rank == 0 || (err & PRCR_ST_NO_BLOCK))) atomicOr(a.status, err);
+}
+
+template <int D>
+cudaError_t launch_cluster(const WeightsArgs& a, cudaStream_t stream) {
+    const size_t smem = weights_smem(D, a.group, a.slots_per_cta);
+    const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(weights_kernel<D>), smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(int64_t(a.n_seqs) * a.n_layers * a.n_kv_heads * a.cluster));
+    cfg.blockDim = dim3(kWarps * 32);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = unsigned(a.cluster);
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, weights_kernel<D>, a);
+}
+
 }  // namespace
 
+size_t weights_smem(int head_dim, int group, int slots) {
+    const size_t frag = size_t(3) * (head_dim / 16) * 32 * sizeof(uint2);
+    // (the queries lie in the logits' place first)
+    return frag + std::max(size_t(group) * logit_stride(slots), size_t(8) * head_dim) * sizeof(float);
+}
+
 cudaError_t launch_weights(const WeightsArgs& a, cudaStream_t stream) {
+    if (a.cluster > 0) {
+        if (a.head_dim == 64) return launch_cluster<64>(a, stream);
+        if (a.head_dim == 128) return launch_cluster<128>(a, stream);
+        return launch_cluster<256>(a, stream);
+    }
     const int64_t parts = (a.max_len + kSlotsPerCta - 1) / kSlotsPerCta;
     cudaError_t e = launch_pdl(weights_logits_kernel, dim3(unsigned(parts), unsigned(a.n_layers * a.n_kv_heads), unsigned(a.n_seqs)),
                                dim3(kWeightsThreads), size_t(a.group) * a.head_dim * sizeof(float), stream, a);

@@ -454,6 +454,8 @@ class Weights:
     (8, 4, 128, 2, [1, 0, 300], 16), (4, 7, 128, 1, [933, 17], 0), (2, 1, 64, 3, [129, 128], 7), (1, 8, 128, 2, [2500], 64),
     (2, 4, 256, 2, [65, 700], 16), (3, 8, 64, 1, [5000, 3], 0), (1, 1, 256, 1, [16, 15, 17, 1], 1), (2, 4, 128, 1, [40000], 16),
     (8, 4, 128, 36, [200], 16), (2, 3, 128, 1, [20000, 9], 16), (1, 8, 256, 1, [17000], 16),
+    (1, 8, 64, 1, [60000, 31], 16),  # beyond a cluster's shared memory: through the workspace
+    (1, 1, 64, 1, [2000, 100, 1], 0), (1, 2, 256, 1, [300, 1000], 7),  # few: a cluster of eight
 ], ids=lambda v: str(v))
 def test_weights(H, g, D, L, lens, block):
     w = Weights(H, g, D, L, lens, block, seed=H + g, gap=8 if block == 7 else 0,
