@@ -93,9 +93,11 @@ __global__ void __launch_bounds__(512) append_kernel(const __grid_constant__ App
     if (dst < 0) return;
     float c[8], s[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-        c[u] = cos_s[my_t * P + v * 8 + u];
-        s[u] = sin_s[my_t * P + v * 8 + u];
+    for (int u = 0; u < 2; ++u) {
+        const float4 c4 = *reinterpret_cast<const float4*>(cos_s + my_t * P + v * 8 + 4 * u);
+        const float4 s4 = *reinterpret_cast<const float4*>(sin_s + my_t * P + v * 8 + 4 * u);
+        c[4 * u] = c4.x; c[4 * u + 1] = c4.y; c[4 * u + 2] = c4.z; c[4 * u + 3] = c4.w;
+        s[4 * u] = s4.x; s[4 * u + 1] = s4.y; s[4 * u + 2] = s4.z; s[4 * u + 3] = s4.w;
     }
     const int64_t c_off = dst + int64_t(l0) * a.cache.layer_stride + off;
     uint16_t* ck = a.cache.k + c_off;

@@ -27,6 +27,12 @@ CacheView cache_view(const prcr_cache_desc* c, int layer) {
     v.block_size = c->kind == PRCR_CACHE_PAGED ? c->block_size : 1;
     v.n_blocks = c->n_blocks;
     v.kind = c->kind;
+    // m = ceil(2^(31 + k) / d) with 2^k >= d: m d exceeds 2^(31 + k) by less than 2^k,
+    // so that n m >> (31 + k) is n / d for every n below 2^31
+    int k = 0;
+    while ((int64_t(1) << k) < v.block_size) ++k;
+    v.div_mul = uint32_t(((uint64_t(1) << (31 + k)) + v.block_size - 1) / v.block_size);
+    v.div_shift = 31 + k;
     return v;
 }
 
@@ -140,7 +146,7 @@ int prcr_append_kv(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, int32
     if (cudaGetDevice(&dev) != cudaSuccess) return PRCR_ECUDA;
     const int64_t tiles = std::max<int64_t>(1, (int64_t(total) + T - 1) / T);
     const int64_t slots = int64_t(sm_count(dev)) * blocks_per_sm(dev, block, smem, kAppend);
-    const int G = stream_layers_per_cta(tiles, n_layers, slots, std::max(2, 6 / cfg->n_kv_heads));
+    const int G = stream_layers_per_cta(tiles, n_layers, slots, 8);
     a.layers_per_cta = G;
     const dim3 grid(unsigned(tiles), unsigned((n_layers + G - 1) / G), 1);
     return status_of(launch_append(a, grid, block, smem, static_cast<cudaStream_t>(stream)));

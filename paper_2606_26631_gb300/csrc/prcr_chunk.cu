@@ -535,17 +535,14 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
             auto block_of_tile = [&](int j) -> int32_t {
                 const int64_t slot = w.lo + int64_t(j) * kTile + lw * 32 + lane;
                 if (a.cache.kind != PRCR_CACHE_PAGED || j >= nt || slot >= w.hi) return 0;
-                return bt[uint32_t(slot) / uint32_t(a.cache.block_size)];
+                return bt[block_index(a.cache, uint32_t(slot))];
             };
             auto row_of = [&](int j, int32_t blk) -> int64_t {
                 const int64_t slot = w.lo + int64_t(j) * kTile + lw * 32 + lane;
                 if (j >= nt || slot >= w.hi) return -1;
-                if (a.cache.kind == PRCR_CACHE_CONTIGUOUS) return int64_t(w.b) * a.cache.seq_stride + slot * a.cache.slot_stride;
-                if (blk < 0 || blk >= a.cache.n_blocks) {
-                    missing = true;
-                    return -1;
-                }
-                return int64_t(blk) * a.cache.block_stride + int64_t(uint32_t(slot) % uint32_t(a.cache.block_size)) * a.cache.slot_stride;
+                const int64_t row = row_in_block(a.cache, w.b, uint32_t(slot), blk);
+                missing |= row < 0;
+                return row;
             };
             auto put = [&](const uint16_t* src, int64_t row, int part) -> bool {
                 const int st = e % ST;

@@ -4,17 +4,22 @@
 // 0 .. budget - 1 in their order, in place or into another cache.
 //
 // One CTA per (KV head, layer, sequence):
-//  1. the score at the cut by a radix selection, 8 bits a pass, over the
-//     scores mapped to integers of the same order;
+//  1. the score at the cut by a radix selection, 11 bits a pass, over the
+//     scores mapped to integers of the same order (held in shared memory where they fit);
 //  2. one pass over the slots in order, tile by tile, that gives every kept
 //     slot its place by prefix sums (equal scores at the cut: the lower slots
 //     first), writes the indices and moves the scores;
-//  3. the rows, in order, tile by tile. In place a tile's destinations are
-//     slots below those that later tiles read (slot keep[j] >= j), so reading
-//     a whole tile before writing it is all the order that is needed.
-// Memory-bound: the kept rows are read once and written once.
+//  3. the rows, in order, tile by tile: a thread copies one 16-byte vector of K and one of V of a
+//     tile asynchronously into its own part of a ring in shared memory, several
+//     tiles ahead, and writes them out when they have landed. In place a
+//     tile's destinations are slots below those that later tiles read (slot
+//     keep[j] >= j), so a barrier between a tile's arrival at all threads and its
+//     writes is all the order that is needed.
+// Memory-bound: the kept rows are read once and written once; two CTAs per SM keep up to 192 KB in
+// flight, and one's selection runs during the other's copies.
 #include "prcr_cache.cuh"
 #include "prcr_pdl.cuh"
+#include "prcr_tc.cuh"
 
 namespace prcr {
 namespace {
@@ -22,6 +27,11 @@ namespace {
 constexpr int kEvictThreads = 512;
 constexpr int kEvictWarps = kEvictThreads / 32;
 constexpr unsigned kFull = 0xffffffffu;
+constexpr int kRing = 6;                                     // tiles
+constexpr int kRingBytes = kRing * kEvictThreads * 32;       // 32 bytes a thread and tile
+constexpr int kBins = 2048;
+constexpr size_t kEvictSmem = kRingBytes + 2 * kEvictThreads * 16;
+constexpr int kHeldScores = kRingBytes / 4;                  // the ring holds the scores first
 
 // An integer of the score's order, NaN below everything (equal zeros, whatever
 // their sign).
@@ -31,10 +41,15 @@ __device__ __forceinline__ uint32_t score_key(float f) {
     return (u >> 31) ? ~u : (u | 0x80000000u);
 }
 
-__global__ void __launch_bounds__(kEvictThreads) evict_kernel(const __grid_constant__ EvictArgs a) {
-    __shared__ uint32_t s_hist[256];
+__global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const __grid_constant__ EvictArgs a) {
+    extern __shared__ __align__(16) unsigned char smem[];
     __shared__ int s_scan[2][kEvictWarps];
     __shared__ uint32_t s_pick[2];
+    // the ring, before that the scores; the rows' places, before that the bins
+    float* const s_score = reinterpret_cast<float*>(smem);
+    longlong2* const s_row = reinterpret_cast<longlong2*>(smem + kRingBytes);  // [2][kEvictThreads] (from, to)
+    uint32_t* const s_hist = reinterpret_cast<uint32_t*>(smem + kRingBytes);
+    static_assert(kBins * 4 <= 2 * kEvictThreads * 16, "bins in the rows' place");
     const int h = blockIdx.x, l = blockIdx.y, b = blockIdx.z;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int64_t col = (int64_t(b) * a.n_layers + l) * a.n_kv_heads + h;
@@ -71,6 +86,14 @@ __global__ void __launch_bounds__(kEvictThreads) evict_kernel(const __grid_const
     }
     if (lead && tid == 0) a.len_out[b] = m;
 
+    const bool held = n <= kHeldScores;
+    if (held) {
+#pragma unroll 4
+        for (int i = tid; i < n; i += kEvictThreads) s_score[i] = score[i];
+        __syncthreads();
+    }
+    auto score_at = [&](int i) { return held ? s_score[i] : score[i]; };
+
     // 1. the cut among the slots between the first and the last ones
     const int lo = n > a.budget ? a.n_sink : n, hi = n > a.budget ? n - a.n_recent : n;
     int need = a.budget - a.n_sink - a.n_recent;  // of those
@@ -78,35 +101,43 @@ __global__ void __launch_bounds__(kEvictThreads) evict_kernel(const __grid_const
     int ties = 0;                                 // and so many, the first ones, of those equal to it
     if (n > a.budget && need > 0) {
         uint32_t prefix = 0;
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = tid; i < 256; i += kEvictThreads) s_hist[i] = 0;
+        for (int shift = 21; shift >= -1; shift -= 11) {  // bits 31..21, 20..10, 9..0
+            const int at = max(shift, 0), bits = shift < 0 ? 10 : 11;
+            for (int i = tid; i < kBins; i += kEvictThreads) s_hist[i] = 0;
             __syncthreads();
             for (int i = lo + tid; i < hi; i += kEvictThreads) {
-                const uint32_t k = score_key(score[i]);
-                if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8)))
-                    atomicAdd(&s_hist[(k >> shift) & 255], 1u);
+                const uint32_t k = score_key(score_at(i));
+                if (shift == 21 || (k >> (at + bits)) == (prefix >> (at + bits)))
+                    atomicAdd(&s_hist[(k >> at) & ((1u << bits) - 1)], 1u);
             }
             __syncthreads();
-            if (warp == 0) {  // the bin, from the top, where the count reaches `need`
-                uint32_t own[8], sum = 0;
+            // the bin, from the top, where the count reaches `need`: four bins a thread
+            constexpr int kPer = kBins / kEvictThreads;
+            uint32_t own[kPer], sum = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum += own[i] = s_hist[255 - (lane * 8 + i)];
-                uint32_t upto = sum;
+            for (int i = 0; i < kPer; ++i) sum += own[i] = s_hist[kBins - 1 - (tid * kPer + i)];
+            uint32_t upto = sum;
 #pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const uint32_t o = __shfl_up_sync(kFull, upto, d);
-                    if (lane >= d) upto += o;
-                }
-                uint32_t before = upto - sum;
-                if (before < uint32_t(need) && upto >= uint32_t(need)) {
-                    int i = 0;
-                    while (before + own[i] < uint32_t(need)) before += own[i++];
-                    s_pick[0] = uint32_t(255 - (lane * 8 + i));
-                    s_pick[1] = before;
-                }
+            for (int d = 1; d < 32; d <<= 1) {
+                const uint32_t o = __shfl_up_sync(kFull, upto, d);
+                if (lane >= d) upto += o;
+            }
+            if (lane == 31) s_scan[0][warp] = int(upto);
+            __syncthreads();
+            uint32_t before = upto - sum;
+#pragma unroll
+            for (int w = 0; w < kEvictWarps; ++w)
+                if (w < warp) before += uint32_t(s_scan[0][w]);
+            if (before < uint32_t(need) && before + sum >= uint32_t(need)) {
+                int i = 0;
+#pragma unroll
+                for (int x = 0; x < kPer - 1; ++x)
+                    if (i == x && before + own[x] < uint32_t(need)) before += own[x], ++i;
+                s_pick[0] = uint32_t(kBins - 1 - (tid * kPer + i));
+                s_pick[1] = before;
             }
             __syncthreads();
-            prefix |= s_pick[0] << shift;
+            prefix |= s_pick[0] << at;
             need -= int(s_pick[1]);
         }
         cut = prefix;
@@ -120,7 +151,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_kernel(const __grid_const
         bool above = false, tie = false;
         float x = 0.0f;
         if (i < n) {
-            x = score[i];
+            x = score_at(i);
             if (i < lo || i >= hi) {
                 above = true;
             } else {
@@ -158,36 +189,67 @@ __global__ void __launch_bounds__(kEvictThreads) evict_kernel(const __grid_const
     for (int64_t j = m + tid; j < a.score_stride; j += kEvictThreads) score_out[j] = 0.0f;
     __syncthreads();
 
-    // 3. rows: a thread moves one 16-byte vector of K and of V of kRows rows a tile
-    constexpr int kRows = 4;
-    const int lanes = a.head_dim / 8, per = kEvictThreads / lanes;
-    const int r0 = tid / lanes, v = tid - r0 * lanes;
-    const int64_t col_src = int64_t(l) * a.src.layer_stride + int64_t(h) * a.head_dim + v * 8;
-    const int64_t col_dst = int64_t(l) * a.dst.layer_stride + int64_t(h) * a.head_dim + v * 8;
-    for (int j0 = 0; j0 < m; j0 += per * kRows) {
-        uint4 k[kRows], w[kRows];
-        int64_t to[kRows];
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            const int j = j0 + r * per + r0;
-            to[r] = -1;
-            if (r0 < per && j < m) {
-                const int i = keep[j];
-                uint32_t e = 0;
-                if (!a.in_place || i != j) {
-                    const int64_t from = slot_row(a.src, b, i, e) + col_src;
-                    to[r] = slot_row(a.dst, b, j, e) + col_dst;
-                    k[r] = *reinterpret_cast<const uint4*>(a.src.k + from);
-                    w[r] = *reinterpret_cast<const uint4*>(a.src.v + from);
-                }
-            }
+    // 3. rows. Their places are looked up by a thread each, for so many tiles at a time
+    const int lanes = a.head_dim / 8, per = kEvictThreads / lanes;  // threads a row, rows a tile
+    const int group = kEvictThreads / per;                          // tiles whose rows a lookup covers
+    const int my = tid / lanes, v = tid - my * lanes;
+    const uint16_t* const sk = a.src.k + int64_t(l) * a.src.layer_stride + int64_t(h) * a.head_dim + v * 8;
+    const uint16_t* const sv = a.src.v + (sk - a.src.k);
+    uint16_t* const dk = a.dst.k + int64_t(l) * a.dst.layer_stride + int64_t(h) * a.head_dim + v * 8;
+    uint16_t* const dv = a.dst.v + (dk - a.dst.k);
+    const uint32_t ring = smem_u32(smem) + uint32_t(tid) * 16;  // a tile: the threads' vectors of K, then of V
+    auto look_up = [&](int c) {
+        const int j = c * group * per + tid;
+        longlong2 r = make_longlong2(-1, -1);
+        if (tid < group * per && j < m) {
+            const int i = keep[j];
+            uint32_t e = 0;
+            if (!a.in_place || i != j) r = make_longlong2(slot_row(a.src, b, i, e), slot_row(a.dst, b, j, e));
         }
-        if (a.in_place) __syncthreads();
+        s_row[(c & 1) * kEvictThreads + tid] = r;
+    };
+    const int n_tiles = (m + per - 1) / per;
+    look_up(0);
+    int64_t to[kRing];
+    int c = 0, in = 0;  // the lookup in use, and the next tile's place in it
+    for (int t0 = 0; t0 < n_tiles + kRing - 1; t0 += kRing) {
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            if (to[r] >= 0) {
-                st_row(a.dst.k + to[r], k[r]);
-                st_row(a.dst.v + to[r], w[r]);
+        for (int u = 0; u < kRing; ++u) {
+            const int t = t0 + u;
+            if (t < n_tiles) {
+                if (in == 0) {
+                    __syncthreads();  // lookup c is there, and c - 1 no longer needed
+                    look_up(c + 1);
+                }
+                to[u] = -1;
+                if (my < per) {
+                    const longlong2 r = s_row[(c & 1) * kEvictThreads + in * per + my];
+                    to[u] = r.y;
+                    if (r.x >= 0) {
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + uint32_t(u) * (kEvictThreads * 32)),
+                                     "l"(sk + r.x)
+                                     : "memory");
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + uint32_t(u) * (kEvictThreads * 32) + kEvictThreads * 16),
+                                     "l"(sv + r.x)
+                                     : "memory");
+                    }
+                }
+                if (++in == group) in = 0, ++c;
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            constexpr int kBack = kRing - 1;
+            if (t >= kBack && t - kBack < n_tiles) {  // the tile kBack before has landed
+                const int o = (u + 1) % kRing;
+                asm volatile("cp.async.wait_group %0;" ::"n"(kBack) : "memory");
+                if (a.in_place) __syncthreads();
+                if (to[o] >= 0) {
+                    uint4 x, y;
+                    const uint32_t p = ring + uint32_t(o) * (kEvictThreads * 32);
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(p) : "memory");
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y.x), "=r"(y.y), "=r"(y.z), "=r"(y.w) : "r"(p + kEvictThreads * 16) : "memory");
+                    st_row(dk + to[o], x);
+                    st_row(dv + to[o], y);
+                }
             }
         }
     }
@@ -197,7 +259,9 @@ __global__ void __launch_bounds__(kEvictThreads) evict_kernel(const __grid_const
 
 cudaError_t launch_evict(const EvictArgs& a, int n_seqs, cudaStream_t stream) {
     const dim3 grid(unsigned(a.n_kv_heads), unsigned(a.n_layers), unsigned(n_seqs));
-    return launch_pdl(evict_kernel, grid, dim3(kEvictThreads), 0, stream, a);
+    const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(evict_kernel), kEvictSmem);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(evict_kernel, grid, dim3(kEvictThreads), kEvictSmem, stream, a);
 }
 
 }  // namespace prcr

@@ -358,6 +358,9 @@ struct CacheView {
     int32_t block_size;         // 1 for a contiguous cache
     int32_t n_blocks;
     int32_t kind;
+    // slot / block_size = slot * div_mul >> div_shift, for slots below 2^31
+    uint32_t div_mul;
+    int32_t div_shift;
 };
 
 struct AppendArgs {

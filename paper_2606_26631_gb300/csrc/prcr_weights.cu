@@ -14,8 +14,8 @@
 //  2. Maxima, then exp and sums, of each head over all slots; a cluster's CTAs write theirs into
 //     one another's shared memory.
 //  3. The slot's weights, normalised, are added to its score.
-// Memory-bound: keys and scores are touched once. A warp keeps two tiles (8 KB at head_dim 128) in
-// flight, two CTAs of 8 warps fit an SM.
+// Memory-bound: keys and scores are touched once. A warp has a tile (4 KB at
+// head_dim 128) in flight behind the one in use; two CTAs of 8 warps fit an SM.
 // Where the logits of a sequence do not fit a cluster's shared memory (above
 // 400,000 / group slots), they go through the workspace instead (weights_logits_kernel,
 // weights_sum_kernel).
@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) weights_kernel(const __grid_co
     constexpr int P = D / 2, KS = Sh::kSteps, LV = Sh::kLoads, PARTS = Sh::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float s_part[kWarps][8], s_peer[2][kMaxRanks][8];
-    uint2* const frag = reinterpret_cast<uint2*>(smem);  // [3][KS][32]: the query's B fragments
+    uint4* const frag = reinterpret_cast<uint4*>(smem);  // [3][KS / 2][32]: the query's B fragments of two k-steps
     float* const logit = reinterpret_cast<float*>(smem + Sh::kFragBytes);
     const int C = a.cluster, rank = int(blockIdx.x) % C;
     const int unit = int(blockIdx.x) / C;
@@ -188,42 +188,43 @@ __global__ void __launch_bounds__(kWarps * 32, 2) weights_kernel(const __grid_co
     const int64_t pos = a.q_pos[b];
     const int per = ((len + 15) / 16 + C - 1) / C * 16;  // slots of a CTA, at most slots_per_cta
     const int s0 = min(len, rank * per), n = min(len, s0 + per) - s0;
-    const int n_tiles = (n + 15) / 16;
+    const int n_pairs = (n + 31) / 32;  // a warp's turn is two tiles of 16 slots
 
-    // keys: this lane's two rows of a tile, slots gid and gid + 8
+    // keys: a lane looks up the row of one of the 32 slots, a turn ahead, its block
+    // two; it reads 16-byte chunks of rows gid and gid + 8 of each tile
     const uint16_t* const kbase = a.cache.k + int64_t(l) * a.cache.layer_stride + int64_t(h) * D + t * 8;
     const int32_t* const bt = a.cache.block_table + int64_t(b) * a.cache.bt_stride;
     const bool paged = a.cache.kind == PRCR_CACHE_PAGED;
-    auto block_of = [&](int i, int half) -> int32_t {
-        const int s = i * 16 + half * 8 + gid;
-        return paged && s < n ? bt[uint32_t(s0 + s) / uint32_t(a.cache.block_size)] : 0;
+    auto block_of = [&](int i) -> int32_t {
+        const int s = i * 32 + lane;
+        return paged && s < n ? bt[block_index(a.cache, uint32_t(s0 + s))] : 0;
     };
-    auto row_of = [&](int i, int half, int32_t blk) -> int64_t {
-        const int s = i * 16 + half * 8 + gid;
+    auto row_of = [&](int i, int32_t blk) -> int64_t {
+        const int s = i * 32 + lane;
         if (s >= n) return -1;
-        if (!paged) return int64_t(b) * a.cache.seq_stride + int64_t(s0 + s) * a.cache.slot_stride;
-        if (blk < 0 || blk >= a.cache.n_blocks) {
-            err |= PRCR_ST_NO_BLOCK;
-            return -1;
-        }
-        return int64_t(blk) * a.cache.block_stride + int64_t(uint32_t(s0 + s) % uint32_t(a.cache.block_size)) * a.cache.slot_stride;
+        const int64_t row = row_in_block(a.cache, b, uint32_t(s0 + s), blk);
+        if (row < 0) err |= PRCR_ST_NO_BLOCK;
+        return row;
     };
     struct Stage {
         uint4 w0[LV], w1[LV];
     };
-    auto load = [&](Stage& s, int64_t r0, int64_t r1, int part) {
+    auto load = [&](Stage& s, int64_t row, int half, int part) {
+        const int64_t r0 = __shfl_sync(kFull, row, half * 16 + gid), r1 = __shfl_sync(kFull, row, half * 16 + 8 + gid);
+        const uint16_t* const p0 = kbase + r0 + part * Sh::kDims;
+        const uint16_t* const p1 = kbase + r1 + part * Sh::kDims;
 #pragma unroll
         for (int u = 0; u < LV; ++u) {
-            s.w0[u] = r0 >= 0 ? ld_stream(kbase + r0 + part * Sh::kDims + 32 * u) : make_uint4(0, 0, 0, 0);
-            s.w1[u] = r1 >= 0 ? ld_stream(kbase + r1 + part * Sh::kDims + 32 * u) : make_uint4(0, 0, 0, 0);
+            s.w0[u] = s.w1[u] = make_uint4(0, 0, 0, 0);
+            if (r0 >= 0) s.w0[u] = ld_stream(p0 + 32 * u);
+            if (r1 >= 0) s.w1[u] = ld_stream(p1 + 32 * u);
         }
     };
-    // (stages in the order of use: the parts of tile `warp`, of tile warp + 8, ..)
-    int tile = warp;
-    int32_t nb0 = block_of(tile + kWarps, 0), nb1 = block_of(tile + kWarps, 1);
-    int64_t r0 = row_of(tile, 0, block_of(tile, 0)), r1 = row_of(tile, 1, block_of(tile, 1));
-    Stage sa, sb;
-    if (tile < n_tiles) load(sa, r0, r1, 0);
+    int pair = warp;
+    int64_t row = row_of(pair, block_of(pair));
+    int32_t blk = block_of(pair + kWarps);
+    Stage st[2];
+    if (pair < n_pairs) load(st[0], row, 0, 0);
 
     // the group's queries, rotated and scaled, as fragments of three bf16 terms:
     // k-step j of lane group t covers dims 8 (t + 4 (j / 2)) + 4 (j % 2) + 0..3, as
@@ -251,7 +252,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) weights_kernel(const __grid_co
 #pragma unroll
         for (int term = 0; term < 3; ++term) {
             const uint2 f = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-            frag[(term * KS + j) * 32 + ln] = f;
+            reinterpret_cast<uint2*>(frag)[((term * KS + (j & ~1)) * 32 + 2 * ln) + (j & 1)] = f;
             v[0] -= lo_f32(f.x);
             v[1] -= hi_f32(f.x);
             v[2] -= lo_f32(f.y);
@@ -272,43 +273,35 @@ __global__ void __launch_bounds__(kWarps * 32, 2) weights_kernel(const __grid_co
             const int j = (part * Sh::kDims / 16) + 2 * u;
 #pragma unroll
             for (int term = 0; term < 3; ++term) {
-                const uint2 f0 = frag[(term * KS + j) * 32 + lane], f1 = frag[(term * KS + j + 1) * 32 + lane];
-                mma_16816(acc[term], s.w0[u].x, s.w1[u].x, s.w0[u].y, s.w1[u].y, f0.x, f0.y);
-                mma_16816(acc[term], s.w0[u].z, s.w1[u].z, s.w0[u].w, s.w1[u].w, f1.x, f1.y);
+                const uint4 f = frag[(term * (KS / 2) + (j >> 1)) * 32 + lane];
+                mma_16816(acc[term], s.w0[u].x, s.w1[u].x, s.w0[u].y, s.w1[u].y, f.x, f.y);
+                mma_16816(acc[term], s.w0[u].z, s.w1[u].z, s.w0[u].w, s.w1[u].w, f.z, f.w);
             }
         }
     };
     // the next stage is asked for, then this one's products are made; after a
     // tile's last part its logits are kept
-    int part = 0;
-    auto step = [&](Stage& now, Stage& next) {
-        const bool last = part == PARTS - 1;
-        const int64_t c0 = r0, c1 = r1;
-        const int i = tile;
-        if (last) {
-            tile += kWarps;
-            r0 = row_of(tile, 0, nb0);
-            r1 = row_of(tile, 1, nb1);
-            nb0 = block_of(tile + kWarps, 0);
-            nb1 = block_of(tile + kWarps, 1);
-        }
-        if (tile < n_tiles) load(next, r0, r1, last ? 0 : part + 1);
-        products(now, part);
-        if (last) {
+    for (; pair < n_pairs; pair += kWarps) {
+        const int64_t next = row_of(pair + kWarps, blk);
+        blk = block_of(pair + 2 * kWarps);
+        const uint32_t there = __ballot_sync(kFull, row >= 0);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int head = 2 * t + (e & 1), s = i * 16 + (e >> 1) * 8 + gid;
-                const float x = (e < 2 ? c0 : c1) >= 0 ? acc[0][e] + (acc[1][e] + acc[2][e]) : -INFINITY;
-                if (head < g) logit[head * stride + s] = x;
-                mx[e & 1] = fmaxf(mx[e & 1], x);
+        for (int i = 0; i < 2 * PARTS; ++i) {
+            const int half = i / PARTS, part = i % PARTS;
+            if (i + 1 < 2 * PARTS) load(st[(i + 1) & 1], row, (i + 1) / PARTS, (i + 1) % PARTS);
+            else if (pair + kWarps < n_pairs) load(st[0], next, 0, 0);
+            products(st[i & 1], part);
+            if (part == PARTS - 1) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int head = 2 * t + (e & 1), s = half * 16 + (e >> 1) * 8 + gid;
+                    const float x = (there >> s) & 1u ? acc[0][e] + (acc[1][e] + acc[2][e]) : -INFINITY;
+                    if (head < g) logit[head * stride + pair * 32 + s] = x;
+                    mx[e & 1] = fmaxf(mx[e & 1], x);
+                }
             }
         }
-        part = last ? 0 : part + 1;
-    };
-    while (tile < n_tiles) {
-        step(sa, sb);
-        if (tile >= n_tiles) break;
-        step(sb, sa);
+        row = next;
     }
 
     // each head's maximum over the cluster
