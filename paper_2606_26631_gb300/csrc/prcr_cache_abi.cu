@@ -44,21 +44,22 @@ bool heads_ok(const prcr_rope_cfg* cfg, int32_t n_q_heads) {
            int64_t(n_q_heads) * D <= PRCR_DECODE_MAX_Q_ELEMS;
 }
 
-// How a chunk call splits the slot axis: where its tiles of rows are fewer than
-// the SMs, into parts of whole 128-slot tiles.
+// How a chunk call splits the slots that a unit (rows of a tile, a KV head) sees. With
+// few rows in a unit the keys' and values' bytes bound it: about four CTAs per SM, which
+// even out lengths that differ. With many, where there are fewer units than
+// SMs, as many as fill them. (items: at most; the lengths are on the device.)
 struct ChunkSplit {
-    int64_t items, splits, len;
+    int64_t items, splits;
     size_t bytes;  // of the partials of this call, and of any shorter max_len
 };
 ChunkSplit chunk_split(const prcr_rope_cfg* cfg, int64_t n_seqs, int64_t n_q_heads, int64_t total_q, int64_t max_len, int sms) {
-    const int64_t group = n_q_heads / cfg->n_kv_heads;
+    const int64_t group = n_q_heads / cfg->n_kv_heads, rows = chunk_rows(cfg->head_dim);
     ChunkSplit c;
-    c.items = total_q * group / chunk_rows(cfg->head_dim) + std::min(n_seqs, total_q);
+    c.items = total_q * group / rows + std::min(n_seqs, total_q);
     const int64_t units = c.items * cfg->n_kv_heads, tiles = std::max<int64_t>(1, (max_len + 127) / 128);
-    const int64_t most = std::max<int64_t>(1, std::min(tiles, sms / units));
-    c.len = (tiles + most - 1) / most * 128;
-    c.splits = (tiles * 128 + c.len - 1) / c.len;
-    c.bytes = most > 1 ? size_t(total_q) * n_q_heads * most * (cfg->head_dim + 2) * sizeof(float) : 0;
+    const bool few_rows = total_q * group <= 64 * c.items;
+    c.splits = std::max<int64_t>(1, std::min(tiles, few_rows ? (4 * int64_t(sms) + units - 1) / units : sms / units));
+    c.bytes = c.splits > 1 ? size_t(total_q) * n_q_heads * c.splits * (cfg->head_dim + 2) * sizeof(float) : 0;
     return c;
 }
 
@@ -193,7 +194,6 @@ int prcr_chunk_attention(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache,
     }
     a.items = int32_t(split.items);
     a.splits = int32_t(split.splits);
-    a.split_len = split.len;
     a.cache = cache_view(cache, layer);
     a.q = static_cast<const uint16_t*>(q);
     a.q_stride = q_token_stride;
@@ -203,7 +203,7 @@ int prcr_chunk_attention(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache,
     a.out = static_cast<uint16_t*>(out);
     a.out_stride = out_token_stride;
     a.status = status;
-    a.max_len = max_len;
+    a.top = int32_t(max_len);  // (at most the capacity)
     a.n_seqs = n_seqs;
     a.total_q = total_q;
     a.n_kv_heads = cfg->n_kv_heads;

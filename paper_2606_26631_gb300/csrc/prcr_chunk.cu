@@ -133,6 +133,23 @@ __device__ __forceinline__ void store_row(void* p, const uint32_t* v, bool wide)
     }
 }
 
+struct ChunkSeq {
+    int t0, n, len;  // its first token of the call, its new tokens, its slots
+};
+__device__ __forceinline__ ChunkSeq chunk_seq(const ChunkArgs& a, int b) {
+    ChunkSeq s;
+    s.t0 = a.q_off[b];
+    s.n = a.q_off[b + 1] - s.t0;
+    s.len = a.seq_len[b];
+    return s;
+}
+// Tiles of each split of the slots that rows row0 .. of a sequence see.
+__device__ __forceinline__ int split_tiles(const ChunkArgs& a, int64_t first, int row0, int rows) {
+    const int64_t seen = min(int64_t(a.top), first + (row0 + rows - 1) / a.group + 1);
+    const int tiles = seen > 0 ? int((seen + kTile - 1) / kTile) : 0;
+    return (tiles + a.splits - 1) / a.splits;
+}
+
 // What a CTA works on, and the barriers of its roles.
 struct ChunkWork {
     int b, row0, rows, t0;        // sequence, first row, rows, the sequence's first token
@@ -186,56 +203,58 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
     if (tid < P) s_freq[tid] = a.turn_freq[tid];
     pdl_wait();
 
-    // this CTA's rows: items are tiles of 128 NQ rows, a sequence's last one
-    // (which sees the most slots) first
+    // This CTA's rows: an item is a sequence's rows of a tile; its last one, which sees
+    // the most slots, first, and of up to 32 sequences the longest first, so that
+    // the last CTAs to begin are short ones.
     if (warp == 0) {
-        int before = 0, b = -1, cnt = 0, local = 0, off = 0, end = 0, len = 0;
-        for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
-            int c = 0;
-            if (b0 + lane < a.n_seqs) {
-                off = a.q_off[b0 + lane];
-                end = a.q_off[b0 + lane + 1];
-                len = a.seq_len[b0 + lane];
-                const int64_t n = int64_t(end) - off;
-                c = n > 0 ? int((min(n, int64_t(a.total_q)) * G + Sh::kRows - 1) / Sh::kRows) : 0;
-            }
-            int upto = c;
+        int b = -1;
+        ChunkSeq seq = {};
+        for (int b0 = 0, before = 0; b0 < a.n_seqs; b0 += 32) {
+            ChunkSeq q = {};
+            if (b0 + lane < a.n_seqs) q = chunk_seq(a, b0 + lane);
+            const int c = q.n > 0 ? int((min(int64_t(q.n), int64_t(a.total_q)) * G + Sh::kRows - 1) / Sh::kRows) : 0;
+            int first = before;
+            if (a.n_seqs <= 32) {
+                for (int o = 0; o < a.n_seqs; ++o) {
+                    const int len = __shfl_sync(kFull, q.len, o), n = __shfl_sync(kFull, c, o);
+                    if (len > q.len || (len == q.len && o < lane)) first += n;
+                }
+            } else {
+                int upto = c;
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int o = __shfl_up_sync(kFull, upto, d);
-                if (lane >= d) upto += o;
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int o = __shfl_up_sync(kFull, upto, d);
+                    if (lane >= d) upto += o;
+                }
+                first += upto - c;
+                before += __shfl_sync(kFull, upto, 31);
             }
-            const bool here = item >= before + upto - c && item < before + upto;
-            const uint32_t who = __ballot_sync(kFull, here);
+            const uint32_t who = __ballot_sync(kFull, item >= first && item < first + c);
             if (who) {
                 const int src = __ffs(int(who)) - 1;
                 b = b0 + src;
-                cnt = __shfl_sync(kFull, c, src);
-                local = item - before - __shfl_sync(kFull, upto - c, src);
-                off = __shfl_sync(kFull, off, src);
-                end = __shfl_sync(kFull, end, src);
-                len = __shfl_sync(kFull, len, src);
+                seq.t0 = __shfl_sync(kFull, q.t0, src);
+                seq.n = __shfl_sync(kFull, q.n, src);
+                seq.len = __shfl_sync(kFull, q.len, src);
+                w.row0 = __shfl_sync(kFull, (c - 1 - (item - first)) * Sh::kRows, src);
                 break;
             }
-            before += __shfl_sync(kFull, upto, 31);
         }
         if (lane == 0) {
             w.b = b;
             if (b >= 0) {
-                const int t0 = off, n = end - off;
-                const int64_t top = min(a.cache.capacity, a.max_len);
-                if (len < 0 || len > top) atomicOr(a.status, PRCR_ST_CAPACITY);
-                w.t0 = t0;
-                w.row0 = (cnt - 1 - local) * Sh::kRows;
-                w.rows = min(Sh::kRows, n * G - w.row0);
-                w.first = int64_t(len) - n;
-                w.lo = int64_t(split) * a.split_len;
+                if (seq.len < 0 || seq.len > a.top) atomicOr(a.status, PRCR_ST_CAPACITY);
+                w.t0 = seq.t0;
+                w.rows = min(Sh::kRows, seq.n * G - w.row0);
+                w.first = int64_t(seq.len) - seq.n;
+                const int per = split_tiles(a, w.first, w.row0, w.rows);
+                w.lo = int64_t(split) * per * kTile;
                 int64_t hi = 0;
                 for (int q = 0; q < 2; ++q) {
                     w.tiles[q] = 0;
                     if (q < NQ && q * 128 < w.rows) {
                         const int last = (w.row0 + min(w.rows, q * 128 + 128) - 1) / G;
-                        hi = min(min(top, w.first + last + 1), w.lo + a.split_len);
+                        hi = min(min(int64_t(a.top), w.first + last + 1), w.lo + int64_t(per) * kTile);
                         w.tiles[q] = hi > w.lo ? int((hi - w.lo + kTile - 1) / kTile) : 0;
                     }
                 }
@@ -369,17 +388,20 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                     }
                 }
                 const float mt = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * scale;
-                const bool raise = mt > m_run + kRaise || m_run == -INFINITY;
+                const bool raise = mt > m_run + kRaise;
+                bool summed = j == 0;  // whether the last tile's products are known to be done
                 if (j == 0) {
                     m_run = mt;
-                } else if (__any_sync(kFull, raise && mt > m_run)) {
+                } else if (__any_sync(kFull, raise)) {
+                    // (NQ = 2: this S was made behind the last tile's products)
                     if (NQ == 1 && !mbar_wait(smem_u32(&bars.o[0]), uint32_t((j - 1) & 1))) {
                         failed = true;
                         break;
                     }
+                    summed = true;
                     tc_fence_after();
                     float f = 1.0f;
-                    if (raise && mt > m_run) {
+                    if (raise) {
                         f = exp2_fast(m_run - mt);
                         m_run = mt;
                     }
@@ -423,6 +445,11 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                 }
                 const uint64_t sum = add2(sum0, sum1);
                 l_run += lo32(sum) + hi32(sum);
+                // (every phase of this barrier is waited for: parities tell one from the next)
+                if (NQ == 1 && !summed && !mbar_wait(smem_u32(&bars.o[0]), uint32_t((j - 1) & 1))) {
+                    failed = true;
+                    break;
+                }
             }
             // all of this half's products are done
             if (!failed && w.tiles[qi] > 0) {
@@ -707,11 +734,11 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
     if (warp == kSoft + 4) tmem_free(tmem, 512);
 }
 
-// Joins the splits of a row: (max, sum, accumulator) of the splits that it sees.
-template <int D>
+// Joins the splits of a row: (max, sum, accumulator) of those that it sees.
+template <int D, int NQ>
 __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant__ ChunkArgs a) {
-    constexpr int E = D / 32;
-    const int lane = threadIdx.x & 31, Hq = a.n_kv_heads * a.group;
+    constexpr int E = D / 32, kRows = ChunkShape<D, NQ>::kRows;
+    const int lane = threadIdx.x & 31, G = a.group, Hq = a.n_kv_heads * G;
     const int64_t row = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
     pdl_allow();
     pdl_wait();
@@ -719,9 +746,12 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
     if (row >= int64_t(a.total_q) * Hq) return;
     const int t = int(row / Hq), hq = int(row - int64_t(t) * Hq);
     const int b = sequence_of(a.q_off, a.n_seqs, t);
-    if (t >= a.q_off[b + 1]) return;  // behind the last sequence
-    const int64_t lim = min(min(a.cache.capacity, a.max_len), int64_t(a.seq_len[b]) - (a.q_off[b + 1] - 1 - t));
-    const int n = lim > 0 ? int((lim + a.split_len - 1) / a.split_len) : 0;
+    const ChunkSeq q = chunk_seq(a, b);
+    if (t >= q.t0 + q.n) return;  // behind the last sequence
+    const int64_t first = int64_t(q.len) - q.n, lim = min(int64_t(a.top), first + (t - q.t0) + 1);
+    const int row0 = ((t - q.t0) * G + hq % G) / kRows * kRows;
+    const int per = split_tiles(a, first, row0, min(kRows, q.n * G - row0)) * kTile;
+    const int n = lim > 0 ? int((lim + per - 1) / per) : 0;
     float m = -INFINITY, l = 0.0f, o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.0f;
@@ -729,6 +759,7 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, d));
     const float mu = m == -INFINITY ? 0.0f : m;
+#pragma unroll 4
     for (int s = 0; s < n; ++s) {
         const float2 ml = a.partial_ml[row * a.splits + s];
         const float f = exp2f(ml.x - mu);
@@ -752,7 +783,7 @@ cudaError_t launch_shape(const ChunkArgs& a, cudaStream_t stream) {
     const cudaError_t r = launch_pdl(chunk_kernel<D, NQ>, grid, dim3(Sh::kThreads), Sh::kSmem, stream, a);
     if (r != cudaSuccess || a.splits == 1) return r;
     const int64_t rows = int64_t(a.total_q) * a.n_kv_heads * a.group;
-    return launch_pdl(chunk_merge_kernel<D>, dim3(unsigned((rows + 7) / 8)), dim3(256), 0, stream, a);
+    return launch_pdl(chunk_merge_kernel<D, NQ>, dim3(unsigned((rows + 7) / 8)), dim3(256), 0, stream, a);
 }
 
 }  // namespace

@@ -398,7 +398,7 @@ struct ChunkArgs {
     uint16_t* out;
     int64_t out_stride;
     uint32_t* status;
-    int64_t max_len;
+    int32_t top;                // the longest length read: max_len, at most the capacity
     int32_t n_seqs;
     int32_t total_q;
     int32_t n_kv_heads;
@@ -410,8 +410,7 @@ struct ChunkArgs {
     int32_t sec_w;
     float scale_log2;           // log2(e) / sqrt(head_dim)
     int32_t items;              // tiles of rows, of all sequences, at most
-    int32_t splits;             // parts of the slot axis
-    int64_t split_len;          // slots of each, a multiple of 128
+    int32_t splits;             // parts of the slots that an item sees
     float* partial;             // workspace when splits > 1: [total_q][n_q_heads][splits][D]
     float2* partial_ml;         // [total_q][n_q_heads][splits] (maximum, sum)
     uint64_t turn_freq[kMaxPairs];

@@ -36,8 +36,13 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
     };
     if (ready()) return true;
     const long long t0 = clock64();
-    while (!ready())
-        if (clock64() - t0 > kWaitCycles) return false;
+    while (!ready()) {
+        if (clock64() - t0 > kWaitCycles) {
+            // (looked at once more, later than any lane of the warp gives up: one answer for all)
+            __nanosleep(2000);
+            return ready();
+        }
+    }
     return true;
 }
 

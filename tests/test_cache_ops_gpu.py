@@ -191,7 +191,8 @@ def test_chunk(H, g, D, block, kind):
 @pytest.mark.parametrize("H,g,D,block,new,lens", [
     (8, 4, 128, 16, [1], [9000]), (1, 1, 128, 16, [2], [40000]), (2, 7, 128, 0, [5, 1], [20011, 3]), (4, 4, 64, 32, [3], [12345]),
     (2, 8, 256, 16, [4, 2], [5000, 6001]), (2, 4, 128, 16, [300], [20000]), (1, 8, 128, 0, [1024], [1024]), (2, 2, 64, 16, [2500], [2500]),
-    (1, 2, 256, 16, [1500], [1700]),
+    (1, 2, 256, 16, [1500], [1700]), (8, 4, 128, 16, [1900, 0, 800], [1900, 7, 3000]), (4, 8, 256, 0, [1000, 400], [1300, 400]),
+    (8, 8, 64, 7, [1500], [1500]), (8, 4, 128, 64, [2600], [2600]), (8, 4, 128, 256, [300, 2300], [5000, 2300]),
 ], ids=lambda v: str(v))
 def test_chunk_long(H, g, D, block, new, lens):
     c = Chunk(H, g, D, new, lens, block, seed=5)
@@ -248,6 +249,27 @@ def test_chunk_hidden_slots_do_not_matter(H, g, D, block, bad):
         seeing = U.f64(c.out[at + free:at + n])
         assert not np.isfinite(seeing).any()
         at += n
+
+
+@pytest.mark.parametrize("H,g,D,block", [(8, 4, 128, 16), (4, 8, 256, 16), (8, 8, 64, 0)])
+def test_chunk_many_rows_with_bad_slots(H, g, D, block):
+    """Whole units (many rows): a value that is not finite reaches the queries that see it and no others; an unmapped block
+    is left out of every query's slots."""
+    c = Chunk(H, g, D, [1900, 40], [1900, 300], block, seed=3)
+    w = c.cache.where(0, [1500])
+    c.cache.v[w] = float("nan")
+    assert c.run().done() == 0
+    got = U.f64(c.out[:1940])
+    assert np.isfinite(got[:1500]).all() and np.isnan(got[1500:1900]).all() and np.isfinite(got[1900:]).all()
+    i = np.unique(np.r_[0:5, 700:705, 1490:1500])
+    K, V = (U.f64(c.cache.rows(x, 0, 1500)[1]) for x in (c.cache.k, c.cache.v))
+    ref, bar = U.chunk64(U.f64(c.q[i]), c.pos[i], K, V, U.causal(1900, 1900, 1500)[i])
+    assert (np.abs(got[i] - ref) <= bar).all()
+    c.check(seqs=[1], rows=5)
+    if block:
+        c = Chunk(H, g, D, [1900, 40], [1900, 300], block, seed=4, unmapped=[(0, 100)])
+        assert c.run().done() == prcr.ST_NO_BLOCK
+        c.check(rows=12, drop=lambda b, s: (s // block == 100) if b == 0 else s < 0)
 
 
 def test_chunk_nan_key_reaches_those_that_see_it():
