@@ -432,12 +432,13 @@ def _small(name: str, t: torch.Tensor, dtype, numel: int):
 
 def _same_device(first: torch.Tensor, *others):
     """The library works on the current device: tensors of another one are refused."""
+    index = first.get_device()  # -1 on the CPU
     for t in others:
-        if t is not None and t.device != first.device:
+        if t is not None and t.get_device() != index:
             raise ValueError("all tensors must be on one device")
-    if first.device.type != "cuda":
+    if index < 0:
         raise ValueError("tensors must be on a CUDA device")
-    if first.device.index != torch.cuda.current_device():
+    if index != (torch.cuda.current_device() if _raw_device is None else _raw_device()):
         raise ValueError(f"tensors are on {first.device}, which is not the current CUDA device")
 
 

@@ -44,10 +44,13 @@ bool heads_ok(const prcr_rope_cfg* cfg, int32_t n_q_heads) {
            int64_t(n_q_heads) * D <= PRCR_DECODE_MAX_Q_ELEMS;
 }
 
-// How a chunk call splits the slots that a unit (rows of a tile, a KV head) sees. With
-// few rows in a unit the keys' and values' bytes bound it: about four CTAs per SM, which
-// even out lengths that differ. With many, where there are fewer units than
-// SMs, as many as fill them. (items: at most; the lengths are on the device.)
+// How a chunk call splits the slots that a unit (rows of a tile, a KV head) sees, one
+// CTA to an SM: into as many as give every SM one. With few rows in a unit the keys' and
+// values' bytes bound it and its partials are small, so the number is rounded up: a
+// second, partial wave evens out lengths that differ (16 sequences of up to 8198 slots,
+// 8 rows a unit, 128 units on 152 SMs: 2 splits 69 us, 1 split 87, 3 76, 5 88, 8 113).
+// With many rows it is rounded down: the partials cost more than the idle SMs (D = 256:
+// up 183 us, down 178). (items: at most; the lengths are on the device.)
 struct ChunkSplit {
     int64_t items, splits;
     size_t bytes;  // of the partials of this call, and of any shorter max_len
@@ -58,7 +61,7 @@ ChunkSplit chunk_split(const prcr_rope_cfg* cfg, int64_t n_seqs, int64_t n_q_hea
     c.items = total_q * group / rows + std::min(n_seqs, total_q);
     const int64_t units = c.items * cfg->n_kv_heads, tiles = std::max<int64_t>(1, (max_len + 127) / 128);
     const bool few_rows = total_q * group <= 64 * c.items;
-    c.splits = std::max<int64_t>(1, std::min(tiles, few_rows ? (4 * int64_t(sms) + units - 1) / units : sms / units));
+    c.splits = std::max<int64_t>(1, std::min(tiles, (sms + (few_rows ? units - 1 : 0)) / units));
     c.bytes = c.splits > 1 ? size_t(total_q) * n_q_heads * c.splits * (cfg->head_dim + 2) * sizeof(float) : 0;
     return c;
 }
