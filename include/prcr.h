@@ -436,16 +436,17 @@ PRCR_API int prcr_append_kv(const prcr_rope_cfg* cfg, const prcr_cache_desc* cac
  *            otherwise PRCR_ST_CSR and nothing is written
  *   seq_len  device int32 [n_seqs]; max_len >= every seq_len is a host bound
  *   out      device bf16: out[t*out_token_stride + h*D]; rows behind q_off[n_seqs]
- *            are left as they were. out may not overlap q
+ *            are left as they were. out must not overlap q
  * q and out are 16-byte aligned, their strides multiples of 8. Limits: D in {64,
  * 128, 256}, at most 8 query heads per KV head, n_q_heads * D <= PRCR_DECODE_MAX_Q_ELEMS.
  * The rotated query and the probabilities are rounded to bf16 for the tensor
  * cores; sums, maxima and the output's accumulator are float32.
- * workspace: device, >= prcr_chunk_workspace_size(...) bytes (0 where the call
- * needs none), 16-byte aligned, not shared with a concurrent call.
+ * workspace: device, prcr_chunk_workspace_size(...) bytes are enough for every call
+ * of at most so many sequences, tokens and slots (many need none); 16-byte
+ * aligned, not shared with a concurrent call.
  * A seq_len that is negative, beyond the capacity or above max_len sets
- * PRCR_ST_CAPACITY (slots past either are left out); an unmapped block in
- * range sets PRCR_ST_NO_BLOCK and its slots are left out. A query that sees no
+ * PRCR_ST_CAPACITY (slots past either are left out; a sequence without new tokens
+ * is not looked at); an unmapped block in range sets PRCR_ST_NO_BLOCK and its slots are left out. A query that sees no
  * slot gets zeros. Slots that a query does not see have no influence on its
  * output, whatever they hold (infinities and NaN included).                   */
 PRCR_API size_t prcr_chunk_workspace_size(const prcr_rope_cfg* cfg, int32_t n_seqs,
@@ -471,6 +472,7 @@ PRCR_API int prcr_chunk_attention(const prcr_rope_cfg* cfg, const prcr_cache_des
  *            are left as they were
  * Limits, a seq_len beyond the capacity or max_len, a q_pos of magnitude 2^31 or
  * more, and unmapped blocks are prcr_decode_attention's (such slots get weight 0).
+ * With max_len 0 nothing is done.
  * workspace: device, >= prcr_weights_workspace_size(...) bytes (0 unless max_len is
  * above 400,000 / query heads per KV head), 16-byte aligned, not shared with a
  * concurrent call.                                                            */
@@ -496,8 +498,8 @@ PRCR_API int prcr_accumulate_weights(const prcr_rope_cfg* cfg, const prcr_cache_
  *               memory); the rows read must not be among those written
  *   seq_len     device int32 [n_seqs]; max_len >= every seq_len is a host bound
  *   score       device float32 as for prcr_accumulate_weights (score_stride >= max_len)
- *   score_out   device, same layout; may be score itself. Entries from the new
- *               length to score_stride become 0
+ *   score_out   device, same layout; score itself or apart from it. Entries from the
+ *               new length to score_stride become 0
  *   keep_out    device int32 [n_seqs][n_layers][n_kv_heads][budget]: the slots kept,
  *               ascending; -1 behind the new length
  *   seq_len_out device int32 [n_seqs]: min(seq_len, budget) (must not alias seq_len)

@@ -229,7 +229,7 @@ def cache_contiguous(k: torch.Tensor, v: torch.Tensor) -> CacheDesc:
     d.seq_stride, d.layer_stride, d.slot_stride = k.stride(0), k.stride(1), k.stride(2)
     d.block_stride, d.block_table, d.bt_stride, d.n_blocks = 0, None, 0, 0
     d.max_slots, d.n_seqs = k.shape[2], k.shape[0]
-    d._keep = (k, v)
+    d._keep, d._rows = (k, v), (k.shape[1], k.shape[3], k.shape[4])
     return d
 
 
@@ -247,7 +247,7 @@ def cache_paged(k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor) -> 
     d.block_stride, d.slot_stride = k.stride(1), k.stride(2)
     d.block_table, d.bt_stride = block_table.data_ptr(), block_table.stride(0)
     d.n_blocks, d.max_slots, d.n_seqs = k.shape[1], 0, block_table.shape[0]
-    d._keep = (k, v, block_table)
+    d._keep, d._rows = (k, v, block_table), (k.shape[0], k.shape[3], k.shape[4])
     return d
 
 
@@ -430,6 +430,29 @@ def _small(name: str, t: torch.Tensor, dtype, numel: int):
         raise TypeError(f"{name} must be a contiguous {dtype} tensor of at least {numel} entries")
 
 
+def _strides(t: torch.Tensor, dims: int, name: str):
+    """Element strides of a tensor of heads' rows; a dimension of one entry may have any, and counts
+    as packed."""
+    stride, shape = t.stride(), t.shape
+    if len(shape) != dims:
+        raise ValueError(f"{name} must have {dims} dimensions")
+    if shape[0] > 1 and shape[-3] > 1:
+        return stride
+    stride = list(stride)
+    for i in range(dims - 3, -1, -1):
+        if shape[i] <= 1:
+            stride[i] = stride[i + 1] * shape[i + 1]
+    return tuple(stride)
+
+
+def _cache_rows(cfg, cache, n_layers: int):
+    """The cache's tensors hold so many layers of the configuration's heads."""
+    layers, heads, dim = cache._rows
+    if layers < n_layers or heads != cfg.n_kv_heads or dim != cfg.head_dim:
+        raise ValueError(f"the cache holds {layers} layers of {heads} heads of {dim}, the call is for "
+                         f"{n_layers} of {cfg.n_kv_heads} heads of {cfg.head_dim}")
+
+
 def _same_device(first: torch.Tensor, *others):
     """The library works on the current device: tensors of another one are refused."""
     index = first.get_device()  # -1 on the CPU
@@ -449,18 +472,19 @@ def append_kv(cfg, cache, layer_begin: int, k_src: torch.Tensor, v_src: torch.Te
     bf16 (row-contiguous), coords int32 [total, 3], tok_off int32 [B + 1], cache_len_in /
     cache_len_out int32 [B]."""
     _bf16(k_src, "k_src"); _bf16(v_src, "v_src")
-    stride, shape = k_src.stride(), k_src.shape
-    if stride != v_src.stride() or shape != v_src.shape or len(shape) != 4:
+    stride, (nl, total, heads, dim) = _strides(k_src, 4, "k_src"), k_src.shape
+    if k_src.shape != v_src.shape or stride != _strides(v_src, 4, "v_src"):
         raise ValueError("k_src and v_src must be [n_layers, total, H, D] with the same strides")
-    if shape[2] != cfg.n_kv_heads or shape[3] != cfg.head_dim:
+    if heads != cfg.n_kv_heads or dim != cfg.head_dim:
         raise ValueError("k_src rows must be [n_kv_heads, head_dim]")
-    n_seqs, total = cache_len_in.numel(), shape[1]
+    _cache_rows(cfg, cache, layer_begin + nl)
+    n_seqs = cache_len_in.numel()
     _small("coords", coords, torch.int32, 3 * total)
     _small("tok_off", tok_off, torch.int32, n_seqs + 1)
     _small("cache_len_in", cache_len_in, torch.int32, 0)
     _small("cache_len_out", cache_len_out, torch.int32, n_seqs)
     _same_device(cache._keep[0], k_src, v_src, coords, tok_off, cache_len_in, cache_len_out, status)
-    rc = lib().prcr_append_kv(C.byref(cfg), C.byref(cache), n_seqs, int(layer_begin), shape[0],
+    rc = lib().prcr_append_kv(C.byref(cfg), C.byref(cache), n_seqs, int(layer_begin), nl,
                               k_src.data_ptr(), v_src.data_ptr(), stride[0], stride[1],
                               coords.data_ptr(), tok_off.data_ptr(), total,
                               cache_len_in.data_ptr(), cache_len_out.data_ptr(), status.data_ptr(),
@@ -479,19 +503,22 @@ def chunk_attention(cfg, cache, layer: int, q: torch.Tensor, coords: torch.Tenso
     """prcr_chunk_attention: q and out [total_q, Hq, D] bf16 (a token's [Hq, D] contiguous, any
     token stride), coords int32 [total_q, 3], q_off int32 [B + 1], seq_len int32 [B]."""
     _bf16(q, "q"); _bf16(out, "out")
-    if q.shape != out.shape or q.dim() != 3 or q.shape[2] != cfg.head_dim:
+    qs, os = _strides(q, 3, "q"), _strides(out, 3, "out")
+    total, heads, dim = q.shape
+    if q.shape != out.shape or dim != cfg.head_dim:
         raise ValueError("q and out must be [total_q, Hq, head_dim]")
-    n_seqs, total = seq_len.numel(), q.shape[0]
+    _cache_rows(cfg, cache, layer + 1)
+    n_seqs = seq_len.numel()
     _small("coords", coords, torch.int32, 3 * total)
     _small("q_off", q_off, torch.int32, n_seqs + 1)
     _small("seq_len", seq_len, torch.int32, 0)
     _same_device(cache._keep[0], q, coords, q_off, seq_len, out, status, workspace)
     ws = None if workspace is None else workspace.data_ptr()
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = lib().prcr_chunk_attention(C.byref(cfg), C.byref(cache), n_seqs, int(layer), q.shape[1],
-                                    q.data_ptr(), q.stride(0), coords.data_ptr(), q_off.data_ptr(),
+    rc = lib().prcr_chunk_attention(C.byref(cfg), C.byref(cache), n_seqs, int(layer), heads,
+                                    q.data_ptr(), qs[0], coords.data_ptr(), q_off.data_ptr(),
                                     total, seq_len.data_ptr(), int(max_len), out.data_ptr(),
-                                    out.stride(0), status.data_ptr(), ws, nbytes, _stream(stream))
+                                    os[0], status.data_ptr(), ws, nbytes, _stream(stream))
     return _check(rc, "prcr_chunk_attention")
 
 
@@ -515,6 +542,7 @@ def accumulate_weights(cfg, cache, q: torch.Tensor, q_pos: torch.Tensor, seq_len
         raise TypeError("q must be a contiguous bfloat16 [B, n_layers, Hq, D] tensor")
     if q.shape[1] != cfg.n_layers or q.shape[3] != cfg.head_dim:
         raise ValueError("q must be [B, n_layers, Hq, head_dim]")
+    _cache_rows(cfg, cache, cfg.n_layers)
     n_seqs = q.shape[0]
     _small("q_pos", q_pos, torch.int64, n_seqs)
     _small("seq_len", seq_len, torch.int32, n_seqs)
@@ -537,6 +565,9 @@ def evict(cfg, cache, seq_len: torch.Tensor, max_len: int, budget: int, n_sink: 
     score_out (default: score itself) float32 [B, n_layers, n_kv_heads, S], keep_out int32
     [B, n_layers, n_kv_heads, budget]."""
     n_seqs = seq_len.numel()
+    _cache_rows(cfg, cache, cfg.n_layers)
+    if dst is not None:
+        _cache_rows(cfg, dst, cfg.n_layers)
     score_out = score if score_out is None else score_out
     _small("seq_len", seq_len, torch.int32, 0)
     _small("seq_len_out", seq_len_out, torch.int32, n_seqs)
@@ -545,6 +576,8 @@ def evict(cfg, cache, seq_len: torch.Tensor, max_len: int, budget: int, n_sink: 
     if score.shape[3] != score_out.shape[3]:
         raise ValueError("score and score_out must have rows of the same length")
     _small("keep_out", keep_out, torch.int32, n_seqs * cfg.n_layers * cfg.n_kv_heads * int(budget))
+    if keep_out.shape[-1] != budget:
+        raise ValueError("keep_out must be [B, n_layers, n_kv_heads, budget]")
     _same_device(cache._keep[0], seq_len, seq_len_out, score, score_out, keep_out, status,
                  None if dst is None else dst._keep[0])
     rc = lib().prcr_evict(C.byref(cfg), C.byref(cache), None if dst is None else C.byref(dst),

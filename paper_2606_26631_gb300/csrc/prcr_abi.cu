@@ -91,10 +91,14 @@ cudaError_t raise_smem_limit(const void* kernel, size_t smem) {
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     std::lock_guard<std::mutex> g(mu);
-    size_t& have = limits[std::make_pair(dev, kernel)];
-    if (have >= smem) return cudaSuccess;
+    size_t* have = nullptr;
+    try {
+        have = &limits[std::make_pair(dev, kernel)];
+    } catch (...) {  // no memory to note it in
+    }
+    if (have && *have >= smem) return cudaSuccess;
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
-    if (e == cudaSuccess) have = smem;
+    if (have && e == cudaSuccess) *have = smem;
     return e;
 }
 
@@ -198,7 +202,10 @@ int blocks_per_sm(int dev, int block, size_t smem, int kernel) {
                                                : fused_blocks_per_sm(block, smem, &n);
     if (e != cudaSuccess || n < 1) n = 1;
     std::lock_guard<std::mutex> g(mu);
-    cache[key] = n;
+    try {
+        cache[key] = n;
+    } catch (...) {  // no memory to note it in: asked for again
+    }
     return n;
 }
 
@@ -214,7 +221,10 @@ int sm_count(int dev) {
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1)
         n = 1;
     std::lock_guard<std::mutex> g(mu);
-    cache[dev] = n;
+    try {
+        cache[dev] = n;
+    } catch (...) {  // no memory to note it in: asked for again
+    }
     return n;
 }
 

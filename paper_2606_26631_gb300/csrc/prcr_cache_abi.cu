@@ -53,7 +53,6 @@ bool heads_ok(const prcr_rope_cfg* cfg, int32_t n_q_heads) {
 // up 183 us, down 178). (items: at most; the lengths are on the device.)
 struct ChunkSplit {
     int64_t items, splits;
-    size_t bytes;  // of the partials of this call, and of any shorter max_len
 };
 ChunkSplit chunk_split(const prcr_rope_cfg* cfg, int64_t n_seqs, int64_t n_q_heads, int64_t total_q, int64_t max_len, int sms) {
     const int64_t group = n_q_heads / cfg->n_kv_heads, rows = chunk_rows(cfg->head_dim);
@@ -62,8 +61,25 @@ ChunkSplit chunk_split(const prcr_rope_cfg* cfg, int64_t n_seqs, int64_t n_q_hea
     const int64_t units = c.items * cfg->n_kv_heads, tiles = std::max<int64_t>(1, (max_len + 127) / 128);
     const bool few_rows = total_q * group <= 64 * c.items;
     c.splits = std::max<int64_t>(1, std::min(tiles, (sms + (few_rows ? units - 1 : 0)) / units));
-    c.bytes = c.splits > 1 ? size_t(total_q) * n_q_heads * c.splits * (cfg->head_dim + 2) * sizeof(float) : 0;
     return c;
+}
+
+size_t chunk_bytes(const prcr_rope_cfg* cfg, int64_t n_q_heads, int64_t rows) {  // of partials
+    return size_t(rows) * n_q_heads * (cfg->head_dim + 2) * sizeof(float);
+}
+
+// The most that the partials of a call with up to total_q tokens and max_len slots
+// take: for every number of splits, the most tokens that get so many (of one sequence;
+// more of them have more items).
+size_t chunk_most_bytes(const prcr_rope_cfg* cfg, int64_t n_q_heads, int64_t total_q, int64_t max_len, int sms) {
+    const int64_t group = n_q_heads / cfg->n_kv_heads, rows = chunk_rows(cfg->head_dim), tiles = (max_len + 127) / 128;
+    int64_t most = 0;
+    for (int64_t s = 2; s <= std::min<int64_t>(tiles, sms); ++s) {
+        const int64_t items = (sms - 1) / (s - 1) / cfg->n_kv_heads;  // (sms + units - 1) / units >= s
+        if (items < 1) break;
+        most = std::max(most, s * std::min(total_q, (items * rows - 1) / group));
+    }
+    return chunk_bytes(cfg, n_q_heads, most);
 }
 
 // CTAs of a cluster that takes one (sequence, layer, KV head), and its slots per
@@ -161,7 +177,7 @@ size_t prcr_chunk_workspace_size(const prcr_rope_cfg* cfg, int32_t n_seqs, int32
     if (check_cfg(cfg) || n_seqs < 1 || total_q < 1 || max_len < 1 || !heads_ok(cfg, n_q_heads)) return 0;
     int dev = 0, sms = 1;
     if (cudaGetDevice(&dev) == cudaSuccess) sms = sm_count(dev);
-    return chunk_split(cfg, n_seqs, n_q_heads, total_q, max_len, sms).bytes;
+    return chunk_most_bytes(cfg, n_q_heads, total_q, max_len, sms);
 }
 
 int prcr_chunk_attention(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, int32_t n_seqs, int32_t layer,
@@ -177,7 +193,7 @@ int prcr_chunk_attention(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache,
         return PRCR_EINVAL;
     if (n_seqs == 0 || total_q == 0) return PRCR_OK;
     const int64_t row = int64_t(n_q_heads) * cfg->head_dim;
-    if (!q || !coords || !q_off || !seq_len || !out || !status || q_token_stride < row || out_token_stride < row)
+    if (!q || !coords || !q_off || !seq_len || !out || !status || q == out || q_token_stride < row || out_token_stride < row)
         return PRCR_EINVAL;
     if (!aligned16(q) || !aligned16(out) || !mult8(q_token_stride) || !mult8(out_token_stride) || !aligned4(coords) ||
         !aligned4(q_off) || !aligned4(seq_len) || !aligned4(status))
@@ -189,11 +205,11 @@ int prcr_chunk_attention(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache,
         return PRCR_EINVAL;  // rows, grid x
     ChunkArgs a = {};
     if (split.splits > 1) {
-        const size_t rows = size_t(total_q) * n_q_heads * split.splits;
-        if (!workspace || workspace_bytes < rows * (cfg->head_dim + 2) * sizeof(float)) return PRCR_EWORKSPACE;
+        const int64_t rows = int64_t(total_q) * split.splits;
+        if (!workspace || workspace_bytes < chunk_bytes(cfg, n_q_heads, rows)) return PRCR_EWORKSPACE;
         if (!aligned16(workspace)) return PRCR_EALIGN;
         a.partial = static_cast<float*>(workspace);
-        a.partial_ml = reinterpret_cast<float2*>(a.partial + rows * cfg->head_dim);
+        a.partial_ml = reinterpret_cast<float2*>(a.partial + rows * n_q_heads * cfg->head_dim);
     }
     a.items = int32_t(split.items);
     a.splits = int32_t(split.splits);
@@ -282,7 +298,9 @@ int prcr_evict(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, const prc
         max_len > PRCR_CACHE_MAX_LEN || max_len > cache_capacity(cache) || score_stride < max_len || budget < 1 ||
         budget > PRCR_CACHE_MAX_LEN || n_sink < 0 || n_recent < 0 || int64_t(n_sink) + n_recent > budget)
         return PRCR_EINVAL;
-    if (dst && dst->kind == PRCR_CACHE_CONTIGUOUS && (dst->k == cache->k || dst->v == cache->v)) return PRCR_EINVAL;
+    if (dst && (dst->k == cache->k || dst->v == cache->v) &&  // (another part of a pool is another table's)
+        (dst->kind == PRCR_CACHE_CONTIGUOUS || dst->block_table == cache->block_table))
+        return PRCR_EINVAL;
     if (n_seqs == 0) return PRCR_OK;
     if (n_seqs > 65535 || cfg->n_layers > 65535) return PRCR_EINVAL;  // grid z and y
     if (!seq_len || !score || !score_out || !keep_out || !seq_len_out || !status || seq_len == seq_len_out)

@@ -28,7 +28,7 @@ def _paged(**o):
 APPEND = dict(cfg=_cfg(), cache=_flat(), n_seqs=3, l0=0, nl=2, k=FAKE, v=FAKE, ls=40 * 128, ts=128, coords=FAKE, off=FAKE, total=40,
               len_in=FAKE, len_out=FAKE + 64, status=FAKE)
 CHUNK = dict(cfg=_cfg(), cache=_flat(), n_seqs=3, layer=0, hq=8, q=FAKE, qs=512, coords=FAKE, off=FAKE, total=40, len=FAKE, max_len=200,
-             out=FAKE, os=512, status=FAKE, ws=FAKE, ws_bytes=1 << 40)
+             out=FAKE + 2 ** 20, os=512, status=FAKE, ws=FAKE, ws_bytes=1 << 40)
 WEIGHTS = dict(cfg=_cfg(), cache=_flat(), n_seqs=3, hq=8, q=FAKE, pos=FAKE, len=FAKE, max_len=200, score=FAKE, ss=200, decay=1.0, status=FAKE,
                ws=FAKE, ws_bytes=1 << 40)
 EVICT = dict(cfg=_cfg(), cache=_flat(), dst=None, n_seqs=3, len=FAKE, max_len=200, budget=50, sink=4, recent=10, score=FAKE, score_out=FAKE,
@@ -60,7 +60,7 @@ BAD = {
         (dict(cache=_paged(bt_stride=2 ** 30), max_len=2 ** 30 + 1), B.EINVAL), (dict(q=None), B.EINVAL), (dict(out=None), B.EINVAL),
         (dict(qs=504), B.EINVAL), (dict(os=504), B.EINVAL), (dict(coords=None), B.EINVAL), (dict(off=None), B.EINVAL), (dict(len=None), B.EINVAL),
         (dict(q=FAKE + 8), B.EALIGN), (dict(out=FAKE + 8), B.EALIGN), (dict(qs=516), B.EALIGN), (dict(os=516), B.EALIGN),
-        (dict(len=FAKE + 2), B.EALIGN), (dict(cfg=_cfg(D=256, H=8), cache=_flat(slot_stride=2048), hq=64), B.EINVAL)],
+        (dict(out=FAKE, q=FAKE), B.EINVAL), (dict(len=FAKE + 2), B.EALIGN), (dict(cfg=_cfg(D=256, H=8), cache=_flat(slot_stride=2048), hq=64), B.EINVAL)],
     "prcr_accumulate_weights": [
         (dict(cfg=_cfg(D=96)), B.EINVAL), (dict(hq=9), B.EINVAL), (dict(max_len=257), B.EINVAL), (dict(ss=199), B.EINVAL),
         (dict(decay=float("nan")), B.EINVAL), (dict(decay=float("inf")), B.EINVAL), (dict(q=None), B.EINVAL), (dict(pos=None), B.EINVAL),
@@ -69,7 +69,7 @@ BAD = {
         (dict(max_len=257), B.EINVAL), (dict(ss=199), B.EINVAL), (dict(budget=0), B.EINVAL), (dict(sink=-1), B.EINVAL),
         (dict(recent=-1), B.EINVAL), (dict(sink=41), B.EINVAL), (dict(score=None), B.EINVAL), (dict(score_out=None), B.EINVAL),
         (dict(keep=None), B.EINVAL), (dict(len=None), B.EINVAL), (dict(len_out=FAKE), B.EINVAL), (dict(keep=FAKE + 2), B.EALIGN),
-        (dict(dst=_flat()), B.EINVAL), (dict(dst=_flat(k=FAKE + 2 ** 22, v=FAKE + 2 ** 23, n_seqs=2)), B.EINVAL),
+        (dict(dst=_flat()), B.EINVAL), (dict(cache=_paged(), dst=_paged()), B.EINVAL), (dict(cache=_paged(), dst=_paged(k=FAKE + 2 ** 22)), B.EINVAL), (dict(dst=_flat(k=FAKE + 2 ** 22, v=FAKE + 2 ** 23, n_seqs=2)), B.EINVAL),
         (dict(dst=_flat(k=FAKE + 8)), B.EALIGN), (dict(sink=2 ** 31 - 1, recent=2 ** 31 - 1), B.EINVAL)],
 }
 
@@ -134,3 +134,27 @@ def test_binding_refuses():
                 with pytest.raises((TypeError, ValueError)) as e:
                     getattr(prcr, name)(*good[name][:i], v, *good[name][i + 1:])
                 assert "CUDA device" not in str(e.value), (name, i)
+    # a cache of fewer layers, or of other rows, than the call's
+    for other in ((3, 1, 9, 2, 64), (3, 2, 9, 1, 128), (3, 2, 9, 4, 64)):
+        small = prcr.cache_contiguous(_t(other), _t(other))
+        paged = prcr.cache_paged(_t(other[1:]).unsqueeze(1), _t(other[1:]).unsqueeze(1), _t((3, 1), i32))
+        for name, args in good.items():
+            for bad in (small, paged):
+                late = {"append_kv": [], "chunk_attention": [1]}.get(name)  # (the second layer)
+                a = args[:2] + late + args[3:] if late else list(args)
+                a[1] = bad
+                with pytest.raises(ValueError, match="the cache holds"):
+                    getattr(prcr, name)(*a)
+    with pytest.raises(ValueError, match="the cache holds"):
+        prcr.evict(*good["evict"], dst=small)
+    with pytest.raises(ValueError, match="keep_out"):
+        prcr.evict(*good["evict"][:8], _t((3, 2, 2, 9), i32), *good["evict"][9:])
+
+
+def test_strides_of_single_entries():
+    """A dimension of one entry may have any stride: it is read as packed."""
+    assert B._strides(torch.as_strided(_t(4096), (1, 8, 64), (0, 64, 1)), 3, "q")[0] == 512
+    assert B._strides(_t((8, 1, 64)).transpose(0, 1), 3, "q")[0] == 512
+    assert B._strides(_t((2, 5, 2, 64)), 4, "k") == (640, 128, 64, 1)
+    assert B._strides(torch.as_strided(_t(4096), (2, 1, 2, 64), (256, 8, 64, 1)), 4, "k") == (256, 128, 64, 1)
+    assert B._strides(torch.as_strided(_t(4096), (1, 2, 2, 64), (0, 128, 64, 1)), 4, "k") == (256, 128, 64, 1)

@@ -720,3 +720,113 @@ def test_a_dialogue(H, g, D, block):
                     for h in range(H):
                         ref_score[b][l][h] = list(np.array(ref_score[b][l][h]) + w[h])
             at += n
+
+
+def test_the_calls_in_one_graph_and_on_two_streams():
+    """Append, attention, weights and eviction of one step, captured together and replayed over a cache set back, beside a
+    second batch's on another stream: the results of the same calls made one after the other."""
+    L, H, g, D, B, block, budget = 2, 4, 4, 128, 3, 16, 70
+    c = U.cfg_of(L, H, D)
+
+    class Step:
+        def __init__(self, seed):
+            self.cache, self.lens, self.new = Cache(L, H, D, [400, 90, 130], block, seed=seed), i32([390, 60, 70]), [1, 5, 30]
+            self.T, self.top = sum(self.new), 400
+            self.ks, self.vs = normal((L, self.T, H, D), seed + 1), normal((L, self.T, H, D), seed + 2)
+            self.q, self.qw = normal((L, self.T, H * g, D), seed + 3), normal((B, L, H * g, D), seed + 4)
+            self.pos, self.off = i32(positions(self.T, 9, None)), U.offsets(self.new)
+            self.p = torch.tensor([500, 600, 700], device=DEV)
+            self.k0, self.v0 = self.cache.k_all.clone(), self.cache.v_all.clone()
+            self.len1, self.len2, self.status = i32([0] * B), i32([0] * B), status_word()
+            self.out, self.score = torch.zeros_like(self.q), torch.zeros((B, L, H, 400), device=DEV)
+            self.keep = i32(np.zeros((B, L, H, budget)))
+            n = max(prcr.chunk_workspace_size(c, B, H * g, self.T, self.top), prcr.weights_workspace_size(c, B, H * g, self.top))
+            self.ws = torch.zeros(n + 16, dtype=torch.uint8, device=DEV)
+
+        def reset(self):
+            for x, x0 in ((self.cache.k_all, self.k0), (self.cache.v_all, self.v0)):
+                x.copy_(x0)
+            for x in (self.out, self.score, self.keep, self.len1, self.len2):
+                x.zero_()
+            self.ws.fill_(0xff)
+
+        def calls(self, stream=None):
+            d = self.cache.desc()
+            prcr.append_kv(c, d, 0, self.ks, self.vs, self.pos, self.off, self.lens, self.len1, self.status, stream=stream)
+            for l in range(L):
+                prcr.chunk_attention(c, d, l, self.q[l], self.pos, self.off, self.len1, self.top, self.out[l], self.status, self.ws, stream=stream)
+            prcr.accumulate_weights(c, d, self.qw, self.p, self.len1, self.top, self.score, self.status, 1.0, self.ws, stream=stream)
+            prcr.evict(c, d, self.len1, self.top, budget, 4, 16, self.score, self.keep, self.len2, self.status, stream=stream)
+
+        def results(self):
+            torch.cuda.synchronize()
+            assert int(self.status.item()) == 0
+            return [x.clone() for x in (self.out, self.score, self.keep, self.len1, self.len2, self.cache.k_all, self.cache.v_all)]
+
+    a, b = Step(10), Step(30)
+    want = []
+    for x in (a, b):
+        x.calls()
+        want.append(x.results())
+        assert list(x.len1) == [391, 65, 100] and list(x.len2) == [70, 65, 70]
+        assert bool((x.out != 0).any()) and not torch.equal(x.cache.k_all, x.k0)
+    graphs = []
+    for x in (a, b):
+        x.reset()
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            x.calls()
+    side = torch.cuda.Stream()
+    for how in ("graph", "stream"):
+        for x in (a, b):
+            x.reset()
+        torch.cuda.synchronize()
+        if how == "graph":
+            graphs[0].replay()
+            with torch.cuda.stream(side):
+                graphs[1].replay()
+        else:
+            a.calls()
+            b.calls(stream=side)
+        for x, w in zip((a, b), want):
+            for got, ref in zip(x.results(), w):
+                assert torch.equal(got, ref), how
+
+
+def test_evict_of_more_scores_than_shared_memory_holds():
+    for in_place in (True, False):
+        e = Evict(1, 16, 1, [60000, 49153], 16, 20000, 5, 700, in_place, seed=4)
+        assert e.run(score_in_place=in_place) == 0
+        e.check()
+
+
+def test_one_token_of_any_stride():
+    """A dimension of one entry is read as packed, whatever its stride says."""
+    x = Chunk(4, 2, 64, [1], [50], 16, seed=3, pad=0)
+    x.run()
+    assert x.done() == 0
+    x.check()
+    want = x.out.clone()
+    x.q = x.q.transpose(0, 1).contiguous().transpose(0, 1)  # strides (D, D, 1)
+    x.out = torch.zeros((8, 1, 64), dtype=torch.bfloat16, device=DEV).transpose(0, 1)
+    x.run()
+    assert x.done() == 0 and torch.equal(x.out, want)
+
+
+def test_a_workspace_for_the_largest_call_serves_the_others():
+    """One workspace for the longest and fullest call, dirty from the others, in calls of fewer sequences, tokens and slots."""
+    H, g, D, B, T, longest = 2, 4, 128, 3, 600, 9000
+    c = U.cfg_of(2, H, D)
+    most = prcr.chunk_workspace_size(c, B, H * g, T, longest)
+    assert most > 0
+    sizes = [prcr.chunk_workspace_size(c, b, H * g, t, n) for b, t, n in ((1, 1, 1), (1, 1, 300), (1, 60, 300), (3, 60, 300), (3, 60, 9000), (3, 599, 9000))]
+    assert sizes == sorted(sizes) and sizes[-1] <= most and sizes[0] == 0
+    ws = torch.full((most,), 0xff, dtype=torch.uint8, device=DEV)
+    for new, lens in (([9, 500, 1], [9000, 4000, 77]), ([1, 0, 2], [300, 5, 129]), ([64], [9000]), ([30, 5, 5], [128, 2000, 5]),
+                      ([1, 1, 1], [1, 1, 1]), ([1], [9000]), ([590], [7000]), ([3, 40], [8999, 60])):
+        x = Chunk(H, g, D, new, lens, 16, seed=sum(new))
+        x.ws = ws
+        x.run()
+        assert x.done() == 0
+        x.check(rows=40)
