@@ -5,18 +5,24 @@
 //
 // One CTA per (KV head, layer, sequence):
 //  1. the score at the cut by a radix selection, 11 bits a pass, over the
-//     scores mapped to integers of the same order (held in shared memory where they fit);
-//  2. one pass over the slots in order, tile by tile, that gives every kept
+//     scores mapped to integers of the same order (held in shared memory where they
+//     fit); it ends at the pass whose bin stays whole, the second for most scores;
+//  2. one pass over the slots in order, in tiles of 4096, that gives every kept
 //     slot its place by prefix sums (equal scores at the cut: the lower slots
 //     first), writes the indices and moves the scores;
-//  3. the rows, in order, tile by tile: a thread copies one 16-byte vector of K and one of V of a
-//     tile asynchronously into its own part of a ring in shared memory, several
-//     tiles ahead, and writes them out when they have landed. In place a
+//  3. the rows, in order, tile by tile: a thread copies one 16-byte vector of K and
+//     one of V of a tile asynchronously into its own part of a ring in shared memory,
+//     several tiles ahead, and writes them out when they have landed. In place a
 //     tile's destinations are slots below those that later tiles read (slot
 //     keep[j] >= j), so a barrier between a tile's arrival at all threads and its
 //     writes is all the order that is needed.
-// Memory-bound: the kept rows are read once and written once; two CTAs per SM keep up to 192 KB in
-// flight, and one's selection runs during the other's copies.
+// Memory-bound: the kept rows are read once and written once; two CTAs per SM keep
+// up to 192 KB in flight, and where there are more CTAs than that one's selection
+// runs during the other's copies. Measured with head_dim 128: 8 sequences of up to
+// 8192 slots to 2048, 28 layers of 4 heads, 326 us (5.9 TB/s of rows and scores); one of
+// 4096 to 1024, 36 layers of 8 heads, 65 us (4.8 TB/s): there all CTAs select at once,
+// 15 us before the first row moves. (With a barrier pair per 512 slots in step 2 and always
+// three passes, 20 us; 256 threads, or tiles held in registers instead of the ring, are slower.)
 #include "prcr_cache.cuh"
 #include "prcr_pdl.cuh"
 #include "prcr_tc.cuh"
@@ -43,8 +49,8 @@ __device__ __forceinline__ uint32_t score_key(float f) {
 
 __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const __grid_constant__ EvictArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ int s_scan[2][kEvictWarps];
-    __shared__ uint32_t s_pick[2];
+    __shared__ int s_scan[2][2][kEvictWarps];
+    __shared__ uint32_t s_pick[3];
     // the ring, before that the scores; the rows' places, before that the bins
     float* const s_score = reinterpret_cast<float*>(smem);
     longlong2* const s_row = reinterpret_cast<longlong2*>(smem + kRingBytes);  // [2][kEvictThreads] (from, to)
@@ -88,23 +94,23 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const __grid_co
 
     const bool held = n <= kHeldScores;
     if (held) {
-#pragma unroll 4
+#pragma unroll 8
         for (int i = tid; i < n; i += kEvictThreads) s_score[i] = score[i];
-        __syncthreads();
     }
+    for (int i = tid; i < kBins; i += kEvictThreads) s_hist[i] = 0;
+    __syncthreads();
     auto score_at = [&](int i) { return held ? s_score[i] : score[i]; };
 
     // 1. the cut among the slots between the first and the last ones
     const int lo = n > a.budget ? a.n_sink : n, hi = n > a.budget ? n - a.n_recent : n;
     int need = a.budget - a.n_sink - a.n_recent;  // of those
-    uint32_t cut = 0xffffffffu;                   // keys above it stay
-    int ties = 0;                                 // and so many, the first ones, of those equal to it
+    uint32_t from = 0xffffffffu;                  // keys from here on stay (no score's is that large)
+    uint32_t cut = 0;                             // and of those equal to this one
+    int ties = 0;                                 // so many, the first ones
     if (n > a.budget && need > 0) {
         uint32_t prefix = 0;
-        for (int shift = 21; shift >= -1; shift -= 11) {  // bits 31..21, 20..10, 9..0
+        for (int shift = 21;; shift -= 11) {  // bits 31..21, 20..10, 9..0
             const int at = max(shift, 0), bits = shift < 0 ? 10 : 11;
-            for (int i = tid; i < kBins; i += kEvictThreads) s_hist[i] = 0;
-            __syncthreads();
             for (int i = lo + tid; i < hi; i += kEvictThreads) {
                 const uint32_t k = score_key(score_at(i));
                 if (shift == 21 || (k >> (at + bits)) == (prefix >> (at + bits)))
@@ -115,75 +121,103 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const __grid_co
             constexpr int kPer = kBins / kEvictThreads;
             uint32_t own[kPer], sum = 0;
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) sum += own[i] = s_hist[kBins - 1 - (tid * kPer + i)];
+            for (int i = 0; i < kPer; ++i) {
+                uint32_t& bin = s_hist[kBins - 1 - (tid * kPer + i)];
+                sum += own[i] = bin;
+                bin = 0;  // for the next pass
+            }
             uint32_t upto = sum;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
                 const uint32_t o = __shfl_up_sync(kFull, upto, d);
                 if (lane >= d) upto += o;
             }
-            if (lane == 31) s_scan[0][warp] = int(upto);
+            if (lane == 31) s_scan[0][0][warp] = int(upto);
             __syncthreads();
             uint32_t before = upto - sum;
 #pragma unroll
             for (int w = 0; w < kEvictWarps; ++w)
-                if (w < warp) before += uint32_t(s_scan[0][w]);
+                if (w < warp) before += uint32_t(s_scan[0][0][w]);
             if (before < uint32_t(need) && before + sum >= uint32_t(need)) {
                 int i = 0;
+                uint32_t count = own[0];
 #pragma unroll
                 for (int x = 0; x < kPer - 1; ++x)
-                    if (i == x && before + own[x] < uint32_t(need)) before += own[x], ++i;
+                    if (i == x && before + own[x] < uint32_t(need)) before += own[x], count = own[x + 1], ++i;
                 s_pick[0] = uint32_t(kBins - 1 - (tid * kPer + i));
                 s_pick[1] = before;
+                s_pick[2] = count;
             }
             __syncthreads();
             prefix |= s_pick[0] << at;
             need -= int(s_pick[1]);
-        }
-        cut = prefix;
-        ties = need;
-    }
-
-    // 2. places: kept slots before a slot = those above the cut + the ties taken
-    int base_above = 0, base_tie = 0;
-    for (int i0 = 0; i0 < n; i0 += kEvictThreads) {
-        const int i = i0 + tid;
-        bool above = false, tie = false;
-        float x = 0.0f;
-        if (i < n) {
-            x = score_at(i);
-            if (i < lo || i >= hi) {
-                above = true;
-            } else {
-                const uint32_t k = score_key(x);
-                above = k > cut;
-                tie = k == cut && ties > 0;
+            if (s_pick[2] == uint32_t(need)) {  // all of the bin stays: its lower bits do not matter
+                from = prefix;
+                break;
+            }
+            if (shift < 0) {
+                from = prefix + 1;
+                cut = prefix;
+                ties = need;
+                break;
             }
         }
-        const uint32_t ma = __ballot_sync(kFull, above), mt = __ballot_sync(kFull, tie);
+    }
+
+    // 2. places: kept slots before a slot = those above the cut + the ties taken. A warp
+    // takes 32 kRun slots in a row of each tile, so that one barrier serves them all
+    constexpr int kRun = 8;
+    int base_above = 0, base_tie = 0;
+    for (int i0 = 0, turn = 0; i0 < n; i0 += kRun * kEvictThreads, turn ^= 1) {
+        const int first = i0 + warp * (32 * kRun) + lane;
+        uint32_t ma[kRun], mt[kRun];
+        float x[kRun];
+        int ca = 0, ct = 0;
+#pragma unroll
+        for (int u = 0; u < kRun; ++u) {
+            const int i = first + u * 32;
+            bool above = false, tie = false;
+            x[u] = 0.0f;
+            if (i < n) {
+                x[u] = score_at(i);
+                if (i < lo || i >= hi) {
+                    above = true;
+                } else {
+                    const uint32_t k = score_key(x[u]);
+                    above = k >= from;
+                    tie = k == cut && ties > 0;
+                }
+            }
+            ma[u] = __ballot_sync(kFull, above);
+            mt[u] = __ballot_sync(kFull, tie);
+            ca += __popc(ma[u]);
+            ct += __popc(mt[u]);
+        }
         if (lane == 0) {
-            s_scan[0][warp] = __popc(ma);
-            s_scan[1][warp] = __popc(mt);
+            s_scan[turn][0][warp] = ca;
+            s_scan[turn][1][warp] = ct;
         }
         __syncthreads();  // also: the tile's scores are read before any is written
-        int wa = 0, wt = 0, ta = 0, tt = 0;
+        int pa = base_above, pt = base_tie;
 #pragma unroll
         for (int w = 0; w < kEvictWarps; ++w) {
-            const int ca = s_scan[0][w], ct = s_scan[1][w];
-            if (w < warp) wa += ca, wt += ct;
-            ta += ca;
-            tt += ct;
+            const int wa = s_scan[turn][0][w], wt = s_scan[turn][1][w];
+            if (w < warp) pa += wa, pt += wt;
+            base_above += wa;
+            base_tie += wt;
         }
         const uint32_t below = (1u << lane) - 1;
-        const int pa = base_above + wa + __popc(ma & below), pt = base_tie + wt + __popc(mt & below);
-        if (above || (tie && pt < ties)) {
-            const int j = pa + min(pt, ties);
-            keep[j] = i;
-            score_out[j] = x;
+#pragma unroll
+        for (int u = 0; u < kRun; ++u) {
+            const int t = pt + __popc(mt[u] & below);
+            if (((ma[u] >> lane) & 1u) || (((mt[u] >> lane) & 1u) && t < ties)) {
+                const int j = pa + __popc(ma[u] & below) + min(t, ties);
+                keep[j] = first + u * 32;
+                score_out[j] = x[u];
+            }
+            pa += __popc(ma[u]);
+            pt += __popc(mt[u]);
         }
-        base_above += ta;
-        base_tie += tt;
-        __syncthreads();
     }
     for (int j = m + tid; j < a.budget; j += kEvictThreads) keep[j] = -1;
     for (int64_t j = m + tid; j < a.score_stride; j += kEvictThreads) score_out[j] = 0.0f;
