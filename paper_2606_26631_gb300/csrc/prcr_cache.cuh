@@ -50,4 +50,7 @@ __device__ __forceinline__ bool bad_offsets(const int32_t* off, int n, int total
     return bad;
 }
 
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 }  // namespace prcr

@@ -107,6 +107,17 @@ size_t weights_bytes(const prcr_rope_cfg* cfg, int64_t n_seqs, int64_t n_q_heads
     return size_t(n_seqs) * cfg->n_layers * n_q_heads * max_len * sizeof(float);
 }
 
+// CTAs that share the rows of one (sequence, layer, KV head), each with some of the
+// dims: more than one while there are SMs left for them and a row's part is 64 bytes
+// at least. (Head_dim 128, half of 8000 slots, 16 units: 1 CTA 75 us, 4 of 64 bytes 40, 8
+// of 32 bytes 47; 144 units of 4096 to 1024: 1 CTA 46, 2 of 128 bytes 37.)
+int evict_cluster(const prcr_rope_cfg* cfg, int64_t n_seqs, int sms) {
+    const int64_t units = n_seqs * cfg->n_layers * cfg->n_kv_heads;
+    int c = 1;
+    while (c < 8 && cfg->head_dim % (64 * c) == 0 && units * c * 2 <= 2 * int64_t(sms)) c *= 2;
+    return c;
+}
+
 int status_of(cudaError_t e) { return e == cudaSuccess ? PRCR_OK : PRCR_ECUDA; }
 
 }  // namespace
@@ -326,6 +337,9 @@ int prcr_evict(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, const prc
     a.n_kv_heads = cfg->n_kv_heads;
     a.head_dim = cfg->head_dim;
     a.in_place = dst == nullptr;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return PRCR_ECUDA;
+    a.cluster = evict_cluster(cfg, n_seqs, sm_count(dev));
     return status_of(launch_evict(a, n_seqs, static_cast<cudaStream_t>(stream)));
 }
 

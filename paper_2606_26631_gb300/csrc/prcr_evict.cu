@@ -3,7 +3,9 @@
 // of the others, those of the highest score; the kept rows move to slots
 // 0 .. budget - 1 in their order, in place or into another cache.
 //
-// One CTA per (KV head, layer, sequence):
+// One CTA per (KV head, layer, sequence), or where that leaves SMs idle a cluster of
+// up to 8: its first CTA does steps 1 and 2, and in step 3 each takes some of the rows'
+// dims, which move independently of the others also in place.
 //  1. the score at the cut by a radix selection, 11 bits a pass, over the
 //     scores mapped to integers of the same order (held in shared memory where they
 //     fit); it ends at the pass whose bin stays whole, the second for most scores;
@@ -56,7 +58,8 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const __grid_co
     longlong2* const s_row = reinterpret_cast<longlong2*>(smem + kRingBytes);  // [2][kEvictThreads] (from, to)
     uint32_t* const s_hist = reinterpret_cast<uint32_t*>(smem + kRingBytes);
     static_assert(kBins * 4 <= 2 * kEvictThreads * 16, "bins in the rows' place");
-    const int h = blockIdx.x, l = blockIdx.y, b = blockIdx.z;
+    const int C = a.cluster, rank = int(blockIdx.x) % C;
+    const int h = int(blockIdx.x) / C, l = blockIdx.y, b = blockIdx.z;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int64_t col = (int64_t(b) * a.n_layers + l) * a.n_kv_heads + h;
     int32_t* keep = a.keep + col * a.budget;
@@ -83,153 +86,161 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const __grid_co
             if (blk < 0 || blk >= a.dst.n_blocks) err = PRCR_ST_NO_BLOCK;
         }
     }
-    const bool lead = h == 0 && l == 0;
+    const bool lead = h == 0 && l == 0 && rank == 0;
     if (err && lead) atomicOr(a.status, err);
     if (__syncthreads_or(err != 0)) {
-        for (int j = tid; j < a.budget; j += kEvictThreads) keep[j] = -1;
+        if (rank == 0)
+            for (int j = tid; j < a.budget; j += kEvictThreads) keep[j] = -1;
         if (lead && tid == 0) a.len_out[b] = a.in_place ? n : 0;
         return;
     }
     if (lead && tid == 0) a.len_out[b] = m;
 
-    const bool held = n <= kHeldScores;
-    if (held) {
+    if (rank == 0) {
+        const bool held = n <= kHeldScores;
+        if (held) {
 #pragma unroll 8
-        for (int i = tid; i < n; i += kEvictThreads) s_score[i] = score[i];
-    }
-    for (int i = tid; i < kBins; i += kEvictThreads) s_hist[i] = 0;
-    __syncthreads();
-    auto score_at = [&](int i) { return held ? s_score[i] : score[i]; };
-
-    // 1. the cut among the slots between the first and the last ones
-    const int lo = n > a.budget ? a.n_sink : n, hi = n > a.budget ? n - a.n_recent : n;
-    int need = a.budget - a.n_sink - a.n_recent;  // of those
-    uint32_t from = 0xffffffffu;                  // keys from here on stay (no score's is that large)
-    uint32_t cut = 0;                             // and of those equal to this one
-    int ties = 0;                                 // so many, the first ones
-    if (n > a.budget && need > 0) {
-        uint32_t prefix = 0;
-        for (int shift = 21;; shift -= 11) {  // bits 31..21, 20..10, 9..0
-            const int at = max(shift, 0), bits = shift < 0 ? 10 : 11;
-            for (int i = lo + tid; i < hi; i += kEvictThreads) {
-                const uint32_t k = score_key(score_at(i));
-                if (shift == 21 || (k >> (at + bits)) == (prefix >> (at + bits)))
-                    atomicAdd(&s_hist[(k >> at) & ((1u << bits) - 1)], 1u);
-            }
-            __syncthreads();
-            // the bin, from the top, where the count reaches `need`: four bins a thread
-            constexpr int kPer = kBins / kEvictThreads;
-            uint32_t own[kPer], sum = 0;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                uint32_t& bin = s_hist[kBins - 1 - (tid * kPer + i)];
-                sum += own[i] = bin;
-                bin = 0;  // for the next pass
-            }
-            uint32_t upto = sum;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const uint32_t o = __shfl_up_sync(kFull, upto, d);
-                if (lane >= d) upto += o;
-            }
-            if (lane == 31) s_scan[0][0][warp] = int(upto);
-            __syncthreads();
-            uint32_t before = upto - sum;
-#pragma unroll
-            for (int w = 0; w < kEvictWarps; ++w)
-                if (w < warp) before += uint32_t(s_scan[0][0][w]);
-            if (before < uint32_t(need) && before + sum >= uint32_t(need)) {
-                int i = 0;
-                uint32_t count = own[0];
-#pragma unroll
-                for (int x = 0; x < kPer - 1; ++x)
-                    if (i == x && before + own[x] < uint32_t(need)) before += own[x], count = own[x + 1], ++i;
-                s_pick[0] = uint32_t(kBins - 1 - (tid * kPer + i));
-                s_pick[1] = before;
-                s_pick[2] = count;
-            }
-            __syncthreads();
-            prefix |= s_pick[0] << at;
-            need -= int(s_pick[1]);
-            if (s_pick[2] == uint32_t(need)) {  // all of the bin stays: its lower bits do not matter
-                from = prefix;
-                break;
-            }
-            if (shift < 0) {
-                from = prefix + 1;
-                cut = prefix;
-                ties = need;
-                break;
-            }
+            for (int i = tid; i < n; i += kEvictThreads) s_score[i] = score[i];
         }
-    }
+        for (int i = tid; i < kBins; i += kEvictThreads) s_hist[i] = 0;
+        __syncthreads();
+        auto score_at = [&](int i) { return held ? s_score[i] : score[i]; };
 
-    // 2. places: kept slots before a slot = those above the cut + the ties taken. A warp
-    // takes 32 kRun slots in a row of each tile, so that one barrier serves them all
-    constexpr int kRun = 8;
-    int base_above = 0, base_tie = 0;
-    for (int i0 = 0, turn = 0; i0 < n; i0 += kRun * kEvictThreads, turn ^= 1) {
-        const int first = i0 + warp * (32 * kRun) + lane;
-        uint32_t ma[kRun], mt[kRun];
-        float x[kRun];
-        int ca = 0, ct = 0;
+        // 1. the cut among the slots between the first and the last ones
+        const int lo = n > a.budget ? a.n_sink : n, hi = n > a.budget ? n - a.n_recent : n;
+        int need = a.budget - a.n_sink - a.n_recent;  // of those
+        uint32_t from = 0xffffffffu;                  // keys from here on stay (no score's is that large)
+        uint32_t cut = 0;                             // and of those equal to this one
+        int ties = 0;                                 // so many, the first ones
+        if (n > a.budget && need > 0) {
+            uint32_t prefix = 0;
+            for (int shift = 21;; shift -= 11) {  // bits 31..21, 20..10, 9..0
+                const int at = max(shift, 0), bits = shift < 0 ? 10 : 11;
+                for (int i = lo + tid; i < hi; i += kEvictThreads) {
+                    const uint32_t k = score_key(score_at(i));
+                    if (shift == 21 || (k >> (at + bits)) == (prefix >> (at + bits)))
+                        atomicAdd(&s_hist[(k >> at) & ((1u << bits) - 1)], 1u);
+                }
+                __syncthreads();
+                // the bin, from the top, where the count reaches `need`: four bins a thread
+                constexpr int kPer = kBins / kEvictThreads;
+                uint32_t own[kPer], sum = 0;
 #pragma unroll
-        for (int u = 0; u < kRun; ++u) {
-            const int i = first + u * 32;
-            bool above = false, tie = false;
-            x[u] = 0.0f;
-            if (i < n) {
-                x[u] = score_at(i);
-                if (i < lo || i >= hi) {
-                    above = true;
-                } else {
-                    const uint32_t k = score_key(x[u]);
-                    above = k >= from;
-                    tie = k == cut && ties > 0;
+                for (int i = 0; i < kPer; ++i) {
+                    uint32_t& bin = s_hist[kBins - 1 - (tid * kPer + i)];
+                    sum += own[i] = bin;
+                    bin = 0;  // for the next pass
+                }
+                uint32_t upto = sum;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const uint32_t o = __shfl_up_sync(kFull, upto, d);
+                    if (lane >= d) upto += o;
+                }
+                if (lane == 31) s_scan[0][0][warp] = int(upto);
+                __syncthreads();
+                uint32_t before = upto - sum;
+#pragma unroll
+                for (int w = 0; w < kEvictWarps; ++w)
+                    if (w < warp) before += uint32_t(s_scan[0][0][w]);
+                if (before < uint32_t(need) && before + sum >= uint32_t(need)) {
+                    int i = 0;
+                    uint32_t count = own[0];
+#pragma unroll
+                    for (int x = 0; x < kPer - 1; ++x)
+                        if (i == x && before + own[x] < uint32_t(need)) before += own[x], count = own[x + 1], ++i;
+                    s_pick[0] = uint32_t(kBins - 1 - (tid * kPer + i));
+                    s_pick[1] = before;
+                    s_pick[2] = count;
+                }
+                __syncthreads();
+                prefix |= s_pick[0] << at;
+                need -= int(s_pick[1]);
+                if (s_pick[2] == uint32_t(need)) {  // all of the bin stays: its lower bits do not matter
+                    from = prefix;
+                    break;
+                }
+                if (shift < 0) {
+                    from = prefix + 1;
+                    cut = prefix;
+                    ties = need;
+                    break;
                 }
             }
-            ma[u] = __ballot_sync(kFull, above);
-            mt[u] = __ballot_sync(kFull, tie);
-            ca += __popc(ma[u]);
-            ct += __popc(mt[u]);
         }
-        if (lane == 0) {
-            s_scan[turn][0][warp] = ca;
-            s_scan[turn][1][warp] = ct;
-        }
-        __syncthreads();  // also: the tile's scores are read before any is written
-        int pa = base_above, pt = base_tie;
+
+        // 2. places: kept slots before a slot = those above the cut + the ties taken. A warp
+        // takes 32 kRun slots in a row of each tile, so that one barrier serves them all
+        constexpr int kRun = 8;
+        int base_above = 0, base_tie = 0;
+        for (int i0 = 0, turn = 0; i0 < n; i0 += kRun * kEvictThreads, turn ^= 1) {
+            const int first = i0 + warp * (32 * kRun) + lane;
+            uint32_t ma[kRun], mt[kRun];
+            float x[kRun];
+            int ca = 0, ct = 0;
 #pragma unroll
-        for (int w = 0; w < kEvictWarps; ++w) {
-            const int wa = s_scan[turn][0][w], wt = s_scan[turn][1][w];
-            if (w < warp) pa += wa, pt += wt;
-            base_above += wa;
-            base_tie += wt;
-        }
-        const uint32_t below = (1u << lane) - 1;
-#pragma unroll
-        for (int u = 0; u < kRun; ++u) {
-            const int t = pt + __popc(mt[u] & below);
-            if (((ma[u] >> lane) & 1u) || (((mt[u] >> lane) & 1u) && t < ties)) {
-                const int j = pa + __popc(ma[u] & below) + min(t, ties);
-                keep[j] = first + u * 32;
-                score_out[j] = x[u];
+            for (int u = 0; u < kRun; ++u) {
+                const int i = first + u * 32;
+                bool above = false, tie = false;
+                x[u] = 0.0f;
+                if (i < n) {
+                    x[u] = score_at(i);
+                    if (i < lo || i >= hi) {
+                        above = true;
+                    } else {
+                        const uint32_t k = score_key(x[u]);
+                        above = k >= from;
+                        tie = k == cut && ties > 0;
+                    }
+                }
+                ma[u] = __ballot_sync(kFull, above);
+                mt[u] = __ballot_sync(kFull, tie);
+                ca += __popc(ma[u]);
+                ct += __popc(mt[u]);
             }
-            pa += __popc(ma[u]);
-            pt += __popc(mt[u]);
+            if (lane == 0) {
+                s_scan[turn][0][warp] = ca;
+                s_scan[turn][1][warp] = ct;
+            }
+            __syncthreads();  // also: the tile's scores are read before any is written
+            int pa = base_above, pt = base_tie;
+#pragma unroll
+            for (int w = 0; w < kEvictWarps; ++w) {
+                const int wa = s_scan[turn][0][w], wt = s_scan[turn][1][w];
+                if (w < warp) pa += wa, pt += wt;
+                base_above += wa;
+                base_tie += wt;
+            }
+            const uint32_t below = (1u << lane) - 1;
+#pragma unroll
+            for (int u = 0; u < kRun; ++u) {
+                const int t = pt + __popc(mt[u] & below);
+                if (((ma[u] >> lane) & 1u) || (((mt[u] >> lane) & 1u) && t < ties)) {
+                    const int j = pa + __popc(ma[u] & below) + min(t, ties);
+                    keep[j] = first + u * 32;
+                    score_out[j] = x[u];
+                }
+                pa += __popc(ma[u]);
+                pt += __popc(mt[u]);
+            }
         }
+        for (int j = m + tid; j < a.budget; j += kEvictThreads) keep[j] = -1;
+        for (int64_t j = m + tid; j < a.score_stride; j += kEvictThreads) score_out[j] = 0.0f;
     }
-    for (int j = m + tid; j < a.budget; j += kEvictThreads) keep[j] = -1;
-    for (int64_t j = m + tid; j < a.score_stride; j += kEvictThreads) score_out[j] = 0.0f;
+    if (C > 1) {
+        cluster_arrive();
+        cluster_wait();
+    }
     __syncthreads();
 
     // 3. rows. Their places are looked up by a thread each, for so many tiles at a time
-    const int lanes = a.head_dim / 8, per = kEvictThreads / lanes;  // threads a row, rows a tile
+    const int lanes = a.head_dim / 8 / C, per = kEvictThreads / lanes;  // threads a row, rows a tile
     const int group = kEvictThreads / per;                          // tiles whose rows a lookup covers
     const int my = tid / lanes, v = tid - my * lanes;
-    const uint16_t* const sk = a.src.k + int64_t(l) * a.src.layer_stride + int64_t(h) * a.head_dim + v * 8;
+    const int64_t part = int64_t(h) * a.head_dim + (rank * lanes + v) * 8;
+    const uint16_t* const sk = a.src.k + int64_t(l) * a.src.layer_stride + part;
     const uint16_t* const sv = a.src.v + (sk - a.src.k);
-    uint16_t* const dk = a.dst.k + int64_t(l) * a.dst.layer_stride + int64_t(h) * a.head_dim + v * 8;
+    uint16_t* const dk = a.dst.k + int64_t(l) * a.dst.layer_stride + part;
     uint16_t* const dv = a.dst.v + (dk - a.dst.k);
     const uint32_t ring = smem_u32(smem) + uint32_t(tid) * 16;  // a tile: the threads' vectors of K, then of V
     auto look_up = [&](int c) {
@@ -292,10 +303,10 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const __grid_co
 }  // namespace
 
 cudaError_t launch_evict(const EvictArgs& a, int n_seqs, cudaStream_t stream) {
-    const dim3 grid(unsigned(a.n_kv_heads), unsigned(a.n_layers), unsigned(n_seqs));
+    const dim3 grid(unsigned(a.n_kv_heads * a.cluster), unsigned(a.n_layers), unsigned(n_seqs));
     const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(evict_kernel), kEvictSmem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(evict_kernel, grid, dim3(kEvictThreads), kEvictSmem, stream, a);
+    return launch_pdl_clusters(evict_kernel, a.cluster, grid, dim3(kEvictThreads), kEvictSmem, stream, a);
 }
 
 }  // namespace prcr

@@ -456,6 +456,7 @@ struct EvictArgs {
     int32_t n_kv_heads;
     int32_t head_dim;
     int32_t in_place;
+    int32_t cluster;            // CTAs of a (sequence, layer, KV head), a part of its rows' dims each
 };
 
 cudaError_t append_blocks_per_sm(int block, size_t smem, int* out);

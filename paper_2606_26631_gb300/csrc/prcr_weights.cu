@@ -159,8 +159,6 @@ struct WeightsShape {
     static constexpr size_t kFragBytes = size_t(3) * kSteps * 32 * sizeof(uint2);
 };
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void st_peer(const float* p, int rank, float x) {
     asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.f32 [a], %2;\n\t}" ::"r"(smem_u32(p)),
                  "r"(rank), "f"(x)
@@ -386,21 +384,8 @@ cudaError_t launch_cluster(const WeightsArgs& a, cudaStream_t stream) {
     const size_t smem = weights_smem(D, a.group, a.slots_per_cta);
     const cudaError_t e = raise_smem_limit(reinterpret_cast<const void*>(weights_kernel<D>), smem);
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(int64_t(a.n_seqs) * a.n_layers * a.n_kv_heads * a.cluster));
-    cfg.blockDim = dim3(kWarps * 32);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = unsigned(a.cluster);
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = a.cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, weights_kernel<D>, a);
+    const dim3 grid(unsigned(int64_t(a.n_seqs) * a.n_layers * a.n_kv_heads * a.cluster));
+    return launch_pdl_clusters(weights_kernel<D>, a.cluster, grid, dim3(kWarps * 32), smem, stream, a);
 }
 
 }  // namespace
