@@ -172,6 +172,7 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
     __shared__ ChunkWork w;
     __shared__ __align__(8) ChunkBars bars;
     __shared__ uint64_t s_freq[P];
+    __shared__ int s_axis[P];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     // 1024-byte aligned: the swizzle goes by address bits
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -200,7 +201,10 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
         w.unmapped = 0;
     }
     if (warp == kSoft + 4) tmem_alloc(smem_u32(&w.tmem), 512);
-    if (tid < P) s_freq[tid] = a.turn_freq[tid];
+    if (tid < P) {
+        s_freq[tid] = a.turn_freq[tid];
+        s_axis[tid] = pair_axis(tid, a.layout, a.sec_t, a.sec_h, a.sec_w);
+    }
     pdl_wait();
 
     // This CTA's rows: an item is a sequence's rows of a tile; its last one, which sees
@@ -319,7 +323,7 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
 #pragma unroll
                     for (int u = 0; u < 8; ++u) {
                         const int i = m.pc * 8 + u;
-                        const int ax = pair_axis(i, a.layout, a.sec_t, a.sec_h, a.sec_w);
+                        const int ax = s_axis[i];
                         const int p = ax == 0 ? m.pos[0] : ax == 1 ? m.pos[1] : m.pos[2];
                         const int frac = int(uint32_t((uint64_t(int64_t(p)) * s_freq[i]) >> 32));
                         __sincosf(float(frac) * 1.46291807926715968e-09f, &s[u], &c[u]);
