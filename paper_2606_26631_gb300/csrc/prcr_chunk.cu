@@ -28,6 +28,24 @@
 // later tokens can only matter if its value is not finite, and then the row's
 // result is not finite: such rows are computed again, in float32, from their
 // own slots alone. The same path serves a tile with an unmapped block.
+//
+// What bounds it, measured: with many rows the tensor cores. A tile of 128 slots costs
+// 256 rows about 2700 clocks, 2048 of them matrix instructions, the rest the
+// hand-overs between softmax and products; a CTA's start and end (its place in the
+// batch, the queries' angles, the last products and the results' way out) about 17,000.
+// One prompt of 8192 tokens, 32 heads of 128 over 8: 380 us, 1.47 PFLOP/s, 0.77 of a
+// library product's rate; 1024 tokens each of four sequences of up to 16,384 slots:
+// 395 us, 1.57 PFLOP/s; six prompts of up to 2116 tokens, few tiles per CTA: 152 us, 0.73
+// PFLOP/s; head_dim 256 (half as many rows per CTA), 1500 tokens each of two sequences of up to 3500
+// slots: 175 us, 0.98 PFLOP/s.
+// With few rows the keys' and values' bytes: 6 tokens each of 16 sequences of up to
+// 8198 slots 68 us, 4.7 TB/s; one token over 933 slots 12 us, all latency.
+// Tiles and roles that were slower (the prompt of 8192 tokens unless said): CTAs that
+// stay and take runs of tiles 450 us, or whole units 490; queries in tensor memory with
+// tiles of 64 slots 533; a thread of matrix instructions for each half, whose softmaxes
+// then fall into step, 3970 clocks a tile; rows by TMA in boxes of 16 slots (a block of
+// a paged cache) 260 clocks a tile more; CTAs of 128 rows, two per SM, 638 us (and six
+// prompts 201, 6 tokens 73).
 #include "prcr_cache.cuh"
 #include "prcr_pdl.cuh"
 #include "prcr_tc.cuh"
