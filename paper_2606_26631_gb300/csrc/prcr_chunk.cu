@@ -26,8 +26,10 @@
 // there; 0 times an infinity or NaN of a hidden value row would still reach O.
 // Rows behind the sequence's length are never loaded (zeros are); a row of
 // later tokens can only matter if its value is not finite, and then the row's
-// result is not finite: such rows are computed again, in float32, from their
-// own slots alone. The same path serves a tile with an unmapped block.
+// result is not finite: where that is so, a look at the values of the tile's hidden
+// slots decides whether the row is computed again, in float32, from its own slots
+// alone. (A row that sees an infinity or NaN keeps what the tensor cores make of it.)
+// The same path serves the CTAs that meet an unmapped block.
 //
 // What bounds it, measured: with many rows the tensor cores. A tile of 128 slots costs
 // 256 rows about 2700 clocks, 2048 of them matrix instructions, the rest the
@@ -92,11 +94,12 @@ __device__ __forceinline__ uint4 ld_shared(uint32_t p) {
 }
 
 // One query row by one warp in float32: online softmax over slots
-// [lo, hi), E dims a lane (dims lane * E ..). m is in units of log2.
+// [lo, hi), E dims a lane (dims lane * E ..), the rows of eight slots in flight
+// together. m is in units of log2.
 template <int D>
 __device__ __noinline__ void row_attention(const ChunkArgs& a, int b, int t, int hq, int64_t lo, int64_t hi,
                                            float& m, float& l, float (&o)[D / 32], uint32_t& err) {
-    constexpr int E = D / 32;
+    constexpr int E = D / 32, U = 8;
     const int lane = threadIdx.x & 31;
     const int kh = hq / a.group;
     const uint16_t* qr = a.q + int64_t(t) * a.q_stride + int64_t(hq) * D + lane * E;
@@ -114,24 +117,71 @@ __device__ __noinline__ void row_attention(const ChunkArgs& a, int b, int t, int
     l = 0.0f;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.0f;
-    for (int64_t s = lo; s < hi; ++s) {
-        const int64_t row = slot_row(a.cache, b, s, err);
-        if (row < 0) continue;
-        const uint16_t* k = a.cache.k + row + int64_t(kh) * D + lane * E;
-        const uint16_t* v = a.cache.v + row + int64_t(kh) * D + lane * E;
-        float x = 0.0f;
+    const int64_t mine = int64_t(kh) * D + lane * E;
+    for (int64_t s0 = lo; s0 < hi; s0 += 32) {
+        const int64_t row = s0 + lane < hi ? slot_row(a.cache, b, s0 + lane, err) : int64_t(-1);
+        for (int i0 = 0; i0 < min(int64_t(32), hi - s0); i0 += U) {
+            uint32_t k[U][E / 2], v[U][E / 2];
+            float x[U];
 #pragma unroll
-        for (int e = 0; e < E; ++e) x = fmaf(q[e], lo_f32(k[e]), x);
+            for (int u = 0; u < U; ++u) {
+                const int64_t r = __shfl_sync(kFull, row, i0 + u);
+                x[u] = r >= 0 ? 0.0f : -INFINITY;
 #pragma unroll
-        for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(kFull, x, d);
-        const float mn = fmaxf(m, x);
-        const float mu = mn == -INFINITY ? 0.0f : mn;
-        const float r = exp2f(m - mu), p = exp2f(x - mu);
-        m = mn;
-        l = fmaf(l, r, p);
+                for (int e = 0; e < E / 2; ++e) {
+                    k[u][e] = r >= 0 ? *reinterpret_cast<const uint32_t*>(a.cache.k + r + mine + 2 * e) : 0u;
+                    v[u][e] = r >= 0 ? *reinterpret_cast<const uint32_t*>(a.cache.v + r + mine + 2 * e) : 0u;
+                }
+            }
+            float mn = m;
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], r, p * lo_f32(v[e]));
+            for (int u = 0; u < U; ++u) {
+                float y = 0.0f;
+#pragma unroll
+                for (int e = 0; e < E / 2; ++e) y = fmaf(q[2 * e + 1], hi_f32(k[u][e]), fmaf(q[2 * e], lo_f32(k[u][e]), y));
+#pragma unroll
+                for (int d = 16; d; d >>= 1) y += __shfl_xor_sync(kFull, y, d);
+                x[u] += y;
+                mn = fmaxf(mn, x[u]);
+            }
+            const float mu = mn == -INFINITY ? 0.0f : mn;
+            const float r = exp2f(m - mu);
+            m = mn;
+            l *= r;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] *= r;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float p = exp2f(x[u] - mu);
+                l += p;
+#pragma unroll
+                for (int e = 0; e < E / 2; ++e) {
+                    o[2 * e] = fmaf(p, lo_f32(v[u][e]), o[2 * e]);
+                    o[2 * e + 1] = fmaf(p, hi_f32(v[u][e]), o[2 * e + 1]);
+                }
+            }
+        }
     }
+}
+
+// The last of slots [lo, hi) whose value row (this KV head's) holds an infinity or
+// NaN, or -1; by one warp, a slot a lane.
+template <int D>
+__device__ __noinline__ int64_t last_bad_value(const ChunkArgs& a, int b, int kh, int64_t lo, int64_t hi) {
+    for (int64_t end = hi; end > lo; end -= 32) {
+        const int64_t s = end - 1 - int64_t(threadIdx.x & 31);
+        uint32_t err = 0;
+        const int64_t row = s >= lo ? slot_row(a.cache, b, s, err) : int64_t(-1);
+        bool bad = false;
+        for (int i = 0; row >= 0 && i < D; i += 8) {
+            const uint4 x = *reinterpret_cast<const uint4*>(a.cache.v + row + int64_t(kh) * D + i);
+            for (const uint32_t w : {x.x, x.y, x.z, x.w})
+                bad |= (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+        }
+        const uint32_t who = __ballot_sync(kFull, bad);
+        if (who) return end - 1 - (__ffs(int(who)) - 1);
+    }
+    return -1;
 }
 
 template <int N>
@@ -539,8 +589,18 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
             __syncwarp();
         }
         if (a.splits > 1 && live) a.partial_ml[prow * a.splits + split] = make_float2(m_run, l_run);
-        // rows to be computed again from their own slots
-        uint32_t again = __ballot_sync(kFull, live && any && (odd[0] + odd[1] + (odd[2] + odd[3]) != 0.0f || w.unmapped));
+        // rows to be computed again from their own slots: those that are not finite and
+        // whose tiles held a value row that they do not see and that is not finite, and
+        // all of a CTA with unmapped blocks
+        const bool odd_row = live && any && odd[0] + odd[1] + (odd[2] + odd[3]) != 0.0f;
+        uint32_t again = w.unmapped ? __ballot_sync(kFull, live && any) : 0u;
+        if (!w.unmapped && __any_sync(kFull, odd_row)) {
+            int64_t from = odd_row ? lim : w.hi;
+#pragma unroll
+            for (int d = 16; d; d >>= 1) from = min(from, __shfl_xor_sync(kFull, from, d));
+            const int64_t bad = last_bad_value<D>(a, w.b, kh, from, min(w.hi, w.lo + int64_t(w.tiles[qi]) * kTile));
+            again = __ballot_sync(kFull, odd_row && bad >= lim);
+        }
         if (w.unmapped && tid == 0) atomicOr(a.status, PRCR_ST_NO_BLOCK);
         while (again) {
             const int src = __ffs(int(again)) - 1;

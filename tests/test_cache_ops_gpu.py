@@ -272,6 +272,26 @@ def test_chunk_many_rows_with_bad_slots(H, g, D, block):
         c.check(rows=12, drop=lambda b, s: (s // block == 100) if b == 0 else s < 0)
 
 
+@pytest.mark.parametrize("H,g,D,block", [(2, 4, 128, 16), (1, 8, 256, 7), (2, 3, 64, 0)])
+def test_chunk_a_bad_element_reaches_its_dim_alone(H, g, D, block):
+    """A NaN in one dim of a value that all queries see, an infinity in another dim of one that the later ones see: the
+    other dims, and this one before them, are what the formula gives without the two."""
+    c = Chunk(H, g, D, [300], [340], block, seed=6)
+    first, late = c.cache.where(0, [5]), c.cache.where(0, [200])  # the late one is query 160's own
+    K, V = (U.f64(c.cache.rows(x, 0, 340)[1]) for x in (c.cache.k, c.cache.v))
+    for w, d, bad in ((first, 3, float("nan")), (late, 17, float("inf"))):
+        rows = c.cache.v[w]
+        rows[..., d] = bad
+        c.cache.v[w] = rows
+    assert c.run().done() == 0
+    got = U.f64(c.out[:300])
+    ref, bar = U.chunk64(U.f64(c.q[:300]), c.pos[:300], K, V, U.causal(300, 340, 340))
+    ok = np.abs(got - ref) <= bar
+    assert np.isnan(got[..., 3]).all() and not np.isfinite(got[160:, :, 17]).any()
+    ok[..., 3] = ok[160:, :, 17] = True
+    assert ok.all()
+
+
 def test_chunk_nan_key_reaches_those_that_see_it():
     c = Chunk(2, 4, 128, [100], [400], 16, seed=4)
     c.cache.k[c.cache.where(0, [350])] = float("nan")
