@@ -47,7 +47,8 @@
 // tiles of 64 slots 533; a thread of matrix instructions for each half, whose softmaxes
 // then fall into step, 3970 clocks a tile; rows by TMA in boxes of 16 slots (a block of
 // a paged cache) 260 clocks a tile more; CTAs of 128 rows, two per SM, 638 us (and six
-// prompts 201, 6 tokens 73).
+// prompts 201, 6 tokens 73); two threads a row, 64 slots each, whose 24 warps leave 80
+// registers a thread, 906 (at head_dim 256, where 16 warps are enough, 168 for 176).
 #include "prcr_cache.cuh"
 #include "prcr_pdl.cuh"
 #include "prcr_tc.cuh"
