@@ -44,23 +44,33 @@ bool heads_ok(const prcr_rope_cfg* cfg, int32_t n_q_heads) {
            int64_t(n_q_heads) * D <= PRCR_DECODE_MAX_Q_ELEMS;
 }
 
-// How a chunk call splits the slots that a unit (rows of a tile, a KV head) sees, one
-// CTA to an SM: into as many as give every SM one. With few rows in a unit the keys' and
-// values' bytes bound it and its partials are small, so the number is rounded up: a
-// second, partial wave evens out lengths that differ (16 sequences of up to 8198 slots,
-// 8 rows a unit, 128 units on 152 SMs: 2 splits 69 us, 1 split 87, 3 76, 5 88, 8 113).
-// With many rows it is rounded down: the partials cost more than the idle SMs (D = 256:
-// up 183 us, down 178). (items: at most; the lengths are on the device.)
+// How a chunk call is cut into CTAs, one to an SM: units of the rows of a tile and a KV
+// head, and parts of the slots that a unit sees. (items: at most; the lengths are
+// on the device.)
+//
+// few: sequences of up to 160 rows (tokens by heads of a group) on average, in units of 128
+// rows, whose next tile's products do not wait for the last one's softmax, instead
+// of 256, which read the keys once. 16 sequences of up to 8198 slots, 8 heads of groups of 4:
+// of up to 6 tokens 64 us | 69, 24 tokens 77 | 87, 40 tokens 77 | 100, 64 tokens 79 |
+// 101, 100 tokens 120 | 100.
+//
+// splits: as many as give every SM a CTA. Few rows are bound by the keys' and values'
+// bytes, and their partials are small: where that is below 4, it is rounded up, and a
+// second, partial wave evens out lengths that differ (sequences of 8 heads as above: 5 of
+// them 31 us up | 34 down, 8 40 | 48, 12 62 | 72, 16 64 | 75; but 2 31 | 26, 4 35 | 31).
+// With many rows the partials cost more than the idle SMs (D = 256: up 183, down 178).
 struct ChunkSplit {
     int64_t items, splits;
+    bool few;
 };
 ChunkSplit chunk_split(const prcr_rope_cfg* cfg, int64_t n_seqs, int64_t n_q_heads, int64_t total_q, int64_t max_len, int sms) {
-    const int64_t group = n_q_heads / cfg->n_kv_heads, rows = chunk_rows(cfg->head_dim);
+    const int64_t group = n_q_heads / cfg->n_kv_heads, seqs = std::min(n_seqs, total_q);
     ChunkSplit c;
-    c.items = total_q * group / rows + std::min(n_seqs, total_q);
+    c.few = total_q * group <= 160 * seqs;
+    c.items = total_q * group / chunk_rows(cfg->head_dim, c.few) + seqs;
     const int64_t units = c.items * cfg->n_kv_heads, tiles = std::max<int64_t>(1, (max_len + 127) / 128);
-    const bool few_rows = total_q * group <= 64 * c.items;
-    c.splits = std::max<int64_t>(1, std::min(tiles, (sms + (few_rows ? units - 1 : 0)) / units));
+    const int64_t down = sms / units;
+    c.splits = std::max<int64_t>(1, std::min(tiles, c.few && down < 4 ? (sms + units - 1) / units : down));
     return c;
 }
 
@@ -72,7 +82,7 @@ size_t chunk_bytes(const prcr_rope_cfg* cfg, int64_t n_q_heads, int64_t rows) { 
 // take: for every number of splits, the most tokens that get so many (of one sequence;
 // more of them have more items).
 size_t chunk_most_bytes(const prcr_rope_cfg* cfg, int64_t n_q_heads, int64_t total_q, int64_t max_len, int sms) {
-    const int64_t group = n_q_heads / cfg->n_kv_heads, rows = chunk_rows(cfg->head_dim), tiles = (max_len + 127) / 128;
+    const int64_t group = n_q_heads / cfg->n_kv_heads, rows = chunk_rows(cfg->head_dim, false), tiles = (max_len + 127) / 128;
     int64_t most = 0;
     for (int64_t s = 2; s <= std::min<int64_t>(tiles, sms); ++s) {
         const int64_t items = (sms - 1) / (s - 1) / cfg->n_kv_heads;  // (sms + units - 1) / units >= s
@@ -224,6 +234,7 @@ int prcr_chunk_attention(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache,
     }
     a.items = int32_t(split.items);
     a.splits = int32_t(split.splits);
+    a.few = split.few;
     a.cache = cache_view(cache, layer);
     a.q = static_cast<const uint16_t*>(q);
     a.q_stride = q_token_stride;

@@ -11,10 +11,11 @@
 //   P = exp2(S scale - m) by one thread per row, written back over S as bf16.
 // Roles: 4 warps of softmax per 128 rows, 4 warps that copy K and V rows, and one
 // thread that issues the matrix instructions.
-//  - head_dim 64 and 128 (NQ = 2): while the tensor cores work for one half of the
+//  - NQ = 2 (head_dim 64 and 128): while the tensor cores work for one half of the
 //    rows, the other half's softmax runs.
-//  - head_dim 256 (NQ = 1, its accumulator is 256 columns): two S buffers; the next
-//    tile's S is made before this tile's O.
+//  - NQ = 1 (head_dim 256, whose accumulator is 256 columns, and sequences of few
+//    rows, which one half would hold): two S buffers; the next tile's S is made before
+//    this tile's O.
 // The running maximum m is only raised when it grows by more than 8 (in log2
 // units): P then holds values up to 2^8, which bf16 represents as exactly as
 // values up to 1, the sums are float32, and the accumulator is rarely read back
@@ -41,7 +42,7 @@
 // PFLOP/s; head_dim 256 (half as many rows per CTA), 1500 tokens each of two sequences of up to 3500
 // slots: 175 us, 0.98 PFLOP/s.
 // With few rows the keys' and values' bytes: 6 tokens each of 16 sequences of up to
-// 8198 slots 68 us, 4.7 TB/s; one token over 933 slots 12 us, all latency.
+// 8198 slots 63 us, 5.1 TB/s (69 with NQ = 2); one token over 933 slots 12 us, all latency.
 // Tiles and roles that were slower (the prompt of 8192 tokens unless said): CTAs that
 // stay and take runs of tiles 450 us, or whole units 490; queries in tensor memory with
 // tiles of 64 slots 533; a thread of matrix instructions for each half, whose softmaxes
@@ -67,7 +68,7 @@ struct ChunkShape {
     static constexpr int kPanel = kTile * 128;           // bytes: 64 dims of 128 rows
     static constexpr int kEntry = kTile * kDims * 2;
     static constexpr int kQTile = 128 * D * 2;
-    static constexpr int kStages = D == 64 ? 6 : 5;
+    static constexpr int kStages = D == 64 || (D == 128 && NQ == 1) ? 6 : 5;  // what an SM holds (64: what is enough)
     static constexpr int kSoftWarps = 4 * NQ;
     static constexpr int kThreads = (kSoftWarps + 8) * 32;
     static constexpr int kRows = 128 * NQ;
@@ -871,11 +872,11 @@ cudaError_t launch_shape(const ChunkArgs& a, cudaStream_t stream) {
 
 }  // namespace
 
-int chunk_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
+int chunk_rows(int head_dim, bool few) { return head_dim == 256 || few ? 128 : 256; }
 
 cudaError_t launch_chunk(const ChunkArgs& a, cudaStream_t stream) {
-    if (a.head_dim == 64) return launch_shape<64, 2>(a, stream);
-    if (a.head_dim == 128) return launch_shape<128, 2>(a, stream);
+    if (a.head_dim == 64) return a.few ? launch_shape<64, 1>(a, stream) : launch_shape<64, 2>(a, stream);
+    if (a.head_dim == 128) return a.few ? launch_shape<128, 1>(a, stream) : launch_shape<128, 2>(a, stream);
     return launch_shape<256, 1>(a, stream);
 }
 

@@ -411,6 +411,7 @@ struct ChunkArgs {
     float scale_log2;           // log2(e) / sqrt(head_dim)
     int32_t items;              // tiles of rows, of all sequences, at most
     int32_t splits;             // parts of the slots that an item sees
+    bool few;                   // sequences of few rows: CTAs of 128
     float* partial;             // workspace when splits > 1: [total_q][n_q_heads][splits][D]
     float2* partial_ml;         // [total_q][n_q_heads][splits] (maximum, sum)
     uint64_t turn_freq[kMaxPairs];
@@ -462,7 +463,7 @@ struct EvictArgs {
 cudaError_t append_blocks_per_sm(int block, size_t smem, int* out);
 cudaError_t launch_append(const AppendArgs& a, dim3 grid, int block, size_t smem, cudaStream_t stream);
 cudaError_t launch_chunk(const ChunkArgs& a, cudaStream_t stream);
-int chunk_rows(int head_dim);  // rows (token, query head of a group) that a CTA takes
+int chunk_rows(int head_dim, bool few);  // rows (token, query head of a group) that a CTA takes
 size_t weights_smem(int head_dim, int group, int slots);  // of a CTA with so many slots
 cudaError_t launch_weights(const WeightsArgs& a, cudaStream_t stream);
 cudaError_t launch_evict(const EvictArgs& a, int n_seqs, cudaStream_t stream);

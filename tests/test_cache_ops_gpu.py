@@ -193,6 +193,8 @@ def test_chunk(H, g, D, block, kind):
     (2, 8, 256, 16, [4, 2], [5000, 6001]), (2, 4, 128, 16, [300], [20000]), (1, 8, 128, 0, [1024], [1024]), (2, 2, 64, 16, [2500], [2500]),
     (1, 2, 256, 16, [1500], [1700]), (8, 4, 128, 16, [1900, 0, 800], [1900, 7, 3000]), (4, 8, 256, 0, [1000, 400], [1300, 400]),
     (8, 8, 64, 7, [1500], [1500]), (8, 4, 128, 64, [2600], [2600]), (8, 4, 128, 256, [300, 2300], [5000, 2300]),
+    (4, 4, 128, 16, [50, 3, 20], [9000, 4100, 77]), (8, 2, 64, 0, [70, 79], [3000, 5000]), (1, 8, 128, 7, [6] * 24, [2000] * 24),  # few rows
+    (3, 1, 64, 32, [160, 160], [160, 4000]), (1, 8, 64, 1, [16, 1], [5000, 130]),
 ], ids=lambda v: str(v))
 def test_chunk_long(H, g, D, block, new, lens):
     c = Chunk(H, g, D, new, lens, block, seed=5)
@@ -223,16 +225,17 @@ def test_chunk_rows_that_see_nothing(D, block):
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-@pytest.mark.parametrize("H,g,D,block", [(2, 4, 128, 16), (1, 8, 64, 0), (2, 2, 256, 7)])
-def test_chunk_hidden_slots_do_not_matter(H, g, D, block, bad):
+@pytest.mark.parametrize("H,g,D,block,new", [(2, 4, 128, 16, [40, 150, 1]), (1, 8, 64, 0, [40, 150, 1]), (2, 2, 256, 7, [40, 150, 1]),
+                                             (2, 4, 128, 16, [12, 20, 1]), (1, 8, 64, 0, [12, 20, 1])])
+def test_chunk_hidden_slots_do_not_matter(H, g, D, block, new, bad):
     """Slots behind the length, and slots of later tokens, have no influence whatever they hold; queries that see them do
     get what the formula gives."""
-    new, lens = [40, 150, 1], [300, 150, 17]
+    lens = [300, 150, 17]
     c = Chunk(H, g, D, new, lens, block, seed=2)
     for b, n in enumerate(lens):  # rows behind the length
         w = c.cache.where(b, np.arange(n, n + 3))
         c.cache.k[w], c.cache.v[w] = bad, bad
-    hidden = {0: 290, 1: 100}  # a slot that later queries see
+    hidden = {0: 300 - new[0] // 4, 1: 150 - new[1] // 3}  # a slot that later queries see
     for b, s in hidden.items():
         w = c.cache.where(b, [s])
         c.cache.v[w] = bad
