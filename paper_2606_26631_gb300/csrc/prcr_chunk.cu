@@ -33,17 +33,17 @@
 // The same path serves the CTAs that meet an unmapped block.
 //
 // What bounds it, measured: with many rows the tensor cores. A tile of 128 slots costs
-// 256 rows about 2700 clocks, 2048 of them matrix instructions, the rest the
+// 256 rows about 2600 clocks, 2048 of them matrix instructions, the rest the
 // hand-overs between softmax and products; a CTA's start and end (its place in the
 // batch, the queries' angles, the last products and the results' way out) about 17,000.
-// One prompt of 8192 tokens, 32 heads of 128 over 8: 380 us, 1.47 PFLOP/s, 0.77 of a
+// One prompt of 8192 tokens, 32 heads of 128 over 8: 366 us, 1.52 PFLOP/s, 0.79 of a
 // library product's rate; 1024 tokens each of four sequences of up to 16,384 slots:
-// 395 us, 1.57 PFLOP/s; six prompts of up to 2116 tokens, few tiles per CTA: 152 us, 0.73
+// 382 us, 1.63 PFLOP/s; six prompts of up to 2116 tokens, few tiles per CTA: 152 us, 0.73
 // PFLOP/s; head_dim 256 (half as many rows per CTA), 1500 tokens each of two sequences of up to 3500
 // slots: 175 us, 0.98 PFLOP/s.
 // With few rows the keys' and values' bytes: 6 tokens each of 16 sequences of up to
 // 8198 slots 63 us, 5.1 TB/s (69 with NQ = 2); one token over 933 slots 12 us, all latency.
-// Tiles and roles that were slower (the prompt of 8192 tokens unless said): CTAs that
+// Tiles and roles that were slower (that prompt, then at 375 to 430 us, unless said): CTAs that
 // stay and take runs of tiles 450 us, or whole units 490; queries in tensor memory with
 // tiles of 64 slots 533; a thread of matrix instructions for each half, whose softmaxes
 // then fall into step, 3970 clocks a tile; rows by TMA in boxes of 16 slots (a block of
@@ -497,7 +497,9 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                 }
                 const float mu = m_run == -INFINITY ? 0.0f : m_run;
                 const uint64_t c2 = pair64(scale, scale), m2 = pair64(-mu, -mu);
-                uint64_t sum0 = 0, sum1 = 0;
+                // (three chains of sums: two leave the additions' latency on the way to the products,
+                // one prompt of 8192 tokens 376 us for 366; four 368, eight 375)
+                uint64_t sums[3] = {};
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     uint32_t p[32];
@@ -507,8 +509,7 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                         const uint64_t x = fma2(uint64_t(s[k]) | (uint64_t(s[k + 1]) << 32), c2, m2);
                         const float e0 = exp2_fast(lo32(x)), e1 = exp2_fast(hi32(x));
                         const uint64_t e = pair64(e0, e1);
-                        if (i & 1) sum1 = add2(sum1, e);
-                        else sum0 = add2(sum0, e);
+                        sums[i % 3] = add2(sums[i % 3], e);
                         p[i] = pack_bf16x2(e0, e1);
                     }
                     tmem_st32(s_t + 32 * half, p);
@@ -517,7 +518,7 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&bars.p[buf][half]));
                 }
-                const uint64_t sum = add2(sum0, sum1);
+                const uint64_t sum = add2(add2(sums[0], sums[1]), sums[2]);
                 l_run += lo32(sum) + hi32(sum);
                 // (every phase of this barrier is waited for: parities tell one from the next)
                 if (NQ == 1 && !summed && !mbar_wait(smem_u32(&bars.o[0]), uint32_t((j - 1) & 1))) {
