@@ -59,6 +59,10 @@ bool heads_ok(const prcr_rope_cfg* cfg, int32_t n_q_heads) {
 // second, partial wave evens out lengths that differ (sequences of 8 heads as above: 5 of
 // them 31 us up | 34 down, 8 40 | 48, 12 62 | 72, 16 64 | 75; but 2 31 | 26, 4 35 | 31).
 // With many rows the partials cost more than the idle SMs (D = 256: up 183, down 178).
+// Up to 4 tiles of slots, or 12 with many rows, are not split: the kernel that joins the
+// parts costs what they save (few rows, us split | not: 2 tiles 10.5 | 8.4, 4 10.9 | 10.1, 6
+// 10.4 | 11.8; many: a prompt of 200 tokens 18.8 | 13.1, of 500 24 | 16, 300 tokens over 9
+// tiles 24.5 | 22.3, 400 over 13 29.2 | 26.7, 256 over 17 25.8 | 31.3).
 struct ChunkSplit {
     int64_t items, splits;
     bool few;
@@ -70,7 +74,7 @@ ChunkSplit chunk_split(const prcr_rope_cfg* cfg, int64_t n_seqs, int64_t n_q_hea
     c.items = total_q * group / chunk_rows(cfg->head_dim, c.few) + seqs;
     const int64_t units = c.items * cfg->n_kv_heads, tiles = std::max<int64_t>(1, (max_len + 127) / 128);
     const int64_t down = sms / units;
-    c.splits = std::max<int64_t>(1, std::min(tiles, c.few && down < 4 ? (sms + units - 1) / units : down));
+    c.splits = tiles <= (c.few ? 4 : 12) ? 1 : std::max<int64_t>(1, std::min(tiles, c.few && down < 4 ? (sms + units - 1) / units : down));
     return c;
 }
 
