@@ -447,7 +447,9 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                 float x[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i] = tmem_ld32_max(s_t + 32 * i, s + 32 * i);
-                tmem_wait_ld();
+                tmem_wait_ld(s);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) asm volatile("" : "+f"(x[i]));
                 const int64_t at = w.lo + int64_t(j) * kTile;
                 if (at + kTile > lim_lo) {  // some row of the warp does not see all of the tile
                     const int n = int(max(int64_t(0), min(int64_t(kTile), lim - at)));
@@ -485,7 +487,7 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                     for (int c = 0; c < D; c += 32) {
                         uint32_t o[32];
                         tmem_ld32(o_t + c, o);
-                        tmem_wait_ld();
+                        tmem_wait_ld(o);
 #pragma unroll
                         for (int i = 0; i < 32; i += 2) {
                             const uint64_t y = mul2(uint64_t(o[i]) | (uint64_t(o[i + 1]) << 32), f2);
@@ -558,7 +560,7 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
             for (int c = 0; c < D; c += 32) {
                 uint32_t o[32];
                 tmem_ld32(o_t + c, o);
-                tmem_wait_ld();
+                tmem_wait_ld(o);
 #pragma unroll
                 for (int i = 0; i < 32; ++i) odd[i & 3] = fmaf(__uint_as_float(o[i]), 0.0f, odd[i & 3]);
                 if (a.splits == 1) {
