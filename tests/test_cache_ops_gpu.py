@@ -195,6 +195,8 @@ def test_chunk(H, g, D, block, kind):
     (8, 8, 64, 7, [1500], [1500]), (8, 4, 128, 64, [2600], [2600]), (8, 4, 128, 256, [300, 2300], [5000, 2300]),
     (4, 4, 128, 16, [50, 3, 20], [9000, 4100, 77]), (8, 2, 64, 0, [70, 79], [3000, 5000]), (1, 8, 128, 7, [6] * 24, [2000] * 24),  # few rows
     (3, 1, 64, 32, [160, 160], [160, 4000]), (1, 8, 64, 1, [16, 1], [5000, 130]),
+    (8, 4, 128, 16, [6, 1, 0, 40] * 13, [300, 700, 20, 41] * 13), (16, 2, 64, 0, [3, 70] * 10, [500, 90] * 10),  # and many sequences
+    (16, 2, 128, 7, [1] * 24, [1, 128, 129, 257] * 6),
 ], ids=lambda v: str(v))
 def test_chunk_long(H, g, D, block, new, lens):
     c = Chunk(H, g, D, new, lens, block, seed=5)
