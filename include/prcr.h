@@ -411,7 +411,7 @@ PRCR_API int prcr_select_topk_cached(const prcr_rope_cfg* cfg, const prcr_cache_
  *               (rows behind it are padding); otherwise PRCR_ST_CSR, and nothing
  *               is appended
  *   cache_len_out device int32 [n_seqs]: cache_len_in + the sequence's tokens (must
- *               not alias cache_len_in)
+ *               not overlap cache_len_in)
  * A slot beyond the capacity or in an unmapped block sets PRCR_ST_CAPACITY /
  * PRCR_ST_NO_BLOCK and its rows are skipped. Source and cache must not overlap. */
 PRCR_API int prcr_append_kv(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, int32_t n_seqs,
@@ -502,7 +502,7 @@ PRCR_API int prcr_accumulate_weights(const prcr_rope_cfg* cfg, const prcr_cache_
  *               new length to score_stride become 0
  *   keep_out    device int32 [n_seqs][n_layers][n_kv_heads][budget]: the slots kept,
  *               ascending; -1 behind the new length
- *   seq_len_out device int32 [n_seqs]: min(seq_len, budget) (must not alias seq_len)
+ *   seq_len_out device int32 [n_seqs]: min(seq_len, budget) (must not overlap seq_len)
  * Any head_dim. A block must not be mapped twice. A seq_len that is negative,
  * beyond the capacity or max_len, a new length beyond dst's capacity, or an unmapped
  * block in either sets PRCR_ST_CAPACITY / PRCR_ST_NO_BLOCK, and that sequence is left as it was: its

@@ -132,6 +132,12 @@ int evict_cluster(const prcr_rope_cfg* cfg, int64_t n_seqs, int sms) {
     return c;
 }
 
+// Whether two arrays of n lengths share an entry.
+bool overlap(const int32_t* a, const int32_t* b, int64_t n) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return (x < y ? y - x : x - y) < uintptr_t(n) * sizeof(int32_t);
+}
+
 int status_of(cudaError_t e) { return e == cudaSuccess ? PRCR_OK : PRCR_ECUDA; }
 
 }  // namespace
@@ -153,7 +159,8 @@ int prcr_append_kv(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, int32
         return PRCR_EINVAL;
     if (n_seqs == 0) return PRCR_OK;
     const int64_t row = int64_t(cfg->n_kv_heads) * cfg->head_dim;
-    if (!tok_off || !cache_len_in || !cache_len_out || !status || cache_len_in == cache_len_out) return PRCR_EINVAL;
+    if (!tok_off || !cache_len_in || !cache_len_out || !status || overlap(cache_len_in, cache_len_out, n_seqs))
+        return PRCR_EINVAL;
     if (total > 0 && (!k_src || !v_src || !coords || src_token_stride < row || src_layer_stride < 0))
         return PRCR_EINVAL;
     if (!aligned4(tok_off) || !aligned4(cache_len_in) || !aligned4(cache_len_out) || !aligned4(status))
@@ -329,7 +336,8 @@ int prcr_evict(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, const prc
         return PRCR_EINVAL;
     if (n_seqs == 0) return PRCR_OK;
     if (n_seqs > 65535 || cfg->n_layers > 65535) return PRCR_EINVAL;  // grid z and y
-    if (!seq_len || !score || !score_out || !keep_out || !seq_len_out || !status || seq_len == seq_len_out)
+    if (!seq_len || !score || !score_out || !keep_out || !seq_len_out || !status ||
+        overlap(seq_len, seq_len_out, n_seqs))
         return PRCR_EINVAL;
     if (!aligned4(seq_len) || !aligned4(score) || !aligned4(score_out) || !aligned4(keep_out) ||
         !aligned4(seq_len_out) || !aligned4(status))

@@ -52,7 +52,7 @@ BAD = {
     "prcr_append_kv": [
         (dict(l0=-1), B.EINVAL), (dict(l0=1), B.EINVAL), (dict(nl=0), B.EINVAL), (dict(total=-1), B.EINVAL), (dict(k=None), B.EINVAL),
         (dict(v=None), B.EINVAL), (dict(ts=64), B.EINVAL), (dict(ls=-8), B.EINVAL), (dict(coords=None), B.EINVAL), (dict(off=None), B.EINVAL),
-        (dict(len_in=None), B.EINVAL), (dict(len_out=None), B.EINVAL), (dict(len_out=FAKE), B.EINVAL), (dict(k=FAKE + 8), B.EALIGN),
+        (dict(len_in=None), B.EINVAL), (dict(len_out=None), B.EINVAL), (dict(len_out=FAKE), B.EINVAL), (dict(len_out=FAKE + 8), B.EINVAL), (dict(len_in=FAKE + 72), B.EINVAL), (dict(k=FAKE + 8), B.EALIGN),
         (dict(ts=132), B.EALIGN), (dict(ls=4), B.EALIGN), (dict(off=FAKE + 2), B.EALIGN), (dict(coords=FAKE + 1), B.EALIGN)],
     "prcr_chunk_attention": [
         (dict(cfg=_cfg(D=96)), B.EINVAL), (dict(hq=9), B.EINVAL), (dict(hq=1), B.EINVAL), (dict(hq=18), B.EINVAL), (dict(layer=-1), B.EINVAL),
@@ -68,7 +68,7 @@ BAD = {
     "prcr_evict": [
         (dict(max_len=257), B.EINVAL), (dict(ss=199), B.EINVAL), (dict(budget=0), B.EINVAL), (dict(sink=-1), B.EINVAL),
         (dict(recent=-1), B.EINVAL), (dict(sink=41), B.EINVAL), (dict(score=None), B.EINVAL), (dict(score_out=None), B.EINVAL),
-        (dict(keep=None), B.EINVAL), (dict(len=None), B.EINVAL), (dict(len_out=FAKE), B.EINVAL), (dict(keep=FAKE + 2), B.EALIGN),
+        (dict(keep=None), B.EINVAL), (dict(len=None), B.EINVAL), (dict(len_out=FAKE), B.EINVAL), (dict(len_out=FAKE + 4), B.EINVAL), (dict(keep=FAKE + 2), B.EALIGN),
         (dict(dst=_flat()), B.EINVAL), (dict(cache=_paged(), dst=_paged()), B.EINVAL), (dict(cache=_paged(), dst=_paged(k=FAKE + 2 ** 22)), B.EINVAL), (dict(dst=_flat(k=FAKE + 2 ** 22, v=FAKE + 2 ** 23, n_seqs=2)), B.EINVAL),
         (dict(dst=_flat(k=FAKE + 8)), B.EALIGN), (dict(sink=2 ** 31 - 1, recent=2 ** 31 - 1), B.EINVAL)],
 }
