@@ -51,6 +51,7 @@
 // prompts 201, 6 tokens 73); two threads a row, 64 slots each, whose 24 warps leave 80
 // registers a thread, 906 (at head_dim 256, where 16 warps are enough, 168 for 176).
 #include "prcr_cache.cuh"
+#include "prcr_chunk_phases.h"
 #include "prcr_pdl.cuh"
 #include "prcr_tc.cuh"
 
@@ -435,10 +436,10 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
             const uint32_t o_t = tmem + 256 + uint32_t(qi) * D + lanes;
             const float scale = a.scale_log2;
             for (int j = 0; j < w.tiles[qi]; ++j) {
-                const int buf = NQ == 2 ? qi : (j & 1);
-                const uint32_t ph = NQ == 2 ? uint32_t(j & 1) : uint32_t((j >> 1) & 1);
+                const ChunkPhase sc = chunk_scores(NQ, qi, j), before = chunk_products(NQ, qi, j - 1);
+                const int buf = sc.bar;
                 const uint32_t s_t = tmem + uint32_t(buf) * 128 + lanes;
-                if (!mbar_wait(smem_u32(&bars.s[buf]), ph)) {
+                if (!mbar_wait(smem_u32(&bars.s[buf]), sc.parity)) {
                     failed = true;
                     break;
                 }
@@ -470,7 +471,7 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                     m_run = mt;
                 } else if (__any_sync(kFull, raise)) {
                     // (NQ = 2: this S was made behind the last tile's products)
-                    if (NQ == 1 && !mbar_wait(smem_u32(&bars.o[0]), uint32_t((j - 1) & 1))) {
+                    if (NQ == 1 && !mbar_wait(smem_u32(&bars.o[before.bar]), before.parity)) {
                         failed = true;
                         break;
                     }
@@ -522,16 +523,16 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                 }
                 const uint64_t sum = add2(add2(sums[0], sums[1]), sums[2]);
                 l_run += lo32(sum) + hi32(sum);
-                // (every phase of this barrier is waited for: parities tell one from the next)
-                if (NQ == 1 && !summed && !mbar_wait(smem_u32(&bars.o[0]), uint32_t((j - 1) & 1))) {
+                // (each tile's phase is waited for before the next on its barrier can complete)
+                if (NQ == 1 && !summed && !mbar_wait(smem_u32(&bars.o[before.bar]), before.parity)) {
                     failed = true;
                     break;
                 }
             }
             // all of this half's products are done
             if (!failed && w.tiles[qi] > 0) {
-                const uint32_t ph = NQ == 2 ? 0u : uint32_t((w.tiles[0] - 1) & 1);
-                if (!mbar_wait(smem_u32(&bars.o[qi]), ph)) failed = true;
+                const ChunkPhase last = chunk_products(NQ, qi, w.tiles[qi] - 1);
+                if (!mbar_wait(smem_u32(&bars.o[last.bar]), last.parity)) failed = true;
                 tc_fence_after();
             }
           }
@@ -713,7 +714,8 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                     return ok;
                 };
                 // S of 128 rows: entries e0 .. hold the tile's keys
-                auto qk = [&](int q, int buf, int e0) {
+                auto qk = [&](int q, int j, int e0) {
+                    const int buf = chunk_scores(NQ, q, j).bar;
                     tc_fence_after();
 #pragma unroll
                     for (int part = 0; part < PARTS; ++part) {
@@ -725,20 +727,22 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                             tc_mma_ss(tmem + uint32_t(buf) * 128, da + step, db + step, id_qk, part + k > 0, on);
                         }
                     }
+                    tc_commit(smem_u32(&bars.s[buf]), on);
                 };
                 // O += P V of 128 rows, each half of the slots as soon as its P is there
-                auto pv = [&](int q, int buf, int e0, uint32_t ph, bool add) -> bool {
+                auto pv = [&](int q, int j, int e0) -> bool {
+                    const ChunkPhase sc = chunk_scores(NQ, q, j);
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        if (!mbar_wait(smem_u32(&bars.p[buf][half]), ph)) return false;
+                        if (!mbar_wait(smem_u32(&bars.p[sc.bar][half]), sc.parity)) return false;
                         tc_fence_after();
 #pragma unroll
                         for (int part = 0; part < PARTS; ++part) {
                             const uint64_t db = dv + uint32_t((e0 + part) % ST) * (Sh::kEntry >> 4);
 #pragma unroll
                             for (int k = half * 4; k < half * 4 + 4; ++k)
-                                tc_mma_ts(tmem + 256 + uint32_t(q) * D + uint32_t(part) * DIMS, tmem + uint32_t(buf) * 128 + uint32_t(k) * 8,
-                                          db + uint32_t(k) * (2048 >> 4), id_pv, add || k > 0, on);
+                                tc_mma_ts(tmem + 256 + uint32_t(q) * D + uint32_t(part) * DIMS, tmem + uint32_t(sc.bar) * 128 + uint32_t(k) * 8,
+                                          db + uint32_t(k) * (2048 >> 4), id_pv, j > 0 || k > 0, on);
                         }
                     }
                     return true;
@@ -749,10 +753,7 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                 bool ok = mbar_wait(smem_u32(&bars.q), 0) && ready(0);
                 if (ok) {
                     for (int q = 0; q < NQ; ++q)
-                        if (w.tiles[q] > 0) {
-                            qk(q, q, 0);
-                            tc_commit(smem_u32(&bars.s[q]), on);
-                        }
+                        if (w.tiles[q] > 0) qk(q, 0, 0);
                     release(0);
                     e = PARTS;
                 }
@@ -766,16 +767,15 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                         for (int q = 0; q < 2; ++q) {
                             const int n = q ? n1 : n0;
                             if (!ok || j >= n) continue;
-                            ok = pv(q, q, ev, uint32_t(j & 1), j > 0);
+                            ok = pv(q, j, ev);
                             if (!ok) continue;
                             if (j + 1 < n) {
                                 if (!have) ok = ready(ek);
                                 have = true;
                                 if (!ok) continue;
-                                qk(q, q, ek);
-                                tc_commit(smem_u32(&bars.s[q]), on);
+                                qk(q, j + 1, ek);
                             } else {
-                                tc_commit(smem_u32(&bars.o[q]), on);
+                                tc_commit(smem_u32(&bars.o[chunk_products(NQ, q, j).bar]), on);
                             }
                         }
                         if (ok && j + 1 < nt) {
@@ -789,15 +789,14 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                         if (j + 1 < nt) {
                             ok = ready(e);
                             if (!ok) break;
-                            qk(0, (j + 1) & 1, e);
-                            tc_commit(smem_u32(&bars.s[(j + 1) & 1]), on);
+                            qk(0, j + 1, e);
                             release(e);
                             e += PARTS;
                         }
-                        ok = ready(e) && pv(0, j & 1, e, uint32_t((j >> 1) & 1), j > 0);
+                        ok = ready(e) && pv(0, j, e);
                         if (!ok) break;
                         if (j + 1 < nt) release(e);
-                        tc_commit(smem_u32(&bars.o[0]), on);
+                        tc_commit(smem_u32(&bars.o[chunk_products(NQ, 0, j).bar]), on);
                         e += PARTS;
                     }
                 }

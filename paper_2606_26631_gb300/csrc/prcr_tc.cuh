@@ -19,8 +19,9 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 }
 
 // Whether the barrier's phase of this parity has completed, after waiting for it
-// at most kWaitCycles (about two seconds): a wait that runs out means that
-// another warp gave up, and ends the kernel instead of hanging it.
+// at most kWaitCycles (about two seconds): a wait that runs out ends the kernel instead
+// of hanging it. (The caller sees to it that the barrier cannot complete another phase
+// first: two would have the awaited parity again.)
 constexpr long long kWaitCycles = 1ll << 32;
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
     auto ready = [&]() {

@@ -855,3 +855,25 @@ def test_a_workspace_for_the_largest_call_serves_the_others():
         x.run()
         assert x.done() == 0
         x.check(rows=40)
+
+
+@pytest.mark.parametrize("H,g,D,new,lens", [(8, 4, 128, [6] * 16, [8198 - 300 * i for i in range(16)]), (2, 8, 64, [1], [2000]),
+                                            (4, 2, 64, [3] * 40, [700] * 40), (4, 8, 256, [90, 200], [2500, 3000])], ids=str)
+def test_chunk_calls_in_a_row_beside_copies(H, g, D, new, lens):
+    """The kernels with two S buffers, whose warps run a tile ahead of the products, hundreds of times while another stream
+    keeps the memory busy: no wait runs out, and every call gives the same."""
+    c = Chunk(H, g, D, new, lens, 16, seed=7)
+    assert c.run().done() == 0
+    c.check(rows=9)
+    want, side = c.out.clone(), torch.cuda.Stream()
+    a, b = (torch.empty(1 << 28, dtype=torch.uint8, device=DEV) for _ in range(2))
+    for turn in range(10):
+        c.out.fill_(U.CANARY)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(8):
+                b.copy_(a)
+        for _ in range(40):
+            c.run()
+        assert c.done() == 0
+        assert torch.equal(c.out[:sum(new)], want[:sum(new)])
