@@ -583,6 +583,8 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
             // the queries' place now holds the results (this half's products with
             // them are done): whole rows go out, 16 bytes a lane
             constexpr int CPR = D / 8, RPI = 32 / CPR;
+            // (a row that sees no slot is zeros, also where a value hidden from it is not finite)
+            const uint32_t seeing = __ballot_sync(kFull, live && any);
             __syncwarp();
 #pragma unroll 4
             for (int i = 0; i < 32 / RPI; ++i) {
@@ -590,7 +592,7 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                 const int64_t to = __shfl_sync(kFull, row_ok ? dst : int64_t(-1), src);
                 if (to >= 0)
                     st_row(a.out + to + (lane % CPR) * 8,
-                           any ? ld_shared(q_s + chunk_at<Sh>((r & ~31) + src, lane % CPR)) : make_uint4(0, 0, 0, 0));
+                           (seeing >> src) & 1u ? ld_shared(q_s + chunk_at<Sh>((r & ~31) + src, lane % CPR)) : make_uint4(0, 0, 0, 0));
             }
             __syncwarp();
         }

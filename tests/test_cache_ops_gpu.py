@@ -877,3 +877,26 @@ def test_chunk_calls_in_a_row_beside_copies(H, g, D, new, lens):
             c.run()
         assert c.done() == 0
         assert torch.equal(c.out[:sum(new)], want[:sum(new)])
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("H,g,D,block,new,lens,slot", [
+    (2, 4, 128, 16, [9, 3], [4, 3], 2), (1, 8, 64, 0, [50, 30], [37, 30], 20), (2, 2, 256, 7, [70, 1], [60, 1], 59),
+    (2, 4, 128, 0, [300, 20], [230, 20], 100), (4, 2, 64, 16, [700, 3], [650, 3], 0),
+    (1, 1, 128, 16, [1710], [1700], 1600),  # the slots in parts
+], ids=str)
+def test_chunk_rows_that_see_nothing_beside_bad_values(H, g, D, block, new, lens, slot, bad):
+    """More new tokens than slots, and a value that is not finite in one of these: zeros for the queries that see no slot,
+    the formula's for those that do not see this one."""
+    c = Chunk(H, g, D, new, lens, block, seed=13)
+    c.cache.v[c.cache.where(0, [slot])] = bad
+    assert c.run().done() == 0
+    out, none = U.f64(c.out[:new[0]]), new[0] - lens[0]
+    assert (out[:none] == 0).all()
+    i = np.unique(np.linspace(none, none + slot - 1, 20).astype(int)) if slot else np.arange(0)
+    K, V = (U.f64(c.cache.rows(x, 0, lens[0])[1]) for x in (c.cache.k, c.cache.v))
+    V[slot] = 0.0
+    ref, bar = U.chunk64(U.f64(c.q)[i], c.pos[i], K, V, U.causal(new[0], lens[0], lens[0])[i])
+    assert (np.abs(out[i] - ref) <= bar).all()
+    assert not np.isfinite(out[none + slot:]).any()
+    c.check(seqs=[1])
