@@ -169,12 +169,66 @@ __device__ __forceinline__ void st_peer(const float* p, int rank, float x) {
                  : "memory");
 }
 
+// The NaN among a CTA's exponentials again, from float32 FMAs, and the heads' sums over the
+// cluster: an infinite key times a later term of the query, of the other sign or 0, makes a
+// NaN where the product with the whole query is an infinity (and a logit of -inf a weight of
+// 0). A call, for the rare sum that is a NaN: a test of each logit in the kernel took 3 %
+// longer. smem: the query's fragments, no longer needed, and the exponentials; s0, n: the
+// CTA's slots; head: in, the maxima, out, the sums; peer: the cluster's CTAs' sums.
+template <int D>
+__device__ __noinline__ void exact_nans(const WeightsArgs& a, unsigned char* smem, int s0, int n, float* head, float (*peer)[8]) {
+    const int C = a.cluster, H = a.n_kv_heads, unit = int(blockIdx.x) / C, h = unit % H, l = unit / H % a.n_layers, b = unit / (H * a.n_layers);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, stride = logit_stride(a.slots_per_cta);
+    float* const q_s = reinterpret_cast<float*>(smem);  // [group][D]
+    float* const e = reinterpret_cast<float*>(smem + WeightsShape<D>::kFragBytes);
+    const uint16_t* const q = a.q + int64_t(unit) * a.group * D;
+    for (int i = tid; i < a.group * (D / 2); i += kWarps * 32) {
+        const int j = i / (D / 2), d = i % (D / 2);
+        float s, c;
+        sincos_turns(double(a.q_pos[b]), a.turn_freq[d], &s, &c);
+        const float u = lo_f32(q[j * D + d]), v = lo_f32(q[j * D + d + D / 2]);
+        q_s[j * D + d] = fmaf(u, c, -v * s) * a.scale_log2;
+        q_s[j * D + d + D / 2] = fmaf(v, c, u * s) * a.scale_log2;
+    }
+    __syncthreads();
+    const uint16_t* const k = a.cache.k + int64_t(l) * a.cache.layer_stride + int64_t(h) * D;
+    for (int s = tid; s < n; s += kWarps * 32)
+        for (int j = 0; j < a.group; ++j) {
+            if (e[j * stride + s] == e[j * stride + s]) continue;
+            uint32_t err = 0;
+            const int64_t row = slot_row(a.cache, b, s0 + s, err);
+            float x = row < 0 ? -INFINITY : 0.0f;
+            for (int d = 0; d < D && row >= 0; ++d) x = fmaf(q_s[j * D + d], lo_f32(k[row + d]), x);
+            // (plus infinity was not among the maxima: less itself it would be the NaN that it is here)
+            e[j * stride + s] = x == INFINITY ? NAN : exp2_fast(x - head[j]);
+        }
+    __syncthreads();
+    static_assert(kWarps == 8, "a warp a head");
+    float sum = 0.0f;
+    for (int s = lane; warp < a.group && s < n; s += 32) sum += e[warp * stride + s];
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
+    if (C == 1) {
+        if (lane == 0) head[warp] = sum;
+    } else {
+        if (lane < C) st_peer(&peer[int(blockIdx.x) % C][warp], lane, sum);
+        cluster_arrive();
+        cluster_wait();
+        if (tid < 8) {
+            float x = 0.0f;
+            for (int r = 0; r < C; ++r) x += peer[r][tid];
+            head[tid] = x;
+        }
+    }
+    __syncthreads();
+}
+
 template <int D>
 __global__ void __launch_bounds__(kWarps * 32, 2) weights_kernel(const __grid_constant__ WeightsArgs a) {
     using Sh = WeightsShape<D>;
     constexpr int P = D / 2, KS = Sh::kSteps, LV = Sh::kLoads, PARTS = Sh::kParts;
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ float s_part[kWarps][8], s_peer[2][kMaxRanks][8];
+    __shared__ float s_part[kWarps][8], s_peer[3][kMaxRanks][8];
     uint4* const frag = reinterpret_cast<uint4*>(smem);  // [3][KS / 2][32]: the query's B fragments of two k-steps
     float* const logit = reinterpret_cast<float*>(smem + Sh::kFragBytes);
     const int C = a.cluster, rank = int(blockIdx.x) % C;
@@ -368,6 +422,19 @@ __global__ void __launch_bounds__(kWarps * 32, 2) weights_kernel(const __grid_co
     const float v0 = t == 0 ? sum[0] : t == 1 ? sum[2] : t == 2 ? sum[4] : sum[6];
     const float v1 = t == 0 ? sum[1] : t == 1 ? sum[3] : t == 2 ? sum[5] : sum[7];
     join(v0, v1, 1, [](float x, float y) { return x + y; }, 0.0f, inv);
+    float all = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) all += inv[j];
+    if (all != all) {  // the same in all of the cluster's CTAs
+        if (tid == 0) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s_part[0][j] = m[j];
+        }
+        __syncthreads();
+        exact_nans<D>(a, smem, s0, n, s_part[0], s_peer[2]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) inv[j] = s_part[0][j];
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) inv[j] = inv[j] == 0.0f ? 0.0f : 1.0f / inv[j];
 

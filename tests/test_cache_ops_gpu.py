@@ -900,3 +900,41 @@ def test_chunk_rows_that_see_nothing_beside_bad_values(H, g, D, block, new, lens
     assert (np.abs(out[i] - ref) <= bar).all()
     assert not np.isfinite(out[none + slot:]).any()
     c.check(seqs=[1])
+
+
+@pytest.mark.parametrize("H,g,D,lens,block", [(2, 4, 128, [300, 40], 16), (1, 8, 64, [60000], 16), (1, 1, 256, [700, 9], 0), (3, 2, 64, [129], 7)], ids=str)
+@pytest.mark.parametrize("moved", [False, True])
+def test_weights_infinite_keys(H, g, D, lens, block, moved):
+    """A key whose logit is minus infinity gets weight 0 and the others theirs as without it, in a cluster and through the
+    workspace (60,000 slots); one of plus infinity or NaN makes that KV head's weights NaN, as the formula does."""
+    w = Weights(H, g, D, 2, lens, block, seed=g)
+    at, d = 7, 5
+    if moved:  # heads of one sign in that dim, at positions that rotate
+        w.q[:] = w.q[:, :, ::g].repeat_interleave(g, 2)
+        qr = np.stack([U.rope64(U.f64(w.q[b])[:, ::g], np.full((2, 3), float(w.pos[b])), D, w.layout) for b in range(len(lens))])
+        sign = np.sign(qr[..., d])
+    else:
+        w.pos[:] = 0
+        w.q[..., d] = w.q[..., d].abs() + 0.01
+        sign = np.ones((len(lens), 2, H))
+    for b in range(len(lens)):
+        where = w.cache.where(b, [at])
+        rows = w.cache.k[where]
+        rows[:, 0, :, d] = torch.from_numpy(-np.inf * sign[b]).to(DEV).bfloat16()
+        w.cache.k[where] = rows
+    assert w.run() == 0
+    finite = w.cache.k.clone()
+    for b in range(len(lens)):
+        w.cache.k[w.cache.where(b, [at])] = 0.0
+    w.check(drop=lambda b, s: s == at)
+    w.cache.k.copy_(finite)
+    for bad in (float("inf"), float("nan")):  # in head 0 alone
+        where = w.cache.where(0, [at])
+        rows = w.cache.k[where]
+        for l in range(2):
+            rows[l, 0, 0, d] = bad * sign[0, l, 0]
+        w.cache.k[where] = rows
+        w.score.copy_(torch.from_numpy(w.before))
+        assert w.run() == 0
+        got = w.score.cpu().numpy()
+        assert np.isnan(got[0, :, 0, :lens[0]]).all() and np.isfinite(got[0, :, 1:]).all() and np.isfinite(got[1:]).all()
