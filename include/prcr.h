@@ -473,8 +473,8 @@ PRCR_API int prcr_chunk_attention(const prcr_rope_cfg* cfg, const prcr_cache_des
  * Limits, a seq_len beyond the capacity or max_len, a q_pos of magnitude 2^31 or
  * more, and unmapped blocks are prcr_decode_attention's (such slots get weight 0).
  * With max_len 0 nothing is done.
- * workspace: device, >= prcr_weights_workspace_size(...) bytes (0 unless max_len is
- * above 400,000 / query heads per KV head), 16-byte aligned, not shared with a
+ * workspace: device, >= prcr_weights_workspace_size(...) bytes (0 for every max_len
+ * up to 399,000 / query heads per KV head), 16-byte aligned, not shared with a
  * concurrent call.                                                            */
 PRCR_API size_t prcr_weights_workspace_size(const prcr_rope_cfg* cfg, int32_t n_seqs,
                                             int32_t n_q_heads, int64_t max_len);

@@ -20,9 +20,9 @@
 // slots beside the queries' angles). Measured with 8 heads of 128 in groups of 4, 36 layers:
 // 16 sequences of up to 4096 slots 520 us, 5.5 TB/s; one of 933 slots 18.5 us,
 // 3.9 TB/s: one wave, whose first rows wait for the queries and whose last for the sums.
-// Where the logits of a sequence do not fit a cluster's shared memory (above
-// 400,000 / group slots), they go through the workspace instead (weights_logits_kernel,
-// weights_sum_kernel).
+// Where the logits of a sequence do not fit a cluster's shared memory (above 399,360 / group
+// slots at head_dim 256, 417,792 at 64), they go through the workspace instead
+// (weights_logits_kernel, weights_sum_kernel).
 #include <algorithm>
 
 #include "prcr_cache.cuh"

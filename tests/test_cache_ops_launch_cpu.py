@@ -71,3 +71,16 @@ def test_shared_memory_and_limits():
     names = {k for k, _ in F.launches()}
     assert any("weights_kernel" in k for k in names) and any("weights_sum" in k for k in names)
     assert F.lib().fake_lowered() == 0
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_weights_need_no_workspace_up_to_the_documented_length(D):
+    """399,000 / query heads per KV head slots, and every length below: no bytes are asked for, and none is a call's."""
+    for g in range(1, 9):
+        c, most = F.cfg(1, 1, D), 399000 // g
+        rng = random.Random(g)
+        for n in [most, most - 1, most - 15, most // 2, most // 8 + 1] + [rng.randint(1, most) for _ in range(40)]:
+            for seqs in (1, 16):
+                assert F.lib().prcr_weights_workspace_size(C.byref(c), seqs, g, n) == 0, (D, g, n)
+                assert weights(c, seqs, g, n, 0) == B.OK, (D, g, n)
+    F.launches()
