@@ -140,3 +140,39 @@ def evict64(score, n, budget, sink, recent):
         return list(range(n))
     mid = score_order(score, sink, n - recent, budget - sink - recent)
     return sorted(list(range(sink)) + mid + list(range(n - recent, n)))
+
+
+def chunk64_exact(q, K, V, sees):
+    """out [n, Hq, D] and a bound on its error as chunk64 gives them, for queries at position 0: these are not rotated, so the
+    kernel's bf16 ones are exact, and large logits do not blur the bound.
+
+    A float32 dot of D products is off by at most e = D 2^-23 sum |q k| / sqrt(D) (its D additions by 2^-23 of a partial sum
+    each), whatever their order. That moves a weight w by a factor within exp(+-2 e), and so 1 - w, the others' sum: by at most
+    expm1(2 e) min(w, 1 - w). The probabilities and the output are rounded by 2^-8."""
+    n, Hq, D = q.shape
+    g = Hq // K.shape[1]
+    out, bound = np.zeros_like(q), np.zeros_like(q)
+    for h in range(Hq):
+        k, v = K[:, h // g], V[:, h // g]
+        x = q[:, h] @ k.T / np.sqrt(D)
+        e = D * 2.0 ** -23 * (np.abs(q[:, h]) @ np.abs(k).T) / np.sqrt(D)
+        for i in range(n):
+            s = sees[i]
+            if not s.any():
+                continue
+            w = softmax64(x[i, s])
+            out[i, h] = w @ v[s]
+            off = 2.0 ** -8 * w + np.expm1(2 * e[i, s].max()) * np.minimum(w, 1 - w)
+            bound[i, h] = (2.0 ** -8 * np.abs(out[i, h]) + off @ np.abs(v[s])) * 1.001 + 1e-30
+    return out, bound
+
+
+EXACT_NORM = 3.5e-3  # two roundings, of 1.6e-3 in the mean square each, make 2.3e-3 of the 2-norm; half as much again
+
+
+def assert_close(got, ref, bound):
+    """Every element within its bound, and the whole within EXACT_NORM of the 2-norm."""
+    d = np.abs(got - ref)
+    assert (d <= bound).all(), (np.unravel_index((d - bound).argmax(), d.shape), (d / bound).max())
+    norm = np.sqrt((ref ** 2).sum())
+    assert np.sqrt((d ** 2).sum()) <= EXACT_NORM * norm, np.sqrt((d ** 2).sum()) / norm

@@ -2,9 +2,11 @@
 host refuses, before any CUDA call (the addresses below are never read)."""
 import ctypes as C
 
+import numpy as np
 import pytest
 import torch
 
+import cache_ops_util as U
 import paper_2606_26631_gb300 as prcr
 from paper_2606_26631_gb300 import _binding as B
 
@@ -158,3 +160,31 @@ def test_strides_of_single_entries():
     assert B._strides(_t((2, 5, 2, 64)), 4, "k") == (640, 128, 64, 1)
     assert B._strides(torch.as_strided(_t(4096), (2, 1, 2, 64), (256, 8, 64, 1)), 4, "k") == (256, 128, 64, 1)
     assert B._strides(torch.as_strided(_t(4096), (1, 2, 2, 64), (0, 128, 64, 1)), 4, "k") == (256, 128, 64, 1)
+
+
+def _wrong(ref, V, sees, g):
+    """Results as mistakes would make them: nothing, the sign, a slot too many or too few, a lost part of the slots."""
+    yield np.zeros_like(ref)
+    yield -ref
+    yield ref * (1 + 2.0 ** -6)
+    yield np.roll(ref, 1, axis=0)
+    yield np.repeat(V[:1].mean(0)[None], ref.shape[0], 0).repeat(g, 1)
+
+
+@pytest.mark.parametrize("scale", [1.0, 30.0, 1000.0])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_the_bars_of_large_logits_see_wrong_results(D, scale):
+    """What chunk_attention is held to at large logits is not wider than the results: wrong ones fail, and the right one
+    rounded to bf16 passes."""
+    rng = np.random.default_rng(D)
+    bf16 = lambda x: torch.from_numpy(x).bfloat16().double().numpy()
+    q, K, V = (bf16(rng.standard_normal(s) * f) for s, f in (((20, 4, D), scale), ((300, 2, D), 1.0), ((300, 2, D), 1.0)))
+    sees = U.causal(20, 300, 300)
+    ref, bar = U.chunk64_exact(q, K, V, sees)
+    U.assert_close(bf16(ref), ref, bar)
+    for bad in _wrong(ref, V, sees, 2):
+        with pytest.raises(AssertionError):
+            U.assert_close(bad, ref, bar)
+    fewer, _ = U.chunk64_exact(q, K[:256], V[:256], U.causal(20, 300, 256))
+    with pytest.raises(AssertionError):
+        U.assert_close(fewer, ref, bar)

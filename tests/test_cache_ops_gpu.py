@@ -938,3 +938,136 @@ def test_weights_infinite_keys(H, g, D, lens, block, moved):
         assert w.run() == 0
         got = w.score.cpu().numpy()
         assert np.isnan(got[0, :, 0, :lens[0]]).all() and np.isfinite(got[0, :, 1:]).all() and np.isfinite(got[1:]).all()
+
+
+# ----------------------------------------------------------------------------
+# chunk attention at position 0, where the queries are exact (cache_ops_util.chunk64_exact)
+# ----------------------------------------------------------------------------
+EXACT = [  # H, g, D, block, new, lens: few rows, many, in parts, head_dim 64 and 256
+    (2, 4, 128, 16, [40, 1], [500, 2000]), (2, 4, 128, 0, [350, 20], [700, 300]), (1, 8, 64, 0, [9, 3], [300, 1500]), (4, 2, 64, 16, [600], [640]),
+    (2, 4, 256, 7, [30, 1], [200, 900]), (2, 4, 256, 0, [300], [420]), (2, 7, 128, 16, [5], [9000]), (1, 4, 128, 16, [600], [4000]),
+]
+
+
+class Exact(Chunk):
+    def __init__(self, *args, **kw):
+        super().__init__(*args, **kw)
+        self.pos[:] = 0
+        self.args = (i32(self.pos),) + self.args[1:]
+
+    def check(self, rows=24, upto=None, slots=None):
+        """Queries of each sequence (those below upto[b], over slots[b] slots) against the reference, over the finite rows."""
+        at = 0
+        for b, (n, length) in enumerate(zip(self.new, self.lens)):
+            free = n if upto is None else upto[b]
+            i = np.unique(np.linspace(0, max(free - 1, 0), min(rows, max(free, 1))).astype(int))
+            S = length if slots is None else slots[b]
+            if free > 0:
+                K, V = (U.f64(self.cache.rows(x, b, S)[self.layer]) for x in (self.cache.k, self.cache.v))
+                U.assert_close(U.f64(self.out)[at + i], *U.chunk64_exact(U.f64(self.q)[at + i], K, V, U.causal(n, length, S)[i]))
+            at += n
+
+
+@pytest.mark.parametrize("scale", [0.0, 1.0, 30.0, 1000.0])
+@pytest.mark.parametrize("H,g,D,block,new,lens", EXACT, ids=str)
+def test_chunk_exact_logits_of_any_size(H, g, D, block, new, lens, scale):
+    """From equal logits to some so far apart that one slot takes all."""
+    c = Exact(H, g, D, new, lens, block, q_scale=scale, seed=8)
+    assert c.run().done() == 0
+    c.check()
+
+
+@pytest.mark.parametrize("H,g,D,block,new,lens", EXACT, ids=str)
+@pytest.mark.parametrize("how", ["rising", "falling", "one tile"])
+def test_chunk_exact_maxima(H, g, D, block, new, lens, how):
+    """Keys that grow along the sequence (every tile raises the running maximum), that shrink (none does), and that are large in
+    one late tile alone."""
+    c = Exact(H, g, D, new, lens, block, seed=12)
+    for b, n in enumerate(lens):
+        f = torch.linspace(0.1, 12.0, n, device=DEV)
+        f = f.flip(0) if how == "falling" else f
+        if how == "one tile":
+            f = torch.where((torch.arange(n, device=DEV) // 128) == (n * 2 // 3) // 128, 20.0, 0.5)
+        w = c.cache.where(b, np.arange(n))
+        x = c.cache.k[w].float()
+        c.cache.k[w] = (x * f.view((1, n, 1, 1) if x.dim() == 4 else (n, 1, 1))).bfloat16()
+    assert c.run().done() == 0
+    c.check()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("H,g,D,block,new,lens", EXACT, ids=str)
+def test_chunk_exact_beside_bad_slots(H, g, D, block, new, lens, bad):
+    """Values that are not finite behind the lengths and in a slot that only later queries see: those before it get what the
+    formula gives without it."""
+    c = Exact(H, g, D, new, lens, block, seed=2)
+    upto, slots = [], []
+    for b, (n, length) in enumerate(zip(new, lens)):
+        w = c.cache.where(b, np.arange(length, length + 3))
+        c.cache.k[w], c.cache.v[w] = bad, bad
+        s = length - (n + 1) // 2
+        c.cache.v[c.cache.where(b, [s])] = bad
+        upto.append(n - (length - s))
+        slots.append(s)
+    assert c.run().done() == 0
+    c.check(upto=upto, slots=slots)
+    at = 0
+    for n, free in zip(new, upto):
+        assert not np.isfinite(U.f64(c.out)[at + free:at + n]).any()
+        at += n
+
+
+@pytest.mark.parametrize("H,g,D,block,new,lens", EXACT, ids=str)
+def test_chunk_exact_beside_nan_keys(H, g, D, block, new, lens):
+    c = Exact(H, g, D, new, lens, block, seed=4)
+    upto, slots = [], []
+    for b, (n, length) in enumerate(zip(new, lens)):
+        s = length - (n + 1) // 2
+        c.cache.k[c.cache.where(b, [s])] = float("nan")
+        upto.append(n - (length - s))
+        slots.append(s)
+    assert c.run().done() == 0
+    c.check(upto=upto, slots=slots)
+    at = 0
+    for n, free in zip(new, upto):
+        assert np.isnan(U.f64(c.out)[at + free:at + n]).all()
+        at += n
+
+
+def test_layer_by_layer_as_a_decoder_runs():
+    """Each layer's rows appended and attended over before the next layer's exist, through two prompts, tokens, an eviction in
+    place and tokens behind it: each attention against the 64-bit formula on the rows that the cache holds."""
+    L, H, g, D, block, budget = 3, 4, 4, 128, 16, 60
+    c, st = U.cfg_of(L, H, D), status_word()
+    cache = Cache(L, H, D, [160, 160], block, fill=0.0)
+    length = i32([0, 0])
+    top, turn = 160, 0
+    ws = torch.empty(max(16, prcr.chunk_workspace_size(c, 2, H * g, 140, top)), dtype=torch.uint8, device=DEV)
+    for new in ([90, 50], [1, 1], [6, 3], "evict", [1, 1], [5, 40]):
+        if new == "evict":
+            score = torch.rand((2, L, H, top), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV)
+            keep, cut = i32(np.zeros((2, L, H, budget))), i32([0, 0])
+            prcr.evict(c, cache.desc(), length, top, budget, 4, 16, score, keep, cut, st)
+            length = cut
+            continue
+        turn += 1
+        T, off, after = sum(new), U.offsets(new), i32([0, 0])
+        pos = np.concatenate([positions(n, 200 * turn, None) for n in new]).astype(np.int32)
+        for l in range(L):
+            k, v, q = normal((1, T, H, D), 10 * turn + l), normal((1, T, H, D), 100 * turn + l), normal((T, H * g, D), 1000 * turn + l)
+            out = torch.empty_like(q)
+            prcr.append_kv(c, cache.desc(), l, k, v, i32(pos), off, length, after, st)
+            prcr.chunk_attention(c, cache.desc(), l, q, i32(pos), off, after, top, out, st, ws)
+            torch.cuda.synchronize()
+            assert int(st.item()) == 0
+            at = 0
+            for b, n in enumerate(new):
+                S = int(after[b])
+                K, V = (U.f64(cache.rows(x, b, S)[l]) for x in (cache.k, cache.v))
+                assert torch.equal(cache.rows(cache.v, b, S)[l, S - n:], v[0, at:at + n])
+                ref, bar = U.chunk64(U.f64(q[at:at + n]), pos[at:at + n], K, V, U.causal(n, S, S))
+                d = np.abs(U.f64(out[at:at + n]) - ref)
+                assert (d <= bar).all() and np.sqrt((d ** 2).sum() / (ref ** 2).sum()) <= NORM
+                at += n
+        assert [int(x) for x in after] == [int(x) + n for x, n in zip(length, new)]
+        length = after
