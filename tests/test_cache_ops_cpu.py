@@ -162,6 +162,17 @@ def test_strides_of_single_entries():
     assert B._strides(torch.as_strided(_t(4096), (1, 2, 2, 64), (0, 128, 64, 1)), 4, "k") == (256, 128, 64, 1)
 
 
+def test_weights_workspace_refusals():
+    """A call of lengths that need a workspace: none, one a byte short, and one that is not aligned."""
+    c, n = _cfg(D=128, H=8, L=36), 120000
+    need = prcr.weights_workspace_size(c, 3, 32, n)
+    assert need == 3 * 36 * 32 * n * 4
+    a = dict(cfg=c, cache=_flat(slot_stride=1024, layer_stride=n * 1024, seq_stride=36 * n * 1024, max_slots=n), hq=32, max_len=n, ss=n)
+    assert call("prcr_accumulate_weights", **a, ws_bytes=need - 1) == B.EWORKSPACE
+    assert call("prcr_accumulate_weights", **a, ws=None, ws_bytes=need) == B.EWORKSPACE
+    assert call("prcr_accumulate_weights", **a, ws=FAKE + 8, ws_bytes=need) == B.EALIGN
+
+
 def _wrong(ref, V, sees, g):
     """Results as mistakes would make them: nothing, the sign, a slot too many or too few, a lost part of the slots."""
     yield np.zeros_like(ref)
