@@ -254,6 +254,8 @@ int layers_per_cta(int64_t tiles, int n_layers, int64_t slots) {
     return best;
 }
 
+}  // namespace
+
 // Layers each CTA walks in the kernels that stream rows from HBM (rebind,
 // capture): the fewest, up to `few`, that make at most `wave` CTAs; else `few`, so
 // that many short CTAs overlap one another's prologues and end together. Groups are
@@ -266,8 +268,6 @@ int layers_per_cta(int64_t tiles, int n_layers, int64_t slots) {
 // 33, of 11 22 us, with eight of 128 x 22 x 1344 of 4 42.6, of 11 43.5. Capture (few 6
 // / heads, two at least; a wave is all resident CTAs): one head of 128 x 18 layers x
 // 3410 tokens 90 us at 2, 71 at 6; eight x 36 x 768 x 3 images 158 at 2, 161 at 4.
-}  // namespace
-
 int stream_layers_per_cta(int64_t tiles, int n_layers, int64_t wave, int few) {
     if (n_layers > 65535) return layers_per_cta(tiles, n_layers, wave);  // grid y
     auto even = [&](int g) {
