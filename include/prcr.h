@@ -386,7 +386,10 @@ PRCR_API int prcr_select_topk(const prcr_rope_cfg* cfg, const prcr_store_desc* s
  *               (equal relevance: lower index first)
  * Other arguments, outputs, limits and the workspace (prcr_select_workspace_size
  * with the same n_seqs, n_q_heads, n_tokens) are those of prcr_select_topk;
- * head_dim must be 64, 128 or 256 (PRCR_EINVAL otherwise).               */
+ * head_dim must be 64, 128 or 256 (PRCR_EINVAL otherwise).
+ * Not for a cache that prcr_evict has cut: its KV heads keep different slots, so that no
+ * img_slot0 says where the image's tokens are, and the call cannot see that. (The raw
+ * store is not touched by an eviction: prcr_select_topk stays right.)    */
 PRCR_API int prcr_select_topk_cached(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache,
                                      int32_t n_seqs, int32_t layer, int32_t n_q_heads,
                                      int32_t n_tokens, const int32_t* img_slot0, const void* q,
@@ -412,6 +415,8 @@ PRCR_API int prcr_select_topk_cached(const prcr_rope_cfg* cfg, const prcr_cache_
  *               is appended
  *   cache_len_out device int32 [n_seqs]: cache_len_in + the sequence's tokens (must
  *               not overlap cache_len_in)
+ * A decoder whose layer needs the last one's output calls it layer by layer, with the
+ * same offsets and lengths, each before that layer's prcr_chunk_attention.
  * A slot beyond the capacity or in an unmapped block sets PRCR_ST_CAPACITY /
  * PRCR_ST_NO_BLOCK and its rows are skipped. Source and cache must not overlap. */
 PRCR_API int prcr_append_kv(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache, int32_t n_seqs,
@@ -434,11 +439,13 @@ PRCR_API int prcr_append_kv(const prcr_rope_cfg* cfg, const prcr_cache_desc* cac
  *   coords   device int32 [total_q][3] (t, h, w); (p, p, p) for a text token
  *   q_off    device int32 [n_seqs+1]: [0] = 0, not decreasing, [n_seqs] <= total_q;
  *            otherwise PRCR_ST_CSR and nothing is written
- *   seq_len  device int32 [n_seqs]; max_len >= every seq_len is a host bound
+ *   seq_len  device int32 [n_seqs]; max_len >= every seq_len is a host bound, at most
+ *            the cache's capacity and PRCR_CACHE_MAX_LEN
  *   out      device bf16: out[t*out_token_stride + h*D]; rows behind q_off[n_seqs]
  *            are left as they were. out must not overlap q
  * q and out are 16-byte aligned, their strides multiples of 8. Limits: D in {64,
- * 128, 256}, at most 8 query heads per KV head, n_q_heads * D <= PRCR_DECODE_MAX_Q_ELEMS.
+ * 128, 256}, at most 8 query heads per KV head, n_q_heads * D <= PRCR_DECODE_MAX_Q_ELEMS,
+ * total_q * n_q_heads < 2^31 (and CTAs of the launch: tiles of rows by KV heads by parts).
  * The rotated query and the probabilities are rounded to bf16 for the tensor
  * cores; sums, maxima and the output's accumulator are float32.
  * workspace: device, prcr_chunk_workspace_size(...) bytes are enough for every call
@@ -472,6 +479,8 @@ PRCR_API int prcr_chunk_attention(const prcr_rope_cfg* cfg, const prcr_cache_des
  *            are left as they were
  * Limits, a seq_len beyond the capacity or max_len, a q_pos of magnitude 2^31 or
  * more, and unmapped blocks are prcr_decode_attention's (such slots get weight 0).
+ * Beyond these, max_len is at most the cache's capacity and PRCR_CACHE_MAX_LEN, and n_layers *
+ * n_kv_heads at most 65535.
  * With max_len 0 nothing is done.
  * workspace: device, >= prcr_weights_workspace_size(...) bytes (0 for every max_len
  * up to 399,000 / query heads per KV head), 16-byte aligned, not shared with a
@@ -496,14 +505,17 @@ PRCR_API int prcr_accumulate_weights(const prcr_rope_cfg* cfg, const prcr_cache_
  *   dst         NULL: in place. Otherwise the cache that the kept rows are written to
  *               (other blocks of the same pool under their own table, or other
  *               memory); the rows read must not be among those written
- *   seq_len     device int32 [n_seqs]; max_len >= every seq_len is a host bound
+ *   seq_len     device int32 [n_seqs]; max_len >= every seq_len is a host bound, at
+ *               most the cache's capacity and PRCR_CACHE_MAX_LEN
  *   score       device float32 as for prcr_accumulate_weights (score_stride >= max_len)
  *   score_out   device, same layout; score itself or apart from it. Entries from the
  *               new length to score_stride become 0
  *   keep_out    device int32 [n_seqs][n_layers][n_kv_heads][budget]: the slots kept,
  *               ascending; -1 behind the new length
  *   seq_len_out device int32 [n_seqs]: min(seq_len, budget) (must not overlap seq_len)
- * Any head_dim. A block must not be mapped twice. A seq_len that is negative,
+ * Behind an eviction a slot is another token's in each KV head, so that
+ * prcr_select_topk_cached no longer applies to the cache (prcr_select_topk does).
+ * Any head_dim; n_seqs and n_layers at most 65535. A block must not be mapped twice. A seq_len that is negative,
  * beyond the capacity or max_len, a new length beyond dst's capacity, or an unmapped
  * block in either sets PRCR_ST_CAPACITY / PRCR_ST_NO_BLOCK, and that sequence is left as it was: its
  * keep_out is -1, seq_len_out is seq_len in place and 0 otherwise, rows and

@@ -199,3 +199,18 @@ def test_the_bars_of_large_logits_see_wrong_results(D, scale):
     fewer, _ = U.chunk64_exact(q, K[:256], V[:256], U.causal(20, 300, 256))
     with pytest.raises(AssertionError):
         U.assert_close(fewer, ref, bar)
+
+
+def test_documented_limits():
+    """The largest numbers of layers, sequences and rows that a launch holds, and one more."""
+    wide = dict(seq_stride=1 << 40, slot_stride=128)
+    layers = lambda n: dict(cfg=_cfg(H=2, L=n), cache=_flat(**wide))
+    assert call("prcr_accumulate_weights", **layers(32768)) == B.EINVAL  # 65536 layers by KV heads
+    assert call("prcr_evict", **layers(65536)) == B.EINVAL
+    many = _flat(n_seqs=70000)
+    assert call("prcr_accumulate_weights", cache=many, n_seqs=65536) == B.EINVAL
+    assert call("prcr_evict", cache=many, n_seqs=65536, len_out=FAKE + 2 ** 20) == B.EINVAL
+    for name in ("prcr_chunk_attention", "prcr_accumulate_weights", "prcr_evict"):  # max_len at most the capacity, and 2^30
+        assert call(name, max_len=257, **({} if name == "prcr_chunk_attention" else dict(ss=300))) == B.EINVAL
+        big = dict(cache=_paged(bt_stride=2 ** 30, n_blocks=2 ** 30), max_len=2 ** 30 + 1)
+        assert call(name, **big, **({} if name == "prcr_chunk_attention" else dict(ss=2 ** 31))) == B.EINVAL
