@@ -52,7 +52,8 @@ bool heads_ok(const prcr_rope_cfg* cfg, int32_t n_q_heads) {
 // rows, whose next tile's products do not wait for the last one's softmax, instead
 // of 256, which read the keys once. 16 sequences of up to 8198 slots, 8 heads of groups of 4:
 // of up to 6 tokens 64 us | 69, 24 tokens 77 | 87, 40 tokens 77 | 100, 64 tokens 79 |
-// 101, 100 tokens 120 | 100.
+// 101, 100 tokens 120 | 100. (Every sequence there has new tokens. One without counts too,
+// as the offsets are on the device: it lowers the average, and its item's CTAs end at once.)
 //
 // splits: as many as give every SM a CTA. Few rows are bound by the keys' and values'
 // bytes, and their partials are small: where that is below 4, it is rounded up, and a

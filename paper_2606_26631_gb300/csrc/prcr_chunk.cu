@@ -36,14 +36,14 @@
 // 256 rows about 2600 clocks, 2048 of them matrix instructions, the rest the
 // hand-overs between softmax and products; a CTA's start and end (its place in the
 // batch, the queries' angles, the last products and the results' way out) about 17,000.
-// One prompt of 8192 tokens, 32 heads of 128 over 8: 366 us, 1.52 PFLOP/s, 0.79 of a
+// One prompt of 8192 tokens, 32 heads of 128 over 8: 390 us, 1.43 PFLOP/s, 0.75 of a
 // library product's rate; 1024 tokens each of four sequences of up to 16,384 slots:
-// 382 us, 1.63 PFLOP/s; six prompts of up to 2116 tokens, few tiles per CTA: 152 us, 0.73
-// PFLOP/s; head_dim 256 (half as many rows per CTA), 1500 tokens each of two sequences of up to 3500
-// slots: 175 us, 0.98 PFLOP/s.
+// 416 us, 1.50 PFLOP/s (in a row, with queries in L2, 366 and 382); six prompts of up to
+// 2116 tokens, few tiles per CTA: 150 us, 0.74 PFLOP/s; head_dim 256 (half as many rows per
+// CTA), 1500 tokens each of two sequences of up to 3500 slots: 175 us, 0.98 PFLOP/s.
 // With few rows the keys' and values' bytes: 6 tokens each of 16 sequences of up to
 // 8198 slots 63 us, 5.1 TB/s (69 with NQ = 2); one token over 933 slots 12 us, all latency.
-// Tiles and roles that were slower (that prompt, then at 375 to 430 us, unless said): CTAs that
+// Tiles and roles that were slower (that prompt in a row, then at 375 to 430 us, unless said): CTAs that
 // stay and take runs of tiles 450 us, or whole units 490; queries in tensor memory with
 // tiles of 64 slots 533; a thread of matrix instructions for each half, whose softmaxes
 // then fall into step, 3970 clocks a tile; rows by TMA in boxes of 16 slots (a block of
@@ -501,7 +501,7 @@ __global__ void __launch_bounds__(ChunkShape<D, NQ>::kThreads, 1) chunk_kernel(c
                 const float mu = m_run == -INFINITY ? 0.0f : m_run;
                 const uint64_t c2 = pair64(scale, scale), m2 = pair64(-mu, -mu);
                 // (three chains of sums: two leave the additions' latency on the way to the products,
-                // one prompt of 8192 tokens 376 us for 366; four 368, eight 375)
+                // one prompt of 8192 tokens 376 us for 366, calls in a row; four 368, eight 375)
                 uint64_t sums[3] = {};
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {

@@ -18,7 +18,7 @@
 // head_dim 128) in flight behind the one in use; two CTAs of 8 warps fit an SM (6
 // warps with three tiles each in flight were slower, and so was an L2 prefetch of the first
 // slots beside the queries' angles). Measured with 8 heads of 128 in groups of 4, 36 layers:
-// 16 sequences of up to 4096 slots 520 us, 5.5 TB/s; one of 933 slots 18.5 us,
+// 16 sequences of up to 4096 slots 515 us, 5.6 TB/s; one of 933 slots 18.5 us,
 // 3.9 TB/s: one wave, whose first rows wait for the queries and whose last for the sums.
 // Where the logits of a sequence do not fit a cluster's shared memory (above 399,360 / group
 // slots at head_dim 256, 417,792 at 64), they go through the workspace instead
