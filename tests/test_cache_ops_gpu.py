@@ -1071,3 +1071,28 @@ def test_layer_by_layer_as_a_decoder_runs():
                 at += n
         assert [int(x) for x in after] == [int(x) + n for x, n in zip(length, new)]
         length = after
+
+
+@pytest.mark.parametrize("H,g,D,block,new,lens", [
+    (8, 4, 128, 16, [2600], [2600]), (8, 4, 128, 64, [300, 2300], [5000, 2300]), (4, 7, 128, 0, [900, 0, 1, 333], [900, 5, 4000, 1333]),
+    (2, 8, 256, 16, [1000, 400], [1300, 400]), (8, 2, 64, 7, [1500, 20], [1500, 3000]), (8, 4, 128, 16, [6, 1, 0, 5] * 4, [8198, 2193, 20, 4100] * 4),
+    (4, 4, 64, 0, [40, 3], [9000, 4100]), (2, 1, 256, 16, [7], [20000]),
+], ids=str)
+def test_chunk_every_row_of_long_calls(H, g, D, block, new, lens):
+    """Every element of long calls, at position 0, against chunk64_exact's formula and bound (in float64 on the GPU)."""
+    c = Exact(H, g, D, new, lens, block, seed=21)
+    assert c.run().done() == 0
+    at = 0
+    for b, (n, S) in enumerate(zip(new, lens)):
+        sees = torch.from_numpy(U.causal(n, S, S)).to(DEV)
+        for h in range(H * g if n else 0):
+            K, V = (c.cache.rows(x, b, S)[c.layer, :, h // g].double() for x in (c.cache.k, c.cache.v))
+            q, got = c.q[at:at + n, h].double(), c.out[at:at + n, h].double()
+            w = torch.softmax((q @ K.T / D ** 0.5).masked_fill(~sees, float("-inf")), 1)
+            e = (D * 2.0 ** -23 * (q.abs() @ K.abs().T) / D ** 0.5).masked_fill(~sees, 0.0).amax(1, keepdim=True)
+            ref = w @ V
+            bar = (2.0 ** -8 * ref.abs() + (2.0 ** -8 * w + torch.expm1(2 * e) * torch.minimum(w, 1 - w)) @ V.abs()) * 1.001 + 1e-30
+            d = (got - ref).abs()
+            assert bool((d <= bar).all()), (b, h, float((d / bar).max()))
+            assert float(d.norm()) <= 2 * U.EXACT_NORM * float(ref.norm())  # (few elements in a short one: less of a mean)
+        at += n
