@@ -109,6 +109,10 @@ extern "C" {
 #define PRCR_CACHE_CONTIGUOUS 0
 #define PRCR_CACHE_PAGED      1
 
+/* Formats of a quantised cache */
+#define PRCR_QFMT_E4M3 0
+#define PRCR_QFMT_E2M1 1
+
 #define PRCR_MAX_HEAD_DIM 256
 #define PRCR_MAX_ROW_ELEMS 8192   /* n_kv_heads * head_dim */
 
@@ -163,6 +167,47 @@ typedef struct prcr_cache_desc {
     int32_t        max_slots;     /* contiguous only: slots per sequence              */
     int32_t        n_seqs;        /* sequences the cache / block table holds          */
 } prcr_cache_desc;
+
+/* A decoder cache held in 8 or 4 bits: for every slot, KV head and K / V a row of codes and
+ * powers of two that scale them. All strides are in bytes.
+ *   PRCR_QFMT_E4M3: a byte per dim, an E4M3 float (1 sign, 4 exponent bits of bias 7, 3 mantissa
+ *     bits; largest 448, 0x7f and 0xff NaN); one scale per row. Any head_dim.
+ *   PRCR_QFMT_E2M1: four bits per dim, dim 2i in the low half of byte i (1 sign, 2
+ *     exponent bits, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6); a scale for each of D/32
+ *     groups of 32 dims, group j the dims d with (d / 4) % (D/32) = j. head_dim 64, 128 or 256.
+ *   A scale is a byte s and stands for 2^(s - 127); 255 makes its group NaN. Calls that write
+ *   choose the least s >= 10 for which the group's largest magnitude is at most 448 (6)
+ *   times it, and for each value the nearest code (ties to the even one; where that would
+ *   stand for 2^128, the one below). What such a code stands for is exact in bf16, and quantising
+ *   it again gives the same. A group with an infinity or a NaN gets codes 0 and scale 255.
+ * CONTIGUOUS: codes of (b, l, slot s, head h) at k[b*seq_stride + l*layer_stride +
+ *   s*slot_stride + h*R], R = D or D/2, its n = 1 or D/32 scales at k_scale[b*scale_seq_stride
+ *   + l*scale_layer_stride + s*scale_slot_stride + h*n].
+ * PAGED: as in prcr_cache_desc, with block_stride and scale_block_stride.
+ * k, v and the strides of codes are multiples of 16, scales' addresses and strides of n. */
+typedef struct prcr_qcache_desc {
+    int32_t        format;        /* PRCR_QFMT_*                                      */
+    int32_t        kind;          /* PRCR_CACHE_*                                     */
+    void*          k;             /* device, codes                                    */
+    void*          v;             /* device, codes                                    */
+    uint8_t*       k_scale;       /* device                                           */
+    uint8_t*       v_scale;       /* device                                           */
+    int64_t        seq_stride;    /* contiguous only                                  */
+    int64_t        layer_stride;
+    int64_t        block_stride;  /* paged only                                       */
+    int64_t        slot_stride;
+    int64_t        scale_seq_stride;
+    int64_t        scale_layer_stride;
+    int64_t        scale_block_stride;
+    int64_t        scale_slot_stride;
+    const int32_t* block_table;   /* paged only, device int32 [n_seqs][bt_stride]     */
+    int32_t        bt_stride;     /* paged only                                       */
+    int32_t        block_size;    /* paged only                                       */
+    int32_t        n_blocks;      /* paged only                                       */
+    int32_t        max_slots;     /* contiguous only                                  */
+    int32_t        n_seqs;
+    int32_t        reserved;      /* must be 0                                        */
+} prcr_qcache_desc;
 
 /* One decode step's revisits (Algorithm 1, Require line): for each sequence
  * b, revisits seq_rev_off[b] .. seq_rev_off[b+1]-1; revisit r selects the
@@ -398,7 +443,7 @@ PRCR_API int prcr_select_topk_cached(const prcr_rope_cfg* cfg, const prcr_cache_
                                      uint32_t* status, void* workspace, size_t workspace_bytes,
                                      void* stream);
 
-/* Longest max_len of the four entry points below. */
+/* Longest max_len of the entry points below. */
 #define PRCR_CACHE_MAX_LEN (1 << 30)
 
 /* prcr_append_kv - the K/V rows of new tokens that have no raw store (text
@@ -525,6 +570,68 @@ PRCR_API int prcr_evict(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache,
                         int64_t max_len, int32_t budget, int32_t n_sink, int32_t n_recent,
                         const float* score, float* score_out, int64_t score_stride,
                         int32_t* keep_out, int32_t* seq_len_out, uint32_t* status, void* stream);
+
+/* prcr_append_kv_quant - prcr_append_kv into a quantised cache: keys rotated as there (in
+ * float32, not rounded to bf16 in between) and values, rounded to the cache's format. Arguments,
+ * checks, status bits and what is skipped are prcr_append_kv's.                   */
+PRCR_API int prcr_append_kv_quant(const prcr_rope_cfg* cfg, const prcr_qcache_desc* cache,
+                                  int32_t n_seqs, int32_t layer_begin, int32_t n_layers,
+                                  const void* k_src, const void* v_src, int64_t src_layer_stride,
+                                  int64_t src_token_stride, const int32_t* coords,
+                                  const int32_t* tok_off, int32_t total,
+                                  const int32_t* cache_len_in, int32_t* cache_len_out,
+                                  uint32_t* status, void* stream);
+
+/* prcr_quantize_cache - slots of a bf16 cache into a quantised one (rows that
+ * prcr_prefill_capture, prcr_rebind_inject or prcr_evict wrote): slot src_begin[b] + i of
+ * sequence b, layer src_layer + j, goes to slot dst_begin[b] + i, layer dst_layer + j, for i <
+ * count[b] and j < n_layers, keys and values alike.
+ * prcr_dequantize_cache - the same slots back, as bf16, which holds them exactly (for
+ * prcr_chunk_attention, prcr_select_topk_cached, prcr_accumulate_weights or prcr_evict). Scales
+ * that no call here writes (below 10) may make values that bf16 does not hold: they are rounded.
+ *   src_begin, dst_begin, count   device int32 [n_seqs]
+ *   max_count                     >= every count: a host bound, at most PRCR_CACHE_MAX_LEN
+ * Any head_dim that the format has; n_seqs at most 65535. A count that is negative or above
+ * max_count, a negative begin or a slot beyond the capacity sets PRCR_ST_CAPACITY, an unmapped
+ * block PRCR_ST_NO_BLOCK, in either cache; those rows (of a count above max_count, the ones past
+ * it) are skipped, and what they would have been written to is left as it was. The caches
+ * must not overlap; a block that is written must not be mapped twice.              */
+PRCR_API int prcr_quantize_cache(const prcr_rope_cfg* cfg, const prcr_cache_desc* src,
+                                 int32_t src_layer, const prcr_qcache_desc* dst, int32_t dst_layer,
+                                 int32_t n_layers, int32_t n_seqs, const int32_t* src_begin,
+                                 const int32_t* dst_begin, const int32_t* count, int32_t max_count,
+                                 uint32_t* status, void* stream);
+PRCR_API int prcr_dequantize_cache(const prcr_rope_cfg* cfg, const prcr_qcache_desc* src,
+                                   int32_t src_layer, const prcr_cache_desc* dst, int32_t dst_layer,
+                                   int32_t n_layers, int32_t n_seqs, const int32_t* src_begin,
+                                   const int32_t* dst_begin, const int32_t* count,
+                                   int32_t max_count, uint32_t* status, void* stream);
+
+/* prcr_decode_attention_quant - prcr_decode_attention over a quantised cache, at layers
+ * layer_begin .. layer_begin+n_layers-1:
+ *   out[b][i][h] = softmax(RoPE(q[b][i][h], (p, p, p)) K^T / sqrt(D)) V,  layer layer_begin + i,
+ * p = q_pos[b], over slots [0, seq_len[b]), K and V what their codes stand for.
+ *   q        device bf16 [n_seqs][n_layers][n_q_heads][D] raw (pre-rotation), 4-byte aligned
+ *   out      device float32, the same shape, 16-byte aligned; must not overlap q
+ *   q_pos, seq_len, max_len, status as in prcr_decode_attention; max_len at most the cache's
+ *            capacity and PRCR_CACHE_MAX_LEN
+ * The rotated query and the weights enter the tensor cores as two fp16 each (22 bits); codes are
+ * exact there, sums, maxima and the output float32.
+ * Limits: D in {64, 128, 256}, at most 8 query heads per KV head, n_q_heads * D <=
+ * PRCR_DECODE_MAX_Q_ELEMS, and below 2^31 CTAs (sequences by layers by KV heads by splits).
+ * workspace: device, >= prcr_decode_quant_workspace_size(...) bytes (0 where the slots are not
+ * split), 16-byte aligned, not shared with a concurrent call.
+ * Status bits and what is left out are prcr_decode_attention's (slots past max_len are left
+ * out); a sequence that reads no slot gets zeros, with max_len 0 all of them.       */
+PRCR_API size_t prcr_decode_quant_workspace_size(const prcr_rope_cfg* cfg, int32_t format,
+                                                 int32_t n_seqs, int32_t n_layers,
+                                                 int32_t n_q_heads, int64_t max_len);
+PRCR_API int prcr_decode_attention_quant(const prcr_rope_cfg* cfg, const prcr_qcache_desc* cache,
+                                         int32_t n_seqs, int32_t layer_begin, int32_t n_layers,
+                                         int32_t n_q_heads, const void* q, const int64_t* q_pos,
+                                         const int32_t* seq_len, int64_t max_len, float* out,
+                                         uint32_t* status, void* workspace, size_t workspace_bytes,
+                                         void* stream);
 
 /* prcr_next_text_pos - host helper: the position the next text token takes
  * after a revisit appended k_seq tokens to a sequence whose latest text token

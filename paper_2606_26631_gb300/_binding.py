@@ -23,6 +23,7 @@ MODE_PCR, MODE_ORIGINAL, MODE_UIR, MODE_LPA = 0, 1, 2, 3
 FLAG_DEGENERATE_CENTER = 1
 LAYOUT_SECTIONED, LAYOUT_INTERLEAVED = 0, 1
 CACHE_CONTIGUOUS, CACHE_PAGED = 0, 1
+QFMT_E4M3, QFMT_E2M1 = 0, 1
 
 EXPORTS = ("prcr_workspace_size", "prcr_rebind_inject", "prcr_plan", "prcr_rebind_apply",
            "prcr_store_raw", "prcr_next_text_pos", "prcr_error_string", "prcr_version",
@@ -30,7 +31,8 @@ EXPORTS = ("prcr_workspace_size", "prcr_rebind_inject", "prcr_plan", "prcr_rebin
            "prcr_decode_attention", "prcr_select_workspace_size", "prcr_select_topk",
            "prcr_select_topk_cached", "prcr_append_kv", "prcr_chunk_workspace_size",
            "prcr_chunk_attention", "prcr_weights_workspace_size", "prcr_accumulate_weights",
-           "prcr_evict")
+           "prcr_evict", "prcr_append_kv_quant", "prcr_quantize_cache", "prcr_dequantize_cache",
+           "prcr_decode_quant_workspace_size", "prcr_decode_attention_quant")
 STATIC_MAX_TOKENS = 65536
 
 
@@ -53,6 +55,17 @@ class CacheDesc(C.Structure):
                 ("block_stride", C.c_int64), ("slot_stride", C.c_int64),
                 ("block_table", C.c_void_p), ("bt_stride", C.c_int32), ("n_blocks", C.c_int32),
                 ("max_slots", C.c_int32), ("n_seqs", C.c_int32)]
+
+
+class QCacheDesc(C.Structure):
+    _fields_ = [("format", C.c_int32), ("kind", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("seq_stride", C.c_int64),
+                ("layer_stride", C.c_int64), ("block_stride", C.c_int64), ("slot_stride", C.c_int64),
+                ("scale_seq_stride", C.c_int64), ("scale_layer_stride", C.c_int64),
+                ("scale_block_stride", C.c_int64), ("scale_slot_stride", C.c_int64),
+                ("block_table", C.c_void_p), ("bt_stride", C.c_int32), ("block_size", C.c_int32),
+                ("n_blocks", C.c_int32), ("max_slots", C.c_int32), ("n_seqs", C.c_int32),
+                ("reserved", C.c_int32)]
 
 
 class RevisitBatch(C.Structure):
@@ -138,6 +151,22 @@ def lib():
                              C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
                              C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
     L.prcr_evict.restype = C.c_int
+    L.prcr_append_kv_quant.argtypes = [P(RopeCfg), P(QCacheDesc)] + L.prcr_append_kv.argtypes[2:]
+    L.prcr_append_kv_quant.restype = C.c_int
+    rows = [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+            C.c_void_p]
+    L.prcr_quantize_cache.argtypes = [P(RopeCfg), P(CacheDesc), C.c_int32, P(QCacheDesc), C.c_int32] + rows
+    L.prcr_quantize_cache.restype = C.c_int
+    L.prcr_dequantize_cache.argtypes = [P(RopeCfg), P(QCacheDesc), C.c_int32, P(CacheDesc), C.c_int32] + rows
+    L.prcr_dequantize_cache.restype = C.c_int
+    L.prcr_decode_quant_workspace_size.argtypes = [P(RopeCfg), C.c_int32, C.c_int32, C.c_int32,
+                                                   C.c_int32, C.c_int64]
+    L.prcr_decode_quant_workspace_size.restype = C.c_size_t
+    L.prcr_decode_attention_quant.argtypes = [P(RopeCfg), P(QCacheDesc), C.c_int32, C.c_int32,
+                                              C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                              C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                              C.c_void_p, C.c_size_t, C.c_void_p]
+    L.prcr_decode_attention_quant.restype = C.c_int
     L.prcr_next_text_pos.argtypes = [C.c_int64, C.c_int64, C.c_int32]
     L.prcr_next_text_pos.restype = C.c_int64
     L.prcr_error_string.argtypes = [C.c_int]
@@ -248,6 +277,70 @@ def cache_paged(k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor) -> 
     d.block_table, d.bt_stride = block_table.data_ptr(), block_table.stride(0)
     d.n_blocks, d.max_slots, d.n_seqs = k.shape[1], 0, block_table.shape[0]
     d._keep, d._rows = (k, v, block_table), (k.shape[0], k.shape[3], k.shape[4])
+    return d
+
+
+def _codes(k, v, k_scale, v_scale):
+    """The format, head_dim and the checks of a quantised cache's tensors."""
+    if k.dtype not in (torch.float8_e4m3fn, torch.uint8):
+        raise TypeError("codes must be float8_e4m3fn, or uint8 for pairs of 4-bit codes")
+    fmt = QFMT_E4M3 if k.dtype == torch.float8_e4m3fn else QFMT_E2M1
+    if v.dtype != k.dtype or k_scale.dtype != torch.uint8 or v_scale.dtype != torch.uint8:
+        raise TypeError("k and v must be of one type, k_scale and v_scale uint8")
+    if k.dim() != 5 or k_scale.dim() != 5:
+        raise ValueError("codes and scales must have 5 dimensions")
+    if k.shape != v.shape or k.stride() != v.stride() or k_scale.shape != v_scale.shape or k_scale.stride() != v_scale.stride():
+        raise ValueError("k and v, and k_scale and v_scale, must have the same shape and strides")
+    heads, width = k.shape[3:]
+    dim, n = (width, 1) if fmt == QFMT_E4M3 else (2 * width, width // 16)
+    if k_scale.shape != k.shape[:4] + (n,):
+        raise ValueError(f"scales must be {list(k.shape[:4])} x {n}")
+    for name, t in (("codes", k), ("scales", k_scale)):
+        if (t.shape[4] > 1 and t.stride(4) != 1) or (heads > 1 and t.stride(3) != t.shape[4]):
+            raise ValueError(f"{name}: a slot's heads must be contiguous")
+    index = k.get_device()
+    if any(t.get_device() != index for t in (v, k_scale, v_scale)):
+        raise ValueError("codes and scales must be on one device")
+    return fmt, dim, heads
+
+
+def _qcache(k, v, k_scale, v_scale, rows) -> QCacheDesc:
+    fmt, dim, heads = _codes(k, v, k_scale, v_scale)
+    d = QCacheDesc()
+    d.format, d.reserved = fmt, 0
+    d.k, d.v, d.k_scale, d.v_scale = k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr()
+    d._rows = (k.shape[rows], heads, dim)
+    return d
+
+
+def qcache_contiguous(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor,
+                      v_scale: torch.Tensor) -> QCacheDesc:
+    """k, v: [B, n_L, S, H, D] float8_e4m3fn with scales [B, n_L, S, H, 1] uint8, or [B, n_L, S, H,
+    D/2] uint8 with scales [B, n_L, S, H, D/32] uint8."""
+    d = _qcache(k, v, k_scale, v_scale, 1)
+    d.kind, d.block_size = CACHE_CONTIGUOUS, 1
+    d.seq_stride, d.layer_stride, d.slot_stride = _strides(k, 5, "k")[:3]
+    d.scale_seq_stride, d.scale_layer_stride, d.scale_slot_stride = _strides(k_scale, 5, "k_scale")[:3]
+    d.block_stride, d.scale_block_stride, d.block_table, d.bt_stride, d.n_blocks = 0, 0, None, 0, 0
+    d.max_slots, d.n_seqs = k.shape[2], k.shape[0]
+    d._keep = (k, v, k_scale, v_scale)
+    return d
+
+
+def qcache_paged(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                 block_table: torch.Tensor) -> QCacheDesc:
+    """k, v: [n_L, n_blocks, block_size, H, D] float8_e4m3fn (or D/2 uint8), scales as for
+    qcache_contiguous; block_table: [B, max_blocks] int32."""
+    if block_table.dtype != torch.int32 or block_table.stride(-1) != 1:
+        raise ValueError("block_table must be int32 [B, max_blocks] with contiguous rows")
+    d = _qcache(k, v, k_scale, v_scale, 0)
+    d.kind, d.block_size = CACHE_PAGED, k.shape[2]
+    d.layer_stride, d.block_stride, d.slot_stride = _strides(k, 5, "k")[:3]
+    d.scale_layer_stride, d.scale_block_stride, d.scale_slot_stride = _strides(k_scale, 5, "k_scale")[:3]
+    d.seq_stride, d.scale_seq_stride, d.max_slots = 0, 0, 0
+    d.block_table, d.bt_stride = block_table.data_ptr(), block_table.stride(0)
+    d.n_blocks, d.n_seqs = k.shape[1], block_table.shape[0]
+    d._keep = (k, v, k_scale, v_scale, block_table)
     return d
 
 
@@ -465,12 +558,8 @@ def _same_device(first: torch.Tensor, *others):
         raise ValueError(f"tensors are on {first.device}, which is not the current CUDA device")
 
 
-def append_kv(cfg, cache, layer_begin: int, k_src: torch.Tensor, v_src: torch.Tensor,
-              coords: torch.Tensor, tok_off: torch.Tensor, cache_len_in: torch.Tensor,
-              cache_len_out: torch.Tensor, status: torch.Tensor, stream=None):
-    """prcr_append_kv: k_src / v_src are the new tokens' pre-rotation rows [n_layers, total, H, D]
-    bf16 (row-contiguous), coords int32 [total, 3], tok_off int32 [B + 1], cache_len_in /
-    cache_len_out int32 [B]."""
+def _append(name: str, cfg, cache, layer_begin: int, k_src, v_src, coords, tok_off, cache_len_in,
+            cache_len_out, status, stream):
     _bf16(k_src, "k_src"); _bf16(v_src, "v_src")
     stride, (nl, total, heads, dim) = _strides(k_src, 4, "k_src"), k_src.shape
     if k_src.shape != v_src.shape or stride != _strides(v_src, 4, "v_src"):
@@ -484,12 +573,22 @@ def append_kv(cfg, cache, layer_begin: int, k_src: torch.Tensor, v_src: torch.Te
     _small("cache_len_in", cache_len_in, torch.int32, 0)
     _small("cache_len_out", cache_len_out, torch.int32, n_seqs)
     _same_device(cache._keep[0], k_src, v_src, coords, tok_off, cache_len_in, cache_len_out, status)
-    rc = lib().prcr_append_kv(C.byref(cfg), C.byref(cache), n_seqs, int(layer_begin), nl,
+    rc = getattr(lib(), name)(C.byref(cfg), C.byref(cache), n_seqs, int(layer_begin), nl,
                               k_src.data_ptr(), v_src.data_ptr(), stride[0], stride[1],
                               coords.data_ptr(), tok_off.data_ptr(), total,
                               cache_len_in.data_ptr(), cache_len_out.data_ptr(), status.data_ptr(),
                               _stream(stream))
-    return _check(rc, "prcr_append_kv")
+    return _check(rc, name)
+
+
+def append_kv(cfg, cache, layer_begin: int, k_src: torch.Tensor, v_src: torch.Tensor,
+              coords: torch.Tensor, tok_off: torch.Tensor, cache_len_in: torch.Tensor,
+              cache_len_out: torch.Tensor, status: torch.Tensor, stream=None):
+    """prcr_append_kv: k_src / v_src are the new tokens' pre-rotation rows [n_layers, total, H, D]
+    bf16 (row-contiguous), coords int32 [total, 3], tok_off int32 [B + 1], cache_len_in /
+    cache_len_out int32 [B]."""
+    return _append("prcr_append_kv", cfg, cache, layer_begin, k_src, v_src, coords, tok_off,
+                   cache_len_in, cache_len_out, status, stream)
 
 
 def chunk_workspace_size(cfg, n_seqs: int, n_q_heads: int, total_q: int, max_len: int) -> int:
@@ -586,6 +685,83 @@ def evict(cfg, cache, seq_len: torch.Tensor, max_len: int, budget: int, n_sink: 
                           keep_out.data_ptr(), seq_len_out.data_ptr(), status.data_ptr(),
                           _stream(stream))
     return _check(rc, "prcr_evict")
+
+
+def append_kv_quant(cfg, cache: QCacheDesc, layer_begin: int, k_src: torch.Tensor,
+                    v_src: torch.Tensor, coords: torch.Tensor, tok_off: torch.Tensor,
+                    cache_len_in: torch.Tensor, cache_len_out: torch.Tensor, status: torch.Tensor,
+                    stream=None):
+    """prcr_append_kv_quant: append_kv into a quantised cache (qcache_contiguous, qcache_paged)."""
+    return _append("prcr_append_kv_quant", cfg, cache, layer_begin, k_src, v_src, coords, tok_off,
+                   cache_len_in, cache_len_out, status, stream)
+
+
+def _cast(name: str, cfg, src, src_layer, dst, dst_layer, n_layers, src_begin, dst_begin, count,
+          max_count, status, stream):
+    _cache_rows(cfg, src, src_layer + n_layers)
+    _cache_rows(cfg, dst, dst_layer + n_layers)
+    n_seqs = count.numel()
+    _small("src_begin", src_begin, torch.int32, n_seqs)
+    _small("dst_begin", dst_begin, torch.int32, n_seqs)
+    _small("count", count, torch.int32, 0)
+    _same_device(src._keep[0], dst._keep[0], src_begin, dst_begin, count, status)
+    rc = getattr(lib(), name)(C.byref(cfg), C.byref(src), int(src_layer), C.byref(dst), int(dst_layer),
+                              int(n_layers), n_seqs, src_begin.data_ptr(), dst_begin.data_ptr(),
+                              count.data_ptr(), int(max_count), status.data_ptr(), _stream(stream))
+    return _check(rc, name)
+
+
+def quantize_cache(cfg, src: CacheDesc, src_layer: int, dst: QCacheDesc, dst_layer: int,
+                   n_layers: int, src_begin: torch.Tensor, dst_begin: torch.Tensor,
+                   count: torch.Tensor, max_count: int, status: torch.Tensor, stream=None):
+    """prcr_quantize_cache: slots src_begin[b] .. + count[b] of the bf16 cache src to slots
+    dst_begin[b] .. of dst (int32 [B] each; max_count >= every count)."""
+    if not isinstance(src, CacheDesc) or not isinstance(dst, QCacheDesc):
+        raise TypeError("src must be a bf16 cache and dst a quantised one")
+    return _cast("prcr_quantize_cache", cfg, src, src_layer, dst, dst_layer, n_layers, src_begin,
+                 dst_begin, count, max_count, status, stream)
+
+
+def dequantize_cache(cfg, src: QCacheDesc, src_layer: int, dst: CacheDesc, dst_layer: int,
+                     n_layers: int, src_begin: torch.Tensor, dst_begin: torch.Tensor,
+                     count: torch.Tensor, max_count: int, status: torch.Tensor, stream=None):
+    """prcr_dequantize_cache: quantize_cache's slots back, as bf16."""
+    if not isinstance(src, QCacheDesc) or not isinstance(dst, CacheDesc):
+        raise TypeError("src must be a quantised cache and dst a bf16 one")
+    return _cast("prcr_dequantize_cache", cfg, src, src_layer, dst, dst_layer, n_layers, src_begin,
+                 dst_begin, count, max_count, status, stream)
+
+
+def decode_quant_workspace_size(cfg, cache: QCacheDesc, n_seqs: int, n_layers: int, n_q_heads: int,
+                                max_len: int) -> int:
+    return int(lib().prcr_decode_quant_workspace_size(C.byref(cfg), cache.format, int(n_seqs),
+                                                      int(n_layers), int(n_q_heads), int(max_len)))
+
+
+def decode_attention_quant(cfg, cache: QCacheDesc, layer_begin: int, q: torch.Tensor,
+                           q_pos: torch.Tensor, seq_len: torch.Tensor, max_len: int,
+                           out: torch.Tensor, status: torch.Tensor,
+                           workspace: Optional[torch.Tensor] = None, stream=None):
+    """prcr_decode_attention_quant: q [B, n, Hq, D] bf16 (contiguous) for layers layer_begin ..
+    layer_begin + n - 1, q_pos int64 [B], seq_len int32 [B], out float32 shaped like q."""
+    if q.dtype != torch.bfloat16 or not q.is_contiguous() or q.dim() != 4:
+        raise TypeError("q must be a contiguous bfloat16 [B, n_layers, Hq, D] tensor")
+    if out.dtype != torch.float32 or not out.is_contiguous() or out.shape != q.shape:
+        raise TypeError("out must be a contiguous float32 tensor shaped like q")
+    n_seqs, layers, heads, dim = q.shape
+    if dim != cfg.head_dim:
+        raise ValueError("q must be [B, n_layers, Hq, head_dim]")
+    _cache_rows(cfg, cache, layer_begin + layers)
+    _small("q_pos", q_pos, torch.int64, n_seqs)
+    _small("seq_len", seq_len, torch.int32, n_seqs)
+    _same_device(cache._keep[0], q, q_pos, seq_len, out, status, workspace)
+    ws = None if workspace is None else workspace.data_ptr()
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = lib().prcr_decode_attention_quant(C.byref(cfg), C.byref(cache), n_seqs, int(layer_begin),
+                                           layers, heads, q.data_ptr(), q_pos.data_ptr(),
+                                           seq_len.data_ptr(), int(max_len), out.data_ptr(),
+                                           status.data_ptr(), ws, nbytes, _stream(stream))
+    return _check(rc, "prcr_decode_attention_quant")
 
 
 def next_text_pos(p_txt: int, k_seq: int, mode: int = MODE_PCR) -> int:

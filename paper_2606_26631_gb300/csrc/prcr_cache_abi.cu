@@ -7,7 +7,6 @@
 #include "prcr_internal.h"
 
 namespace prcr {
-namespace {
 
 int64_t cache_capacity(const prcr_cache_desc* c) {
     return c->kind == PRCR_CACHE_CONTIGUOUS ? int64_t(c->max_slots) : int64_t(c->bt_stride) * c->block_size;
@@ -27,13 +26,17 @@ CacheView cache_view(const prcr_cache_desc* c, int layer) {
     v.block_size = c->kind == PRCR_CACHE_PAGED ? c->block_size : 1;
     v.n_blocks = c->n_blocks;
     v.kind = c->kind;
-    // m = ceil(2^(31 + k) / d) with 2^k >= d: m d exceeds 2^(31 + k) by less than 2^k,
-    // so that n m >> (31 + k) is n / d for every n below 2^31
-    int k = 0;
-    while ((int64_t(1) << k) < v.block_size) ++k;
-    v.div_mul = uint32_t(((uint64_t(1) << (31 + k)) + v.block_size - 1) / v.block_size);
-    v.div_shift = 31 + k;
+    fill_div(v.block_size, &v.div_mul, &v.div_shift);
     return v;
+}
+
+// m = ceil(2^(31 + k) / d) with 2^k >= d: m d exceeds 2^(31 + k) by less than 2^k,
+// so that n m >> (31 + k) is n / d for every n below 2^31
+void fill_div(int32_t block_size, uint32_t* mul, int32_t* shift) {
+    int k = 0;
+    while ((int64_t(1) << k) < block_size) ++k;
+    *mul = uint32_t(((uint64_t(1) << (31 + k)) + block_size - 1) / block_size);
+    *shift = 31 + k;
 }
 
 // query heads that the attention kernels take
@@ -43,6 +46,14 @@ bool heads_ok(const prcr_rope_cfg* cfg, int32_t n_q_heads) {
            n_q_heads % cfg->n_kv_heads == 0 && n_q_heads / cfg->n_kv_heads <= 8 &&
            int64_t(n_q_heads) * D <= PRCR_DECODE_MAX_Q_ELEMS;
 }
+
+// Whether two arrays of n lengths share an entry.
+bool overlap(const int32_t* a, const int32_t* b, int64_t n) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return (x < y ? y - x : x - y) < uintptr_t(n) * sizeof(int32_t);
+}
+
+namespace {
 
 // How a chunk call is cut into CTAs, one to an SM: units of the rows of a tile and a KV
 // head, and parts of the slots that a unit sees. (items: at most; the lengths are
@@ -131,12 +142,6 @@ int evict_cluster(const prcr_rope_cfg* cfg, int64_t n_seqs, int sms) {
     int c = 1;
     while (c < 8 && cfg->head_dim % (64 * c) == 0 && units * c * 2 <= 2 * int64_t(sms)) c *= 2;
     return c;
-}
-
-// Whether two arrays of n lengths share an entry.
-bool overlap(const int32_t* a, const int32_t* b, int64_t n) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return (x < y ? y - x : x - y) < uintptr_t(n) * sizeof(int32_t);
 }
 
 int status_of(cudaError_t e) { return e == cudaSuccess ? PRCR_OK : PRCR_ECUDA; }

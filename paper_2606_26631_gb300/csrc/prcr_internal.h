@@ -460,6 +460,107 @@ struct EvictArgs {
     int32_t cluster;            // CTAs of a (sequence, layer, KV head), a part of its rows' dims each
 };
 
+// A quantised cache as its kernels see it; strides are in bytes.
+struct QCacheView {
+    uint8_t* k;
+    uint8_t* v;
+    uint8_t* k_scale;
+    uint8_t* v_scale;
+    int64_t seq_stride;         // contiguous
+    int64_t layer_stride;
+    int64_t block_stride;       // paged
+    int64_t slot_stride;
+    int64_t scale_seq_stride;
+    int64_t scale_layer_stride;
+    int64_t scale_block_stride;
+    int64_t scale_slot_stride;
+    int64_t capacity;           // slots per sequence
+    const int32_t* block_table;
+    int32_t bt_stride;
+    int32_t block_size;         // 1 for a contiguous cache
+    int32_t n_blocks;
+    int32_t kind;
+    uint32_t div_mul;           // as in CacheView
+    int32_t div_shift;
+};
+
+struct AppendQuantArgs {
+    QCacheView cache;           // shifted to layer_begin
+    const uint16_t* src_k;
+    const uint16_t* src_v;
+    int64_t src_layer_stride;
+    int64_t src_token_stride;
+    const int32_t* coords;      // [total][3]
+    const int32_t* tok_off;     // [n_seqs + 1]
+    const int32_t* len_in;      // [n_seqs]
+    int32_t* len_out;           // [n_seqs]
+    uint32_t* status;
+    int32_t n_seqs;
+    int32_t total;
+    int32_t n_layers;
+    int32_t head_dim;
+    int32_t format;
+    int32_t n_scales;           // of a head's row
+    int32_t n_kv_heads;
+    int32_t pad;                // threads of a head: head_dim / 16, rounded up to a power of two
+    int32_t lanes;              // threads per token: those of the heads that a CTA takes
+    int32_t tok_per_cta;
+    int32_t layers_per_cta;
+    int32_t layout;
+    int32_t sec_t;
+    int32_t sec_h;
+    int32_t sec_w;
+    uint64_t turn_freq[kMaxPairs];
+};
+
+// Slots between a bf16 cache and a quantised one.
+struct CastArgs {
+    CacheView wide;             // both shifted to their first layer
+    QCacheView few;
+    const int32_t* src_begin;   // [n_seqs]
+    const int32_t* dst_begin;   // [n_seqs]
+    const int32_t* count;       // [n_seqs]
+    uint32_t* status;
+    int32_t max_count;
+    int32_t n_layers;
+    int32_t head_dim;
+    int32_t format;
+    int32_t n_scales;
+    int32_t pad;                // threads of a head: head_dim / 8 (quantising: rounded up to a power of two)
+    int32_t lanes;
+    int32_t units;              // lanes of the CTA's tokens (quantising: in whole warps)
+    int32_t tok_per_cta;
+    int32_t layers_per_cta;
+};
+
+struct DecodeQuantArgs {
+    QCacheView cache;           // shifted to layer_begin
+    const uint16_t* q;          // [B][n_layers][n_q_heads][D]
+    const int64_t* q_pos;       // [B]
+    const int32_t* seq_len;     // [B]
+    float* out;                 // [B][n_layers][n_q_heads][D]
+    float* partial;             // [B][n_layers][n_q_heads][splits][D + 2] when splits > 1
+    uint32_t* status;
+    int32_t n_seqs;
+    int32_t n_layers;
+    int32_t n_kv_heads;
+    int32_t group;
+    int32_t head_dim;
+    int32_t format;
+    int32_t warps;              // of a CTA
+    int32_t splits;
+    int32_t chunk;              // slots of a split
+    int32_t max_len;
+    float scale_log2;           // log2(e) / sqrt(head_dim)
+    uint64_t turn_freq[kMaxPairs];
+};
+
+cudaError_t launch_append_quant(const AppendQuantArgs& a, dim3 grid, int block, size_t smem, cudaStream_t stream);
+cudaError_t launch_quantize(const CastArgs& a, dim3 grid, cudaStream_t stream);
+cudaError_t launch_dequantize(const CastArgs& a, dim3 grid, cudaStream_t stream);
+cudaError_t launch_decode_quant(const DecodeQuantArgs& a, cudaStream_t stream);
+int decode_quant_tile(int format, int head_dim);  // slots that a warp takes at once
+
 cudaError_t append_blocks_per_sm(int block, size_t smem, int* out);
 cudaError_t launch_append(const AppendArgs& a, dim3 grid, int block, size_t smem, cudaStream_t stream);
 cudaError_t launch_chunk(const ChunkArgs& a, cudaStream_t stream);
@@ -494,6 +595,11 @@ inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3
 inline bool mult8(int64_t s) { return s >= 0 && (s & 7) == 0; }
 int check_cfg(const prcr_rope_cfg* c);
 int check_cache(const prcr_rope_cfg* c, const prcr_cache_desc* k);
+int64_t cache_capacity(const prcr_cache_desc* c);
+CacheView cache_view(const prcr_cache_desc* c, int layer);
+void fill_div(int32_t block_size, uint32_t* mul, int32_t* shift);  // of a view
+bool heads_ok(const prcr_rope_cfg* cfg, int32_t n_q_heads);        // query heads that the attention kernels take
+bool overlap(const int32_t* a, const int32_t* b, int64_t n);       // whether two arrays of n lengths share an entry
 void copy_turn_freq(const prcr_rope_cfg* cfg, uint64_t* out);
 int sm_count(int dev);
 enum KernelId { kRebind = 0, kCapture = 1, kFused = 2, kAppend = 3 };
