@@ -539,7 +539,8 @@ struct DecodeQuantArgs {
     const int64_t* q_pos;       // [B]
     const int32_t* seq_len;     // [B]
     float* out;                 // [B][n_layers][n_q_heads][D]
-    float* partial;             // [B][n_layers][n_q_heads][splits][D + 2] when splits > 1
+    float* partial;             // workspace [teams][2][team][group][D + 2]: a warp's parts of units shared with other teams
+    int64_t* tiles_before;      // workspace [B + 1]: tiles of a unit (layer, set of KV heads) of the sequences before
     uint32_t* status;
     int32_t n_seqs;
     int32_t n_layers;
@@ -547,9 +548,9 @@ struct DecodeQuantArgs {
     int32_t group;
     int32_t head_dim;
     int32_t format;
-    int32_t warps;              // of a CTA
-    int32_t splits;
-    int32_t chunk;              // slots of a split
+    int32_t team;               // warps that take the same slots of neighbouring KV heads: 1, 2 or 4
+    int32_t head_sets;          // n_kv_heads / team, rounded up
+    int32_t teams;              // that share the tiles, at most
     int32_t max_len;
     float scale_log2;           // log2(e) / sqrt(head_dim)
     uint64_t turn_freq[kMaxPairs];
@@ -559,7 +560,8 @@ cudaError_t launch_append_quant(const AppendQuantArgs& a, dim3 grid, int block, 
 cudaError_t launch_quantize(const CastArgs& a, dim3 grid, cudaStream_t stream);
 cudaError_t launch_dequantize(const CastArgs& a, dim3 grid, cudaStream_t stream);
 cudaError_t launch_decode_quant(const DecodeQuantArgs& a, cudaStream_t stream);
-int decode_quant_tile(int format, int head_dim);  // slots that a warp takes at once
+int decode_quant_tile(int format, int head_dim);  // slots of a warp's tile
+constexpr int decode_quant_warps(int head_dim) { return head_dim == 256 ? 8 : 16; }  // that an SM's registers hold
 
 cudaError_t append_blocks_per_sm(int block, size_t smem, int* out);
 cudaError_t launch_append(const AppendArgs& a, dim3 grid, int block, size_t smem, cudaStream_t stream);

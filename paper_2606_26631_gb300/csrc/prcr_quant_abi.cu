@@ -81,30 +81,25 @@ int layers_per_cta(int64_t tiles, int n_layers, int64_t ctas, int most) {
     return (n_layers + groups - 1) / groups;
 }
 
-// How a decode step is cut into CTAs of `warps` warps: a (sequence, layer, KV head) and a
-// chunk of its slots each.
-struct DecodeQuantSplit {
-    int warps, chunk;
-    int64_t splits;
+// How a decode step's warps take its tiles: teams of warps with the same slots of as many neighbouring KV heads, as
+// many teams as the SMs hold, unless there are fewer tiles.
+struct DecodeQuantTeams {
+    int team, head_sets;
+    int64_t teams;
 };
-DecodeQuantSplit decode_quant_split(int format, int head_dim, int64_t units, int64_t max_len, int sms) {
-    DecodeQuantSplit s;
+DecodeQuantTeams decode_quant_teams(int format, int head_dim, int n_kv_heads, int64_t seq_layers, int64_t max_len, int sms) {
+    DecodeQuantTeams s;
+    const int row = format == PRCR_QFMT_E4M3 ? head_dim : head_dim / 2;
+    s.team = n_kv_heads % 4 == 0 ? 4 : n_kv_heads % 2 == 0 || (row < 128 && n_kv_heads > 1) ? 2 : 1;
+    s.head_sets = (n_kv_heads + s.team - 1) / s.team;
     const int64_t tile = decode_quant_tile(format, head_dim), tiles = std::max<int64_t>(1, (max_len + tile - 1) / tile);
-    const int per_sm = head_dim == 256 ? 8 : 16;  // warps
-    s.warps = 4;
-    const int64_t slots = int64_t(sms) * (per_sm / s.warps);
-    int64_t splits = std::max<int64_t>(1, slots / units);
-    splits = std::min(splits, (tiles + 2 * s.warps - 1) / (2 * s.warps));
-    const int64_t longest = 4096;
-    splits = std::max(splits, (max_len + longest - 1) / longest);
-    const int64_t per = (tiles + splits - 1) / splits;
-    s.chunk = int(per * tile);
-    s.splits = std::max<int64_t>(1, (tiles + per - 1) / per);
+    const int64_t units = seq_layers * s.head_sets, most = int64_t(sms) * decode_quant_warps(head_dim) / s.team;
+    s.teams = units > most / tiles ? most : units * tiles;
     return s;
 }
 
-size_t decode_quant_bytes(int64_t heads, int64_t splits, int head_dim) {
-    return splits > 1 ? size_t(heads) * splits * (head_dim + 2) * sizeof(float) : 0;
+size_t decode_quant_parts(const DecodeQuantTeams& s, int group, int head_dim) {
+    return align256(size_t(s.teams) * 2 * s.team * group * (head_dim + 2) * sizeof(float));
 }
 
 // Fills what both directions share; *go is false where nothing is to be done.
@@ -236,14 +231,13 @@ int prcr_dequantize_cache(const prcr_rope_cfg* cfg, const prcr_qcache_desc* src,
 
 size_t prcr_decode_quant_workspace_size(const prcr_rope_cfg* cfg, int32_t format, int32_t n_seqs, int32_t n_layers, int32_t n_q_heads,
                                         int64_t max_len) {
-    if (check_cfg(cfg) || n_seqs < 1 || n_layers < 1 || max_len < 1 || max_len > PRCR_CACHE_MAX_LEN || !heads_ok(cfg, n_q_heads) ||
+    if (check_cfg(cfg) || n_seqs < 1 || n_layers < 1 || max_len < 0 || max_len > PRCR_CACHE_MAX_LEN || !heads_ok(cfg, n_q_heads) ||
         (format != PRCR_QFMT_E4M3 && format != PRCR_QFMT_E2M1))
         return 0;
     int dev = 0, sms = 1;
     if (cudaGetDevice(&dev) == cudaSuccess) sms = sm_count(dev);
-    const int64_t units = int64_t(n_seqs) * n_layers * cfg->n_kv_heads;
-    return decode_quant_bytes(int64_t(n_seqs) * n_layers * n_q_heads, decode_quant_split(format, cfg->head_dim, units, max_len, sms).splits,
-                              cfg->head_dim);
+    const DecodeQuantTeams s = decode_quant_teams(format, cfg->head_dim, cfg->n_kv_heads, int64_t(n_seqs) * n_layers, max_len, sms);
+    return decode_quant_parts(s, n_q_heads / cfg->n_kv_heads, cfg->head_dim) + (size_t(n_seqs) + 1) * sizeof(int64_t);
 }
 
 int prcr_decode_attention_quant(const prcr_rope_cfg* cfg, const prcr_qcache_desc* cache, int32_t n_seqs, int32_t layer_begin, int32_t n_layers,
@@ -261,15 +255,17 @@ int prcr_decode_attention_quant(const prcr_rope_cfg* cfg, const prcr_qcache_desc
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return PRCR_ECUDA;
     const int64_t units = int64_t(n_seqs) * n_layers * cfg->n_kv_heads;
-    const DecodeQuantSplit s = decode_quant_split(cache->format, cfg->head_dim, units, max_len, sm_count(dev));
-    if (units * s.splits > INT32_MAX) return PRCR_EINVAL;  // grid x
+    if (units * (n_q_heads / cfg->n_kv_heads) > INT32_MAX) return PRCR_EINVAL;  // the join's grid x
     DecodeQuantArgs a = {};
-    const size_t need = decode_quant_bytes(int64_t(n_seqs) * n_layers * n_q_heads, s.splits, cfg->head_dim);
-    if (need > 0) {
-        if (!workspace || workspace_bytes < need) return PRCR_EWORKSPACE;
-        if (!aligned16(workspace)) return PRCR_EALIGN;
-        a.partial = static_cast<float*>(workspace);
-    }
+    const DecodeQuantTeams s = decode_quant_teams(cache->format, cfg->head_dim, cfg->n_kv_heads, int64_t(n_seqs) * n_layers, max_len, sm_count(dev));
+    const size_t parts = decode_quant_parts(s, n_q_heads / cfg->n_kv_heads, cfg->head_dim);
+    if (!workspace || workspace_bytes < parts + (size_t(n_seqs) + 1) * sizeof(int64_t)) return PRCR_EWORKSPACE;
+    if (!aligned16(workspace)) return PRCR_EALIGN;
+    a.team = s.team;
+    a.head_sets = s.head_sets;
+    a.teams = int32_t(s.teams);
+    a.partial = static_cast<float*>(workspace);
+    a.tiles_before = reinterpret_cast<int64_t*>(static_cast<char*>(workspace) + parts);
     a.cache = qcache_view(cache, layer_begin);
     a.q = static_cast<const uint16_t*>(q);
     a.q_pos = q_pos;
@@ -282,9 +278,6 @@ int prcr_decode_attention_quant(const prcr_rope_cfg* cfg, const prcr_qcache_desc
     a.group = n_q_heads / cfg->n_kv_heads;
     a.head_dim = cfg->head_dim;
     a.format = cache->format;
-    a.warps = s.warps;
-    a.splits = int32_t(s.splits);
-    a.chunk = s.chunk;
     a.max_len = int32_t(max_len);
     a.scale_log2 = float(1.4426950408889634 / std::sqrt(double(cfg->head_dim)));
     copy_turn_freq(cfg, a.turn_freq);

@@ -27,6 +27,8 @@
 // largest x and x + e, but only when one is more than 2^4 past them, so that most tiles
 // rescale nothing and need no reduction over the lanes; w stays below 2^15, and what fp16 loses
 // of it is 2^-36 of the largest at most.
+#include <algorithm>
+
 #include <cuda_fp16.h>
 
 #include "prcr_pdl.cuh"
@@ -39,7 +41,8 @@ constexpr unsigned kFull = 0xffffffffu;
 constexpr float kNone = -3.0e38f;   // reference of no slot yet: below every logit, and finite
 constexpr float kSlack = 4.0f;      // log2 of how far past its reference a weight may go
 constexpr float kWeightLog2 = 11.0f;
-constexpr int kMaxWarps = 16;
+constexpr int kCtaWarps = 4;
+constexpr int kLeastTiles = 2;      // of a warp's share
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -73,10 +76,31 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     return y;
 }
 
-// N words from p, or zeros.
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+    const __half2 c = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&c);
+}
+
+// The two powers of two (bf16) of scales' bytes; 255 gives NaN.
+__device__ __forceinline__ uint32_t bf16_of_scales(uint32_t two) {
+    uint32_t r;
+    asm("{\n.reg .b16 l, u;\nmov.b32 {l, u}, %1;\ncvt.rn.bf16x2.ue8m0x2 %0, l;\n}" : "=r"(r) : "r"(two));
+    return r;
+}
+
+// N words from p; `ok`: all of them, or zeros. (A load that waits for nothing: `ok ? *p : 0` would wait at once.)
 template <int N>
-__device__ __forceinline__ void load_codes(uint32_t* w, const uint8_t* p, bool ok) {
+__device__ __forceinline__ void load_words(uint32_t* w, const uint8_t* p) {
     static_assert(N == 1 || N == 2 || N == 4, "4, 8 or 16 bytes");
+    if constexpr (N == 4)
+        asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
+    else if constexpr (N == 2)
+        asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+    else
+        asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+}
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t* w, const uint8_t* p, bool ok) {
     if constexpr (N == 4) {
         asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %5, 0;\nmov.b32 %0, 0;\nmov.b32 %1, 0;\nmov.b32 %2, 0;\nmov.b32 %3, 0;\n"
                      "@p ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n}"
@@ -91,7 +115,21 @@ __device__ __forceinline__ void load_codes(uint32_t* w, const uint8_t* p, bool o
     }
 }
 
-// Sizes of a format's rows: RB bytes of codes; a warp takes SUB x 16 slots at once.
+// A row's N scales' bytes, or zeros.
+template <int N>
+__device__ __forceinline__ void load_row_scales(uint32_t* w, const uint8_t* p, bool ok) {
+    if constexpr (N == 8)
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %3, 0;\nmov.b32 %0, 0;\nmov.b32 %1, 0;\n@p ld.global.nc.v2.u32 {%0, %1}, [%2];\n}"
+                     : "=&r"(w[0]), "=&r"(w[1]) : "l"(p), "r"(int(ok)));
+    else if constexpr (N == 4)
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\nmov.b32 %0, 0;\n@p ld.global.nc.u32 %0, [%1];\n}" : "=&r"(w[0]) : "l"(p), "r"(int(ok)));
+    else if constexpr (N == 2)
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\nmov.b32 %0, 0;\n@p ld.global.nc.u16 %0, [%1];\n}" : "=&r"(w[0]) : "l"(p), "r"(int(ok)));
+    else
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\nmov.b32 %0, 0;\n@p ld.global.nc.u8 %0, [%1];\n}" : "=&r"(w[0]) : "l"(p), "r"(int(ok)));
+}
+
+// Sizes of a format's rows: RB bytes of codes; a warp takes tiles of SUB x 16 slots.
 template <int FMT, int D> struct Shape {
     static constexpr bool kFour = FMT == PRCR_QFMT_E2M1;
     static constexpr int RB = kFour ? D / 2 : D;
@@ -99,10 +137,16 @@ template <int FMT, int D> struct Shape {
     static constexpr int TS = 16 * SUB;
     static constexpr int N = kFour ? D / 32 : 1;  // scales of a row
     static constexpr int KW = RB / 16, VW = RB / 32;  // a lane's words of a row
+    static constexpr int KP = KW < 4 ? KW : 4, VP = VW < 4 ? VW : 4;  // of which it loads so many at once
     static constexpr int KS = D / 16;  // k-steps of S^T, products of O^T
     static constexpr int SW = (N + 3) / 4;  // words of a row's scales
-    static constexpr int OWN = (TS + 31) / 32;  // slots that a lane looks up
-    static constexpr int kThreads = D == 256 ? 256 : 512;
+    static constexpr int OWN = (TS + 31) / 32;  // slots whose scales a lane loads
+    static constexpr int kThreads = 32 * decode_quant_warps(D);
+    // a warp's shared memory: a group's rows of floats, or its queries' fragments
+    static constexpr __host__ __device__ int warp_bytes(bool pair, int group) {
+        const int rows = group * (D + 4) * 4, fragments = KS * (pair ? 1 : 2) * 256;
+        return rows > fragments ? rows : fragments;
+    }
     // the dim of word i's first code in lane t of a key's row, and in lane group r of a value's
     static __device__ __forceinline__ int kdim(int t, int i) {
         const int byte = RB >= 64 ? 16 * (t + 4 * (i / 4)) + 4 * (i % 4) : 8 * t + 4 * i;
@@ -114,37 +158,14 @@ template <int FMT, int D> struct Shape {
     }
 };
 
-// What a lane knows of a slot that it looked up.
-template <int SW> struct Slot {
-    int64_t codes;       // -1: not there
-    uint32_t ks[SW], vs[SW];  // scales' bytes
-    float bias;          // added to a logit: 0, -inf for a slot that is not there, NaN for a key that reads as NaN
-    float kf, ve;        // E4M3: the key's scale; the value's exponent (E2M1: the largest of its groups')
-};
+// Whether a byte of the word is 255.
+__device__ __forceinline__ bool any_255(uint32_t w) { return ((~w - 0x01010101u) & w & 0x80808080u) != 0; }
 
-template <int FMT, int D, bool PAIR>
-__global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kernel(const __grid_constant__ DecodeQuantArgs a) {
-    using S = Shape<FMT, D>;
-    constexpr bool kFour = S::kFour;
-    constexpr int SUB = S::SUB, TS = S::TS, N = S::N, KW = S::KW, VW = S::VW, KS = S::KS, SW = S::SW, OWN = S::OWN;
-    constexpr int P = D / 2, PITCH = D + 4, QP = PAIR ? 1 : 2, LS = PAIR ? 1 : 2;  // query pieces in registers, slots of a lane's logits
-    extern __shared__ __align__(16) float smem[];
-    __shared__ float s_cos[P], s_sin[P], s_qs[8];
-    __shared__ float s_m[kMaxWarps][8], s_l[kMaxWarps][8], s_r[kMaxWarps][8];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, t = lane & 3, W = blockDim.x >> 5;
-    const int H = a.n_kv_heads, g = a.group;
-    // this CTA's part: of a (sequence, layer) and split, heads fastest
-    uint32_t unit = blockIdx.x;
-    const int kh = int(unit % uint32_t(H));
-    unit /= uint32_t(H);
-    const int split = int(unit % uint32_t(a.splits));
-    unit /= uint32_t(a.splits);
-    const int l = int(unit % uint32_t(a.n_layers)), b = int(unit / uint32_t(a.n_layers));
-    const int64_t head0 = ((int64_t(b) * a.n_layers + l) * H + kh) * g;  // this group's first query head
-    pdl_wait();
+// Tiles of TS slots of a sequence, and its length: none where its position or its length allows none.
+template <int TS>
+__device__ __forceinline__ int tiles_of(const DecodeQuantArgs& a, int b, int& len, uint32_t& err) {
     const int64_t pos = a.q_pos[b];
-    int len = a.seq_len[b];
-    uint32_t err = 0;
+    len = a.seq_len[b];
     if (len < 0 || len > a.max_len) {  // (max_len is at most the capacity)
         err |= PRCR_ST_CAPACITY;
         len = len < 0 ? 0 : a.max_len;
@@ -153,235 +174,443 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
         err |= PRCR_ST_POS_RANGE;
         len = 0;
     }
-    const int s_begin = min(len, split * a.chunk), s_end = min(len, s_begin + a.chunk);
-    const int tiles = (s_end - s_begin + TS - 1) / TS;
-    if (tiles == 0 && a.splits > 1) {
-        for (int h = threadIdx.x; h < g; h += blockDim.x)
-            *reinterpret_cast<float2*>(a.partial + ((head0 + h) * a.splits + split) * (D + 2) + D) = make_float2(kNone, 0.0f);
-        if (err && threadIdx.x == 0) atomicOr(a.status, err);
+    return (len + TS - 1) / TS;
+}
+
+// How `total` tiles are cut into the teams' shares: the first `more` have one tile more than the others.
+struct Cut {
+    int64_t each, more;
+    __device__ __forceinline__ int64_t begin_of(int w) const { return w * each + min(int64_t(w), more); }
+    __device__ __forceinline__ int team_of(int64_t tile) const {
+        const int64_t big = more * (each + 1);
+        return int(tile < big ? tile / (each + 1) : more + (tile - big) / each);
+    }
+};
+__device__ __forceinline__ Cut cut_of(const DecodeQuantArgs& a, int64_t total) {
+    const int64_t teams = max(int64_t(1), min(int64_t(a.teams), total / kLeastTiles));
+    Cut c;
+    c.each = total / teams;
+    c.more = total - c.each * teams;
+    return c;
+}
+
+// A team's share of all sequences', layers' and sets of KV heads' tiles, in that order: tiles begin .. end - 1, the
+// first one tile `tile` of `tiles` of unit `unit` (layer, set of heads) of sequence `b`.
+struct Share {
+    int64_t begin, end;
+    int team, b, unit, tile, tiles, len;
+};
+template <int TS>
+__device__ __forceinline__ Share share_of(const DecodeQuantArgs& a, uint32_t& err) {
+    const int lane = threadIdx.x & 31, per_seq = a.n_layers * a.head_sets;
+    const int warp = __shfl_sync(kFull, int(blockIdx.x * kCtaWarps + (threadIdx.x >> 5)), 0);
+    Share s;
+    s.team = warp / a.team;
+    uint32_t e = 0;
+    int len;
+    int64_t sum = 0;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
+        int n = b0 + lane < a.n_seqs ? tiles_of<TS>(a, b0 + lane, len, e) : 0;
+        // (below 2^31 together: 2^30 slots each, sixteen to a tile, 32 of them)
+        if (warp == 0) {  // for the kernel that joins
+            int64_t upto = n;
+            for (int k = 1; k < 32; k *= 2) {
+                const int64_t x = __shfl_up_sync(kFull, upto, k);
+                if (lane >= k) upto += x;
+            }
+            if (b0 + lane < a.n_seqs) a.tiles_before[b0 + lane + 1] = sum + upto;
+            if (b0 + lane == 0) a.tiles_before[0] = 0;
+        }
+        sum += __reduce_add_sync(kFull, unsigned(n));
+    }
+    if (warp == 0) err |= __reduce_or_sync(kFull, e);
+    const Cut cut = cut_of(a, sum * per_seq);
+    s.begin = min(sum * per_seq, cut.begin_of(s.team));
+    s.end = min(sum * per_seq, cut.begin_of(s.team + 1));
+    s.b = s.unit = s.tile = s.tiles = s.len = 0;
+    if (s.begin >= s.end) return s;
+    int64_t before = 0;  // tiles of a unit of the sequences passed
+    for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
+        const int n = b0 + lane < a.n_seqs ? tiles_of<TS>(a, b0 + lane, len, e) : 0;
+        int upto = n;
+        for (int k = 1; k < 32; k *= 2) {
+            const int x = __shfl_up_sync(kFull, upto, k);
+            if (lane >= k) upto += x;
+        }
+        const uint32_t behind = __ballot_sync(kFull, (before + upto) * per_seq > s.begin);
+        if (behind) {
+            const int at = __ffs(int(behind)) - 1;
+            s.b = b0 + at;
+            s.tiles = __shfl_sync(kFull, n, at);
+            s.len = __shfl_sync(kFull, len, at);
+            before += __shfl_sync(kFull, upto, at) - s.tiles;
+            break;
+        }
+        before += __shfl_sync(kFull, upto, 31);
+    }
+    const int64_t in = s.begin - before * per_seq;
+    s.unit = int(in / s.tiles);
+    s.tile = int(in - int64_t(s.unit) * s.tiles);
+    return s;
+}
+
+// RUNS: sixteen slots from a multiple of sixteen on lie slot_stride apart (a contiguous cache,
+// or blocks of a multiple of 16 slots), so that a lane's rows follow from where the first one
+// is. Otherwise lanes look a slot up each and pass its place on.
+template <int FMT, int D, bool PAIR, bool RUNS>
+__global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kernel(const __grid_constant__ DecodeQuantArgs a) {
+    using S = Shape<FMT, D>;
+    constexpr bool kFour = S::kFour;
+    constexpr int SUB = S::SUB, TS = S::TS, N = S::N, KW = S::KW, VW = S::VW, KP = S::KP, VP = S::VP, KS = S::KS, SW = S::SW, OWN = S::OWN;
+    constexpr int P = D / 2, PITCH = D + 4, NP = PAIR ? 1 : 2, LS = PAIR ? 1 : 2;  // products for the pieces of a query or a weight, slots of a lane's logits
+    extern __shared__ __align__(16) float smem[];
+    const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, gid = lane >> 2, t = lane & 3;
+    const int H = a.n_kv_heads, g = a.group, per_seq = a.n_layers * a.head_sets;
+    const int member = warp % a.team;  // (teams do not cross CTAs)
+    // a warp's own: its query, as numbers and then as B fragments, and at the end its accumulators
+    float* mine = smem + warp * (S::warp_bytes(PAIR, g) / 4);
+    uint2* q_frag = reinterpret_cast<uint2*>(mine);
+    pdl_wait();
+    uint32_t err = 0;
+    const Share share = share_of<TS>(a, err);
+    if (share.begin >= share.end) {
+        if (err) atomicOr(a.status, err);
         return;
     }
-    const int64_t head_codes = int64_t(l) * a.cache.layer_stride + int64_t(kh) * S::RB;
-    const int64_t head_scales = int64_t(l) * a.cache.scale_layer_stride + int64_t(kh) * N;
-    const uint8_t *kb = a.cache.k + head_codes, *vb = a.cache.v + head_codes;
-    const uint8_t *kf = a.cache.k_scale + head_scales, *vf = a.cache.v_scale + head_scales;
 
-    // A lane looks up slots (lane + 32 j) % TS of a tile: its block, then where it lies.
-    auto slot_of = [&](int tile, int j) { return s_begin + tile * TS + (TS == 16 ? lane & 15 : lane + 32 * j); };
-    auto blocks = [&](int tile, int32_t (&blk)[OWN]) {
+    // where the next tile to load is: tile `at` of `n` of unit `unit` of sequence `b`
+    bool there;  // whether the set of heads has this warp's
+    int b = share.b, unit = share.unit, at = share.tile, n = share.tiles, s_end = share.len;
+    const uint8_t *kb, *vb, *kf, *vf;
+    auto point = [&]() {  // at the unit's rows
+        const int l = unit / a.head_sets, kh = (unit - l * a.head_sets) * a.team + member;
+        there = kh < H;
+        const int64_t codes = int64_t(l) * a.cache.layer_stride + int64_t(kh) * S::RB;
+        const int64_t scales = int64_t(l) * a.cache.scale_layer_stride + int64_t(kh) * N;
+        kb = a.cache.k + codes;
+        vb = a.cache.v + codes;
+        kf = a.cache.k_scale + scales;
+        vf = a.cache.v_scale + scales;
+    };
+    point();
+    int64_t left = share.end - share.begin;  // tiles to load
+    auto advance = [&]() {
+        if (--left <= 0) return;
+        if (++at < n) return;
+        at = 0;
+        if (++unit == per_seq) {
+            unit = 0;
+            do n = tiles_of<TS>(a, ++b, s_end, err); while (n == 0);  // (there is one: tiles are left)
+        }
+        point();
+    };
+
+    // A lane's pieces of a run's rows (RUNS: from the run's first one; strides are below 2^27). Lanes whose slots
+    // are not there have the last one's that is, whatever they make of it.
+    const uint32_t k_off = S::RB >= 64 ? 16 * t : 8 * t, v_off = gid * (S::RB == 256 ? 16 : S::RB / 8);
+    uint32_t k_row[SUB][2], v_row[SUB][4], f_row[OWN];
+    int rows[SUB];  // of a run that are there
+    auto lay_out = [&]() {
+        const uint32_t stride = uint32_t(a.cache.slot_stride);
 #pragma unroll
-        for (int j = 0; j < OWN; ++j) {
-            const int s = slot_of(tile, j);
-            blk[j] = tile < tiles && s < s_end ? qblock(a.cache, b, uint32_t(s)) : -1;
+        for (int u = 0; u < SUB; ++u) {
+            const int last = rows[u] - 1;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) k_row[u][i] = uint32_t(min(gid + 8 * i, last)) * stride + k_off;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v_row[u][i] = uint32_t(min(2 * t + (i & 1) + 8 * (i >> 1), last)) * stride + v_off;
+        }
+#pragma unroll
+        for (int j = 0; j < OWN; ++j)
+            f_row[j] = uint32_t(min(lane & 15, (SUB > 1 && lane >= 16 ? rows[(2 * j + 1) % SUB] : rows[2 * j % SUB]) - 1)) * uint32_t(a.cache.scale_slot_stride);
+    };
+    // Blocks and places of the tile's runs (RUNS), or of slots (lane + 32 j) % TS.
+    constexpr int LOOK = RUNS ? SUB : OWN;
+    int32_t blk[LOOK];
+    auto looked = [&](int j) { return at * TS + (RUNS ? 16 * j : TS == 16 ? lane & 15 : lane + 32 * j); };
+    auto blocks = [&]() {
+#pragma unroll
+        for (int j = 0; j < LOOK; ++j) {
+            const int s = looked(j);
+            blk[j] = left > 0 && there && s < s_end ? qblock(a.cache, b, uint32_t(s)) : -1;
         }
     };
-    Slot<SW> own[OWN];
-    int64_t scales_at[OWN];
-    auto places = [&](int tile, const int32_t (&blk)[OWN]) {
+    QPlace place[LOOK];
+    bool full;  // whether all of the tile's slots are there
+    if (RUNS) {
 #pragma unroll
-        for (int j = 0; j < OWN; ++j) {
-            const int s = slot_of(tile, j);
-            own[j].codes = -1;
-            scales_at[j] = 0;
-            if (tile < tiles && s < s_end) {
-                const QPlace p = qplace_in_block(a.cache, b, uint32_t(s), blk[j]);
-                if (p.codes < 0) err |= PRCR_ST_NO_BLOCK;
-                own[j].codes = p.codes;
-                scales_at[j] = p.scales;
+        for (int u = 0; u < SUB; ++u) rows[u] = 16;
+        lay_out();
+    }
+    auto places = [&]() {
+        bool same = true;
+        full = true;
+#pragma unroll
+        for (int j = 0; j < LOOK; ++j) {
+            const int s = looked(j);
+            place[j] = {-1, 0};
+            if (left > 0 && there && s < s_end) {
+                place[j] = qplace_in_block(a.cache, b, uint32_t(s), blk[j]);
+                if (place[j].codes < 0) err |= PRCR_ST_NO_BLOCK;
+            }
+            if (RUNS) {
+                const int n = place[j].codes < 0 ? 0 : min(16, s_end - s);
+                same = same && n == rows[j];
+                rows[j] = n;
+                full = full && n == 16;
+            } else {
+                full = full && place[j].codes >= 0;
             }
         }
+        if (RUNS) {
+            if (!same) lay_out();
+        } else {
+            full = __all_sync(kFull, full);
+        }
     };
+    uint32_t ks[OWN][SW], vs[OWN][SW];  // scales' bytes of slots lane + 32 j
+    float bias[OWN];                    // added to their logits: 0, or -inf for a slot that is not there
     auto load_scales = [&]() {
 #pragma unroll
         for (int j = 0; j < OWN; ++j) {
-            const bool ok = own[j].codes >= 0;
-            const uint8_t *pk = kf + scales_at[j], *pv = vf + scales_at[j];
-            if constexpr (N == 8) {
-                load_codes<2>(own[j].ks, pk, ok);
-                load_codes<2>(own[j].vs, pv, ok);
-            } else if constexpr (N == 4) {
-                load_codes<1>(own[j].ks, pk, ok);
-                load_codes<1>(own[j].vs, pv, ok);
-            } else if constexpr (N == 2) {
-                own[j].ks[0] = ok ? *reinterpret_cast<const uint16_t*>(pk) : 0u;
-                own[j].vs[0] = ok ? *reinterpret_cast<const uint16_t*>(pv) : 0u;
-            } else {
-                own[j].ks[0] = ok ? *pk : 0u;
-                own[j].vs[0] = ok ? *pv : 0u;
+            int64_t at = place[RUNS ? 0 : j].scales;
+            bool ok = place[RUNS ? 0 : j].codes >= 0, row = ok;
+            if (RUNS) {
+                const bool second = SUB > 1 && lane >= 16;
+                const int n = second ? rows[(2 * j + 1) % SUB] : rows[2 * j % SUB];
+                at = (second ? place[(2 * j + 1) % SUB].scales : place[2 * j % SUB].scales) + f_row[j];
+                ok = (lane & 15) < n;
+                row = n > 0;
             }
+            bias[j] = ok ? 0.0f : -INFINITY;
+            load_row_scales<N>(ks[j], kf + at, row);
+            load_row_scales<N>(vs[j], vf + at, row);
         }
     };
-    const uint8_t* kl = kb + (S::RB >= 64 ? 16 * t : 8 * t);
-    const uint8_t* vl = vb + gid * (S::RB == 256 ? 16 : S::RB / 8);
     uint32_t kw[SUB][2][KW], vw[SUB][4][VW];
     auto load_k = [&]() {
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
+        for (int u = 0; u < SUB; ++u) {
+            if (RUNS) {
+                if (rows[u] > 0) {
+                    const uint8_t* run = kb + place[u % LOOK].codes;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int64_t at = __shfl_sync(kFull, own[u / 2].codes, (16 * u + gid + 8 * i) & 31);
-                if constexpr (KW >= 4) {
+                    for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int c = 0; c < KW / 4; ++c) load_codes<4>(kw[u][i] + 4 * c, kl + at + 64 * c, at >= 0);
+                        for (int c = 0; c < KW / KP; ++c) load_words<KP>(kw[u][i] + KP * c, run + k_row[u][i] + 64 * c);
                 } else {
-                    load_codes<KW>(kw[u][i], kl + at, at >= 0);
+#pragma unroll
+                    for (int i = 0; i < 2 * KW; ++i) kw[u][i / KW][i % KW] = 0;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int64_t at = __shfl_sync(kFull, place[u / 2 % LOOK].codes, (16 * u + gid + 8 * i) & 31);
+#pragma unroll
+                    for (int c = 0; c < KW / KP; ++c) load_words<KP>(kw[u][i] + KP * c, kb + at + k_off + 64 * c, at >= 0);
                 }
             }
+        }
     };
     auto load_v = [&]() {
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
+        for (int u = 0; u < SUB; ++u) {
+            if (RUNS) {
+                if (rows[u] > 0) {
+                    const uint8_t* run = vb + place[u % LOOK].codes;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t at = __shfl_sync(kFull, own[u / 2].codes, (16 * u + 2 * t + (i & 1) + 8 * (i >> 1)) & 31);
-                if constexpr (VW >= 4) {
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int c = 0; c < VW / 4; ++c) load_codes<4>(vw[u][i] + 4 * c, vl + at + 128 * c, at >= 0);
+                        for (int c = 0; c < VW / VP; ++c) load_words<VP>(vw[u][i] + VP * c, run + v_row[u][i] + 128 * c);
                 } else {
-                    load_codes<VW>(vw[u][i], vl + at, at >= 0);
+#pragma unroll
+                    for (int i = 0; i < 4 * VW; ++i) vw[u][i / VW][i % VW] = 0;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t at = __shfl_sync(kFull, place[u / 2 % LOOK].codes, (16 * u + 2 * t + (i & 1) + 8 * (i >> 1)) & 31);
+#pragma unroll
+                    for (int c = 0; c < VW / VP; ++c) load_words<VP>(vw[u][i] + VP * c, vb + at + v_off + 128 * c, at >= 0);
                 }
             }
+        }
     };
 
     // the first tile is requested before the query is read
-    int32_t blk[OWN];
-    blocks(warp, blk);
-    places(warp, blk);
+    blocks();
+    places();
     load_k();
     load_scales();
     load_v();
-    blocks(warp + W, blk);
+    bool whole_tile = full;  // of the tile that is loaded
+    advance();
+    blocks();
 
-    // the group's queries, rotated at (p, p, p): pair i turns by p * rate i whatever its band
-    for (int i = threadIdx.x; i < P; i += blockDim.x) sincos_turns(double(pos), a.turn_freq[i], &s_sin[i], &s_cos[i]);
-    __syncthreads();
-    for (int h = warp; h < g; h += W) {
-        const uint16_t* q = a.q + (head0 + h) * D;
-        float x[P / 32], y[P / 32];
-        uint32_t most = 0;
-#pragma unroll
-        for (int i = 0; i < P / 32; ++i) {
-            const int d = lane + 32 * i;
-            const float qx = __uint_as_float(uint32_t(q[d]) << 16), qy = __uint_as_float(uint32_t(q[d + P]) << 16);
-            x[i] = fmaf(qx, s_cos[d], -qy * s_sin[d]) * a.scale_log2;
-            y[i] = fmaf(qy, s_cos[d], qx * s_sin[d]) * a.scale_log2;
-            most = max(most, max(__float_as_uint(x[i]) & 0x7fffffffu, __float_as_uint(y[i]) & 0x7fffffffu));
-        }
-        most = __reduce_max_sync(kFull, most);
-        // times 2^up: below 2^14 (2^40 at most, so that a logit times it stays finite)
-        const int up = min(40, 13 - (int(most >> 23) - 127));
-        const float f = __uint_as_float(uint32_t(127 + up) << 23);
-#pragma unroll
-        for (int i = 0; i < P / 32; ++i) {
-            smem[h * PITCH + lane + 32 * i] = x[i] * f;
-            smem[h * PITCH + lane + 32 * i + P] = y[i] * f;
-        }
-        if (lane == 0) s_qs[h] = __uint_as_float(uint32_t(127 - up) << 23);
-    }
-    __syncthreads();
-    // B fragments: column r is head r, or with pairs head r % 4, of its first or second piece
-    uint32_t qf[KS][QP][2];
+    // the unit that is attended to
+    int ub = share.b, uu = share.unit, first = share.tile, un = share.tiles;
+    int64_t todo = share.end - share.begin;
+    bool step0 = true;  // the share's first unit
+    const int h0 = PAIR ? 2 * (t & 1) : 2 * t;  // this lane's heads are h0 and h0 + 1, in S^T's columns and in O^T's
+    while (true) {
+    const int layer = uu / a.head_sets, kh = (uu - layer * a.head_sets) * a.team + member;
+    const int64_t head0 = ((int64_t(ub) * a.n_layers + layer) * H + min(kh, H - 1)) * g;  // its group's first query head
+    float qs[2] = {0.0f, 0.0f};
     {
+        // the group's queries, rotated at (p, p, p): pair i turns by p * rate i whatever its band
+        constexpr int PR = P / 64 > 0 ? P / 64 : 1;  // a lane has pairs 2 (lane + 32 i) and the next (D = 64: half of the lanes)
+        const bool has = P >= 64 || lane < P / 2;
+        const double pos = double(a.q_pos[ub]);
+        float cs[PR][2], sn[PR][2];
+#pragma unroll
+        for (int i = 0; i < PR; ++i)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (has) sincos_turns(pos, a.turn_freq[2 * (lane + 32 * i) + k], &sn[i][k], &cs[i][k]);
+        for (int h = 0; h < g; ++h) {
+            const uint32_t* q = reinterpret_cast<const uint32_t*>(a.q + (head0 + h) * D) + lane;
+            float x[PR][2], y[PR][2];
+            uint32_t most = 0;
+#pragma unroll
+            for (int i = 0; i < PR; ++i) {
+                const uint32_t wx = has ? __ldg(q + 32 * i) : 0u, wy = has ? __ldg(q + 32 * i + P / 2) : 0u;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float qx = k ? hi_f32(wx) : lo_f32(wx), qy = k ? hi_f32(wy) : lo_f32(wy);
+                    x[i][k] = has ? fmaf(qx, cs[i][k], -qy * sn[i][k]) * a.scale_log2 : 0.0f;
+                    y[i][k] = has ? fmaf(qy, cs[i][k], qx * sn[i][k]) * a.scale_log2 : 0.0f;
+                    most = max(most, max(__float_as_uint(x[i][k]) & 0x7fffffffu, __float_as_uint(y[i][k]) & 0x7fffffffu));
+                }
+            }
+            most = __reduce_max_sync(kFull, most);
+            // times 2^up: below 2^14 (2^40 at most, so that a logit times it stays finite)
+            const int up = min(40, 13 - (int(most >> 23) - 127));
+            const float f = __uint_as_float(uint32_t(127 + up) << 23), down = __uint_as_float(uint32_t(127 - up) << 23);
+            if (has) {
+#pragma unroll
+                for (int i = 0; i < PR; ++i) {
+                    *reinterpret_cast<float2*>(mine + h * PITCH + 2 * (lane + 32 * i)) = make_float2(x[i][0] * f, x[i][1] * f);
+                    *reinterpret_cast<float2*>(mine + h * PITCH + 2 * (lane + 32 * i) + P) = make_float2(y[i][0] * f, y[i][1] * f);
+                }
+            }
+            if (h == h0) qs[0] = down;
+            if (h == h0 + 1) qs[1] = down;
+        }
+        __syncwarp();
+        // B fragments. Column r of a product is head r, or with pairs head r % 4, r / 4 its first or second piece.
         const int h = PAIR ? gid & 3 : gid;
         const bool hv = h < g;
-        const float* qr = smem + (hv ? h : 0) * PITCH;
+        const float* row = mine + (hv ? h : 0) * PITCH;
+        uint2 f[KS][NP];
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
-            const float4 x = *reinterpret_cast<const float4*>(qr + (kFour ? S::kdim(t, j >> 1) + 4 * (j & 1) : S::kdim(t, j)));
-            uint32_t h0, l0, h1, l1;
-            split_f16x2(hv ? x.x : 0.0f, hv ? x.y : 0.0f, h0, l0);
-            split_f16x2(hv ? x.z : 0.0f, hv ? x.w : 0.0f, h1, l1);
-            if (PAIR) {
-                qf[j][0][0] = gid < 4 ? h0 : l0;
-                qf[j][0][1] = gid < 4 ? h1 : l1;
-            } else {
-                qf[j][0][0] = h0;
-                qf[j][0][1] = h1;
-                qf[j][QP - 1][0] = l0;
-                qf[j][QP - 1][1] = l1;
-            }
+            const float4 v = *reinterpret_cast<const float4*>(row + (kFour ? S::kdim(t, j >> 1) + 4 * (j & 1) : S::kdim(t, j)));
+            uint2 hi, lo;
+            split_f16x2(hv ? v.x : 0.0f, hv ? v.y : 0.0f, hi.x, lo.x);
+            split_f16x2(hv ? v.z : 0.0f, hv ? v.w : 0.0f, hi.y, lo.y);
+            f[j][0] = PAIR && gid >= 4 ? lo : hi;
+            if (!PAIR) f[j][NP - 1] = lo;
         }
+        __syncwarp();  // every lane has read them
+#pragma unroll
+        for (int j = 0; j < KS; ++j)
+#pragma unroll
+            for (int z = 0; z < NP; ++z) q_frag[(j * NP + z) * 32 + lane] = f[j][z];
     }
-    // this lane's heads are h0 and h0 + 1, in S^T's columns and in O^T's
-    const int h0 = PAIR ? 2 * (t & 1) : 2 * t;
-    const float qs[2] = {h0 < g ? s_qs[h0] : 0.0f, h0 + 1 < g ? s_qs[h0 + 1] : 0.0f};
 
     float o[KS][4];
 #pragma unroll
     for (int j = 0; j < KS; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.0f;
+    // references: m of the sums; r, less kWeightLog2, of the accumulators
     float m[2] = {kNone, kNone}, r[2] = {kNone, kNone}, sum[2] = {0.0f, 0.0f};
+    uint32_t nan_groups = 0;  // E2M1: groups of dims that a value makes NaN
 
-    for (int tile = warp; tile < tiles; tile += W) {
-        // what the lanes know of this tile's slots
-        bool v_nan = false;
+    const int steps = int(min(int64_t(un - first), todo));
+    for (int step = 0; step < steps; ++step) {
+        // what the lanes know of this tile's slots: the key's scale (E4M3; E2M1: bf16 of its groups'), the value's exponent
+        // (E2M1: the largest, and fp16 of its groups' scales in units of that one)
+        float kx[OWN], vx[OWN];
+        uint32_t kg[OWN][(N + 1) / 2], vg[OWN][(N + 1) / 2];
 #pragma unroll
         for (int j = 0; j < OWN; ++j) {
-            Slot<SW>& w = own[j];
-            if (kFour) {
+            if constexpr (kFour) {
                 bool nan = false;
+#pragma unroll
+                for (int i = 0; i < SW; ++i) nan |= any_255(vs[j][i]);
+                if (nan) {  // noted for the end, and without influence on the other groups
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        if (((vs[j][i / 4] >> (8 * (i % 4))) & 255) == kScaleNan) {
+                            nan_groups |= 1u << i;
+                            vs[j][i / 4] &= ~(255u << (8 * (i % 4)));
+                        }
+                }
                 int top = 0;
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int bk = (w.ks[i / 4] >> (8 * (i % 4))) & 255, bv = (w.vs[i / 4] >> (8 * (i % 4))) & 255;
-                    nan |= bk == kScaleNan;
-                    v_nan |= bv == kScaleNan;
-                    top = max(top, bv == kScaleNan ? 0 : bv);
+                for (int i = 0; i < N; ++i) top = max(top, int((vs[j][i / 4] >> (8 * (i % 4))) & 255));
+                vx[j] = float(top - 127);
+#pragma unroll
+                for (int i = 0; i < N; i += 2) {
+                    kg[j][i / 2] = bf16_of_scales(ks[j][i / 4] >> (8 * (i % 4)));
+                    vg[j][i / 2] = pack_f16x2(ex2(float(int((vs[j][i / 4] >> (8 * (i % 4))) & 255) - top)),
+                                              ex2(float(int((vs[j][i / 4] >> (8 * (i % 4) + 8)) & 255) - top)));
                 }
-                w.ve = float(top - 127);
-                w.bias = w.codes < 0 ? -INFINITY : nan ? __uint_as_float(0x7fffffffu) : 0.0f;
             } else {
-                w.kf = w.codes < 0 ? 0.0f : scale_value(int(w.ks[0]));
-                w.ve = w.vs[0] == kScaleNan ? __uint_as_float(0x7fffffffu) : float(int(w.vs[0]) - 127);
-                w.bias = w.codes < 0 ? -INFINITY : 0.0f;
+                kx[j] = scale_value(int(ks[j][0]));
+                vx[j] = vs[j][0] == kScaleNan ? __uint_as_float(0x7fffffffu) : float(int(vs[j][0]) - 127);
             }
         }
-        v_nan = kFour && __any_sync(kFull, v_nan);
 
         float x[SUB][LS][2], ve[SUB][LS];
-        uint32_t vs[SUB][LS][SW];
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
-            float c[kFour ? N : 2][4];
+            float d[4];
+            if constexpr (kFour) {
+                float c[N][4];
 #pragma unroll
-            for (int j = 0; j < (kFour ? N : 2); ++j) c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0.0f;
+                for (int j = 0; j < N; ++j) c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < KW; ++i) {
-                if constexpr (kFour) {
+                for (int i = 0; i < KW; ++i) {
                     uint32_t p[4], q[4];
                     f16_of_e2m1(kw[u][0][i], p);
                     f16_of_e2m1(kw[u][1][i], q);
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
 #pragma unroll
-                        for (int z = 0; z < QP; ++z)
-                            mma_f16(c[(2 * i + e) % N], p[2 * e], q[2 * e], p[2 * e + 1], q[2 * e + 1], qf[2 * i + e][z][0], qf[2 * i + e][z][1]);
-                } else {
+                        for (int z = 0; z < NP; ++z) {
+                            const uint2 f = q_frag[((2 * i + e) * NP + z) * 32 + lane];
+                            mma_f16(c[(2 * i + e) % N], p[2 * e], q[2 * e], p[2 * e + 1], q[2 * e + 1], f.x, f.y);
+                        }
+                }
+                d[0] = d[1] = d[2] = d[3] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < N / 2; ++k) {
+                    const uint32_t wa = __shfl_sync(kFull, kg[u / 2][k], (16 * u + gid) & 31);
+                    const uint32_t wb = __shfl_sync(kFull, kg[u / 2][k], (16 * u + gid + 8) & 31);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float fa = e ? hi_f32(wa) : lo_f32(wa), fb = e ? hi_f32(wb) : lo_f32(wb);
+                        d[0] = fmaf(c[2 * k + e][0], fa, d[0]);
+                        d[1] = fmaf(c[2 * k + e][1], fa, d[1]);
+                        d[2] = fmaf(c[2 * k + e][2], fb, d[2]);
+                        d[3] = fmaf(c[2 * k + e][3], fb, d[3]);
+                    }
+                }
+            } else {
+                float c[2][4];
+#pragma unroll
+                for (int z = 0; z < 2; ++z) c[z][0] = c[z][1] = c[z][2] = c[z][3] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < KW; ++i) {
                     uint32_t p[2], q[2];
                     f16_of_e4m3(kw[u][0][i], p);
                     f16_of_e4m3(kw[u][1][i], q);
 #pragma unroll
-                    for (int z = 0; z < QP; ++z) mma_f16(c[(i + z) & 1], p[0], q[0], p[1], q[1], qf[i][z][0], qf[i][z][1]);
-                }
-            }
-            float d[4];
-            if constexpr (kFour) {
-                d[0] = d[1] = d[2] = d[3] = 0.0f;
-#pragma unroll
-                for (int k = 0; k < SW; ++k) {
-                    const uint32_t wa = __shfl_sync(kFull, own[u / 2].ks[k], (16 * u + gid) & 31);
-                    const uint32_t wb = __shfl_sync(kFull, own[u / 2].ks[k], (16 * u + gid + 8) & 31);
-#pragma unroll
-                    for (int i = 4 * k; i < min(N, 4 * k + 4); ++i) {
-                        // the byte as a float's exponent
-                        const float fa = __uint_as_float((i % 4 == 3 ? wa >> 1 : wa << (23 - 8 * (i % 4))) & 0x7f800000u);
-                        const float fb = __uint_as_float((i % 4 == 3 ? wb >> 1 : wb << (23 - 8 * (i % 4))) & 0x7f800000u);
-                        d[0] = fmaf(c[i][0], fa, d[0]);
-                        d[1] = fmaf(c[i][1], fa, d[1]);
-                        d[2] = fmaf(c[i][2], fb, d[2]);
-                        d[3] = fmaf(c[i][3], fb, d[3]);
+                    for (int z = 0; z < NP; ++z) {
+                        const uint2 f = q_frag[(i * NP + z) * 32 + lane];
+                        mma_f16(c[(i + z) & 1], p[0], q[0], p[1], q[1], f.x, f.y);
                     }
                 }
-            } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) d[i] = c[0][i] + c[1][i];
             }
@@ -394,21 +623,22 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 #pragma unroll
             for (int i = 0; i < LS; ++i) {
                 const int from = (16 * u + gid + 8 * (PAIR ? t >> 1 : i)) & 31;
-                const float bias = __shfl_sync(kFull, own[u / 2].bias, from);
-                ve[u][i] = __shfl_sync(kFull, own[u / 2].ve, from);
-                const float f = kFour ? 1.0f : __shfl_sync(kFull, own[u / 2].kf, from);
-                x[u][i][0] = fmaf(kFour ? d[2 * i] : d[2 * i] * f, qs[0], bias);
-                x[u][i][1] = fmaf(kFour ? d[2 * i + 1] : d[2 * i + 1] * f, qs[1], bias);
-                if constexpr (kFour) {
+                ve[u][i] = __shfl_sync(kFull, vx[u / 2], from);
+                const float f = kFour ? 1.0f : __shfl_sync(kFull, kx[u / 2], from);
 #pragma unroll
-                    for (int k = 0; k < SW; ++k) vs[u][i][k] = __shfl_sync(kFull, own[u / 2].vs[k], from);
+                for (int z = 0; z < 2; ++z) x[u][i][z] = (kFour ? d[2 * i + z] : d[2 * i + z] * f) * qs[z];
+                if (!whole_tile) {
+                    const float add = __shfl_sync(kFull, bias[u / 2], from);
+                    x[u][i][0] += add;
+                    x[u][i][1] += add;
                 }
             }
         }
         // the keys' registers are free: the next tile's
-        places(tile + W, blk);
+        places();
         load_k();
         load_scales();
+        whole_tile = full;
 
         // a logit past its reference by more than the slack moves the references
         bool far = false;
@@ -417,7 +647,8 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 #pragma unroll
             for (int i = 0; i < LS; ++i)
 #pragma unroll
-                for (int z = 0; z < 2; ++z) far |= x[u][i][z] > m[z] + kSlack || x[u][i][z] + ve[u][i] > r[z] + kSlack;
+                for (int z = 0; z < 2; ++z)
+                    far |= x[u][i][z] - m[z] > kSlack || (x[u][i][z] + ve[u][i]) - r[z] > kSlack + kWeightLog2;
         if (__any_sync(kFull, far)) {
 #pragma unroll
             for (int z = 0; z < 2; ++z) {
@@ -427,7 +658,7 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 #pragma unroll
                     for (int i = 0; i < LS; ++i) {
                         mx = fmaxf(mx, x[u][i][z]);
-                        rx = fmaxf(rx, x[u][i][z] + ve[u][i]);
+                        rx = fmaxf(rx, x[u][i][z] + ve[u][i] - kWeightLog2);
                     }
 #pragma unroll
                 for (int k = PAIR ? 2 : 4; k < 32; k *= 2) {
@@ -447,19 +678,20 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
         }
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
-            float y[LS][2];  // log2 of the weights, the value's exponent aside
-#pragma unroll
-            for (int i = 0; i < LS; ++i)
-#pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                    sum[z] += ex2(x[u][i][z] - m[z]);
-                    y[i][z] = x[u][i][z] - r[z] + kWeightLog2;
-                }
-            // B fragments of P^T from weights of these exponents: [first and second piece][slots 0..7, 8..15]
-            auto weights = [&](const float (&e)[LS], uint32_t (&pf)[QP][2]) {
+            // B fragments of P^T: [first and second piece][slots 0..7, 8..15]
+            uint32_t pf[NP][2];
+            {
                 uint32_t hi[LS], lo[LS];
 #pragma unroll
-                for (int i = 0; i < LS; ++i) split_f16x2(ex2(y[i][0] + e[i]), ex2(y[i][1] + e[i]), hi[i], lo[i]);
+                for (int i = 0; i < LS; ++i) {
+                    float w[2];
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {
+                        sum[z] += ex2(x[u][i][z] - m[z]);
+                        w[z] = ex2((x[u][i][z] + ve[u][i]) - r[z]);
+                    }
+                    split_f16x2(w[0], w[1], hi[i], lo[i]);
+                }
                 if (PAIR) {
                     const uint32_t got = __shfl_xor_sync(kFull, t < 2 ? lo[0] : hi[0], 2);
                     pf[0][0] = transposed(t < 2 ? hi[0] : got);
@@ -468,11 +700,29 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 #pragma unroll
                     for (int i = 0; i < LS; ++i) {
                         pf[0][i] = transposed(hi[i]);
-                        pf[QP - 1][i] = transposed(lo[i]);
+                        pf[NP - 1][i] = transposed(lo[i]);
                     }
                 }
-            };
+            }
             if constexpr (kFour) {
+                // The groups' scales as factors of P^T's pairs of slots: a matrix of slots by groups, transposed as P is; its rows
+                // (N = 2, 4: of slots 0..7, then of 8..15) are read by every lane.
+                uint32_t rel[2];
+                if (N == 8) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int from = (16 * u + gid + 8 * i) & 31;
+                        const uint32_t w0 = __shfl_sync(kFull, vg[u / 2][0], from), w1 = __shfl_sync(kFull, vg[u / 2][1 % ((N + 1) / 2)], from);
+                        const uint32_t w2 = __shfl_sync(kFull, vg[u / 2][2 % ((N + 1) / 2)], from), w3 = __shfl_sync(kFull, vg[u / 2][3 % ((N + 1) / 2)], from);
+                        rel[i] = transposed(t < 2 ? (t == 0 ? w0 : w1) : (t == 2 ? w2 : w3));
+                    }
+                } else if (N == 4) {
+                    const int from = (16 * u + gid + 8 * (t >> 1)) & 31;
+                    const uint32_t w0 = __shfl_sync(kFull, vg[u / 2][0], from), w1 = __shfl_sync(kFull, vg[u / 2][1 % ((N + 1) / 2)], from);
+                    rel[0] = transposed(t & 1 ? w1 : w0);
+                } else {
+                    rel[0] = transposed(__shfl_sync(kFull, vg[u / 2][0], (16 * u + gid + 8 * (t & 1)) & 31));
+                }
 #pragma unroll
                 for (int i = 0; i < VW; ++i) {
                     // bytes of (slot 2t, slot 2t + 1) and of the slots 8 behind, even dims and odd
@@ -486,24 +736,21 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int grp = 2 * i + e;
-                        float ex[LS];
+                        const uint32_t f0 = __shfl_sync(kFull, rel[0], 4 * grp + t);
+                        const uint32_t f1 = N == 8 ? __shfl_sync(kFull, rel[1], 4 * grp + t) : __shfl_sync(kFull, rel[0], 4 * (grp + N) + t);
+                        uint32_t b[NP][2];
 #pragma unroll
-                        for (int k = 0; k < LS; ++k) {
-                            // the byte behind 2^23's bits: 2^23 + byte
-                            ex[k] = __uint_as_float(__byte_perm(vs[u][k][grp / 4], 0x4b000000u, 0x7650u + grp % 4)) - 8388735.0f;
-                            if (v_nan && ex[k] == 128.0f) ex[k] = __uint_as_float(0x7fffffffu);
+                        for (int z = 0; z < NP; ++z) {
+                            b[z][0] = mul_f16x2(pf[z][0], f0);
+                            b[z][1] = mul_f16x2(pf[z][1], f1);
                         }
-                        uint32_t pf[QP][2];
-                        weights(ex, pf);
 #pragma unroll
                         for (int k = 2 * e; k < 2 * e + 2; ++k)
 #pragma unroll
-                            for (int z = 0; z < QP; ++z) mma_f16(o[4 * i + k], ev[0][k], od[0][k], ev[1][k], od[1][k], pf[z][0], pf[z][1]);
+                            for (int z = 0; z < NP; ++z) mma_f16(o[4 * i + k], ev[0][k], od[0][k], ev[1][k], od[1][k], b[z][0], b[z][1]);
                     }
                 }
             } else {
-                uint32_t pf[QP][2];
-                weights(ve[u], pf);
 #pragma unroll
                 for (int i = 0; i < VW; ++i)
 #pragma unroll
@@ -512,16 +759,16 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
                         f16_of_e4m3(__byte_perm(vw[u][0][i], vw[u][1][i], e ? 0x7362 : 0x5140), p);
                         f16_of_e4m3(__byte_perm(vw[u][2][i], vw[u][3][i], e ? 0x7362 : 0x5140), q);
 #pragma unroll
-                        for (int z = 0; z < QP; ++z) mma_f16(o[2 * i + e], p[0], p[1], q[0], q[1], pf[z][0], pf[z][1]);
+                        for (int z = 0; z < NP; ++z) mma_f16(o[2 * i + e], p[0], p[1], q[0], q[1], pf[z][0], pf[z][1]);
                     }
             }
         }
         load_v();
-        blocks(tile + 2 * W, blk);
+        advance();
+        blocks();
     }
-    pdl_allow();
 
-    // join the lanes' sums, the two pieces, the warps
+    // join the lanes' sums and the two pieces
 #pragma unroll
     for (int z = 0; z < 2; ++z)
 #pragma unroll
@@ -532,110 +779,153 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 #pragma unroll
             for (int z = 0; z < 4; ++z) o[j][z] += __shfl_xor_sync(kFull, o[j][z], 2);
     }
-    __syncthreads();  // the queries are read
+    if (kFour) nan_groups = __reduce_or_sync(kFull, nan_groups);
+    // the whole unit: its outputs; a part of one: what is joined later, in place 0 where it begins with
+    // this team's share, else in place 1
+    const bool whole = first == 0 && steps == un;
+    float* dst = whole ? a.out + head0 * D
+                       : a.partial + ((int64_t(share.team) * 2 + (step0 ? 0 : 1)) * a.team + member) * g * (D + 2);
+    const int pitch = whole ? D : D + 2;
+    __syncwarp();  // the fragments are read
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
         const int h = h0 + z;
-        if (h >= g || (PAIR && t >= 2)) continue;
-        float* row = smem + (warp * g + h) * PITCH;
+        if (h >= g || kh >= H || (PAIR && t >= 2)) continue;
+        const float f = ex2(r[z] - m[z]) * (!whole ? 1.0f : sum[z] == 0.0f ? 0.0f : 1.0f / sum[z]);  // to the sums' reference
 #pragma unroll
-        for (int j = 0; j < KS; ++j)
-            *reinterpret_cast<float2*>(row + (kFour ? S::vdim(gid, j / 4) + 2 * (j % 4) : S::vdim(gid, j / 2) + 2 * (j % 2))) =
-                make_float2(o[j][z], o[j][2 + z]);
-        if (gid == 0) {
-            s_m[warp][h] = m[z];
-            s_l[warp][h] = sum[z];
-            s_r[warp][h] = r[z];
+        for (int j = 0; j < KS; ++j) {
+            const int d = kFour ? S::vdim(gid, j / 4) + 2 * (j % 4) : S::vdim(gid, j / 2) + 2 * (j % 2);
+            const float to = kFour && (nan_groups >> (d / 4 % N) & 1) ? __uint_as_float(0x7fffffffu) : f;
+            *reinterpret_cast<float2*>(mine + h * PITCH + d) = make_float2(o[j][z] * to, o[j][2 + z] * to);
         }
+        if (gid == 0 && !whole) *reinterpret_cast<float2*>(dst + h * pitch + D) = make_float2(m[z], sum[z]);
     }
-    __syncthreads();
-    for (int e = threadIdx.x; e < g * (D / 2); e += blockDim.x) {
-        const int h = e / (D / 2), d = 2 * (e - h * (D / 2));
-        float M = s_m[0][h], R = s_r[0][h];
-        for (int w = 1; w < W; ++w) {
-            M = fmaxf(M, s_m[w][h]);
-            R = fmaxf(R, s_r[w][h]);
-        }
-        float2 acc = make_float2(0.0f, 0.0f);
-        float den = 0.0f;
-        for (int w = 0; w < W; ++w) {
-            const float f = ex2(s_r[w][h] - R);
-            const float2 y = *reinterpret_cast<const float2*>(smem + (w * g + h) * PITCH + d);
-            acc.x = fmaf(f, y.x, acc.x);
-            acc.y = fmaf(f, y.y, acc.y);
-            den = fmaf(ex2(s_m[w][h] - M), s_l[w][h], den);
-        }
-        const float back = ex2(R - M - kWeightLog2);  // to the sums' reference
-        acc.x *= back;
-        acc.y *= back;
-        if (a.splits == 1) {
-            const float inv = den == 0.0f ? 0.0f : 1.0f / den;
-            *reinterpret_cast<float2*>(a.out + (head0 + h) * D + d) = make_float2(acc.x * inv, acc.y * inv);
-        } else {
-            float* part = a.partial + ((head0 + h) * a.splits + split) * (D + 2);
-            *reinterpret_cast<float2*>(part + d) = acc;
-            if (d == 0) *reinterpret_cast<float2*>(part + D) = make_float2(M, den);
-        }
+    __syncwarp();
+    for (int e = lane; e < (kh < H ? g * P : 0); e += 32) {
+        const int h = e / P, d = 2 * (e - h * P);
+        *reinterpret_cast<float2*>(dst + h * pitch + d) = *reinterpret_cast<const float2*>(mine + h * PITCH + d);
     }
+    __syncwarp();
+    todo -= steps;
+    if (todo <= 0) break;
+    step0 = false;
+    first = 0;
+    if (++uu == per_seq) {
+        uu = 0;
+        int len;
+        do un = tiles_of<TS>(a, ++ub, len, err); while (un == 0);
+    }
+    }
+    pdl_allow();
     if (err) atomicOr(a.status, err);
 }
 
-// Joins a query head's splits: a warp each; lanes hold 32 splits' references and sums at a time.
-template <int D>
-__global__ void __launch_bounds__(128) decode_quant_join_kernel(const __grid_constant__ DecodeQuantArgs a, int64_t heads) {
-    constexpr int NV = D / 64;
+// Joins the parts of the units that several teams shared, and writes zeros for sequences without any slot: a query
+// head's row a warp, or, where many teams share a unit, a CTA. Eight parts are requested at once.
+template <int D, int WARPS>
+__global__ void __launch_bounds__(128) decode_quant_join_kernel(const __grid_constant__ DecodeQuantArgs a) {
+    constexpr int NV = D / 64, AHEAD = 8;
+    __shared__ float2 s_acc[WARPS][D / 2];
+    __shared__ float s_top[WARPS], s_den[WARPS];
     pdl_allow();
     pdl_wait();
-    const int lane = threadIdx.x & 31, n = a.splits;
-    const int64_t head = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 5);
-    if (head >= heads) return;
-    const float* part = a.partial + head * n * (D + 2);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = a.group;
+    const int64_t row = WARPS > 1 ? int64_t(blockIdx.x) : int64_t(blockIdx.x) * 4 + warp;
+    const int per_seq = a.n_layers * a.head_sets, heads = a.n_layers * a.n_kv_heads;
+    if (row >= int64_t(a.n_seqs) * heads * g) return;
+    const int64_t head = row / g;
+    const int h = int(row - head * g), b = int(head / heads), lh = int(head - int64_t(b) * heads);
+    const int layer = lh / a.n_kv_heads, kh = lh - layer * a.n_kv_heads, unit = layer * a.head_sets + kh / a.team, member = kh % a.team;
+    const int64_t before = a.tiles_before[b];
+    const int n = int(a.tiles_before[b + 1] - before);
+    float* out = a.out + row * D;
+    if (n == 0) {
+        if (WARPS == 1 || warp == 0)
+            for (int d = lane; d < D; d += 32) out[d] = 0.0f;
+        return;
+    }
+    const Cut cut = cut_of(a, a.tiles_before[a.n_seqs] * per_seq);
+    const int64_t u0 = before * per_seq + int64_t(unit) * n, u1 = u0 + n;
+    const int w0 = cut.team_of(u0), w1 = cut.team_of(u1 - 1);
+    if (w0 == w1) return;
+    const int place0 = cut.begin_of(w0) != u0 ? 1 : 0;  // in the first team's parts; the others' begin with their shares
     float M = kNone, den = 0.0f;
     float2 acc[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) acc[k] = make_float2(0.0f, 0.0f);
-    for (int s0 = 0; s0 < n; s0 += 32) {
-        const float2 mz = s0 + lane < n ? *reinterpret_cast<const float2*>(part + int64_t(s0 + lane) * (D + 2) + D) : make_float2(kNone, 0.0f);
-        float top = fmaxf(M, mz.x);
+    for (int w = w0 + (WARPS > 1 ? warp : 0); w <= w1; w += AHEAD * WARPS) {
+        float2 mz[AHEAD], y[AHEAD][NV];
 #pragma unroll
-        for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, k));
-        const float back = ex2(M - top), w = ex2(mz.x - top);
+        for (int i = 0; i < AHEAD; ++i) {
+            const int at = w + i * WARPS;
+            const float* part = a.partial + (((int64_t(at) * 2 + (at == w0 ? place0 : 0)) * a.team + member) * g + h) * (D + 2);
+            const bool ok = at <= w1;
+            mz[i] = ok ? *reinterpret_cast<const float2*>(part + D) : make_float2(kNone, 0.0f);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) y[i][k] = ok ? *reinterpret_cast<const float2*>(part + 2 * lane + 64 * k) : make_float2(0.0f, 0.0f);
+        }
+        float top = M;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) top = fmaxf(top, mz[i].x);
+        const float old = ex2(M - top);
         M = top;
-        den = den * back + w * mz.y;
+        den *= old;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            acc[k].x *= back;
-            acc[k].y *= back;
+            acc[k].x *= old;
+            acc[k].y *= old;
         }
-        const int cnt = min(32, n - s0);
-        for (int s = 0; s < cnt; ++s) {
-            if (__shfl_sync(kFull, mz.x, s) == kNone) continue;  // nothing was written for it
-            const float f = __shfl_sync(kFull, w, s);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const float f = ex2(mz[i].x - top);
+            den = fmaf(mz[i].y, f, den);
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                const float2 y = *reinterpret_cast<const float2*>(part + int64_t(s0 + s) * (D + 2) + 2 * lane + 64 * k);
-                acc[k].x = fmaf(f, y.x, acc[k].x);
-                acc[k].y = fmaf(f, y.y, acc[k].y);
+                acc[k].x = fmaf(y[i][k].x, f, acc[k].x);
+                acc[k].y = fmaf(y[i][k].y, f, acc[k].y);
             }
         }
     }
+    if constexpr (WARPS > 1) {
 #pragma unroll
-    for (int k = 16; k; k >>= 1) den += __shfl_xor_sync(kFull, den, k);
+        for (int k = 0; k < NV; ++k) s_acc[warp][lane + 32 * k] = acc[k];
+        if (lane == 0) {
+            s_top[warp] = M;
+            s_den[warp] = den;
+        }
+        __syncthreads();
+        if (warp > 0) return;
+        for (int w = 1; w < WARPS; ++w) {
+            const float top = fmaxf(M, s_top[w]), fa = ex2(M - top), fb = ex2(s_top[w] - top);
+            M = top;
+            den = den * fa + s_den[w] * fb;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                acc[k].x = acc[k].x * fa + s_acc[w][lane + 32 * k].x * fb;
+                acc[k].y = acc[k].y * fa + s_acc[w][lane + 32 * k].y * fb;
+            }
+        }
+    }
     const float inv = den == 0.0f ? 0.0f : 1.0f / den;
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-        *reinterpret_cast<float2*>(a.out + head * D + 2 * lane + 64 * k) = make_float2(acc[k].x * inv, acc[k].y * inv);
+    for (int k = 0; k < NV; ++k) *reinterpret_cast<float2*>(out + 2 * lane + 64 * k) = make_float2(acc[k].x * inv, acc[k].y * inv);
 }
 
 template <int FMT, int D>
 cudaError_t launch_fd(const DecodeQuantArgs& a, cudaStream_t stream) {
-    const size_t smem = size_t(a.warps) * a.group * (D + 4) * sizeof(float);
-    auto k = a.group <= 4 ? decode_quant_kernel<FMT, D, true> : decode_quant_kernel<FMT, D, false>;
-    cudaError_t e = smem > 48 * 1024 ? raise_smem_limit(reinterpret_cast<const void*>(k), smem) : cudaSuccess;
-    const int64_t heads = int64_t(a.n_seqs) * a.n_layers * a.n_kv_heads;
-    if (e == cudaSuccess) e = launch_pdl(k, dim3(unsigned(heads * a.splits)), dim3(a.warps * 32), smem, stream, a);
-    if (e != cudaSuccess || a.splits == 1) return e;
-    return launch_pdl(decode_quant_join_kernel<D>, dim3(unsigned((heads * a.group + 3) / 4)), dim3(128), 0, stream, a, heads * a.group);
+    using S = Shape<FMT, D>;
+    const bool pair = a.group <= 4;
+    const bool runs = (a.cache.kind == PRCR_CACHE_CONTIGUOUS || a.cache.block_size % 16 == 0) &&
+                      std::max(a.cache.slot_stride, a.cache.scale_slot_stride) < (int64_t(1) << 27);
+    const size_t smem = size_t(kCtaWarps) * S::warp_bytes(pair, a.group);
+    auto k = pair ? (runs ? decode_quant_kernel<FMT, D, true, true> : decode_quant_kernel<FMT, D, true, false>)
+                  : (runs ? decode_quant_kernel<FMT, D, false, true> : decode_quant_kernel<FMT, D, false, false>);
+    cudaError_t e = smem > 40 * 1024 ? raise_smem_limit(reinterpret_cast<const void*>(k), smem) : cudaSuccess;
+    if (e == cudaSuccess) e = launch_pdl(k, dim3(unsigned((a.teams * a.team + kCtaWarps - 1) / kCtaWarps)), dim3(kCtaWarps * 32), smem, stream, a);
+    if (e != cudaSuccess) return e;
+    const int64_t units = int64_t(a.n_seqs) * a.n_layers * a.head_sets, rows = int64_t(a.n_seqs) * a.n_layers * a.n_kv_heads * a.group;
+    return a.teams >= 8 * units ? launch_pdl(decode_quant_join_kernel<D, 4>, dim3(unsigned(rows)), dim3(128), 0, stream, a)
+                                : launch_pdl(decode_quant_join_kernel<D, 1>, dim3(unsigned((rows + 3) / 4)), dim3(128), 0, stream, a);
 }
 
 template <int FMT>
@@ -649,9 +939,13 @@ cudaError_t launch_decode_quant(const DecodeQuantArgs& a, cudaStream_t stream) {
     return a.format == PRCR_QFMT_E4M3 ? launch_f<PRCR_QFMT_E4M3>(a, stream) : launch_f<PRCR_QFMT_E2M1>(a, stream);
 }
 
+template <int FMT>
+int tile_of(int head_dim) {
+    return head_dim == 64 ? Shape<FMT, 64>::TS : head_dim == 128 ? Shape<FMT, 128>::TS : Shape<FMT, 256>::TS;
+}
+
 int decode_quant_tile(int format, int head_dim) {
-    const int bytes = format == PRCR_QFMT_E4M3 ? head_dim : head_dim / 2;
-    return bytes >= 128 ? 16 : 16 * (128 / bytes);
+    return format == PRCR_QFMT_E4M3 ? tile_of<PRCR_QFMT_E4M3>(head_dim) : tile_of<PRCR_QFMT_E2M1>(head_dim);
 }
 
 }  // namespace prcr
