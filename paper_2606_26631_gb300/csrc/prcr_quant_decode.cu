@@ -69,6 +69,14 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// The same from zero.
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
+
 // Transpose of an 8 x 8 matrix of 16-bit values held as mma fragments.
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     uint32_t y;
@@ -177,19 +185,23 @@ __device__ __forceinline__ int tiles_of(const DecodeQuantArgs& a, int b, int& le
     return (len + TS - 1) / TS;
 }
 
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {  // of numbers that are not negative, mostly small ones
+    return (a | b) >> 32 ? a / b : int64_t(uint32_t(a) / uint32_t(b));
+}
+
 // How `total` tiles are cut into the teams' shares: the first `more` have one tile more than the others.
 struct Cut {
     int64_t each, more;
     __device__ __forceinline__ int64_t begin_of(int w) const { return w * each + min(int64_t(w), more); }
     __device__ __forceinline__ int team_of(int64_t tile) const {
         const int64_t big = more * (each + 1);
-        return int(tile < big ? tile / (each + 1) : more + (tile - big) / each);
+        return int(tile < big ? quotient(tile, each + 1) : more + quotient(tile - big, each));
     }
 };
 __device__ __forceinline__ Cut cut_of(const DecodeQuantArgs& a, int64_t total) {
-    const int64_t teams = max(int64_t(1), min(int64_t(a.teams), total / kLeastTiles));
+    const int64_t teams = max(int64_t(1), min(int64_t(a.teams), quotient(total, kLeastTiles)));
     Cut c;
-    c.each = total / teams;
+    c.each = quotient(total, teams);
     c.more = total - c.each * teams;
     return c;
 }
@@ -207,10 +219,10 @@ __device__ __forceinline__ Share share_of(const DecodeQuantArgs& a, uint32_t& er
     Share s;
     s.team = warp / a.team;
     uint32_t e = 0;
-    int len;
+    int len, n = 0;
     int64_t sum = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
-        int n = b0 + lane < a.n_seqs ? tiles_of<TS>(a, b0 + lane, len, e) : 0;
+        n = b0 + lane < a.n_seqs ? tiles_of<TS>(a, b0 + lane, len, e) : 0;
         // (below 2^31 together: 2^30 slots each, sixteen to a tile, 32 of them)
         if (warp == 0) {  // for the kernel that joins
             int64_t upto = n;
@@ -231,7 +243,7 @@ __device__ __forceinline__ Share share_of(const DecodeQuantArgs& a, uint32_t& er
     if (s.begin >= s.end) return s;
     int64_t before = 0;  // tiles of a unit of the sequences passed
     for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
-        const int n = b0 + lane < a.n_seqs ? tiles_of<TS>(a, b0 + lane, len, e) : 0;
+        if (a.n_seqs > 32) n = b0 + lane < a.n_seqs ? tiles_of<TS>(a, b0 + lane, len, e) : 0;
         int upto = n;
         for (int k = 1; k < 32; k *= 2) {
             const int x = __shfl_up_sync(kFull, upto, k);
@@ -249,7 +261,7 @@ __device__ __forceinline__ Share share_of(const DecodeQuantArgs& a, uint32_t& er
         before += __shfl_sync(kFull, upto, 31);
     }
     const int64_t in = s.begin - before * per_seq;
-    s.unit = int(in / s.tiles);
+    s.unit = int(quotient(in, s.tiles));
     s.tile = int(in - int64_t(s.unit) * s.tiles);
     return s;
 }
@@ -263,6 +275,7 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
     constexpr bool kFour = S::kFour;
     constexpr int SUB = S::SUB, TS = S::TS, N = S::N, KW = S::KW, VW = S::VW, KP = S::KP, VP = S::VP, KS = S::KS, SW = S::SW, OWN = S::OWN;
     constexpr int P = D / 2, PITCH = D + 4, NP = PAIR ? 1 : 2, LS = PAIR ? 1 : 2;  // products for the pieces of a query or a weight, slots of a lane's logits
+    constexpr bool EARLY = !kFour;  // look places up a tile earlier than they are loaded from
     extern __shared__ __align__(16) float smem[];
     const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, gid = lane >> 2, t = lane & 3;
     const int H = a.n_kv_heads, g = a.group, per_seq = a.n_layers * a.head_sets;
@@ -342,9 +355,14 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
         for (int u = 0; u < SUB; ++u) rows[u] = 16;
         lay_out();
     }
+    const uint8_t *kb_at, *vb_at, *kf_at, *vf_at;  // at the rows of the unit that `place` is in
     auto places = [&]() {
         bool same = true;
         full = true;
+        kb_at = kb;
+        vb_at = vb;
+        kf_at = kf;
+        vf_at = vf;
 #pragma unroll
         for (int j = 0; j < LOOK; ++j) {
             const int s = looked(j);
@@ -367,6 +385,16 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
         } else {
             full = __all_sync(kFull, full);
         }
+        // towards the L2 cache, so that the loads, which hold registers, are short: a lane a slot's key or value
+#pragma unroll
+        for (int j = 0; j < (!EARLY ? 0 : RUNS ? SUB : 2 * OWN); ++j) {
+            const uint8_t* base = (RUNS ? lane < 16 : j % 2 == 0) ? kb : vb;
+            const int64_t at = RUNS ? place[j % LOOK].codes + (lane & 15) * int64_t(a.cache.slot_stride) : place[j / 2 % LOOK].codes;
+            const bool ok = RUNS ? (lane & 15) < rows[j % SUB] : at >= 0 && (TS > 16 || lane < 16);
+#pragma unroll
+            for (int c = 0; c < S::RB; c += 128)
+                if (ok) prefetch_l2(base + at + c);
+        }
     };
     uint32_t ks[OWN][SW], vs[OWN][SW];  // scales' bytes of slots lane + 32 j
     float bias[OWN];                    // added to their logits: 0, or -inf for a slot that is not there
@@ -383,8 +411,8 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
                 row = n > 0;
             }
             bias[j] = ok ? 0.0f : -INFINITY;
-            load_row_scales<N>(ks[j], kf + at, row);
-            load_row_scales<N>(vs[j], vf + at, row);
+            load_row_scales<N>(ks[j], kf_at + at, row);
+            load_row_scales<N>(vs[j], vf_at + at, row);
         }
     };
     uint32_t kw[SUB][2][KW], vw[SUB][4][VW];
@@ -393,7 +421,7 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
         for (int u = 0; u < SUB; ++u) {
             if (RUNS) {
                 if (rows[u] > 0) {
-                    const uint8_t* run = kb + place[u % LOOK].codes;
+                    const uint8_t* run = kb_at + place[u % LOOK].codes;
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -407,7 +435,7 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
                 for (int i = 0; i < 2; ++i) {
                     const int64_t at = __shfl_sync(kFull, place[u / 2 % LOOK].codes, (16 * u + gid + 8 * i) & 31);
 #pragma unroll
-                    for (int c = 0; c < KW / KP; ++c) load_words<KP>(kw[u][i] + KP * c, kb + at + k_off + 64 * c, at >= 0);
+                    for (int c = 0; c < KW / KP; ++c) load_words<KP>(kw[u][i] + KP * c, kb_at + at + k_off + 64 * c, at >= 0);
                 }
             }
         }
@@ -417,7 +445,7 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
         for (int u = 0; u < SUB; ++u) {
             if (RUNS) {
                 if (rows[u] > 0) {
-                    const uint8_t* run = vb + place[u % LOOK].codes;
+                    const uint8_t* run = vb_at + place[u % LOOK].codes;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -431,13 +459,31 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
                 for (int i = 0; i < 4; ++i) {
                     const int64_t at = __shfl_sync(kFull, place[u / 2 % LOOK].codes, (16 * u + 2 * t + (i & 1) + 8 * (i >> 1)) & 31);
 #pragma unroll
-                    for (int c = 0; c < VW / VP; ++c) load_words<VP>(vw[u][i] + VP * c, vb + at + v_off + 128 * c, at >= 0);
+                    for (int c = 0; c < VW / VP; ++c) load_words<VP>(vw[u][i] + VP * c, vb_at + at + v_off + 128 * c, at >= 0);
                 }
             }
         }
     };
 
-    // the first tile is requested before the query is read
+    // A group's query rows: a lane has pairs 2 (lane + 32 i) and the next of every head (D = 64: half of the lanes).
+    constexpr int G = PAIR ? 4 : 8, PR = P / 64 > 0 ? P / 64 : 1;
+    const bool has = P >= 64 || lane < P / 2;
+    uint32_t qx[G][PR], qy[G][PR];
+    auto load_query = [&](int b, int unit) {
+        const int layer = unit / a.head_sets, kh = min((unit - layer * a.head_sets) * a.team + member, H - 1);
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(a.q + ((int64_t(b) * a.n_layers + layer) * H + kh) * g * D) + lane;
+#pragma unroll
+        for (int h = 0; h < G; ++h)
+#pragma unroll
+            for (int i = 0; i < PR; ++i) {
+                const bool ok = has && h < g;
+                qx[h][i] = ok ? __ldg(q + h * P + 32 * i) : 0u;
+                qy[h][i] = ok ? __ldg(q + h * P + 32 * i + P / 2) : 0u;
+            }
+    };
+
+    // the first tile is requested before the query is worked on
+    load_query(share.b, share.unit);
     blocks();
     places();
     load_k();
@@ -446,6 +492,11 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
     bool whole_tile = full;  // of the tile that is loaded
     advance();
     blocks();
+    if (EARLY) {
+        places();
+        advance();
+        blocks();
+    }
 
     // the unit that is attended to
     int ub = share.b, uu = share.unit, first = share.tile, un = share.tiles;
@@ -458,8 +509,6 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
     float qs[2] = {0.0f, 0.0f};
     {
         // the group's queries, rotated at (p, p, p): pair i turns by p * rate i whatever its band
-        constexpr int PR = P / 64 > 0 ? P / 64 : 1;  // a lane has pairs 2 (lane + 32 i) and the next (D = 64: half of the lanes)
-        const bool has = P >= 64 || lane < P / 2;
         const double pos = double(a.q_pos[ub]);
         float cs[PR][2], sn[PR][2];
 #pragma unroll
@@ -467,18 +516,19 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 #pragma unroll
             for (int k = 0; k < 2; ++k)
                 if (has) sincos_turns(pos, a.turn_freq[2 * (lane + 32 * i) + k], &sn[i][k], &cs[i][k]);
-        for (int h = 0; h < g; ++h) {
-            const uint32_t* q = reinterpret_cast<const uint32_t*>(a.q + (head0 + h) * D) + lane;
+        if (!step0) load_query(ub, uu);
+#pragma unroll
+        for (int h = 0; h < G; ++h) {
+            if (h >= g) break;
             float x[PR][2], y[PR][2];
             uint32_t most = 0;
 #pragma unroll
             for (int i = 0; i < PR; ++i) {
-                const uint32_t wx = has ? __ldg(q + 32 * i) : 0u, wy = has ? __ldg(q + 32 * i + P / 2) : 0u;
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const float qx = k ? hi_f32(wx) : lo_f32(wx), qy = k ? hi_f32(wy) : lo_f32(wy);
-                    x[i][k] = has ? fmaf(qx, cs[i][k], -qy * sn[i][k]) * a.scale_log2 : 0.0f;
-                    y[i][k] = has ? fmaf(qy, cs[i][k], qx * sn[i][k]) * a.scale_log2 : 0.0f;
+                    const float u = k ? hi_f32(qx[h][i]) : lo_f32(qx[h][i]), v = k ? hi_f32(qy[h][i]) : lo_f32(qy[h][i]);
+                    x[i][k] = has ? fmaf(u, cs[i][k], -v * sn[i][k]) * a.scale_log2 : 0.0f;
+                    y[i][k] = has ? fmaf(v, cs[i][k], u * sn[i][k]) * a.scale_log2 : 0.0f;
                     most = max(most, max(__float_as_uint(x[i][k]) & 0x7fffffffu, __float_as_uint(y[i][k]) & 0x7fffffffu));
                 }
             }
@@ -548,12 +598,14 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
                 int top = 0;
 #pragma unroll
                 for (int i = 0; i < N; ++i) top = max(top, int((vs[j][i / 4] >> (8 * (i % 4))) & 255));
-                vx[j] = float(top - 127);
+                // (a byte behind the bits of 2^23 is 2^23 + byte)
+                const float most = __uint_as_float(0x4b000000u + top);
+                vx[j] = most - 8388735.0f;
 #pragma unroll
                 for (int i = 0; i < N; i += 2) {
                     kg[j][i / 2] = bf16_of_scales(ks[j][i / 4] >> (8 * (i % 4)));
-                    vg[j][i / 2] = pack_f16x2(ex2(float(int((vs[j][i / 4] >> (8 * (i % 4))) & 255) - top)),
-                                              ex2(float(int((vs[j][i / 4] >> (8 * (i % 4) + 8)) & 255) - top)));
+                    vg[j][i / 2] = pack_f16x2(ex2(__uint_as_float(__byte_perm(vs[j][i / 4], 0x4b000000u, 0x7650u + i % 4)) - most),
+                                              ex2(__uint_as_float(__byte_perm(vs[j][i / 4], 0x4b000000u, 0x7651u + i % 4)) - most));
                 }
             } else {
                 kx[j] = scale_value(int(ks[j][0]));
@@ -568,8 +620,6 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
             if constexpr (kFour) {
                 float c[N][4];
 #pragma unroll
-                for (int j = 0; j < N; ++j) c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0.0f;
-#pragma unroll
                 for (int i = 0; i < KW; ++i) {
                     uint32_t p[4], q[4];
                     f16_of_e2m1(kw[u][0][i], p);
@@ -579,10 +629,10 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 #pragma unroll
                         for (int z = 0; z < NP; ++z) {
                             const uint2 f = q_frag[((2 * i + e) * NP + z) * 32 + lane];
-                            mma_f16(c[(2 * i + e) % N], p[2 * e], q[2 * e], p[2 * e + 1], q[2 * e + 1], f.x, f.y);
+                            if (2 * i + e < N && z == 0) mma_f16_first(c[(2 * i + e) % N], p[2 * e], q[2 * e], p[2 * e + 1], q[2 * e + 1], f.x, f.y);
+                            else mma_f16(c[(2 * i + e) % N], p[2 * e], q[2 * e], p[2 * e + 1], q[2 * e + 1], f.x, f.y);
                         }
                 }
-                d[0] = d[1] = d[2] = d[3] = 0.0f;
 #pragma unroll
                 for (int k = 0; k < N / 2; ++k) {
                     const uint32_t wa = __shfl_sync(kFull, kg[u / 2][k], (16 * u + gid) & 31);
@@ -590,16 +640,15 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const float fa = e ? hi_f32(wa) : lo_f32(wa), fb = e ? hi_f32(wb) : lo_f32(wb);
-                        d[0] = fmaf(c[2 * k + e][0], fa, d[0]);
-                        d[1] = fmaf(c[2 * k + e][1], fa, d[1]);
-                        d[2] = fmaf(c[2 * k + e][2], fb, d[2]);
-                        d[3] = fmaf(c[2 * k + e][3], fb, d[3]);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            const float v = c[2 * k + e][y], f = y < 2 ? fa : fb;
+                            d[y] = k + e == 0 ? v * f : fmaf(v, f, d[y]);
+                        }
                     }
                 }
             } else {
                 float c[2][4];
-#pragma unroll
-                for (int z = 0; z < 2; ++z) c[z][0] = c[z][1] = c[z][2] = c[z][3] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < KW; ++i) {
                     uint32_t p[2], q[2];
@@ -608,7 +657,8 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 #pragma unroll
                     for (int z = 0; z < NP; ++z) {
                         const uint2 f = q_frag[(i * NP + z) * 32 + lane];
-                        mma_f16(c[(i + z) & 1], p[0], q[0], p[1], q[1], f.x, f.y);
+                        if (i + z < 2 && (i == 0 || NP == 1)) mma_f16_first(c[(i + z) & 1], p[0], q[0], p[1], q[1], f.x, f.y);
+                        else mma_f16(c[(i + z) & 1], p[0], q[0], p[1], q[1], f.x, f.y);
                     }
                 }
 #pragma unroll
@@ -635,7 +685,7 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
             }
         }
         // the keys' registers are free: the next tile's
-        places();
+        if (!EARLY) places();
         load_k();
         load_scales();
         whole_tile = full;
@@ -764,6 +814,7 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
             }
         }
         load_v();
+        if (EARLY) places();
         advance();
         blocks();
     }
