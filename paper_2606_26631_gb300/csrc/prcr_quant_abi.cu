@@ -132,13 +132,13 @@ int cast_setup(const prcr_rope_cfg* cfg, const prcr_cache_desc* wide, int32_t wi
     a->n_scales = scale_count(few, cfg->head_dim);
     a->pad = quantise ? power_of_two(cfg->head_dim / 8) : cfg->head_dim / 8;
     a->lanes = cfg->n_kv_heads * a->pad;
-    a->tok_per_cta = std::max(1, 256 / a->lanes);
+    a->tok_per_cta = std::max(1, std::min({64, int(max_count), (quantise ? 512 : 1024) / a->lanes}));  // two or four of a thread's
     a->units = a->tok_per_cta * a->lanes;
     if (quantise) a->units = (a->units + 31) / 32 * 32;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return PRCR_ECUDA;
     const int64_t tiles = std::max<int64_t>(1, (int64_t(max_count) + a->tok_per_cta - 1) / a->tok_per_cta);
-    a->layers_per_cta = layers_per_cta(tiles * n_seqs, n_layers, int64_t(sm_count(dev)) * 8, 8);
+    a->layers_per_cta = layers_per_cta(tiles * n_seqs, n_layers, int64_t(sm_count(dev)) * 8, 9);
     *grid = dim3(unsigned(tiles), unsigned((n_layers + a->layers_per_cta - 1) / a->layers_per_cta), unsigned(n_seqs));
     *go = true;
     return PRCR_OK;
@@ -197,11 +197,11 @@ int prcr_append_kv_quant(const prcr_rope_cfg* cfg, const prcr_qcache_desc* cache
     a.sec_w = cfg->sections[2];
     copy_turn_freq(cfg, a.turn_freq);
     const int T = a.tok_per_cta, block = (T * a.lanes + 31) / 32 * 32;
-    const size_t smem = size_t(T) * (cfg->head_dim * sizeof(float) + 2 * sizeof(int64_t));
+    const size_t smem = size_t(T) * (2 * cfg->head_dim * sizeof(float) + 2 * sizeof(int64_t));
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return PRCR_ECUDA;
     const int64_t tiles = std::max<int64_t>(1, (int64_t(total) + T - 1) / T);
-    a.layers_per_cta = layers_per_cta(tiles, n_layers, int64_t(sm_count(dev)) * 4, 8);
+    a.layers_per_cta = layers_per_cta(tiles, n_layers, int64_t(sm_count(dev)) * 3, 16);
     const dim3 grid(unsigned(tiles), unsigned((n_layers + a.layers_per_cta - 1) / a.layers_per_cta),
                     unsigned((cfg->n_kv_heads + heads - 1) / heads));
     return status_of(launch_append_quant(a, grid, block, smem, static_cast<cudaStream_t>(stream)));

@@ -3,10 +3,9 @@
 // back (dequantize_kernel).
 //
 // Memory-bound, every row read once and written once. Neighbouring lanes hold
-// neighbouring 16 bytes of bf16 of one head's row, a group's largest magnitude is
-// a butterfly over the lanes that hold it, and a thread walks its layers with the
-// next one's rows requested before the current ones are converted. Padding a
-// head's lanes to a power of two keeps E4M3's butterflies inside a warp.
+// neighbouring 16 bytes of bf16 of one head's row, and a group's largest magnitude is
+// a butterfly over the lanes that hold it. Padding a head's lanes to a power of two
+// keeps E4M3's butterflies inside a warp.
 #include "prcr_pdl.cuh"
 #include "prcr_quant.cuh"
 
@@ -20,7 +19,22 @@ __device__ __forceinline__ uint32_t lane_max(uint32_t x, int lanes, int step) {
     return x;
 }
 
-__device__ __forceinline__ uint32_t float_abs(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// The larger magnitude, or NaN.
+__device__ __forceinline__ float abs_max(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+__device__ __forceinline__ uint32_t quad_max(const float* x) {
+    return __float_as_uint(abs_max(abs_max(x[0], x[1]), abs_max(x[2], x[3]))) & 0x7fffffffu;
+}
+
+// The largest magnitude of two words' bf16 values, as float32 bits (an infinity's or more for NaN, which
+// are the largest numbers of 15 bits).
+__device__ __forceinline__ uint32_t pair_max(uint32_t a, uint32_t b) {
+    const uint32_t m = __vmaxu2(a & 0x7fff7fffu, b & 0x7fff7fffu);
+    return max(m << 16, m & 0xffff0000u);
+}
 
 // x[0..n) times 2^(127 - byte), held below the code that is 2^128 (QFormat::kHighest); zeros in
 // a group that reads as NaN.
@@ -28,35 +42,59 @@ template <int FMT, int N>
 __device__ __forceinline__ void to_units(float* x, int byte) {
     const float f = __uint_as_float(uint32_t(254 - byte) << 23);  // 2^-126 at least: byte <= 253
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = byte == kScaleNan ? 0.0f : x[i] * f;
-    if (byte == QFormat<FMT>::kHighest) {
+    for (int i = 0; i < N; ++i) x[i] *= f;
+    if (byte >= QFormat<FMT>::kHighest) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = fminf(fmaxf(x[i], -QFormat<FMT>::kHighestTop), QFormat<FMT>::kHighestTop);
+        for (int i = 0; i < N; ++i)
+            x[i] = byte == kScaleNan ? 0.0f : fminf(fmaxf(x[i], -QFormat<FMT>::kHighestTop), QFormat<FMT>::kHighestTop);
     }
 }
 
-// The codes of eight dims, whose quads have these bytes (E4M3: the same), at p.
+// The codes of eight dims in units of their scales.
 template <int FMT>
-__device__ __forceinline__ void store_codes(uint8_t* p, float (&x)[8], int byte0, int byte1) {
+__device__ __forceinline__ uint2 codes8(const float (&x)[8]) {
+    if (FMT == PRCR_QFMT_E4M3) return make_uint2(codes_e4m3(x[0], x[1], x[2], x[3]), codes_e4m3(x[4], x[5], x[6], x[7]));
+    return make_uint2(codes_e2m1(x), 0);
+}
+template <int FMT>
+__device__ __forceinline__ void store_codes(uint8_t* p, uint2 c) {
+    if (FMT == PRCR_QFMT_E4M3) *reinterpret_cast<uint2*>(p) = c;
+    else *reinterpret_cast<uint32_t*>(p) = c.x;
+}
+
+template <int FMT>
+__device__ __forceinline__ void to_units8(float (&x)[8], int byte0, int byte1) {
     if (FMT == PRCR_QFMT_E4M3) {
         to_units<FMT, 8>(x, byte0);
-        *reinterpret_cast<uint2*>(p) = make_uint2(codes_e4m3(x[0], x[1], x[2], x[3]), codes_e4m3(x[4], x[5], x[6], x[7]));
     } else {
         to_units<FMT, 4>(x, byte0);
         to_units<FMT, 4>(x + 4, byte1);
-        *reinterpret_cast<uint32_t*>(p) = codes_e2m1(x);
     }
 }
 
-__device__ __forceinline__ void unpack8(const uint4& w, float (&x)[8]) {
-    x[0] = lo_f32(w.x); x[1] = hi_f32(w.x); x[2] = lo_f32(w.y); x[3] = hi_f32(w.y);
-    x[4] = lo_f32(w.z); x[5] = hi_f32(w.z); x[6] = lo_f32(w.w); x[7] = hi_f32(w.w);
+// Eight dims of bf16 whose quads have these bytes (E4M3: the same).
+template <int FMT>
+__device__ __forceinline__ void store_rounded(uint8_t* p, const uint4& w, int byte0, int byte1) {
+    float x[8] = {lo_f32(w.x), hi_f32(w.x), lo_f32(w.y), hi_f32(w.y), lo_f32(w.z), hi_f32(w.z), lo_f32(w.w), hi_f32(w.w)};
+    to_units8<FMT>(x, byte0, byte1);
+    store_codes<FMT>(p, codes8<FMT>(x));
 }
 
-// Largest magnitudes of the first and the second four, as float32 bits.
-__device__ __forceinline__ void quad_max(const float (&x)[8], uint32_t& a, uint32_t& b) {
-    a = max(max(float_abs(x[0]), float_abs(x[1])), max(float_abs(x[2]), float_abs(x[3])));
-    b = max(max(float_abs(x[4]), float_abs(x[5])), max(float_abs(x[6]), float_abs(x[7])));
+// Scales' bytes of a lane's two quads, given their largest magnitudes; lanes that share a group are `step` apart.
+template <int FMT>
+__device__ __forceinline__ void group_bytes(uint32_t a, uint32_t b, int lanes, int step, int& byte0, int& byte1) {
+    if (FMT == PRCR_QFMT_E4M3) {
+        byte0 = byte1 = scale_byte<FMT>(lane_max(max(a, b), lanes, 1));
+    } else {
+        byte0 = scale_byte<FMT>(lane_max(a, lanes, step));
+        byte1 = scale_byte<FMT>(lane_max(b, lanes, step));
+    }
+}
+
+template <int FMT>
+__device__ __forceinline__ void store_scales(uint8_t* row, int v, int byte0, int byte1) {
+    if (FMT == PRCR_QFMT_E4M3) *row = uint8_t(byte0);
+    else *reinterpret_cast<uint16_t*>(row + 2 * v) = uint16_t(byte0 | byte1 << 8);
 }
 
 // ----------------------------------------------------------------------------
@@ -65,13 +103,73 @@ __device__ __forceinline__ void quad_max(const float (&x)[8], uint32_t& a, uint3
 // One thread: eight dims of a head's first half and the eight that they rotate with,
 // of K and of V. A head has `pad` threads, a power of two; E2M1's quads repeat their
 // groups in the second half, so one butterfly serves both.
+//
+// Keys get the codes that are nearest to the exact rotation. Its cos and sin are pairs of floats, the first of 16
+// bits, so that a bf16 number's products with it are exact: x cos - y sin, of two such products and two small
+// ones, is off by three roundings of 2^-24 of itself, whatever cancels. Only where 2^-20 of itself would change
+// its code (once in 40,000 values) is a value computed again in float64.
+
+// sin and cos of 2^-64 f turns, each as the sum of two floats, off by some 2^-32: Taylor's series about the nearest
+// quarter turn, the first terms' products and sums with their rounding errors (by fused multiply-adds).
+__device__ __forceinline__ void sincos_pair(uint64_t f, float2& sine, float2& cosine) {
+    const uint64_t g = f + (1ull << 61);
+    const int quarter = int(g >> 62);
+    const int64_t rest = int64_t(g & ((1ull << 62) - 1)) - (int64_t(1) << 61);  // from it, 2^61 an eighth of a turn
+    const float rh = float(rest), rl = float(rest - int64_t(rh));
+    const float uh = rh * 0x1p-61f, ul = rl * 0x1p-61f;
+    constexpr float kPh = 0.785398185253143310546875f, kPl = -2.18556941e-8f;  // pi / 4
+    float th = uh * kPh;
+    float tl = fmaf(uh, kPh, -th) + fmaf(uh, kPl, ul * kPh);
+    const float zh = th * th, zl = fmaf(th, th, -zh) + 2.0f * th * tl;
+    // sin t = t - t z / 6 + t z^2 (1/120 - z/5040 + z^2/362880 - ...), z = t^2
+    constexpr float k6h = 0.16666667163372039794921875f, k6l = -4.96705376e-9f;  // 1 / 6
+    const float qh = th * zh, ql = fmaf(th, zh, -qh) + fmaf(th, zl, tl * zh);
+    const float ah = qh * k6h, al = fmaf(qh, k6h, -ah) + fmaf(qh, k6l, ql * k6h);
+    const float w = qh * zh * fmaf(zh, fmaf(zh, fmaf(zh, -2.50521084e-8f, 2.75573192e-6f), -1.98412698e-4f), 8.33333333e-3f);
+    const float s1 = th - ah, sl = ((th - s1) - ah) + ((tl - al) + w);
+    // cos t = 1 - z/2 + z^2/24 - z^3 (1/720 - z/40320 + z^2/3628800 - ...)
+    constexpr float k24h = 0.041666667908430099487305f, k24l = -1.24176344e-9f;  // 1 / 24
+    const float yh = zh * zh, yl = fmaf(zh, zh, -yh) + 2.0f * zh * zl;
+    const float dh = yh * k24h, dl = fmaf(yh, k24h, -dh) + fmaf(yh, k24l, yl * k24h);
+    const float v = -yh * zh * fmaf(zh, fmaf(zh, fmaf(zh, -2.08767570e-9f, 2.75573192e-7f), -2.48015873e-5f), 1.38888889e-3f);
+    const float bh = 0.5f * zh, c1 = 1.0f - bh, c2 = c1 + dh;
+    const float cl = ((1.0f - c1) - bh) + ((c1 - c2) + dh) + ((dl - 0.5f * zl) + v);
+    // the first part's leading 16 bits, the second with what that leaves
+    auto cut = [](float a, float b) {
+        const float h = __uint_as_float(__float_as_uint(a + b) & 0xffffff00u);
+        return make_float2(h, (a - h) + b);
+    };
+    float2 s = cut(s1, sl), c = cut(c2, cl);
+    if (quarter & 1) {
+        const float2 x = s;
+        s = c;
+        c = make_float2(-x.x, -x.y);
+    }
+    if (quarter & 2) {
+        s = make_float2(-s.x, -s.y);
+        c = make_float2(-c.x, -c.y);
+    }
+    sine = s;
+    cosine = c;
+}
+
+// The exact a cos - b sin (second: b cos + a sin) in units of the scale, rounded to odd: any border between codes, of
+// few bits, lies on the same side of it.
+__device__ __noinline__ float settled(float a, float b, bool second, int32_t pos, uint64_t turn_freq, float unit) {
+    double s, c;
+    sincospi(double(int64_t(uint64_t(int64_t(pos)) * turn_freq)) * 0x1p-63, &s, &c);
+    const double exact = (second ? double(b) * c + double(a) * s : double(a) * c - double(b) * s) * unit;
+    const float f = __double2float_rz(exact);
+    return __uint_as_float(__float_as_uint(f) | (double(f) != exact));
+}
+
 template <int FMT>
-__global__ void __launch_bounds__(256) append_quant_kernel(const __grid_constant__ AppendQuantArgs a) {
+__global__ void __launch_bounds__(256, 3) append_quant_kernel(const __grid_constant__ AppendQuantArgs a) {
     extern __shared__ __align__(16) float smem[];
     const int P = a.head_dim >> 1, T = a.tok_per_cta;
-    float* cos_s = smem;
-    float* sin_s = smem + T * P;
-    QPlace* place_s = reinterpret_cast<QPlace*>(sin_s + T * P);
+    // cos and sin of the tokens' pairs: first parts, then second ones
+    float* turn_s[4] = {smem, smem + T * P, smem + 2 * T * P, smem + 3 * T * P};
+    QPlace* place_s = reinterpret_cast<QPlace*>(smem + 4 * T * P);
     const int tok0 = blockIdx.x * T;
     const int my_t = threadIdx.x / a.lanes;
     const int lane = threadIdx.x - my_t * a.lanes;
@@ -83,15 +181,14 @@ __global__ void __launch_bounds__(256) append_quant_kernel(const __grid_constant
     const uint16_t* sk = a.src_k + s_off;
     const uint16_t* sv = a.src_v + s_off;
     uint4 k0 = {}, k1 = {}, v0 = {}, v1 = {};
-    auto load = [&]() {
+    pdl_allow();
+    pdl_wait();
+    if (act) {
         k0 = ld_stream(sk);
         k1 = ld_stream(sk + P);
         v0 = ld_stream(sv);
         v1 = ld_stream(sv + P);
-    };
-    pdl_allow();
-    pdl_wait();
-    if (act) load();
+    }
 
     // the tokens' places: a warp finds a token's sequence with 32 probes a round
     uint32_t err = 0;
@@ -114,13 +211,15 @@ __global__ void __launch_bounds__(256) append_quant_kernel(const __grid_constant
     }
     for (int q = threadIdx.x; q < T * P; q += blockDim.x) {
         const int t = q / P, i = q - t * P, j = tok0 + t;
-        float c = 1.0f, s = 0.0f;
+        float2 c = make_float2(1.0f, 0.0f), s = make_float2(0.0f, 0.0f);
         if (j < a.total) {
             const int ax = pair_axis(i, a.layout, a.sec_t, a.sec_h, a.sec_w);
-            sincos_turns(double(a.coords[3 * int64_t(j) + ax]), a.turn_freq[i], &s, &c);
+            sincos_pair(uint64_t(int64_t(a.coords[3 * int64_t(j) + ax])) * a.turn_freq[i], s, c);
         }
-        cos_s[q] = c;
-        sin_s[q] = s;
+        turn_s[0][q] = c.x;
+        turn_s[1][q] = s.x;
+        turn_s[2][q] = c.y;
+        turn_s[3][q] = s.y;
     }
     const bool bad = __syncthreads_or(bad_offsets(a.tok_off, a.n_seqs, a.total));
     if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) {
@@ -131,17 +230,8 @@ __global__ void __launch_bounds__(256) append_quant_kernel(const __grid_constant
     if (bad) return;
     if (err && blockIdx.y == 0 && (threadIdx.x & 31) == 0) atomicOr(a.status, err);
     QPlace dst = {-1, 0};
-    float c[8] = {}, s[8] = {};
-    if (act) {
-        dst = place_s[my_t];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const float4 c4 = *reinterpret_cast<const float4*>(cos_s + my_t * P + v * 8 + 4 * u);
-            const float4 s4 = *reinterpret_cast<const float4*>(sin_s + my_t * P + v * 8 + 4 * u);
-            c[4 * u] = c4.x; c[4 * u + 1] = c4.y; c[4 * u + 2] = c4.z; c[4 * u + 3] = c4.w;
-            s[4 * u] = s4.x; s[4 * u + 1] = s4.y; s[4 * u + 2] = s4.z; s[4 * u + 3] = s4.w;
-        }
-    }
+    if (act) dst = place_s[my_t];
+    const float* turn = smem + (act ? my_t * P + v * 8 : 0);
     const bool write = dst.codes >= 0;
     constexpr int B8 = QFormat<FMT>::kBytes8;
     const int n = a.n_scales;  // of a head
@@ -151,51 +241,85 @@ __global__ void __launch_bounds__(256) append_quant_kernel(const __grid_constant
     const int half = P / 8 * B8;
     // lanes that share a group: E4M3 all of the head's, E2M1 every n/2-th
     const int step = FMT == PRCR_QFMT_E4M3 ? 1 : n >> 1;
-    const bool keeps = v < step;  // stores its quads' scales
+    const bool keeps = write && v < step;  // stores its quads' scales
     for (int l = l0; l < l1; ++l) {
-        float x0[8], x1[8], y0[8], y1[8];
-        unpack8(k0, x0);
-        unpack8(k1, x1);
-        unpack8(v0, y0);
-        unpack8(v1, y1);
         sk += a.src_layer_stride;
         sv += a.src_layer_stride;
-        if (act && l + 1 < l1) load();
+        const bool more = act && l + 1 < l1;
+        {
+            const uint4 w0 = v0, w1 = v1;
+            if (more) {
+                v0 = ld_stream(sv);
+                v1 = ld_stream(sv + P);
+            }
+            int b0, b1;
+            group_bytes<FMT>(max(pair_max(w0.x, w0.y), pair_max(w1.x, w1.y)), max(pair_max(w0.z, w0.w), pair_max(w1.z, w1.w)), a.pad, step, b0, b1);
+            if (write) {
+                store_rounded<FMT>(cv, w0, b0, b1);
+                store_rounded<FMT>(cv + half, w1, b0, b1);
+            }
+            if (keeps) store_scales<FMT>(fv, v, b0, b1);
+        }
+        const uint4 w0 = k0, w1 = k1;
+        if (more) {
+            k0 = ld_stream(sk);
+            k1 = ld_stream(sk + P);
+        }
+        float x[8] = {lo_f32(w0.x), hi_f32(w0.x), lo_f32(w0.y), hi_f32(w0.y), lo_f32(w0.z), hi_f32(w0.z), lo_f32(w0.w), hi_f32(w0.w)};
+        float y[8] = {lo_f32(w1.x), hi_f32(w1.x), lo_f32(w1.y), hi_f32(w1.y), lo_f32(w1.z), hi_f32(w1.z), lo_f32(w1.w), hi_f32(w1.w)};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float p = fmaf(x0[i], c[i], -x1[i] * s[i]);
-            x1[i] = fmaf(x1[i], c[i], x0[i] * s[i]);
-            x0[i] = p;
-        }
-        int bk[2], bv[2];
-        auto bytes = [&](const float (&p)[8], const float (&q)[8], int (&out)[2]) {
-            uint32_t a0, a1, b0, b1;
-            quad_max(p, a0, a1);
-            quad_max(q, b0, b1);
-            if (FMT == PRCR_QFMT_E4M3) {
-                out[0] = out[1] = scale_byte<FMT>(lane_max(max(max(a0, b0), max(a1, b1)), a.pad, 1));
-            } else {
-                out[0] = scale_byte<FMT>(lane_max(max(a0, b0), a.pad, step));
-                out[1] = scale_byte<FMT>(lane_max(max(a1, b1), a.pad, step));
+        for (int u = 0; u < 8; u += 2) {
+            const float2 c = *reinterpret_cast<const float2*>(turn + u), s = *reinterpret_cast<const float2*>(turn + T * P + u);
+            const float2 cl = *reinterpret_cast<const float2*>(turn + 2 * T * P + u), sl = *reinterpret_cast<const float2*>(turn + 3 * T * P + u);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float p = x[u + i], q = y[u + i];
+                const float ci = i ? c.y : c.x, si = i ? s.y : s.x, cli = i ? cl.y : cl.x, sli = i ? sl.y : sl.x;
+                x[u + i] = fmaf(p, ci, -q * si) + fmaf(p, cli, -q * sli);
+                y[u + i] = fmaf(q, ci, p * si) + fmaf(q, cli, p * sli);
             }
-        };
-        bytes(x0, x1, bk);
-        bytes(y0, y1, bv);
+        }
+        int b0, b1;
+        group_bytes<FMT>(max(quad_max(x), quad_max(y)), max(quad_max(x + 4), quad_max(y + 4)), a.pad, step, b0, b1);
         if (write) {
-            store_codes<FMT>(ck, x0, bk[0], bk[1]);
-            store_codes<FMT>(ck + half, x1, bk[0], bk[1]);
-            store_codes<FMT>(cv, y0, bv[0], bv[1]);
-            store_codes<FMT>(cv + half, y1, bv[0], bv[1]);
-            if (keeps) {
-                if (FMT == PRCR_QFMT_E4M3) {
-                    *fk = uint8_t(bk[0]);
-                    *fv = uint8_t(bv[0]);
-                } else {
-                    *reinterpret_cast<uint16_t*>(fk + 2 * v) = uint16_t(bk[0] | bk[1] << 8);
-                    *reinterpret_cast<uint16_t*>(fv + 2 * v) = uint16_t(bv[0] | bv[1] << 8);
+            to_units8<FMT>(x, b0, b1);
+            to_units8<FMT>(y, b0, b1);
+            constexpr float kLess = 1.0f - 0x1p-20f, kMore = 1.0f + 0x1p-20f;
+            float z[8];
+            auto times = [&](const float (&w)[8], float f) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[i] = w[i] * f;
+                return codes8<FMT>(z);
+            };
+            uint2 cx = times(x, kLess), cy = times(y, kLess);
+            const uint2 mx = times(x, kMore), my = times(y, kMore);
+            if (cx.x != mx.x || cx.y != mx.y || cy.x != my.x || cy.y != my.y) {
+                const uint32_t wx[4] = {w0.x, w0.y, w0.z, w0.w}, wy[4] = {w1.x, w1.y, w1.z, w1.w};
+                constexpr int BITS = FMT == PRCR_QFMT_E4M3 ? 8 : 4;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const bool second = BITS == 8 && i >= 4;
+                    const int shift = BITS * i % 32;
+                    const bool nx = ((second ? cx.y ^ mx.y : cx.x ^ mx.x) >> shift) & ((1u << BITS) - 1);
+                    const bool ny = ((second ? cy.y ^ my.y : cy.x ^ my.x) >> shift) & ((1u << BITS) - 1);
+                    if (nx || ny) {
+                        const float p = i & 1 ? hi_f32(wx[i / 2]) : lo_f32(wx[i / 2]), q = i & 1 ? hi_f32(wy[i / 2]) : lo_f32(wy[i / 2]);
+                        const int32_t pos = a.coords[3 * int64_t(my_j) + pair_axis(v * 8 + i, a.layout, a.sec_t, a.sec_h, a.sec_w)];
+                        const int byte = i < 4 ? b0 : b1;
+                        if (byte < QFormat<FMT>::kHighest) {
+                            const float unit = __uint_as_float(uint32_t(254 - byte) << 23);
+                            if (nx) x[i] = settled(p, q, false, pos, a.turn_freq[v * 8 + i], unit);
+                            if (ny) y[i] = settled(p, q, true, pos, a.turn_freq[v * 8 + i], unit);
+                        }
+                    }
                 }
+                cx = codes8<FMT>(x);
+                cy = codes8<FMT>(y);
             }
+            store_codes<FMT>(ck, cx);
+            store_codes<FMT>(ck + half, cy);
         }
+        if (keeps) store_scales<FMT>(fk, v, b0, b1);
         ck += a.cache.layer_stride;
         cv += a.cache.layer_stride;
         fk += a.cache.scale_layer_stride;
@@ -206,100 +330,112 @@ __global__ void __launch_bounds__(256) append_quant_kernel(const __grid_constant
 // ----------------------------------------------------------------------------
 // slots of one cache into the other
 // ----------------------------------------------------------------------------
-// Token i of sequence b: from slot src_begin[b] + i to slot dst_begin[b] + i. A thread has
-// eight dims of a head; all of a token's threads look its rows up, at the same addresses.
+// Token i of sequence b: from slot src_begin[b] + i to slot dst_begin[b] + i. A CTA looks its tokens' rows up once; then a
+// thread has eight dims of a head of several tokens, requested together, layer by layer.
+constexpr int kCastThreads = 256;
+constexpr int kQuantTokens = 2, kReadTokens = 4;  // of a thread's
+constexpr int kCastMaxTokens = 64;  // of a CTA's
 struct CastRow {
-    int64_t row;   // of the bf16 cache, elements
+    int64_t row;   // of the bf16 cache, elements, or -1
     QPlace place;  // of the quantised one
 };
 
 template <bool READ>
 __device__ __forceinline__ CastRow cast_row(const CastArgs& a, int b, int i, uint32_t& err) {
-    CastRow r = {-1, {-1, 0}};
     const int count = a.count[b];
+    const int64_t s = a.src_begin[b], d = a.dst_begin[b];
     if ((count < 0 || count > a.max_count) && i == 0) err |= PRCR_ST_CAPACITY;
-    if (i >= count) return r;
-    const int64_t s = a.src_begin[b], d = a.dst_begin[b];  // (a negative one is refused by the lookups for its own slots)
-    const int64_t wide = READ ? d : s, few = READ ? s : d;
-    if (s < 0 || d < 0) {
+    CastRow r = {-1, {-1, 0}};
+    if (i >= count || i >= a.max_count) return r;
+    const int64_t wide = (READ ? d : s) + i, few = (READ ? s : d) + i, top = int64_t(1) << 31;  // (slots are counted in an int32)
+    if (s < 0 || d < 0 || wide >= min(a.wide.capacity, top) || few >= min(a.few.capacity, top)) {
         err |= PRCR_ST_CAPACITY;
         return r;
     }
-    r.row = slot_row(a.wide, b, wide + i, err);
-    r.place = qplace(a.few, b, few + i, err);
-    if (r.row < 0 || r.place.codes < 0) r.row = r.place.codes = -1;
+    // both tables are asked at once
+    const int32_t wide_blk = a.wide.kind == PRCR_CACHE_CONTIGUOUS ? 0 : a.wide.block_table[int64_t(b) * a.wide.bt_stride + block_index(a.wide, uint32_t(wide))];
+    const int32_t few_blk = qblock(a.few, b, uint32_t(few));
+    r.row = row_in_block(a.wide, b, uint32_t(wide), wide_blk);
+    r.place = qplace_in_block(a.few, b, uint32_t(few), few_blk);
+    if (r.row < 0 || r.place.codes < 0) {
+        err |= PRCR_ST_NO_BLOCK;
+        r.row = -1;
+    }
     return r;
 }
 
-template <int FMT>
-__global__ void __launch_bounds__(256) quantize_kernel(const __grid_constant__ CastArgs a) {
-    const int b = blockIdx.z, l0 = blockIdx.y * a.layers_per_cta, l1 = min(l0 + a.layers_per_cta, a.n_layers);
-    const int tok0 = blockIdx.x * a.tok_per_cta;
-    constexpr int B8 = QFormat<FMT>::kBytes8;
-    const int n = a.n_scales, step = FMT == PRCR_QFMT_E4M3 ? 1 : n >> 1;
+// The CTA's tokens' rows; false where none of them is to be moved.
+template <bool READ>
+__device__ __forceinline__ bool cast_rows(const CastArgs& a, int b, int tok0, CastRow* rows) {
     uint32_t err = 0;
-    pdl_allow();
-    pdl_wait();
-    if (tok0 >= a.count[b] && tok0 > 0) return;
-    // (whole warps: a head's lanes are a power of two)
-    for (int u = threadIdx.x; u < a.units; u += blockDim.x) {
-        const int t = u / a.lanes, lane = u - t * a.lanes, h = lane / a.pad, v = lane & (a.pad - 1), i = tok0 + t;
-        CastRow r = {-1, {-1, 0}};
-        if (t < a.tok_per_cta && i < a.max_count) r = cast_row<false>(a, b, i, err);
-        const bool act = r.row >= 0 && v < (a.head_dim >> 3);
-        const int64_t off = r.row + int64_t(l0) * a.wide.layer_stride + int64_t(h) * a.head_dim + v * 8;
-        const uint16_t *sk = a.wide.k + off, *sv = a.wide.v + off;
-        const int64_t c_off = r.place.codes + int64_t(l0) * a.few.layer_stride + int64_t(h) * (a.head_dim / 8 * B8) + v * B8;
-        const int64_t f_off = r.place.scales + int64_t(l0) * a.few.scale_layer_stride + int64_t(h) * n;
-        uint8_t *ck = a.few.k + c_off, *cv = a.few.v + c_off, *fk = a.few.k_scale + f_off, *fv = a.few.v_scale + f_off;
-        uint4 wk = {}, wv = {};
-        if (act) {
-            wk = ld_stream(sk);
-            wv = ld_stream(sv);
-        }
-        for (int l = l0; l < l1; ++l) {
-            float x[8], y[8];
-            unpack8(wk, x);
-            unpack8(wv, y);
-            sk += a.wide.layer_stride;
-            sv += a.wide.layer_stride;
-            if (act && l + 1 < l1) {
-                wk = ld_stream(sk);
-                wv = ld_stream(sv);
-            }
-            uint32_t x0, x1, y0, y1;
-            quad_max(x, x0, x1);
-            quad_max(y, y0, y1);
-            int bk[2], bv[2];
-            if (FMT == PRCR_QFMT_E4M3) {
-                bk[0] = bk[1] = scale_byte<FMT>(lane_max(max(x0, x1), a.pad, 1));
-                bv[0] = bv[1] = scale_byte<FMT>(lane_max(max(y0, y1), a.pad, 1));
-            } else {
-                bk[0] = scale_byte<FMT>(lane_max(x0, a.pad, step));
-                bk[1] = scale_byte<FMT>(lane_max(x1, a.pad, step));
-                bv[0] = scale_byte<FMT>(lane_max(y0, a.pad, step));
-                bv[1] = scale_byte<FMT>(lane_max(y1, a.pad, step));
-            }
-            if (act) {
-                store_codes<FMT>(ck, x, bk[0], bk[1]);
-                store_codes<FMT>(cv, y, bv[0], bv[1]);
-                if (v < step) {
-                    if (FMT == PRCR_QFMT_E4M3) {
-                        *fk = uint8_t(bk[0]);
-                        *fv = uint8_t(bv[0]);
-                    } else {
-                        *reinterpret_cast<uint16_t*>(fk + 2 * v) = uint16_t(bk[0] | bk[1] << 8);
-                        *reinterpret_cast<uint16_t*>(fv + 2 * v) = uint16_t(bv[0] | bv[1] << 8);
-                    }
-                }
-            }
-            ck += a.few.layer_stride;
-            cv += a.few.layer_stride;
-            fk += a.few.scale_layer_stride;
-            fv += a.few.scale_layer_stride;
-        }
+    bool any = false;
+    for (int t = threadIdx.x; t < a.tok_per_cta; t += blockDim.x) {
+        const CastRow r = cast_row<READ>(a, b, tok0 + t, err);
+        rows[t] = r;
+        any |= r.row >= 0;
     }
     if (err && blockIdx.y == 0) atomicOr(a.status, err);
+    return __syncthreads_or(any);
+}
+
+template <int FMT>
+__global__ void __launch_bounds__(kCastThreads, 4) quantize_kernel(const __grid_constant__ CastArgs a) {
+    __shared__ CastRow rows[kCastMaxTokens];
+    const int b = blockIdx.z, l0 = blockIdx.y * a.layers_per_cta, l1 = min(l0 + a.layers_per_cta, a.n_layers);
+    constexpr int B8 = QFormat<FMT>::kBytes8;
+    const int n = a.n_scales, step = FMT == PRCR_QFMT_E4M3 ? 1 : n >> 1;
+    pdl_allow();
+    pdl_wait();
+    if (!cast_rows<false>(a, b, blockIdx.x * a.tok_per_cta, rows)) return;
+    // (whole warps: a head's lanes are a power of two)
+    for (int u0 = threadIdx.x; u0 < a.units; u0 += kQuantTokens * kCastThreads) {
+        uint4 wk[kQuantTokens], wv[kQuantTokens];
+        int64_t from[kQuantTokens];
+        QPlace to[kQuantTokens];
+        int v[kQuantTokens];
+        bool act[kQuantTokens];
+#pragma unroll
+        for (int k = 0; k < kQuantTokens; ++k) {
+            const int u = u0 + k * kCastThreads, t = u / a.lanes, lane = u - t * a.lanes, h = lane / a.pad;
+            v[k] = lane & (a.pad - 1);
+            act[k] = t < a.tok_per_cta && v[k] < (a.head_dim >> 3);
+            const CastRow r = act[k] ? rows[t] : CastRow{-1, {-1, 0}};
+            act[k] = act[k] && r.row >= 0;
+            from[k] = r.row + int64_t(l0) * a.wide.layer_stride + int64_t(h) * a.head_dim + v[k] * 8;
+            to[k].codes = r.place.codes + int64_t(l0) * a.few.layer_stride + int64_t(h) * (a.head_dim / 8 * B8) + v[k] * B8;
+            to[k].scales = r.place.scales + int64_t(l0) * a.few.scale_layer_stride + int64_t(h) * n;
+            wk[k] = wv[k] = make_uint4(0, 0, 0, 0);
+        }
+        auto load = [&](int k) {
+            if (act[k]) {
+                wk[k] = ld_stream(a.wide.k + from[k]);
+                wv[k] = ld_stream(a.wide.v + from[k]);
+            }
+            from[k] += a.wide.layer_stride;
+        };
+#pragma unroll
+        for (int k = 0; k < kQuantTokens; ++k) load(k);
+        for (int l = l0; l < l1; ++l) {
+#pragma unroll
+            for (int k = 0; k < kQuantTokens; ++k) {
+                const uint4 x = wk[k], y = wv[k];
+                if (l + 1 < l1) load(k);
+                int k0, k1, v0, v1;
+                group_bytes<FMT>(pair_max(x.x, x.y), pair_max(x.z, x.w), a.pad, step, k0, k1);
+                group_bytes<FMT>(pair_max(y.x, y.y), pair_max(y.z, y.w), a.pad, step, v0, v1);
+                if (act[k]) {
+                    store_rounded<FMT>(a.few.k + to[k].codes, x, k0, k1);
+                    store_rounded<FMT>(a.few.v + to[k].codes, y, v0, v1);
+                    if (v[k] < step) {
+                        store_scales<FMT>(a.few.k_scale + to[k].scales, v[k], k0, k1);
+                        store_scales<FMT>(a.few.v_scale + to[k].scales, v[k], v0, v1);
+                    }
+                }
+                to[k].codes += a.few.layer_stride;
+                to[k].scales += a.few.scale_layer_stride;
+            }
+        }
+    }
 }
 
 // The codes and scales of eight dims.
@@ -309,10 +445,10 @@ template <int FMT> struct Codes8 {
     __device__ __forceinline__ void load(const uint8_t* p, const uint8_t* s) {
         if (FMT == PRCR_QFMT_E4M3) {
             asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w.x), "=r"(w.y) : "l"(p));
-            f = *s;
+            f = __ldg(s);
         } else {
             asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w.x) : "l"(p));
-            f = *reinterpret_cast<const uint16_t*>(s);
+            f = __ldg(reinterpret_cast<const unsigned short*>(s));
         }
     }
     __device__ __forceinline__ uint4 values() const {
@@ -341,45 +477,47 @@ template <int FMT> struct Codes8 {
 };
 
 template <int FMT>
-__global__ void __launch_bounds__(256) dequantize_kernel(const __grid_constant__ CastArgs a) {
+__global__ void __launch_bounds__(kCastThreads, 3) dequantize_kernel(const __grid_constant__ CastArgs a) {
+    __shared__ CastRow rows[kCastMaxTokens];
     const int b = blockIdx.z, l0 = blockIdx.y * a.layers_per_cta, l1 = min(l0 + a.layers_per_cta, a.n_layers);
-    const int tok0 = blockIdx.x * a.tok_per_cta;
     constexpr int B8 = QFormat<FMT>::kBytes8;
     const int n = a.n_scales;
-    uint32_t err = 0;
     pdl_allow();
     pdl_wait();
-    if (tok0 >= a.count[b] && tok0 > 0) return;
-    for (int u = threadIdx.x; u < a.units; u += blockDim.x) {
-        const int t = u / a.lanes, lane = u - t * a.lanes, h = lane / a.pad, v = lane - h * a.pad, i = tok0 + t;
-        if (t >= a.tok_per_cta || i >= a.max_count) continue;
-        const CastRow r = cast_row<true>(a, b, i, err);
-        if (r.row < 0) continue;
-        const int64_t off = r.row + int64_t(l0) * a.wide.layer_stride + int64_t(h) * a.head_dim + v * 8;
-        uint16_t *dk = a.wide.k + off, *dv = a.wide.v + off;
-        const int64_t c_off = r.place.codes + int64_t(l0) * a.few.layer_stride + int64_t(h) * (a.head_dim / 8 * B8) + v * B8;
-        const int64_t f_off = r.place.scales + int64_t(l0) * a.few.scale_layer_stride + int64_t(h) * n + (FMT == PRCR_QFMT_E4M3 ? 0 : 2 * v % n);
-        const uint8_t *ck = a.few.k + c_off, *cv = a.few.v + c_off, *fk = a.few.k_scale + f_off, *fv = a.few.v_scale + f_off;
-        Codes8<FMT> x, y;
-        x.load(ck, fk);
-        y.load(cv, fv);
+    if (!cast_rows<true>(a, b, blockIdx.x * a.tok_per_cta, rows)) return;
+    for (int u0 = threadIdx.x; u0 < a.units; u0 += kReadTokens * kCastThreads) {
+        Codes8<FMT> x[kReadTokens], y[kReadTokens];
+        int64_t to[kReadTokens];
+        QPlace from[kReadTokens];
+        bool act[kReadTokens];
+#pragma unroll
+        for (int k = 0; k < kReadTokens; ++k) {
+            const int u = u0 + k * kCastThreads, t = u / a.lanes, lane = u - t * a.lanes, h = lane / a.pad, v = lane - h * a.pad;
+            const CastRow r = t < a.tok_per_cta ? rows[t] : CastRow{-1, {-1, 0}};
+            act[k] = r.row >= 0;
+            to[k] = r.row + int64_t(l0) * a.wide.layer_stride + int64_t(h) * a.head_dim + v * 8;
+            from[k].codes = r.place.codes + int64_t(l0) * a.few.layer_stride + int64_t(h) * (a.head_dim / 8 * B8) + v * B8;
+            from[k].scales = r.place.scales + int64_t(l0) * a.few.scale_layer_stride + int64_t(h) * n + (FMT == PRCR_QFMT_E4M3 ? 0 : 2 * v % n);
+        }
         for (int l = l0; l < l1; ++l) {
-            const Codes8<FMT> p = x, q = y;
-            ck += a.few.layer_stride;
-            cv += a.few.layer_stride;
-            fk += a.few.scale_layer_stride;
-            fv += a.few.scale_layer_stride;
-            if (l + 1 < l1) {
-                x.load(ck, fk);
-                y.load(cv, fv);
+#pragma unroll
+            for (int k = 0; k < kReadTokens; ++k)
+                if (act[k]) {
+                    x[k].load(a.few.k + from[k].codes, a.few.k_scale + from[k].scales);
+                    y[k].load(a.few.v + from[k].codes, a.few.v_scale + from[k].scales);
+                }
+#pragma unroll
+            for (int k = 0; k < kReadTokens; ++k) {
+                if (act[k]) {
+                    st_row(a.wide.k + to[k], x[k].values());
+                    st_row(a.wide.v + to[k], y[k].values());
+                }
+                to[k] += a.wide.layer_stride;
+                from[k].codes += a.few.layer_stride;
+                from[k].scales += a.few.scale_layer_stride;
             }
-            st_row(dk, p.values());
-            st_row(dv, q.values());
-            dk += a.wide.layer_stride;
-            dv += a.wide.layer_stride;
         }
     }
-    if (err && blockIdx.y == 0) atomicOr(a.status, err);
 }
 
 }  // namespace
@@ -390,13 +528,13 @@ cudaError_t launch_append_quant(const AppendQuantArgs& a, dim3 grid, int block, 
 }
 
 cudaError_t launch_quantize(const CastArgs& a, dim3 grid, cudaStream_t stream) {
-    return a.format == PRCR_QFMT_E4M3 ? launch_pdl(quantize_kernel<PRCR_QFMT_E4M3>, grid, dim3(256), 0, stream, a)
-                                      : launch_pdl(quantize_kernel<PRCR_QFMT_E2M1>, grid, dim3(256), 0, stream, a);
+    return a.format == PRCR_QFMT_E4M3 ? launch_pdl(quantize_kernel<PRCR_QFMT_E4M3>, grid, dim3(kCastThreads), 0, stream, a)
+                                      : launch_pdl(quantize_kernel<PRCR_QFMT_E2M1>, grid, dim3(kCastThreads), 0, stream, a);
 }
 
 cudaError_t launch_dequantize(const CastArgs& a, dim3 grid, cudaStream_t stream) {
-    return a.format == PRCR_QFMT_E4M3 ? launch_pdl(dequantize_kernel<PRCR_QFMT_E4M3>, grid, dim3(256), 0, stream, a)
-                                      : launch_pdl(dequantize_kernel<PRCR_QFMT_E2M1>, grid, dim3(256), 0, stream, a);
+    return a.format == PRCR_QFMT_E4M3 ? launch_pdl(dequantize_kernel<PRCR_QFMT_E4M3>, grid, dim3(kCastThreads), 0, stream, a)
+                                      : launch_pdl(dequantize_kernel<PRCR_QFMT_E2M1>, grid, dim3(kCastThreads), 0, stream, a);
 }
 
 }  // namespace prcr

@@ -94,7 +94,11 @@ def test_append(fmt, L, l0, nl, H, D, block, layout, lens, gap):
             codes, byte = (x[l0:l0 + nl] for x in cache.held("k", b, slots))
             x = U.f64(ks[:, at:at + n])
             pair = np.sqrt(x[..., :D // 2] ** 2 + x[..., D // 2:] ** 2)
-            check_keys(fmt, codes, byte, U.rope64(x, pos[at:at + n], D, layout), np.concatenate([pair, pair], -1))
+            exact = U.rope64(x, pos[at:at + n], D, layout)
+            check_keys(fmt, codes, byte, exact, np.concatenate([pair, pair], -1))
+            if np.abs(pos).max() <= 40000:  # where the oracle's angles are exact to 2^-36 the codes are those of the exact rotation
+                ref = Q.quantize(fmt, exact)
+                assert np.array_equal(byte, ref[1]) and np.array_equal(codes, ref[0])
         for x_ in (cache.k, cache.v, cache.ks, cache.vs):  # back to what they were: nothing else may differ
             w = cache.where(b, slots)
             rows = x_[w]
