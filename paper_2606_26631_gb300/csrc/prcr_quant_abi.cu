@@ -250,7 +250,7 @@ int prcr_decode_attention_quant(const prcr_rope_cfg* cfg, const prcr_qcache_desc
         layer_begin + int64_t(n_layers) > cfg->n_layers || max_len < 0 || max_len > PRCR_CACHE_MAX_LEN || max_len > qcache_capacity(cache))
         return PRCR_EINVAL;
     if (n_seqs == 0) return PRCR_OK;
-    if (!q || !q_pos || !seq_len || !out || !status) return PRCR_EINVAL;
+    if (!q || !q_pos || !seq_len || !out || !status || q == out) return PRCR_EINVAL;
     if (!aligned4(q) || !aligned8(q_pos) || !aligned4(seq_len) || !aligned16(out) || !aligned4(status)) return PRCR_EALIGN;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return PRCR_ECUDA;
