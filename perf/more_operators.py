@@ -279,7 +279,8 @@ def _kept(s):
     h = dict(prcr=prcr, cfg=cfg, cache=cache, status=torch.zeros(1, dtype=torch.int32, device=DEV))
     if s["op"] == "decode":
         h["out"] = torch.empty(s["q"].shape, dtype=torch.float32, device=DEV)
-        nbytes = prcr.decode_quant_workspace_size(cfg, cache, B, L, H * c["group"], max(_lengths(c)))
+        h["max_len"] = max(_lengths(c))
+        nbytes = prcr.decode_quant_workspace_size(cfg, cache, B, L, H * c["group"], h["max_len"])
         h["ws"] = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=DEV)
         return h
     h["k"], h["v"] = (torch.zeros((B, L, c["n_max"], H, D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
@@ -296,7 +297,7 @@ def _run_own(s):
     h, c = s["own"], s["c"]
     prcr = h["prcr"]
     if s["op"] == "decode":
-        prcr.decode_attention_quant(h["cfg"], h["cache"], 0, s["q"], s["q_pos"], s["len"], max(_lengths(c)), h["out"], h["status"], h["ws"])
+        prcr.decode_attention_quant(h["cfg"], h["cache"], 0, s["q"], s["q_pos"], s["len"], h["max_len"], h["out"], h["status"], h["ws"])
         return {"out": h["out"]}
     out = {"k": h["k"], "v": h["v"]}
     if s["op"] == "append":
