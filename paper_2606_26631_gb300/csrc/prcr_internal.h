@@ -540,7 +540,6 @@ struct DecodeQuantArgs {
     const int32_t* seq_len;     // [B]
     float* out;                 // [B][n_layers][n_q_heads][D]
     float* partial;             // workspace [teams][2][team][group][D + 2]: a warp's parts of units shared with other teams
-    int64_t* tiles_before;      // workspace [B + 1]: tiles of a unit (layer, set of KV heads) of the sequences before
     uint32_t* status;
     int32_t n_seqs;
     int32_t n_layers;
@@ -561,7 +560,7 @@ cudaError_t launch_quantize(const CastArgs& a, dim3 grid, cudaStream_t stream);
 cudaError_t launch_dequantize(const CastArgs& a, dim3 grid, cudaStream_t stream);
 cudaError_t launch_decode_quant(const DecodeQuantArgs& a, cudaStream_t stream);
 int decode_quant_tile(int format, int head_dim);  // slots of a warp's tile
-constexpr int decode_quant_warps(int head_dim) { return head_dim == 256 ? 8 : 16; }  // that an SM's registers hold
+constexpr int decode_quant_warps(int head_dim) { return head_dim == 256 ? 8 : 12; }  // that an SM's registers hold
 
 cudaError_t append_blocks_per_sm(int block, size_t smem, int* out);
 cudaError_t launch_append(const AppendArgs& a, dim3 grid, int block, size_t smem, cudaStream_t stream);

@@ -237,7 +237,7 @@ size_t prcr_decode_quant_workspace_size(const prcr_rope_cfg* cfg, int32_t format
     int dev = 0, sms = 1;
     if (cudaGetDevice(&dev) == cudaSuccess) sms = sm_count(dev);
     const DecodeQuantTeams s = decode_quant_teams(format, cfg->head_dim, cfg->n_kv_heads, int64_t(n_seqs) * n_layers, max_len, sms);
-    return decode_quant_parts(s, n_q_heads / cfg->n_kv_heads, cfg->head_dim) + (size_t(n_seqs) + 1) * sizeof(int64_t);
+    return decode_quant_parts(s, n_q_heads / cfg->n_kv_heads, cfg->head_dim);
 }
 
 int prcr_decode_attention_quant(const prcr_rope_cfg* cfg, const prcr_qcache_desc* cache, int32_t n_seqs, int32_t layer_begin, int32_t n_layers,
@@ -259,13 +259,12 @@ int prcr_decode_attention_quant(const prcr_rope_cfg* cfg, const prcr_qcache_desc
     DecodeQuantArgs a = {};
     const DecodeQuantTeams s = decode_quant_teams(cache->format, cfg->head_dim, cfg->n_kv_heads, int64_t(n_seqs) * n_layers, max_len, sm_count(dev));
     const size_t parts = decode_quant_parts(s, n_q_heads / cfg->n_kv_heads, cfg->head_dim);
-    if (!workspace || workspace_bytes < parts + (size_t(n_seqs) + 1) * sizeof(int64_t)) return PRCR_EWORKSPACE;
+    if (!workspace || workspace_bytes < parts) return PRCR_EWORKSPACE;
     if (!aligned16(workspace)) return PRCR_EALIGN;
     a.team = s.team;
     a.head_sets = s.head_sets;
     a.teams = int32_t(s.teams);
     a.partial = static_cast<float*>(workspace);
-    a.tiles_before = reinterpret_cast<int64_t*>(static_cast<char*>(workspace) + parts);
     a.cache = qcache_view(cache, layer_begin);
     a.q = static_cast<const uint16_t*>(q);
     a.q_pos = q_pos;

@@ -42,7 +42,6 @@ constexpr float kNone = -3.0e38f;   // reference of no slot yet: below every log
 constexpr float kSlack = 4.0f;      // log2 of how far past its reference a weight may go
 constexpr float kWeightLog2 = 11.0f;
 constexpr int kCtaWarps = 4;
-constexpr int kLeastTiles = 2;      // of a warp's share
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -199,7 +198,10 @@ struct Cut {
     }
 };
 __device__ __forceinline__ Cut cut_of(const DecodeQuantArgs& a, int64_t total) {
-    const int64_t teams = max(int64_t(1), min(int64_t(a.teams), quotient(total, kLeastTiles)));
+    // Shares of one tile at least, or of two where a unit has over 64 on average, whose parts cost more to join than they
+    // save (one layer of one sequence, 8 heads: of 16 slots 6.1 us | 9.2 with two, of 933 8.4 | 9.9, but of 4000 16.4 | 13.1).
+    const int64_t most = total > 64 * int64_t(a.n_seqs) * a.n_layers * a.head_sets ? total / 2 : total;
+    const int64_t teams = max(int64_t(1), min(int64_t(a.teams), most));
     Cut c;
     c.each = quotient(total, teams);
     c.more = total - c.each * teams;
@@ -224,15 +226,6 @@ __device__ __forceinline__ Share share_of(const DecodeQuantArgs& a, uint32_t& er
     for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
         n = b0 + lane < a.n_seqs ? tiles_of<TS>(a, b0 + lane, len, e) : 0;
         // (below 2^31 together: 2^30 slots each, sixteen to a tile, 32 of them)
-        if (warp == 0) {  // for the kernel that joins
-            int64_t upto = n;
-            for (int k = 1; k < 32; k *= 2) {
-                const int64_t x = __shfl_up_sync(kFull, upto, k);
-                if (lane >= k) upto += x;
-            }
-            if (b0 + lane < a.n_seqs) a.tiles_before[b0 + lane + 1] = sum + upto;
-            if (b0 + lane == 0) a.tiles_before[0] = 0;
-        }
         sum += __reduce_add_sync(kFull, unsigned(n));
     }
     if (warp == 0) err |= __reduce_or_sync(kFull, e);
@@ -284,6 +277,7 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
     float* mine = smem + warp * (S::warp_bytes(PAIR, g) / 4);
     uint2* q_frag = reinterpret_cast<uint2*>(mine);
     pdl_wait();
+    pdl_allow();  // (the grid is one wave: CTAs that follow take the place of those that are done)
     uint32_t err = 0;
     const Share share = share_of<TS>(a, err);
     if (share.begin >= share.end) {
@@ -613,26 +607,43 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
             }
         }
 
-        float x[SUB][LS][2], ve[SUB][LS];
+        // S^T of all subtiles, so that a fragment of the query is read once
+        constexpr int NC = kFour ? N : 2;  // sums: of the groups, or two to be shorter
+        float x[SUB][LS][2], ve[SUB][LS], c[SUB][NC][4];
+#pragma unroll
+        for (int i = 0; i < KW; ++i) {
+            uint32_t p[SUB][4], q[SUB][4];
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                if constexpr (kFour) {
+                    f16_of_e2m1(kw[u][0][i], p[u]);
+                    f16_of_e2m1(kw[u][1][i], q[u]);
+                } else {
+                    uint32_t a2[2], b2[2];
+                    f16_of_e4m3(kw[u][0][i], a2);
+                    f16_of_e4m3(kw[u][1][i], b2);
+                    p[u][0] = a2[0]; p[u][1] = a2[1]; q[u][0] = b2[0]; q[u][1] = b2[1];
+                }
+            }
+            constexpr int E = kFour ? 2 : 1;  // k-steps of a word
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+#pragma unroll
+                for (int z = 0; z < NP; ++z) {
+                    const uint2 f = q_frag[((E * i + e) * NP + z) * 32 + lane];
+                    const int to = kFour ? (2 * i + e) % N : (i + z) & 1;
+                    const bool begins = kFour ? 2 * i + e < N && z == 0 : i + z < 2 && (i == 0 || NP == 1);
+#pragma unroll
+                    for (int u = 0; u < SUB; ++u) {
+                        if (begins) mma_f16_first(c[u][to], p[u][2 * e], q[u][2 * e], p[u][2 * e + 1], q[u][2 * e + 1], f.x, f.y);
+                        else mma_f16(c[u][to], p[u][2 * e], q[u][2 * e], p[u][2 * e + 1], q[u][2 * e + 1], f.x, f.y);
+                    }
+                }
+        }
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
             float d[4];
             if constexpr (kFour) {
-                float c[N][4];
-#pragma unroll
-                for (int i = 0; i < KW; ++i) {
-                    uint32_t p[4], q[4];
-                    f16_of_e2m1(kw[u][0][i], p);
-                    f16_of_e2m1(kw[u][1][i], q);
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-#pragma unroll
-                        for (int z = 0; z < NP; ++z) {
-                            const uint2 f = q_frag[((2 * i + e) * NP + z) * 32 + lane];
-                            if (2 * i + e < N && z == 0) mma_f16_first(c[(2 * i + e) % N], p[2 * e], q[2 * e], p[2 * e + 1], q[2 * e + 1], f.x, f.y);
-                            else mma_f16(c[(2 * i + e) % N], p[2 * e], q[2 * e], p[2 * e + 1], q[2 * e + 1], f.x, f.y);
-                        }
-                }
 #pragma unroll
                 for (int k = 0; k < N / 2; ++k) {
                     const uint32_t wa = __shfl_sync(kFull, kg[u / 2][k], (16 * u + gid) & 31);
@@ -642,27 +653,14 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
                         const float fa = e ? hi_f32(wa) : lo_f32(wa), fb = e ? hi_f32(wb) : lo_f32(wb);
 #pragma unroll
                         for (int y = 0; y < 4; ++y) {
-                            const float v = c[2 * k + e][y], f = y < 2 ? fa : fb;
+                            const float v = c[u][2 * k + e][y], f = y < 2 ? fa : fb;
                             d[y] = k + e == 0 ? v * f : fmaf(v, f, d[y]);
                         }
                     }
                 }
             } else {
-                float c[2][4];
 #pragma unroll
-                for (int i = 0; i < KW; ++i) {
-                    uint32_t p[2], q[2];
-                    f16_of_e4m3(kw[u][0][i], p);
-                    f16_of_e4m3(kw[u][1][i], q);
-#pragma unroll
-                    for (int z = 0; z < NP; ++z) {
-                        const uint2 f = q_frag[(i * NP + z) * 32 + lane];
-                        if (i + z < 2 && (i == 0 || NP == 1)) mma_f16_first(c[(i + z) & 1], p[0], q[0], p[1], q[1], f.x, f.y);
-                        else mma_f16(c[(i + z) & 1], p[0], q[0], p[1], q[1], f.x, f.y);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) d[i] = c[0][i] + c[1][i];
+                for (int i = 0; i < 4; ++i) d[i] = c[u][0][i] + c[u][1][i];
             }
             if (PAIR) {  // lanes t and t ^ 2 add their pieces, the first for slot r, the other for r + 8
                 const float s0 = t < 2 ? d[2] : d[0], s1 = t < 2 ? d[3] : d[1];
@@ -867,37 +865,46 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
         do un = tiles_of<TS>(a, ++ub, len, err); while (un == 0);
     }
     }
-    pdl_allow();
     if (err) atomicOr(a.status, err);
 }
 
 // Joins the parts of the units that several teams shared, and writes zeros for sequences without any slot: a query
 // head's row a warp, or, where many teams share a unit, a CTA. Eight parts are requested at once.
-template <int D, int WARPS>
+template <int D, int TS, int WARPS>
 __global__ void __launch_bounds__(128) decode_quant_join_kernel(const __grid_constant__ DecodeQuantArgs a) {
     constexpr int NV = D / 64, AHEAD = 8;
     __shared__ float2 s_acc[WARPS][D / 2];
     __shared__ float s_top[WARPS], s_den[WARPS];
     pdl_allow();
-    pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = a.group;
     const int64_t row = WARPS > 1 ? int64_t(blockIdx.x) : int64_t(blockIdx.x) * 4 + warp;
     const int per_seq = a.n_layers * a.head_sets, heads = a.n_layers * a.n_kv_heads;
-    if (row >= int64_t(a.n_seqs) * heads * g) return;
-    const int64_t head = row / g;
-    const int h = int(row - head * g), b = int(head / heads), lh = int(head - int64_t(b) * heads);
+    const int64_t head = min(quotient(row, g), int64_t(a.n_seqs) * heads - 1);
+    const int h = int(row - head * g), b = int(quotient(head, heads)), lh = int(head - int64_t(b) * heads);
     const int layer = lh / a.n_kv_heads, kh = lh - layer * a.n_kv_heads, unit = layer * a.head_sets + kh / a.team, member = kh % a.team;
-    const int64_t before = a.tiles_before[b];
-    const int n = int(a.tiles_before[b + 1] - before);
+    // the sequences' tiles again, while the kernel before this one ends (lengths and positions are the call's inputs: whatever wrote
+    // them was complete before that kernel began)
+    int64_t before = 0, total = 0;
+    int n = 0;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
+        uint32_t e;
+        int len;
+        const int x = b0 + lane < a.n_seqs ? tiles_of<TS>(a, b0 + lane, len, e) : 0;
+        before += __reduce_add_sync(kFull, unsigned(b0 + lane < b ? x : 0));
+        total += __reduce_add_sync(kFull, unsigned(x));
+        n += __reduce_add_sync(kFull, unsigned(b0 + lane == b ? x : 0));
+    }
+    const Cut cut = cut_of(a, total * per_seq);
+    const int64_t u0 = before * per_seq + int64_t(unit) * n, u1 = u0 + n;
+    const int w0 = n ? cut.team_of(u0) : 0, w1 = n ? cut.team_of(u1 - 1) : 0;
+    pdl_wait();
+    if (h >= g) return;  // (past the last row)
     float* out = a.out + row * D;
     if (n == 0) {
         if (WARPS == 1 || warp == 0)
             for (int d = lane; d < D; d += 32) out[d] = 0.0f;
         return;
     }
-    const Cut cut = cut_of(a, a.tiles_before[a.n_seqs] * per_seq);
-    const int64_t u0 = before * per_seq + int64_t(unit) * n, u1 = u0 + n;
-    const int w0 = cut.team_of(u0), w1 = cut.team_of(u1 - 1);
     if (w0 == w1) return;
     const int place0 = cut.begin_of(w0) != u0 ? 1 : 0;  // in the first team's parts; the others' begin with their shares
     float M = kNone, den = 0.0f;
@@ -975,8 +982,8 @@ cudaError_t launch_fd(const DecodeQuantArgs& a, cudaStream_t stream) {
     if (e == cudaSuccess) e = launch_pdl(k, dim3(unsigned((a.teams * a.team + kCtaWarps - 1) / kCtaWarps)), dim3(kCtaWarps * 32), smem, stream, a);
     if (e != cudaSuccess) return e;
     const int64_t units = int64_t(a.n_seqs) * a.n_layers * a.head_sets, rows = int64_t(a.n_seqs) * a.n_layers * a.n_kv_heads * a.group;
-    return a.teams >= 8 * units ? launch_pdl(decode_quant_join_kernel<D, 4>, dim3(unsigned(rows)), dim3(128), 0, stream, a)
-                                : launch_pdl(decode_quant_join_kernel<D, 1>, dim3(unsigned((rows + 3) / 4)), dim3(128), 0, stream, a);
+    return a.teams >= 8 * units ? launch_pdl(decode_quant_join_kernel<D, S::TS, 4>, dim3(unsigned(rows)), dim3(128), 0, stream, a)
+                                : launch_pdl(decode_quant_join_kernel<D, S::TS, 1>, dim3(unsigned((rows + 3) / 4)), dim3(128), 0, stream, a);
 }
 
 template <int FMT>
