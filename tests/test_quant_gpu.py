@@ -342,6 +342,30 @@ def test_decode_long(fmt, D, H, g, lens, block):
     check_decode(fmt, 2, (1, 1), H, g, D, lens, block, seed=6, max_len=max(lens) + 700, caps=[max(lens) + 700] * len(lens), layout=prcr.LAYOUT_INTERLEAVED)
 
 
+@pytest.mark.parametrize("fmt,D,H,g,block,lens", [
+    ("e4m3", 128, 2, 4, 16, [0] * 33 + [1, 40, 0, 17]),                      # nothing in the first 32 sequences
+    ("e2m1", 64, 3, 5, 0, [(37 * i) % 150 for i in range(70)]),
+    ("e4m3", 256, 1, 8, 7, [700 if i == 40 else 0 for i in range(65)]),      # all of the work in one of them
+    ("e2m1", 128, 4, 7, 32, [33] * 32 + [0] * 32 + [500]),
+    ("e4m3", 64, 2, 1, 16, [0] * 64)])
+def test_decode_many_sequences(fmt, D, H, g, block, lens):
+    check_decode(fmt, 2, (0, 2), H, g, D, lens, block, seed=len(lens), max_len=800, caps=[800] * len(lens))
+
+
+def test_decode_repeats():
+    """The same call gives the same bits, whatever the workspace held."""
+    c, lens = U.cfg_of(3, 2, 128), [900, 3, 450, 0]
+    cache, q, pos = Q.QCache("e2m1", 3, 2, 128, lens, 16, seed=2), normal((4, 3, 14, 128), 3), torch.tensor([9, 8, 7, 6], device=DEV)
+    d, ln, st = cache.desc(), i32(lens), status_word()
+    need = prcr.decode_quant_workspace_size(c, d, 4, 3, 14, 900)
+    outs = []
+    for fill in (0, 255, 127):
+        ws, out = torch.full((need,), fill, dtype=torch.uint8, device=DEV), torch.full((4, 3, 14, 128), float("nan"), device=DEV)
+        prcr.decode_attention_quant(c, d, 0, q, pos, ln, 900, out, st, ws)
+        outs.append(out)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2]) and int(st.item()) == 0
+
+
 @pytest.mark.parametrize("n", list(range(1, 20)) + [31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 513, 1023, 1025])
 @pytest.mark.parametrize("fmt,D", [("e4m3", 128), ("e2m1", 128), ("e2m1", 64), ("e4m3", 256)])
 def test_decode_lengths(fmt, D, n):
