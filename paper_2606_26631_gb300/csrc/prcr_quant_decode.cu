@@ -95,29 +95,30 @@ __device__ __forceinline__ uint32_t bf16_of_scales(uint32_t two) {
     return r;
 }
 
-// N words from p; `ok`: all of them, or zeros. (A load that waits for nothing: `ok ? *p : 0` would wait at once.)
+// N words from p; `ok`: all of them, or zeros. (A load that waits for nothing: `ok ? *p : 0` would wait at once.
+// Not by the read-only path: this kernel is resident while the append before it in the stream still writes the rows.)
 template <int N>
 __device__ __forceinline__ void load_words(uint32_t* w, const uint8_t* p) {
     static_assert(N == 1 || N == 2 || N == 4, "4, 8 or 16 bytes");
     if constexpr (N == 4)
-        asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
+        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
     else if constexpr (N == 2)
-        asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+        asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
     else
-        asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+        asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
 }
 template <int N>
 __device__ __forceinline__ void load_words(uint32_t* w, const uint8_t* p, bool ok) {
     if constexpr (N == 4) {
         asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %5, 0;\nmov.b32 %0, 0;\nmov.b32 %1, 0;\nmov.b32 %2, 0;\nmov.b32 %3, 0;\n"
-                     "@p ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n}"
+                     "@p ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n}"
                      : "=&r"(w[0]), "=&r"(w[1]), "=&r"(w[2]), "=&r"(w[3]) : "l"(p), "r"(int(ok)));
     } else if constexpr (N == 2) {
         asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %3, 0;\nmov.b32 %0, 0;\nmov.b32 %1, 0;\n"
-                     "@p ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];\n}"
+                     "@p ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];\n}"
                      : "=&r"(w[0]), "=&r"(w[1]) : "l"(p), "r"(int(ok)));
     } else {
-        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\nmov.b32 %0, 0;\n@p ld.global.nc.L1::no_allocate.u32 %0, [%1];\n}"
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\nmov.b32 %0, 0;\n@p ld.global.L1::no_allocate.u32 %0, [%1];\n}"
                      : "=&r"(w[0]) : "l"(p), "r"(int(ok)));
     }
 }
@@ -126,14 +127,14 @@ __device__ __forceinline__ void load_words(uint32_t* w, const uint8_t* p, bool o
 template <int N>
 __device__ __forceinline__ void load_row_scales(uint32_t* w, const uint8_t* p, bool ok) {
     if constexpr (N == 8)
-        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %3, 0;\nmov.b32 %0, 0;\nmov.b32 %1, 0;\n@p ld.global.nc.v2.u32 {%0, %1}, [%2];\n}"
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %3, 0;\nmov.b32 %0, 0;\nmov.b32 %1, 0;\n@p ld.global.v2.u32 {%0, %1}, [%2];\n}"
                      : "=&r"(w[0]), "=&r"(w[1]) : "l"(p), "r"(int(ok)));
     else if constexpr (N == 4)
-        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\nmov.b32 %0, 0;\n@p ld.global.nc.u32 %0, [%1];\n}" : "=&r"(w[0]) : "l"(p), "r"(int(ok)));
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\nmov.b32 %0, 0;\n@p ld.global.u32 %0, [%1];\n}" : "=&r"(w[0]) : "l"(p), "r"(int(ok)));
     else if constexpr (N == 2)
-        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\nmov.b32 %0, 0;\n@p ld.global.nc.u16 %0, [%1];\n}" : "=&r"(w[0]) : "l"(p), "r"(int(ok)));
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\nmov.b32 %0, 0;\n@p ld.global.u16 %0, [%1];\n}" : "=&r"(w[0]) : "l"(p), "r"(int(ok)));
     else
-        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\nmov.b32 %0, 0;\n@p ld.global.nc.u8 %0, [%1];\n}" : "=&r"(w[0]) : "l"(p), "r"(int(ok)));
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %2, 0;\nmov.b32 %0, 0;\n@p ld.global.u8 %0, [%1];\n}" : "=&r"(w[0]) : "l"(p), "r"(int(ok)));
 }
 
 // Sizes of a format's rows: RB bytes of codes; a warp takes tiles of SUB x 16 slots.
@@ -471,8 +472,8 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 #pragma unroll
             for (int i = 0; i < PR; ++i) {
                 const bool ok = has && h < g;
-                qx[h][i] = ok ? __ldg(q + h * P + 32 * i) : 0u;
-                qy[h][i] = ok ? __ldg(q + h * P + 32 * i + P / 2) : 0u;
+                qx[h][i] = ok ? q[h * P + 32 * i] : 0u;
+                qy[h][i] = ok ? q[h * P + 32 * i + P / 2] : 0u;
             }
     };
 

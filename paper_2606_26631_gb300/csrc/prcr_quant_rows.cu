@@ -444,11 +444,11 @@ template <int FMT> struct Codes8 {
     uint32_t f;
     __device__ __forceinline__ void load(const uint8_t* p, const uint8_t* s) {
         if (FMT == PRCR_QFMT_E4M3) {
-            asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w.x), "=r"(w.y) : "l"(p));
-            f = __ldg(s);
+            asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w.x), "=r"(w.y) : "l"(p));
+            f = *s;
         } else {
-            asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w.x) : "l"(p));
-            f = __ldg(reinterpret_cast<const unsigned short*>(s));
+            asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(w.x) : "l"(p));
+            f = *reinterpret_cast<const unsigned short*>(s);
         }
     }
     __device__ __forceinline__ uint4 values() const {
