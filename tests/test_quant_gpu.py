@@ -240,6 +240,12 @@ def test_cast_and_read(fmt, LS, LD, nl, H, D, block, qblock, counts, begins, gap
     assert torch.equal(back.k_all, back_before) and torch.equal(back.v_all, back_before)
 
 
+@pytest.mark.parametrize("fmt,nl,H,D,counts", [("e4m3", 1, 3, 128, [26001, 70]), ("e2m1", 1, 4, 64, [3, 26100, 0]), ("e2m1", 2, 6, 64, [26007])])
+def test_cast_and_read_of_few_layers(fmt, nl, H, D, counts):
+    """So many rows of so few layers that a CTA takes several rounds of them."""
+    test_cast_and_read(fmt, nl, nl, nl, H, D, 16, 7, counts, ([2] * len(counts), [1] * len(counts)), 0)
+
+
 @pytest.mark.parametrize("fmt", ["e4m3", "e2m1"])
 def test_read_every_code(fmt):
     """Every code with every scale's byte, whoever wrote them: rounded to bf16 where that does not hold the value."""
