@@ -571,9 +571,10 @@ PRCR_API int prcr_evict(const prcr_rope_cfg* cfg, const prcr_cache_desc* cache,
                         const float* score, float* score_out, int64_t score_stride,
                         int32_t* keep_out, int32_t* seq_len_out, uint32_t* status, void* stream);
 
-/* prcr_append_kv_quant - prcr_append_kv into a quantised cache: keys rotated as there (in
- * float32, not rounded to bf16 in between) and values, rounded to the cache's format. Arguments,
- * checks, status bits and what is skipped are prcr_append_kv's.                   */
+/* prcr_append_kv_quant - prcr_append_kv into a quantised cache: values, and keys rotated as
+ * there, rounded to the cache's format. A key is not rounded to bf16 in between: it gets the code
+ * nearest to its exact rotation (its group's scale is chosen from float32 ones). Arguments, checks, status
+ * bits and what is skipped are prcr_append_kv's.                                   */
 PRCR_API int prcr_append_kv_quant(const prcr_rope_cfg* cfg, const prcr_qcache_desc* cache,
                                   int32_t n_seqs, int32_t layer_begin, int32_t n_layers,
                                   const void* k_src, const void* v_src, int64_t src_layer_stride,
@@ -618,9 +619,12 @@ PRCR_API int prcr_dequantize_cache(const prcr_rope_cfg* cfg, const prcr_qcache_d
  * The rotated query and the weights enter the tensor cores as two fp16 each (22 bits); codes are
  * exact there, sums, maxima and the output float32.
  * Limits: D in {64, 128, 256}, at most 8 query heads per KV head, n_q_heads * D <=
- * PRCR_DECODE_MAX_Q_ELEMS, and below 2^31 CTAs (sequences by layers by KV heads by splits).
- * workspace: device, >= prcr_decode_quant_workspace_size(...) bytes (0 where the slots are not
- * split), 16-byte aligned, not shared with a concurrent call.
+ * PRCR_DECODE_MAX_Q_ELEMS, and n_seqs * n_layers * n_q_heads below 2^31.
+ * workspace: device, >= prcr_decode_quant_workspace_size(...) bytes, 16-byte aligned, not shared
+ * with a concurrent call. It grows with n_seqs, n_layers and max_len until every SM is taken (by
+ * then 7 to 20 MB for eight query heads per KV head), and what one call needs is enough for any
+ * with less of them. The same call gives the same bits; calls with other sequences, layers or max_len
+ * may sum in another order.
  * Status bits and what is left out are prcr_decode_attention's (slots past max_len are left
  * out); a sequence that reads no slot gets zeros, with max_len 0 all of them.       */
 PRCR_API size_t prcr_decode_quant_workspace_size(const prcr_rope_cfg* cfg, int32_t format,

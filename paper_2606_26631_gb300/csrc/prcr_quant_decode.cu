@@ -7,7 +7,10 @@
 // product, and a byte of codes brings two or four times a bf16 byte's products.
 // So nothing passes through shared memory on its way: a warp loads its tiles'
 // codes straight into the registers in which the matrix instructions want them,
-// the next tile's as soon as a tile's are used up.
+// the next tile's as soon as a tile's are used up. (Rings of tiles in shared memory,
+// filled by asynchronous copies, were slower: they shrink the L1 cache
+// that a load's lines wait in.) tcgen05 wants 64 rows of a product at least, where a
+// group has 8 queries at most, and its operands in shared memory.
 //   S^T (16 slots x 8 heads) = K Q^T. The order of the dims in a dot product is
 //     free, so lane t of a slot's four takes 16-byte pieces t, t + 4, ... of its
 //     row; four dims in a lane are one k-step's share.
@@ -17,16 +20,34 @@
 // Codes are exact in fp16, in which they enter. The query (scaled by a power of
 // two to at most 2^14) and the weights enter as two fp16 each, 22 bits; with up to four
 // heads to a group the two lie side by side in the product's eight columns, so that one
-// product takes both.
-// Scales never touch the codes: E4M3's of a key multiplies the slot's logits, E2M1's the
-// partial sums of their groups' k-steps; a value's goes into the weight's exponent, per
-// group in E2M1 (whose groups take every (D/32)-th quad of dims, so that each
-// lane's piece of a row has quads of all groups).
+// product takes both (four heads to a group, 16 sequences of up to 4096 slots, E4M3, 36
+// layers: 464 us, with two products 492). One fp16 would leave 2^-12 of a weight, a hundred
+// times what the rest loses.
+// Scales never touch the codes. E4M3: a key's multiplies its slot's logits, a value's goes
+// into its weight's exponent. E2M1, whose groups take every (D/32)-th quad of dims, so that
+// each lane's piece of a row has quads of all groups: a key's multiply the partial sums of
+// their groups' k-steps; of a value's the largest goes into the weight's exponent, and what the others
+// are to it multiplies the weights of the products of their groups.
 // Weights are therefore kept against two references, both powers of two: p = 2^(x - m)
-// for the sum, w = 2^(x + e - r + 11) for the accumulator, e the value's scale. m and r follow the
+// for the sum, w = 2^(x + e - r + 11) for the accumulator, e the value's exponent. m and r follow the
 // largest x and x + e, but only when one is more than 2^4 past them, so that most tiles
 // rescale nothing and need no reduction over the lanes; w stays below 2^15, and what fp16 loses
 // of it is 2^-36 of the largest at most.
+//
+// Work is cut by what there is, not by sequence: all (sequence, layer, set of heads) units' tiles
+// in one row, one even share of it to each team of 1, 2 or 4 warps on the same slots of
+// neighbouring KV heads (whose codes are neighbouring bytes: with teams of one, E4M3 reads
+// 501 us for 465, E2M1 at 64 bytes a row 201 for 192; of two 471 and 189). A share's units that
+// it has whole are written at once, the parts of others joined by a second kernel.
+// A grid is one wave: 12 warps an SM, 8 at head_dim 256, which is what the registers hold (E4M3 with 8 for 12:
+// 612 us for 464; with 16, which spill: 462, but one sequence of 933 slots 31 for 27). Rows of 64 bytes go in tiles of
+// 32 slots (E2M1 191 us; of 16 223, of 64 with 8 warps 203).
+//
+// Measured (us, and bytes read per time of the 6.8 TB/s that a copy makes): E4M3, 8 KV heads of 128, 36 layers:
+// 16 sequences of up to 4096 slots 460 (91 %), one of 933 25; one layer, 32 of up to 16,384 117 (83 %);
+// E2M1, 4 KV heads of seven queries, 28 layers, 8 of up to 8192 192 (47 %); E4M3, 4 KV heads of 256, one layer, 8 of up to
+// 8000 31. E4M3 waits for memory; E2M1 for issue slots (62 % of them taken, the
+// tensor cores 35 % busy: some 470 instructions of a warp for 16 slots); what is short, for its launches.
 #include <algorithm>
 
 #include <cuda_fp16.h>
@@ -262,14 +283,17 @@ __device__ __forceinline__ Share share_of(const DecodeQuantArgs& a, uint32_t& er
 
 // RUNS: sixteen slots from a multiple of sixteen on lie slot_stride apart (a contiguous cache,
 // or blocks of a multiple of 16 slots), so that a lane's rows follow from where the first one
-// is. Otherwise lanes look a slot up each and pass its place on.
+// is. Otherwise lanes look a slot up each and pass its place on (taken for every cache: 501 us for
+// 464, 16 sequences of up to 4096 slots, 36 layers).
 template <int FMT, int D, bool PAIR, bool RUNS>
 __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kernel(const __grid_constant__ DecodeQuantArgs a) {
     using S = Shape<FMT, D>;
     constexpr bool kFour = S::kFour;
     constexpr int SUB = S::SUB, TS = S::TS, N = S::N, KW = S::KW, VW = S::VW, KP = S::KP, VP = S::VP, KS = S::KS, SW = S::SW, OWN = S::OWN;
     constexpr int P = D / 2, PITCH = D + 4, NP = PAIR ? 1 : 2, LS = PAIR ? 1 : 2;  // products for the pieces of a query or a weight, slots of a lane's logits
-    constexpr bool EARLY = !kFour;  // look places up a tile earlier than they are loaded from
+    // look places up a tile earlier than they are loaded from, and ask for the rows then (E4M3: 465 us, without 531; E2M1, which
+    // does not wait for memory: 197, without 191)
+    constexpr bool EARLY = !kFour;
     extern __shared__ __align__(16) float smem[];
     const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, gid = lane >> 2, t = lane & 3;
     const int H = a.n_kv_heads, g = a.group, per_seq = a.n_layers * a.head_sets;
@@ -870,7 +894,8 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 }
 
 // Joins the parts of the units that several teams shared, and writes zeros for sequences without any slot: a query
-// head's row a warp, or, where many teams share a unit, a CTA. Eight parts are requested at once.
+// head's row a warp, or, where eight teams or more share a unit, a CTA (8 sequences of one layer, 4 heads of 256: 37 us, by
+// warps 44; 16 of 36 layers: 464 by warps, by CTAs 492). Eight parts are requested at once.
 template <int D, int TS, int WARPS>
 __global__ void __launch_bounds__(128) decode_quant_join_kernel(const __grid_constant__ DecodeQuantArgs a) {
     constexpr int NV = D / 64, AHEAD = 8;

@@ -6,6 +6,16 @@
 // neighbouring 16 bytes of bf16 of one head's row, and a group's largest magnitude is
 // a butterfly over the lanes that hold it. Padding a head's lanes to a power of two
 // keeps E4M3's butterflies inside a warp.
+// What costs beside the bytes is finding them: a token's place hangs on two or three loads one after the other. So
+// a CTA looks its tokens up once and walks several layers with them, the next layer's rows on their way while one is worked on.
+//
+// Measured (us, and bytes moved per time of the 6.8 TB/s that a copy makes):
+//   append      E4M3, 4 KV heads of 128, 28 layers, prompts of 6 sequences, up to 2116 tokens each 160 (71 %);
+//               one token of 16 sequences, 36 layers 7 (in a graph)
+//   quantise    E4M3, 8 KV heads of 128, 36 layers, up to 1024 tokens of 16 sequences 353 (92 %)
+//   dequantise  the same 343 (95 %); one layer, four prompts of up to 16,384 57 (75 %)
+//               E2M1, 4 KV heads, 28 layers, 8 of up to 4096 258 (91 %), in blocks of 7 slots
+// The casts wait for memory; the append for its keys' arithmetic (two conversions of each key's code, and a comparison).
 #include "prcr_pdl.cuh"
 #include "prcr_quant.cuh"
 
