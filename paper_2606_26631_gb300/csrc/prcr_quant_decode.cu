@@ -758,10 +758,10 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
                 }
             }
         }
+        // B fragments of P^T: [first and second piece][slots 0..7, 8..15]; E2M1: factors of them for its groups
+        uint32_t pf[SUB][NP][2], rel[SUB][2];
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
-            // B fragments of P^T: [first and second piece][slots 0..7, 8..15]
-            uint32_t pf[NP][2];
             {
                 uint32_t hi[LS], lo[LS];
 #pragma unroll
@@ -776,37 +776,43 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
                 }
                 if (PAIR) {
                     const uint32_t got = __shfl_xor_sync(kFull, t < 2 ? lo[0] : hi[0], 2);
-                    pf[0][0] = transposed(t < 2 ? hi[0] : got);
-                    pf[0][1] = transposed(t < 2 ? got : lo[0]);
+                    pf[u][0][0] = transposed(t < 2 ? hi[0] : got);
+                    pf[u][0][1] = transposed(t < 2 ? got : lo[0]);
                 } else {
 #pragma unroll
                     for (int i = 0; i < LS; ++i) {
-                        pf[0][i] = transposed(hi[i]);
-                        pf[NP - 1][i] = transposed(lo[i]);
+                        pf[u][0][i] = transposed(hi[i]);
+                        pf[u][NP - 1][i] = transposed(lo[i]);
                     }
                 }
             }
             if constexpr (kFour) {
                 // The groups' scales as factors of P^T's pairs of slots: a matrix of slots by groups, transposed as P is; its rows
                 // (N = 2, 4: of slots 0..7, then of 8..15) are read by every lane.
-                uint32_t rel[2];
                 if (N == 8) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const int from = (16 * u + gid + 8 * i) & 31;
                         const uint32_t w0 = __shfl_sync(kFull, vg[u / 2][0], from), w1 = __shfl_sync(kFull, vg[u / 2][1 % ((N + 1) / 2)], from);
                         const uint32_t w2 = __shfl_sync(kFull, vg[u / 2][2 % ((N + 1) / 2)], from), w3 = __shfl_sync(kFull, vg[u / 2][3 % ((N + 1) / 2)], from);
-                        rel[i] = transposed(t < 2 ? (t == 0 ? w0 : w1) : (t == 2 ? w2 : w3));
+                        rel[u][i] = transposed(t < 2 ? (t == 0 ? w0 : w1) : (t == 2 ? w2 : w3));
                     }
                 } else if (N == 4) {
                     const int from = (16 * u + gid + 8 * (t >> 1)) & 31;
                     const uint32_t w0 = __shfl_sync(kFull, vg[u / 2][0], from), w1 = __shfl_sync(kFull, vg[u / 2][1 % ((N + 1) / 2)], from);
-                    rel[0] = transposed(t & 1 ? w1 : w0);
+                    rel[u][0] = transposed(t & 1 ? w1 : w0);
                 } else {
-                    rel[0] = transposed(__shfl_sync(kFull, vg[u / 2][0], (16 * u + gid + 8 * (t & 1)) & 31));
+                    rel[u][0] = transposed(__shfl_sync(kFull, vg[u / 2][0], (16 * u + gid + 8 * (t & 1)) & 31));
                 }
+            }
+        }
+        // O^T, summed over a tile before it joins the accumulators
 #pragma unroll
-                for (int i = 0; i < VW; ++i) {
+        for (int i = 0; i < VW; ++i) {
+            float part[kFour ? 4 : 2][4];
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                if constexpr (kFour) {
                     // bytes of (slot 2t, slot 2t + 1) and of the slots 8 behind, even dims and odd
                     uint32_t ev[2][4], od[2][4];
 #pragma unroll
@@ -818,37 +824,34 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int grp = 2 * i + e;
-                        const uint32_t f0 = __shfl_sync(kFull, rel[0], 4 * grp + t);
-                        const uint32_t f1 = N == 8 ? __shfl_sync(kFull, rel[1], 4 * grp + t) : __shfl_sync(kFull, rel[0], 4 * (grp + N) + t);
-                        uint32_t b[NP][2];
+                        const uint32_t f0 = __shfl_sync(kFull, rel[u][0], 4 * grp + t);
+                        const uint32_t f1 = N == 8 ? __shfl_sync(kFull, rel[u][1], 4 * grp + t) : __shfl_sync(kFull, rel[u][0], 4 * (grp + N) + t);
 #pragma unroll
                         for (int z = 0; z < NP; ++z) {
-                            b[z][0] = mul_f16x2(pf[z][0], f0);
-                            b[z][1] = mul_f16x2(pf[z][1], f1);
-                        }
+                            const uint32_t b0 = mul_f16x2(pf[u][z][0], f0), b1 = mul_f16x2(pf[u][z][1], f1);
 #pragma unroll
-                        for (int k = 2 * e; k < 2 * e + 2; ++k) {
-                            float part[4];
-                            mma_f16_first(part, ev[0][k], od[0][k], ev[1][k], od[1][k], b[0][0], b[0][1]);
-                            if (NP == 2) mma_f16(part, ev[0][k], od[0][k], ev[1][k], od[1][k], b[NP - 1][0], b[NP - 1][1]);
-                            add_to(o[4 * i + k], part);
+                            for (int k = 2 * e; k < 2 * e + 2; ++k) {
+                                if (u + z == 0) mma_f16_first(part[k], ev[0][k], od[0][k], ev[1][k], od[1][k], b0, b1);
+                                else mma_f16(part[k], ev[0][k], od[0][k], ev[1][k], od[1][k], b0, b1);
+                            }
                         }
                     }
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < VW; ++i)
+                } else {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {  // dims 2e and 2e + 1 of the word, of two slots each
                         uint32_t p[2], q[2];
                         f16_of_e4m3(__byte_perm(vw[u][0][i], vw[u][1][i], e ? 0x7362 : 0x5140), p);
                         f16_of_e4m3(__byte_perm(vw[u][2][i], vw[u][3][i], e ? 0x7362 : 0x5140), q);
-                        float part[4];
-                        mma_f16_first(part, p[0], p[1], q[0], q[1], pf[0][0], pf[0][1]);
-                        if (NP == 2) mma_f16(part, p[0], p[1], q[0], q[1], pf[NP - 1][0], pf[NP - 1][1]);
-                        add_to(o[2 * i + e], part);
+#pragma unroll
+                        for (int z = 0; z < NP; ++z) {
+                            if (u + z == 0) mma_f16_first(part[e], p[0], p[1], q[0], q[1], pf[u][z][0], pf[u][z][1]);
+                            else mma_f16(part[e], p[0], p[1], q[0], q[1], pf[u][z][0], pf[u][z][1]);
+                        }
                     }
+                }
             }
+#pragma unroll
+            for (int k = 0; k < (kFour ? 4 : 2); ++k) add_to(o[(kFour ? 4 : 2) * i + k], part[k]);
         }
         load_v();
         if (EARLY) places();

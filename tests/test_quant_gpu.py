@@ -358,6 +358,36 @@ def test_decode_many_sequences(fmt, D, H, g, block, lens):
     check_decode(fmt, 2, (0, 2), H, g, D, lens, block, seed=len(lens), max_len=800, caps=[800] * len(lens))
 
 
+@pytest.mark.parametrize("fmt,g", [("e4m3", 4), ("e4m3", 8), ("e2m1", 2), ("e2m1", 7)])
+def test_decode_sums_are_rounded(fmt, g):
+    """Values of one sign over 8192 slots in one share (512 sequences of the same blocks): sums of 512 tiles or fewer that are rounded to
+    nearest are off by 2^-24 / sqrt(3) sqrt(512) = 8e-7 in the mean square, without a sign; cut off, by 512 2^-25 = 1.5e-5 and more, all one way."""
+    B, S, H, D, n = 512, 8192, 4, 128, 1 if fmt == "e4m3" else 4
+    rng, blocks = np.random.default_rng(1), 8192 // 16
+    shape = (1, blocks, 16, H, D)
+    if fmt == "e4m3":
+        k, v = normal(shape, 1).to(torch.float8_e4m3fn), (1 + normal(shape, 2).abs().clamp(max=1)).to(torch.float8_e4m3fn)
+        K, V = k.double().cpu().numpy(), v.double().cpu().numpy()
+    else:
+        codes = [rng.integers(0, 16, shape), rng.integers(2, 8, shape)]
+        K, V = (Q.VALUES[fmt][c & 7] * np.where(c > 7, -1.0, 1.0) for c in codes)
+        k, v = (torch.from_numpy((c[..., ::2] | c[..., 1::2] << 4).astype(np.uint8)).to(DEV) for c in codes)
+    scale = torch.full((1, blocks, 16, H, n), 127, dtype=torch.uint8, device=DEV)
+    table = torch.arange(blocks, dtype=torch.int32, device=DEV).repeat(B, 1)
+    c, d, q = U.cfg_of(1, H, D), prcr.qcache_paged(k, v, scale, scale.clone(), table), normal((B, 1, H * g, D), 3)
+    out, st = torch.empty((B, 1, H * g, D), device=DEV), status_word()
+    ws = torch.empty(prcr.decode_quant_workspace_size(c, d, B, 1, H * g, S), dtype=torch.uint8, device=DEV)
+    prcr.decode_attention_quant(c, d, 0, q, torch.zeros(B, dtype=torch.int64, device=DEV), i32([S] * B), S, out, st, ws)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    for b in (0, 300, B - 1):
+        x = np.einsum("hgd,shd->hgs", U.f64(q[b, 0]).reshape(H, g, D), K.reshape(S, H, D)) / np.sqrt(D)
+        p = np.exp(x - x.max(-1, keepdims=True))
+        ref = (np.einsum("hgs,shd->hgd", p, V.reshape(S, H, D)) / p.sum(-1)[..., None]).reshape(H * g, D)
+        off = out[b, 0].double().cpu().numpy() / ref - 1
+        assert abs(off.mean()) < 2e-6 and np.abs(off).max() < 8e-6
+
+
 def test_decode_repeats():
     """The same call gives the same bits, whatever the workspace held."""
     c, lens = U.cfg_of(3, 2, 128), [900, 3, 450, 0]
