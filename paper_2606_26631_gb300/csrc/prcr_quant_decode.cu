@@ -21,7 +21,7 @@
 // two to at most 2^14) and the weights enter as two fp16 each, 22 bits; with up to four
 // heads to a group the two lie side by side in the product's eight columns, so that one
 // product takes both (four heads to a group, 16 sequences of up to 4096 slots, E4M3, 36
-// layers: 464 us, with two products 492). One fp16 would leave 2^-12 of a weight, a hundred
+// layers: 465 us, with two products 538). One fp16 would leave 2^-12 of a weight, a hundred
 // times what the rest loses.
 // Scales never touch the codes. E4M3: a key's multiplies its slot's logits, a value's goes
 // into its weight's exponent. E2M1, whose groups take every (D/32)-th quad of dims, so that
@@ -36,18 +36,18 @@
 //
 // Work is cut by what there is, not by sequence: all (sequence, layer, set of heads) units' tiles
 // in one row, one even share of it to each team of 1, 2 or 4 warps on the same slots of
-// neighbouring KV heads (whose codes are neighbouring bytes: with teams of one, E4M3 reads
-// 501 us for 465, E2M1 at 64 bytes a row 201 for 192; of two 471 and 189). A share's units that
+// neighbouring KV heads (whose codes are neighbouring bytes: teams of one take 500 us for 465, E2M1 at 64 bytes
+// a row 212 for 200; of two 471 and 199). A share's units that
 // it has whole are written at once, the parts of others joined by a second kernel.
 // A grid is one wave: 12 warps an SM, 8 at head_dim 256, which is what the registers hold (E4M3 with 8 for 12:
-// 612 us for 464; with 16, which spill: 462, but one sequence of 933 slots 31 for 27). Rows of 64 bytes go in tiles of
-// 32 slots (E2M1 191 us; of 16 223, of 64 with 8 warps 203).
+// 533 us for 465; with 16, which spill, 459 and E2M1 196 for 200, but one sequence of 933 slots 31 for 27). Rows of 64
+// bytes go in tiles of 32 slots (E2M1 200 us; of 16 242, of 64 with 8 warps 207).
 //
 // Measured (us, and bytes read per time of the 6.8 TB/s that a copy makes): E4M3, 8 KV heads of 128, 36 layers:
 // 16 sequences of up to 4096 slots 460 (91 %), one of 933 25; one layer, 32 of up to 16,384 117 (83 %);
-// E2M1, 4 KV heads of seven queries, 28 layers, 8 of up to 8192 192 (47 %); E4M3, 4 KV heads of 256, one layer, 8 of up to
-// 8000 31. E4M3 waits for memory; E2M1 for issue slots (62 % of them taken, the
-// tensor cores 35 % busy: some 470 instructions of a warp for 16 slots); what is short, for its launches.
+// E2M1, 4 KV heads of seven queries, 28 layers, 8 of up to 8192 197 (46 %); E4M3, 4 KV heads of 256, one layer, 8 of up to
+// 8000 31. E4M3 waits for memory; E2M1 for issue slots (61 % of them taken, the
+// tensor cores 33 % busy: some 470 instructions of a warp for 16 slots); what is short, for its launches.
 #include <algorithm>
 
 #include <cuda_fp16.h>
@@ -292,16 +292,16 @@ __device__ __forceinline__ Share share_of(const DecodeQuantArgs& a, uint32_t& er
 
 // RUNS: sixteen slots from a multiple of sixteen on lie slot_stride apart (a contiguous cache,
 // or blocks of a multiple of 16 slots), so that a lane's rows follow from where the first one
-// is. Otherwise lanes look a slot up each and pass its place on (taken for every cache: 501 us for
-// 464, 16 sequences of up to 4096 slots, 36 layers).
+// is. Otherwise lanes look a slot up each and pass its place on (taken for every cache: 502 us for
+// 465, 16 sequences of up to 4096 slots, 36 layers).
 template <int FMT, int D, bool PAIR, bool RUNS>
 __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kernel(const __grid_constant__ DecodeQuantArgs a) {
     using S = Shape<FMT, D>;
     constexpr bool kFour = S::kFour;
     constexpr int SUB = S::SUB, TS = S::TS, N = S::N, KW = S::KW, VW = S::VW, KP = S::KP, VP = S::VP, KS = S::KS, SW = S::SW, OWN = S::OWN;
     constexpr int P = D / 2, PITCH = D + 4, NP = PAIR ? 1 : 2, LS = PAIR ? 1 : 2;  // products for the pieces of a query or a weight, slots of a lane's logits
-    // look places up a tile earlier than they are loaded from, and ask for the rows then (E4M3: 465 us, without 531; E2M1, which
-    // does not wait for memory: 197, without 191)
+    // look places up a tile earlier than they are loaded from, and ask for the rows then (E4M3: 465 us, without 534; E2M1, which
+    // does not wait for memory: 201, without 200)
     constexpr bool EARLY = !kFour;
     extern __shared__ __align__(16) float smem[];
     const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, gid = lane >> 2, t = lane & 3;
@@ -911,8 +911,8 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 }
 
 // Joins the parts of the units that several teams shared, and writes zeros for sequences without any slot: a query
-// head's row a warp, or, where eight teams or more share a unit, a CTA (8 sequences of one layer, 4 heads of 256: 37 us, by
-// warps 44; 16 of 36 layers: 464 by warps, by CTAs 492). Eight parts are requested at once.
+// head's row a warp, or, where eight teams or more share a unit, a CTA (8 sequences of one layer, 4 heads of 256: 38 us, by
+// warps 45; 16 of 36 layers: 465 by warps, by CTAs 495). Eight parts are requested at once.
 template <int D, int TS, int WARPS>
 __global__ void __launch_bounds__(128) decode_quant_join_kernel(const __grid_constant__ DecodeQuantArgs a) {
     constexpr int NV = D / 64, AHEAD = 8;
