@@ -659,3 +659,31 @@ def test_graph_and_streams():
             K, V = (cache.values(w, b, lens[b] + 1) for w in "kv")
             ref, bar = Q.decode64(U.f64(q[b, 1]), 700, K[1], V[1])
             assert (np.abs(got[b, 1].double().cpu().numpy() - ref) <= bar).all()
+
+
+@pytest.mark.parametrize("fmt,D,g", [("e4m3", 128, 4), ("e2m1", 64, 6)])
+def test_graph_of_growing_lengths(fmt, D, g):
+    """A captured step whose lengths, positions and blocks change in place between replays: what an eager call gives."""
+    L, H, B, c = 3, 4, 40, U.cfg_of(3, 4, D)
+    cache = Q.QCache(fmt, L, H, D, [300] * B, 16, seed=4)
+    d, q, st = cache.desc(), normal((B, L, H * g, D), 3), status_word()
+    ln, pos = i32([0] * B), torch.zeros(B, dtype=torch.int64, device=DEV)
+    out = torch.zeros((B, L, H * g, D), device=DEV)
+    ws = torch.empty(prcr.decode_quant_workspace_size(c, d, B, L, H * g, 300), dtype=torch.uint8, device=DEV)
+    step = lambda out, ws: prcr.decode_attention_quant(c, d, 0, q, pos, ln, 300, out, st, ws)
+    step(out, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out, ws)
+    rng = np.random.default_rng(5)
+    for lens in ([0] * B, [1] * B, [0] * 39 + [300], rng.integers(0, 301, B), [300] * B):
+        ln.copy_(i32(lens))
+        pos.copy_(torch.from_numpy(rng.integers(0, 9000, B)))
+        cache.table.copy_(cache.table[torch.from_numpy(rng.permutation(B)).to(DEV)])  # the same blocks, of other sequences
+        out.fill_(float("nan"))
+        graph.replay()
+        want, ws2 = torch.full_like(out, float("nan")), torch.empty_like(ws)
+        step(want, ws2)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and int(st.item()) == 0 and bool((out[ln == 0] == 0).all())
