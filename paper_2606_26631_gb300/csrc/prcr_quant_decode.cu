@@ -242,15 +242,15 @@ __device__ __forceinline__ Cut cut_of(const DecodeQuantArgs& a, int64_t total) {
 // A team's share of all sequences', layers' and sets of KV heads' tiles, in that order: tiles begin .. end - 1, the
 // first one tile `tile` of `tiles` of unit `unit` (layer, set of heads) of sequence `b`.
 struct Share {
+    Cut cut;
     int64_t begin, end;
     int team, b, unit, tile, tiles, len;
 };
 template <int TS>
-__device__ __forceinline__ Share share_of(const DecodeQuantArgs& a, uint32_t& err) {
+__device__ __forceinline__ Share share_of(const DecodeQuantArgs& a, int team, uint32_t& err) {
     const int lane = threadIdx.x & 31, per_seq = a.n_layers * a.head_sets;
-    const int warp = __shfl_sync(kFull, int(blockIdx.x * kCtaWarps + (threadIdx.x >> 5)), 0);
     Share s;
-    s.team = warp / a.team;
+    s.team = team;
     uint32_t e = 0;
     int len, n = 0;
     int64_t sum = 0;
@@ -259,8 +259,8 @@ __device__ __forceinline__ Share share_of(const DecodeQuantArgs& a, uint32_t& er
         // (below 2^31 together: 2^30 slots each, sixteen to a tile, 32 of them)
         sum += __reduce_add_sync(kFull, unsigned(n));
     }
-    if (warp == 0) err |= __reduce_or_sync(kFull, e);
-    const Cut cut = cut_of(a, sum * per_seq);
+    err = __reduce_or_sync(kFull, e);
+    const Cut cut = s.cut = cut_of(a, sum * per_seq);
     s.begin = min(sum * per_seq, cut.begin_of(s.team));
     s.end = min(sum * per_seq, cut.begin_of(s.team + 1));
     s.b = s.unit = s.tile = s.tiles = s.len = 0;
@@ -312,8 +312,10 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
     uint2* q_frag = reinterpret_cast<uint2*>(mine);
     pdl_wait();
     pdl_allow();  // (the grid is one wave: CTAs that follow take the place of those that are done)
-    uint32_t err = 0;
-    const Share share = share_of<TS>(a, err);
+    uint32_t err;
+    const int cta_warp = __shfl_sync(kFull, int(blockIdx.x * kCtaWarps + (threadIdx.x >> 5)), 0);
+    const Share share = share_of<TS>(a, cta_warp / a.team, err);
+    if (cta_warp > 0) err = 0;  // (one tells of lengths and positions)
     if (share.begin >= share.end) {
         if (err) atomicOr(a.status, err);
         return;
@@ -910,45 +912,13 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
     if (err) atomicOr(a.status, err);
 }
 
-// Joins the parts of the units that several teams shared, and writes zeros for sequences without any slot: a query
-// head's row a warp, or, where eight teams or more share a unit, a CTA (8 sequences of one layer, 4 heads of 256: 38 us, by
-// warps 45; 16 of 36 layers: 465 by warps, by CTAs 495). Eight parts are requested at once.
-template <int D, int TS, int WARPS>
-__global__ void __launch_bounds__(128) decode_quant_join_kernel(const __grid_constant__ DecodeQuantArgs a) {
+// What the join kernels do to a query head's row, a warp or a CTA: parts of teams w0 .. w1, eight of them requested at once.
+template <int D, int WARPS>
+__device__ __forceinline__ void join_row(const DecodeQuantArgs& a, float* out, const Cut& cut, int64_t u0, int w0, int w1, int member, int h) {
     constexpr int NV = D / 64, AHEAD = 8;
     __shared__ float2 s_acc[WARPS][D / 2];
     __shared__ float s_top[WARPS], s_den[WARPS];
-    pdl_allow();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = a.group;
-    const int64_t row = WARPS > 1 ? int64_t(blockIdx.x) : int64_t(blockIdx.x) * 4 + warp;
-    const int per_seq = a.n_layers * a.head_sets, heads = a.n_layers * a.n_kv_heads;
-    const int64_t head = min(quotient(row, g), int64_t(a.n_seqs) * heads - 1);
-    const int h = int(row - head * g), b = int(quotient(head, heads)), lh = int(head - int64_t(b) * heads);
-    const int layer = lh / a.n_kv_heads, kh = lh - layer * a.n_kv_heads, unit = layer * a.head_sets + kh / a.team, member = kh % a.team;
-    // the sequences' tiles again, while the kernel before this one ends (lengths and positions are the call's inputs: whatever wrote
-    // them was complete before that kernel began)
-    int64_t before = 0, total = 0;
-    int n = 0;
-    for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
-        uint32_t e;
-        int len;
-        const int x = b0 + lane < a.n_seqs ? tiles_of<TS>(a, b0 + lane, len, e) : 0;
-        before += __reduce_add_sync(kFull, unsigned(b0 + lane < b ? x : 0));
-        total += __reduce_add_sync(kFull, unsigned(x));
-        n += __reduce_add_sync(kFull, unsigned(b0 + lane == b ? x : 0));
-    }
-    const Cut cut = cut_of(a, total * per_seq);
-    const int64_t u0 = before * per_seq + int64_t(unit) * n, u1 = u0 + n;
-    const int w0 = n ? cut.team_of(u0) : 0, w1 = n ? cut.team_of(u1 - 1) : 0;
-    pdl_wait();
-    if (h >= g) return;  // (past the last row)
-    float* out = a.out + row * D;
-    if (n == 0) {
-        if (WARPS == 1 || warp == 0)
-            for (int d = lane; d < D; d += 32) out[d] = 0.0f;
-        return;
-    }
-    if (w0 == w1) return;
     const int place0 = cut.begin_of(w0) != u0 ? 1 : 0;  // in the first team's parts; the others' begin with their shares
     float M = kNone, den = 0.0f;
     float2 acc[NV];
@@ -1012,6 +982,69 @@ __global__ void __launch_bounds__(128) decode_quant_join_kernel(const __grid_con
     for (int k = 0; k < NV; ++k) *reinterpret_cast<float2*>(out + 2 * lane + 64 * k) = make_float2(acc[k].x * inv, acc[k].y * inv);
 }
 
+// Joins the parts of the units that several teams shared, and writes zeros for sequences without any slot: a query
+// head's row a warp, or, where eight teams or more share a unit, a CTA (8 sequences of one layer, 4 heads of 256: 38 us, by
+// warps 45; 16 of 36 layers: 465 by warps, by CTAs 495).
+template <int D, int TS, int WARPS>
+__global__ void __launch_bounds__(128) decode_quant_join_kernel(const __grid_constant__ DecodeQuantArgs a) {
+    pdl_allow();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = a.group;
+    const int64_t row = WARPS > 1 ? int64_t(blockIdx.x) : int64_t(blockIdx.x) * 4 + warp;
+    const int per_seq = a.n_layers * a.head_sets, heads = a.n_layers * a.n_kv_heads;
+    const int64_t head = min(quotient(row, g), int64_t(a.n_seqs) * heads - 1);
+    const int h = int(row - head * g), b = int(quotient(head, heads)), lh = int(head - int64_t(b) * heads);
+    const int layer = lh / a.n_kv_heads, kh = lh - layer * a.n_kv_heads, unit = layer * a.head_sets + kh / a.team, member = kh % a.team;
+    // the sequences' tiles again, while the kernel before this one ends (lengths and positions are the call's inputs: whatever wrote
+    // them was complete before that kernel began)
+    int64_t before = 0, total = 0;
+    int n = 0;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
+        uint32_t e;
+        int len;
+        const int x = b0 + lane < a.n_seqs ? tiles_of<TS>(a, b0 + lane, len, e) : 0;
+        before += __reduce_add_sync(kFull, unsigned(b0 + lane < b ? x : 0));
+        total += __reduce_add_sync(kFull, unsigned(x));
+        n += __reduce_add_sync(kFull, unsigned(b0 + lane == b ? x : 0));
+    }
+    const Cut cut = cut_of(a, total * per_seq);
+    const int64_t u0 = before * per_seq + int64_t(unit) * n, u1 = u0 + n;
+    const int w0 = n ? cut.team_of(u0) : 0, w1 = n ? cut.team_of(u1 - 1) : 0;
+    pdl_wait();
+    if (h >= g) return;  // (past the last row)
+    float* out = a.out + row * D;
+    if (n == 0) {
+        if (WARPS == 1 || warp == 0)
+            for (int d = lane; d < D; d += 32) out[d] = 0.0f;
+        return;
+    }
+    if (w0 != w1) join_row<D, WARPS>(a, out, cut, u0, w0, w1, member, h);
+}
+
+// The same where there are twice as many rows as teams and heads of theirs, or more, so that most units are one team's: a warp for
+// a row of the unit in which a team's share begins, if that is the unit's first such share (32 sequences of 100 slots, 36 layers: 68
+// us for 80, 1024 of them 1.7 ms for 3.6; but 8 sequences, 28 layers of 4 heads 204 for 200).
+template <int D, int TS>
+__global__ void __launch_bounds__(128) decode_quant_join_teams_kernel(const __grid_constant__ DecodeQuantArgs a) {
+    pdl_allow();
+    const int lane = threadIdx.x & 31, warp = int(blockIdx.x * 4 + (threadIdx.x >> 5)), rows = a.team * a.group;
+    const int w = warp / rows, member = (warp - w * rows) / a.group, h = warp % a.group;
+    uint32_t e;
+    const Share s = share_of<TS>(a, w, e);
+    pdl_wait();
+    const int layer = s.unit / a.head_sets, kh = (s.unit - layer * a.head_sets) * a.team + member;
+    const int64_t u0 = s.begin - s.tile;
+    if (s.begin < s.end && s.tile > 0 && kh < a.n_kv_heads && s.cut.begin_of(w - 1) <= u0) {
+        const int64_t row = ((int64_t(s.b) * a.n_layers + layer) * a.n_kv_heads + kh) * a.group + h;
+        join_row<D, 1>(a, a.out + row * D, s.cut, u0, w - 1, s.cut.team_of(u0 + s.tiles - 1), member, h);
+    }
+    const int64_t all = int64_t(a.n_layers) * a.n_kv_heads * a.group * D;
+    for (int b = warp; b < a.n_seqs; b += int(gridDim.x) * 4) {
+        int len;
+        if (tiles_of<TS>(a, b, len, e)) continue;
+        for (int64_t i = lane; i < all / 4; i += 32) reinterpret_cast<float4*>(a.out + b * all)[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+}
+
 template <int FMT, int D>
 cudaError_t launch_fd(const DecodeQuantArgs& a, cudaStream_t stream) {
     using S = Shape<FMT, D>;
@@ -1025,6 +1058,8 @@ cudaError_t launch_fd(const DecodeQuantArgs& a, cudaStream_t stream) {
     if (e == cudaSuccess) e = launch_pdl(k, dim3(unsigned((a.teams * a.team + kCtaWarps - 1) / kCtaWarps)), dim3(kCtaWarps * 32), smem, stream, a);
     if (e != cudaSuccess) return e;
     const int64_t units = int64_t(a.n_seqs) * a.n_layers * a.head_sets, rows = int64_t(a.n_seqs) * a.n_layers * a.n_kv_heads * a.group;
+    const int64_t by_team = int64_t(a.teams) * a.team * a.group;
+    if (rows >= 2 * by_team) return launch_pdl(decode_quant_join_teams_kernel<D, S::TS>, dim3(unsigned((by_team + 3) / 4)), dim3(128), 0, stream, a);
     return a.teams >= 8 * units ? launch_pdl(decode_quant_join_kernel<D, S::TS, 4>, dim3(unsigned(rows)), dim3(128), 0, stream, a)
                                 : launch_pdl(decode_quant_join_kernel<D, S::TS, 1>, dim3(unsigned((rows + 3) / 4)), dim3(128), 0, stream, a);
 }

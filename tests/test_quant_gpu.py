@@ -358,6 +358,13 @@ def test_decode_many_sequences(fmt, D, H, g, block, lens):
     check_decode(fmt, 2, (0, 2), H, g, D, lens, block, seed=len(lens), max_len=800, caps=[800] * len(lens))
 
 
+@pytest.mark.parametrize("fmt,D,H,g,long", [("e4m3", 128, 2, 4, 0), ("e2m1", 64, 3, 1, 3000), ("e4m3", 256, 1, 5, 700), ("e2m1", 128, 1, 1, 0)])
+def test_decode_of_many_rows(fmt, D, H, g, long):
+    """Many more rows than warps: units that one warp has whole, units that two share, one that many do, sequences without a slot."""
+    lens = [(29 * i) % 90 if i % 7 else 0 for i in range(299)] + [long]
+    check_decode(fmt, 9, (1, 8), H, g, D, lens, 16, seed=2, max_len=3000, caps=[n + 1 for n in lens[:-1]] + [3000])
+
+
 @pytest.mark.parametrize("fmt,g", [("e4m3", 4), ("e4m3", 8), ("e2m1", 2), ("e2m1", 7)])
 def test_decode_sums_are_rounded(fmt, g):
     """Values of one sign over 8192 slots in one share (512 sequences of the same blocks): sums of 512 tiles or fewer that are rounded to
