@@ -10,10 +10,10 @@
 // a CTA looks its tokens up once and walks several layers with them, the next layer's rows on their way while one is worked on.
 //
 // Measured (us, and bytes moved per time of the 6.8 TB/s that a copy makes):
-//   append      E4M3, 4 KV heads of 128, 28 layers, prompts of 6 sequences, up to 2116 tokens each 160 (71 %);
+//   append      E4M3, 4 KV heads of 128, 28 layers, prompts of 6 sequences, up to 2116 tokens each 158 (72 %);
 //               one token of 16 sequences, 36 layers 7 (in a graph)
-//   quantise    E4M3, 8 KV heads of 128, 36 layers, up to 1024 tokens of 16 sequences 353 (92 %)
-//   dequantise  the same 343 (95 %); one layer, four prompts of up to 16,384 57 (75 %)
+//   quantise    E4M3, 8 KV heads of 128, 36 layers, up to 1024 tokens of 16 sequences 351 (92 %)
+//   dequantise  the same 344 (94 %); one layer, four prompts of up to 16,384 57 (75 %)
 //               E2M1, 4 KV heads, 28 layers, 8 of up to 4096 258 (91 %), in blocks of 7 slots
 // The casts wait for memory; the append for its keys' arithmetic (two conversions of each key's code, and a comparison).
 #include "prcr_pdl.cuh"
@@ -27,6 +27,26 @@ constexpr unsigned kFull = 0xffffffffu;
 __device__ __forceinline__ uint32_t lane_max(uint32_t x, int lanes, int step) {
     for (int o = step; o < lanes; o *= 2) x = max(x, __shfl_xor_sync(kFull, x, o));
     return x;
+}
+
+// Two floats at a time: a b, a + b, a b + c, each rounded once.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n.reg .b64 a, b;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n.reg .b64 a, b;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("{\n.reg .b64 a, b, c;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 a, a, b, c;\nmov.b64 {%0, %1}, a;\n}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
 }
 
 // The larger magnitude, or NaN.
@@ -52,7 +72,11 @@ template <int FMT, int N>
 __device__ __forceinline__ void to_units(float* x, int byte) {
     const float f = __uint_as_float(uint32_t(254 - byte) << 23);  // 2^-126 at least: byte <= 253
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] *= f;
+    for (int i = 0; i < N; i += 2) {
+        const float2 two = mul2(make_float2(x[i], x[i + 1]), make_float2(f, f));
+        x[i] = two.x;
+        x[i + 1] = two.y;
+    }
     if (byte >= QFormat<FMT>::kHighest) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -281,13 +305,14 @@ __global__ void __launch_bounds__(256, 3) append_quant_kernel(const __grid_const
         for (int u = 0; u < 8; u += 2) {
             const float2 c = *reinterpret_cast<const float2*>(turn + u), s = *reinterpret_cast<const float2*>(turn + T * P + u);
             const float2 cl = *reinterpret_cast<const float2*>(turn + 2 * T * P + u), sl = *reinterpret_cast<const float2*>(turn + 3 * T * P + u);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float p = x[u + i], q = y[u + i];
-                const float ci = i ? c.y : c.x, si = i ? s.y : s.x, cli = i ? cl.y : cl.x, sli = i ? sl.y : sl.x;
-                x[u + i] = fmaf(p, ci, -q * si) + fmaf(p, cli, -q * sli);
-                y[u + i] = fmaf(q, ci, p * si) + fmaf(q, cli, p * sli);
-            }
+            // (the products with the first parts are exact, so their difference is rounded once)
+            const float2 p = make_float2(x[u], x[u + 1]), q = make_float2(y[u], y[u + 1]), minus = make_float2(-1.0f, -1.0f);
+            const float2 dx = add2(fma2(mul2(q, s), minus, mul2(p, c)), fma2(mul2(q, sl), minus, mul2(p, cl)));
+            const float2 dy = add2(fma2(q, c, mul2(p, s)), fma2(q, cl, mul2(p, sl)));
+            x[u] = dx.x;
+            x[u + 1] = dx.y;
+            y[u] = dy.x;
+            y[u + 1] = dy.y;
         }
         int b0, b1;
         group_bytes<FMT>(max(quad_max(x), quad_max(y)), max(quad_max(x + 4), quad_max(y + 4)), a.pad, step, b0, b1);
@@ -298,7 +323,11 @@ __global__ void __launch_bounds__(256, 3) append_quant_kernel(const __grid_const
             float z[8];
             auto times = [&](const float (&w)[8], float f) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) z[i] = w[i] * f;
+                for (int i = 0; i < 8; i += 2) {
+                    const float2 two = mul2(make_float2(w[i], w[i + 1]), make_float2(f, f));
+                    z[i] = two.x;
+                    z[i + 1] = two.y;
+                }
                 return codes8<FMT>(z);
             };
             uint2 cx = times(x, kLess), cy = times(y, kLess);
