@@ -343,7 +343,13 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
         at = 0;
         if (++unit == per_seq) {
             unit = 0;
-            do n = tiles_of<TS>(a, ++b, s_end, err); while (n == 0);  // (there is one: tiles are left)
+            do {
+                if (++b == a.n_seqs) {  // (tiles are left: not unless lengths change under the call)
+                    left = 0;
+                    return;
+                }
+                n = tiles_of<TS>(a, b, s_end, err);
+            } while (n == 0);
         }
         point();
     };
@@ -906,7 +912,8 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
     if (++uu == per_seq) {
         uu = 0;
         int len;
-        do un = tiles_of<TS>(a, ++ub, len, err); while (un == 0);
+        do un = ++ub < a.n_seqs ? tiles_of<TS>(a, ub, len, err) : -1; while (un == 0);
+        if (un < 0) break;
     }
     }
     if (err) atomicOr(a.status, err);
