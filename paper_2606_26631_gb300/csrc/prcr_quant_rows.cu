@@ -59,11 +59,13 @@ __device__ __forceinline__ uint32_t quad_max(const float* x) {
     return __float_as_uint(abs_max(abs_max(x[0], x[1]), abs_max(x[2], x[3]))) & 0x7fffffffu;
 }
 
-// The largest magnitude of two words' bf16 values, as float32 bits (an infinity's or more for NaN, which
-// are the largest numbers of 15 bits).
-__device__ __forceinline__ uint32_t pair_max(uint32_t a, uint32_t b) {
-    const uint32_t m = __vmaxu2(a & 0x7fff7fffu, b & 0x7fff7fffu);
-    return max(m << 16, m & 0xffff0000u);
+// The largest magnitudes of eight bf16 values' two quads, as bf16 bits side by side (those of infinities and NaN, which
+// are the largest numbers of 15 bits, among them).
+__device__ __forceinline__ uint32_t halves_max(uint32_t a, uint32_t b) {  // of a's two, of b's two
+    return __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+}
+__device__ __forceinline__ uint32_t quads_max(const uint4& w) {
+    return halves_max(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
 }
 
 // x[0..n) times 2^(127 - byte), held below the code that is 2^128 (QFormat::kHighest); zeros in
@@ -114,15 +116,30 @@ __device__ __forceinline__ void store_rounded(uint8_t* p, const uint4& w, int by
     store_codes<FMT>(p, codes8<FMT>(x));
 }
 
-// Scales' bytes of a lane's two quads, given their largest magnitudes; lanes that share a group are `step` apart.
-template <int FMT>
-__device__ __forceinline__ void group_bytes(uint32_t a, uint32_t b, int lanes, int step, int& byte0, int& byte1) {
+// The larger ones over the lanes that share a group: E4M3 all `lanes` of a head's, E2M1 2^ROUNDS that are `step` apart.
+template <int FMT, int ROUNDS>
+__device__ __forceinline__ uint32_t group_max(uint32_t x, int lanes, int step) {
+    if (FMT == PRCR_QFMT_E4M3) return lane_max(x, lanes, 1);
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) x = max(x, __shfl_xor_sync(kFull, x, step << r));
+    return x;
+}
+template <int FMT, int ROUNDS>
+__device__ __forceinline__ uint32_t group_max2(uint32_t two, int lanes, int step) {
     if (FMT == PRCR_QFMT_E4M3) {
-        byte0 = byte1 = scale_byte<FMT>(lane_max(max(a, b), lanes, 1));
+        for (int o = 1; o < lanes; o *= 2) two = __vmaxu2(two, __shfl_xor_sync(kFull, two, o));
     } else {
-        byte0 = scale_byte<FMT>(lane_max(a, lanes, step));
-        byte1 = scale_byte<FMT>(lane_max(b, lanes, step));
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) two = __vmaxu2(two, __shfl_xor_sync(kFull, two, step << r));
     }
+    return two;
+}
+
+// Scales' bytes of two groups' largest magnitudes, of bf16 bits side by side.
+template <int FMT>
+__device__ __forceinline__ void bytes_of(uint32_t two, int& byte0, int& byte1) {
+    byte0 = scale_byte<FMT>(two << 16);
+    byte1 = scale_byte<FMT>(two & 0xffff0000u);
 }
 
 template <int FMT>
@@ -287,7 +304,9 @@ __global__ void __launch_bounds__(256, 3) append_quant_kernel(const __grid_const
                 v1 = ld_stream(sv + P);
             }
             int b0, b1;
-            group_bytes<FMT>(max(pair_max(w0.x, w0.y), pair_max(w1.x, w1.y)), max(pair_max(w0.z, w0.w), pair_max(w1.z, w1.w)), a.pad, step, b0, b1);
+            uint32_t quads = __vmaxu2(quads_max(w0), quads_max(w1));
+            if (FMT == PRCR_QFMT_E4M3) quads = halves_max(quads, quads);
+            bytes_of<FMT>(group_max2<FMT, 2>(quads, a.pad, step), b0, b1);
             if (write) {
                 store_rounded<FMT>(cv, w0, b0, b1);
                 store_rounded<FMT>(cv + half, w1, b0, b1);
@@ -315,7 +334,13 @@ __global__ void __launch_bounds__(256, 3) append_quant_kernel(const __grid_const
             y[u + 1] = dy.y;
         }
         int b0, b1;
-        group_bytes<FMT>(max(quad_max(x), quad_max(y)), max(quad_max(x + 4), quad_max(y + 4)), a.pad, step, b0, b1);
+        const uint32_t first = max(quad_max(x), quad_max(y)), second = max(quad_max(x + 4), quad_max(y + 4));
+        if (FMT == PRCR_QFMT_E4M3) {
+            b0 = b1 = scale_byte<FMT>(group_max<FMT, 0>(max(first, second), a.pad, step));
+        } else {
+            b0 = scale_byte<FMT>(group_max<FMT, 2>(first, a.pad, step));
+            b1 = scale_byte<FMT>(group_max<FMT, 2>(second, a.pad, step));
+        }
         if (write) {
             to_units8<FMT>(x, b0, b1);
             to_units8<FMT>(y, b0, b1);
@@ -461,8 +486,14 @@ __global__ void __launch_bounds__(kCastThreads, 4) quantize_kernel(const __grid_
                 const uint4 x = wk[k], y = wv[k];
                 if (l + 1 < l1) load(k);
                 int k0, k1, v0, v1;
-                group_bytes<FMT>(pair_max(x.x, x.y), pair_max(x.z, x.w), a.pad, step, k0, k1);
-                group_bytes<FMT>(pair_max(y.x, y.y), pair_max(y.z, y.w), a.pad, step, v0, v1);
+                if (FMT == PRCR_QFMT_E4M3) {  // one butterfly for both rows
+                    bytes_of<FMT>(group_max2<FMT, 0>(halves_max(quads_max(x), quads_max(y)), a.pad, step), k0, v0);
+                    k1 = k0;
+                    v1 = v0;
+                } else {
+                    bytes_of<FMT>(group_max2<FMT, 3>(quads_max(x), a.pad, step), k0, k1);
+                    bytes_of<FMT>(group_max2<FMT, 3>(quads_max(y), a.pad, step), v0, v1);
+                }
                 if (act[k]) {
                     store_rounded<FMT>(a.few.k + to[k].codes, x, k0, k1);
                     store_rounded<FMT>(a.few.v + to[k].codes, y, v0, v1);
