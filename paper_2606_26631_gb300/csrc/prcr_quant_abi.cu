@@ -74,9 +74,9 @@ int power_of_two(int n) {
 
 // Layers that a CTA walks: as few as make at most `ctas` CTAs, else `most`, evened out; as
 // many as the launch grid needs. Measured, us. Casts, 8 CTAs an SM, else 9 layers: E4M3, 36 layers of 16 sequences' up to 1024
-// slots written in 353, read in 344 (one layer 590, 422; 36 layers 364, 345); E2M1, one sequence's 933 slots 46, 35 (of 2 CTAs
-// an SM 50, 40; of 32 51, 41). Appends, 3 an SM, else 16: 28 layers of six prompts 160 (four layers 197, all 164); 24 layers
-// of two prompts' pieces 26.6 (of one CTA an SM 27.3, of 12 30.7).
+// slots written in 341, read in 343 (one layer 531, 412; 36 layers 355, 345); E2M1, one sequence's 933 slots 35, 35 (of 2 CTAs
+// an SM 37, 40; of 32 43, 42). Appends, 3 an SM, else 16: 28 layers of six prompts 156 (four layers 191, all 158); 24 layers
+// of two prompts' pieces 24.7 (of one CTA an SM 26.6, of 12 30.7).
 int layers_per_cta(int64_t tiles, int n_layers, int64_t ctas, int most) {
     int g = 1;
     while (g < most && tiles * ((n_layers + g - 1) / g) > ctas) ++g;
@@ -139,7 +139,7 @@ int cast_setup(const prcr_rope_cfg* cfg, const prcr_cache_desc* wide, int32_t wi
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return PRCR_ECUDA;
     // A CTA takes two (reading: four) tokens of a thread's, or as much in few layers as make eight CTAs an SM, so that its look-ups
-    // weigh less (one layer of four prompts of up to 16,384 slots, E4M3: written in 84 | 71 us, read in 62 | 57).
+    // weigh less (one layer of four prompts of up to 16,384 slots, E4M3: written in 78 | 64 us, read in 62 | 56).
     int units = quantise ? 512 : 1024;
     const int most = units * 4 / n_layers;
     while (units * 2 <= most && int64_t(n_seqs) * max_count * a->lanes / (units * 2) >= int64_t(sm_count(dev)) * 8) units *= 2;

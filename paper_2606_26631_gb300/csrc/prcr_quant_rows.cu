@@ -10,9 +10,9 @@
 // a CTA looks its tokens up once and walks several layers with them, the next layer's rows on their way while one is worked on.
 //
 // Measured (us, and bytes moved per time of the 6.8 TB/s that a copy makes):
-//   append      E4M3, 4 KV heads of 128, 28 layers, prompts of 6 sequences, up to 2116 tokens each 158 (72 %);
+//   append      E4M3, 4 KV heads of 128, 28 layers, prompts of 6 sequences, up to 2116 tokens each 156 (73 %);
 //               one token of 16 sequences, 36 layers 7 (in a graph)
-//   quantise    E4M3, 8 KV heads of 128, 36 layers, up to 1024 tokens of 16 sequences 351 (92 %)
+//   quantise    E4M3, 8 KV heads of 128, 36 layers, up to 1024 tokens of 16 sequences 341 (95 %)
 //   dequantise  the same 344 (94 %); one layer, four prompts of up to 16,384 57 (75 %)
 //               E2M1, 4 KV heads, 28 layers, 8 of up to 4096 258 (91 %), in blocks of 7 slots
 // The casts wait for memory; the append for its keys' arithmetic (two conversions of each key's code, and a comparison).
@@ -442,6 +442,13 @@ __device__ __forceinline__ bool cast_rows(const CastArgs& a, int b, int tok0, Ca
     return __syncthreads_or(any);
 }
 
+// Of a cache: not by the read-only path, as this kernel may be resident while the one before it in the stream writes the rows.
+__device__ __forceinline__ uint4 ld_row(const uint16_t* p) {
+    uint4 r;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
+}
+
 template <int FMT>
 __global__ void __launch_bounds__(kCastThreads, 4) quantize_kernel(const __grid_constant__ CastArgs a) {
     __shared__ CastRow rows[kCastMaxTokens];
@@ -473,8 +480,8 @@ __global__ void __launch_bounds__(kCastThreads, 4) quantize_kernel(const __grid_
         }
         auto load = [&](int k) {
             if (act[k]) {
-                wk[k] = ld_stream(a.wide.k + from[k]);
-                wv[k] = ld_stream(a.wide.v + from[k]);
+                wk[k] = ld_row(a.wide.k + from[k]);
+                wv[k] = ld_row(a.wide.v + from[k]);
             }
             from[k] += a.wide.layer_stride;
         };
