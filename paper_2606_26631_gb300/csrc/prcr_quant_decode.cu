@@ -45,7 +45,7 @@
 //
 // Measured (us, and bytes read per time of the 6.8 TB/s that a copy makes): E4M3, 8 KV heads of 128, 36 layers:
 // 16 sequences of up to 4096 slots 452 (93 %), one of 933 22; one layer, 32 of up to 16,384 116 (84 %);
-// E2M1, 4 KV heads of seven queries, 28 layers, 8 of up to 8192 197 (46 %); E4M3, 4 KV heads of 256, one layer, 8 of up to
+// E2M1, 4 KV heads of seven queries, 28 layers, 8 of up to 8192 195 (47 %); E4M3, 4 KV heads of 256, one layer, 8 of up to
 // 8000 33. E4M3 waits for memory; E2M1 for issue slots (61 % of them taken, the
 // tensor cores 33 % busy: some 470 instructions of a warp for 16 slots); what is short, for its launches.
 #include <algorithm>

@@ -7,7 +7,8 @@
 // a butterfly over the lanes that hold it. Padding a head's lanes to a power of two
 // keeps E4M3's butterflies inside a warp.
 // What costs beside the bytes is finding them: a token's place hangs on two or three loads one after the other. So
-// a CTA looks its tokens up once and walks several layers with them, the next layer's rows on their way while one is worked on.
+// a CTA looks its tokens up once and walks several layers with them, the next layer's rows on their way while one is worked on
+// (reading back: four tokens' requested together).
 //
 // Measured (us, and bytes moved per time of the 6.8 TB/s that a copy makes):
 //   append      E4M3, 4 KV heads of 128, 28 layers, prompts of 6 sequences, up to 2116 tokens each 156 (73 %);
@@ -15,7 +16,8 @@
 //   quantise    E4M3, 8 KV heads of 128, 36 layers, up to 1024 tokens of 16 sequences 341 (95 %)
 //   dequantise  the same 344 (94 %); one layer, four prompts of up to 16,384 57 (75 %)
 //               E2M1, 4 KV heads, 28 layers, 8 of up to 4096 258 (91 %), in blocks of 7 slots
-// The casts wait for memory; the append for its keys' arithmetic (two conversions of each key's code, and a comparison).
+// The casts wait for memory (E2M1's rounding for issue slots, 78 % taken), the append as much for its keys' arithmetic: two
+// conversions of each key's code, and a comparison.
 #include "prcr_pdl.cuh"
 #include "prcr_quant.cuh"
 
@@ -23,11 +25,6 @@ namespace prcr {
 namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
-
-__device__ __forceinline__ uint32_t lane_max(uint32_t x, int lanes, int step) {
-    for (int o = step; o < lanes; o *= 2) x = max(x, __shfl_xor_sync(kFull, x, o));
-    return x;
-}
 
 // Two floats at a time: a b, a + b, a b + c, each rounded once.
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
@@ -119,7 +116,10 @@ __device__ __forceinline__ void store_rounded(uint8_t* p, const uint4& w, int by
 // The larger ones over the lanes that share a group: E4M3 all `lanes` of a head's, E2M1 2^ROUNDS that are `step` apart.
 template <int FMT, int ROUNDS>
 __device__ __forceinline__ uint32_t group_max(uint32_t x, int lanes, int step) {
-    if (FMT == PRCR_QFMT_E4M3) return lane_max(x, lanes, 1);
+    if (FMT == PRCR_QFMT_E4M3) {
+        for (int o = 1; o < lanes; o *= 2) x = max(x, __shfl_xor_sync(kFull, x, o));
+        return x;
+    }
 #pragma unroll
     for (int r = 0; r < ROUNDS; ++r) x = max(x, __shfl_xor_sync(kFull, x, step << r));
     return x;
