@@ -11,7 +11,9 @@
 // call, the rebind kernel's lookups of the rows that it prefetches: the plan
 // releases it only after its own wait, so that whatever wrote the batch is
 // done. Those values are checked against their ranges and used for nothing
-// else. A kernel whose predecessor is not one of
+// else. In the same way the join kernels of a quantised cache's decode step read
+// the call's lengths and positions: the kernel before them releases them only
+// after its own wait. A kernel whose predecessor is not one of
 // these (it never allows dependents) is launched when the predecessor
 // completes, as with a plain launch, and its wait returns at once.
 #pragma once
