@@ -157,11 +157,15 @@ __device__ __forceinline__ void store_scales(uint8_t* row, int v, int byte0, int
 //
 // Keys get the codes that are nearest to the exact rotation. Its cos and sin are pairs of floats, the first of 16
 // bits, so that a bf16 number's products with it are exact: x cos - y sin, of two such products and two small
-// ones, is off by three roundings of 2^-24 of itself, whatever cancels. Only where 2^-20 of itself would change
-// its code (once in 40,000 values) is a value computed again in float64.
+// ones, is off by three roundings of 2^-24 of itself and by 2^-28.9 of the pair's norm, which is what cos and sin are
+// off by. A value is computed again in float64 where its code would change within 2^-20 of itself and, in E4M3, 2^-18 of the
+// scale's unit more: a pair's norm is at most 448 sqrt(2) units there, so that cos and sin move a value by 2^-19.6 units at most.
+// (E2M1: by 6 sqrt(2) 2^-28.9, less than 2^-20 of the least border, a quarter.) That is one value in 40,000.
 
-// sin and cos of 2^-64 f turns, each as the sum of two floats, off by some 2^-32: Taylor's series about the nearest
-// quarter turn, the first terms' products and sums with their rounding errors (by fused multiply-adds).
+// sin and cos of 2^-64 f turns, each as the sum of two floats: Taylor's series about the nearest quarter turn, the first
+// terms' products and sums with their rounding errors (by fused multiply-adds). The terms from t^5 on are single floats, some
+// twelve roundings of the t^5 / 120 that is 2^-8.6 at an eighth of a turn: together sin and cos are off by 2^-28.9 there, by 2^-32
+// in the mean square.
 __device__ __forceinline__ void sincos_pair(uint64_t f, float2& sine, float2& cosine) {
     const uint64_t g = f + (1ull << 61);
     const int quarter = int(g >> 62);
@@ -345,35 +349,44 @@ __global__ void __launch_bounds__(256, 3) append_quant_kernel(const __grid_const
             to_units8<FMT>(x, b0, b1);
             to_units8<FMT>(y, b0, b1);
             constexpr float kLess = 1.0f - 0x1p-20f, kMore = 1.0f + 0x1p-20f;
+            // the least magnitude that a value may have (and its sign turned over in E4M3), and the largest
             float z[8];
             auto times = [&](const float (&w)[8], float f) {
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) {
-                    const float2 two = mul2(make_float2(w[i], w[i + 1]), make_float2(f, f));
-                    z[i] = two.x;
-                    z[i + 1] = two.y;
+                    const float2 two = make_float2(w[i], w[i + 1]), by = make_float2(f, f);
+                    const float2 off = make_float2(copysignf(0x1p-18f, w[i]), copysignf(0x1p-18f, w[i + 1]));
+                    const float2 end = FMT == PRCR_QFMT_E4M3 ? fma2(two, by, off) : mul2(two, by);
+                    z[i] = end.x;
+                    z[i + 1] = end.y;
                 }
                 return codes8<FMT>(z);
             };
-            uint2 cx = times(x, kLess), cy = times(y, kLess);
-            const uint2 mx = times(x, kMore), my = times(y, kMore);
-            if (cx.x != mx.x || cx.y != mx.y || cy.x != my.x || cy.y != my.y) {
+            constexpr float kLeast = FMT == PRCR_QFMT_E4M3 ? -kLess : kLess;
+            const uint2 lx = times(x, kLeast), ly = times(y, kLeast);
+            uint2 cx = times(x, kMore), cy = times(y, kMore);
+            constexpr uint32_t kMagnitudes = FMT == PRCR_QFMT_E4M3 ? 0x7f7f7f7fu : 0x77777777u;
+            const uint2 nx = make_uint2((cx.x ^ lx.x) & kMagnitudes, (cx.y ^ lx.y) & kMagnitudes);
+            const uint2 ny = make_uint2((cy.x ^ ly.x) & kMagnitudes, (cy.y ^ ly.y) & kMagnitudes);
+            if (nx.x | nx.y | ny.x | ny.y) {
                 const uint32_t wx[4] = {w0.x, w0.y, w0.z, w0.w}, wy[4] = {w1.x, w1.y, w1.z, w1.w};
                 constexpr int BITS = FMT == PRCR_QFMT_E4M3 ? 8 : 4;
+                constexpr float kTop = QFormat<FMT>::kHighestTop;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const bool second = BITS == 8 && i >= 4;
-                    const int shift = BITS * i % 32;
-                    const bool nx = ((second ? cx.y ^ mx.y : cx.x ^ mx.x) >> shift) & ((1u << BITS) - 1);
-                    const bool ny = ((second ? cy.y ^ my.y : cy.x ^ my.x) >> shift) & ((1u << BITS) - 1);
-                    if (nx || ny) {
+                    const uint32_t mask = ((1u << BITS) - 1) << (BITS * i % 32);
+                    const bool near_x = (second ? nx.y : nx.x) & mask, near_y = (second ? ny.y : ny.x) & mask;
+                    if (near_x || near_y) {
                         const float p = i & 1 ? hi_f32(wx[i / 2]) : lo_f32(wx[i / 2]), q = i & 1 ? hi_f32(wy[i / 2]) : lo_f32(wy[i / 2]);
                         const int32_t pos = a.coords[3 * int64_t(my_j) + pair_axis(v * 8 + i, a.layout, a.sec_t, a.sec_h, a.sec_w)];
-                        const int byte = i < 4 ? b0 : b1;
-                        if (byte < QFormat<FMT>::kHighest) {
-                            const float unit = __uint_as_float(uint32_t(254 - byte) << 23);
-                            if (nx) x[i] = settled(p, q, false, pos, a.turn_freq[v * 8 + i], unit);
-                            if (ny) y[i] = settled(p, q, true, pos, a.turn_freq[v * 8 + i], unit);
+                        const int byte = i < 4 ? b0 : b1;  // (not that of NaN, whose values are all 0)
+                        const float unit = __uint_as_float(uint32_t(254 - byte) << 23);
+                        if (near_x) x[i] = settled(p, q, false, pos, a.turn_freq[v * 8 + i], unit);
+                        if (near_y) y[i] = settled(p, q, true, pos, a.turn_freq[v * 8 + i], unit);
+                        if (byte >= QFormat<FMT>::kHighest) {  // held as in to_units
+                            x[i] = fminf(fmaxf(x[i], -kTop), kTop);
+                            y[i] = fminf(fmaxf(y[i], -kTop), kTop);
                         }
                     }
                 }

@@ -1,0 +1,88 @@
+"""Numbers at which the quantised cache's operators can go wrong: keys whose rotation cancels next to a border between two codes,
+groups of a value's dims that lie far below its others, logits and codes that are not finite, the longest sequences."""
+import numpy as np
+import pytest
+import torch
+
+import cache_ops_util as U
+import paper_2606_26631_gb300 as prcr
+import quant_util as Q
+from cache_ops_util import DEV, i32, normal
+
+pytestmark = pytest.mark.gpu
+
+
+def status_word():
+    return torch.zeros(1, dtype=torch.int32, device=DEV)
+
+
+# (pair, position, first, second): pairs of head_dim 128 at theta 1e6 of which one rotated value is some 2^-9 to 2^-17 of the pair's norm and
+# 2^-26 to 2^-21 units of an E4M3 scale from a border between two codes, on the side that sin and cos off by 2^-29 miss.
+NEAR_BORDERS = [
+    (12, 9876, 1.6328125, 1.75), (20, 16313, 1.984375, -1.9140625), (5, 39792, 1.828125, -1.65625), (4, 2483, 1.90625, -2.515625),
+    (24, 25524, 1.296875, 1.9375), (11, 8954, 1.2578125, -1.0859375), (6, 2567, 1.140625, 1.09375), (7, 33160, 1.140625, -1.0859375),
+    (16, 24466, 1.0546875, -1.203125), (29, 32521, 1.890625, 1.546875), (13, 11293, 1.96875, -1.6796875), (14, 27886, 1.8515625, -1.8671875),
+    (19, 23496, 1.1171875, 1.0234375), (21, 36628, 1.71875, -2.203125), (2, 23668, 1.09375, -1.359375), (22, 25664, 1.578125, 1.6640625),
+    (17, 29559, 1.0625, 0.953125), (8, 16284, 1.859375, 1.90625), (31, 34701, 1.9609375, 2.578125), (0, 39877, 1.1484375, -1.1015625),
+    (0, 6416, 1.0234375, 0.8671875), (1, 21825, 1.1796875, -1.3984375), (1, 21825, 1.3984375, 1.1796875), (11, 38900, 1.0390625, 0.98828125)]
+
+
+def append_keys(fmt, k, pos):
+    """(codes [n, H, D], scales' bytes) of keys k [n, H, D] appended at (p, p, p)."""
+    n, H, D = k.shape
+    cache = Q.QCache(fmt, 1, H, D, [n], 0, fill=0x5a)
+    out, st = i32([0]), status_word()
+    prcr.append_kv_quant(U.cfg_of(1, H, D), cache.desc(), 0, k[None].contiguous(), torch.zeros_like(k)[None], i32(np.stack([pos] * 3, 1)), i32([0, n]),
+                         i32([0]), out, st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0 and out.tolist() == [n]
+    codes, byte = cache.held("k", 0, np.arange(n))
+    return codes[0], byte[0]
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e2m1"])
+def test_append_next_to_borders(fmt):
+    """The code nearest to the exact rotation, however far a pair cancels. (The 64-bit rotation is off by 2^-38 of the pair's norm at these positions,
+    2^-28 units; the nearest of these values lies 2^-26 from its border.)"""
+    D, H = 128, 4
+    pos = np.array([c[1] for c in NEAR_BORDERS])
+    k = np.zeros((len(pos), H, D))
+    for t, (i, _, x, y) in enumerate(NEAR_BORDERS):
+        for h, e in enumerate((0, -30, 60, 127)):  # (at 2^127: those that stay below 2^128; their scale is the highest)
+            top = np.hypot(x, y) * 2.0 ** e
+            k[t, h, i], k[t, h, i + D // 2] = (x * 2.0 ** e, y * 2.0 ** e) if top < 3.38e38 else (0.0, 0.0)
+    assert np.count_nonzero(k[:, 3]) > 0
+    k = torch.from_numpy(k).float().bfloat16().to(DEV)
+    codes, byte = append_keys(fmt, k, pos)
+    ref = Q.quantize(fmt, U.rope64(U.f64(k), np.stack([pos] * 3, 1), D))
+    assert np.array_equal(byte, ref[1])
+    mag = 127 if fmt == "e4m3" else 7
+    assert np.array_equal(codes & mag, ref[0] & mag)
+    assert np.array_equal((codes > mag) & (codes & mag > 0), (ref[0] > mag) & (ref[0] & mag > 0))
+
+
+@pytest.mark.parametrize("fmt,D", [("e4m3", 128), ("e4m3", 80), ("e2m1", 64)])
+def test_append_of_pairs_that_cancel(fmt, D):
+    """Rows all of whose pairs cancel to 2^-7 of their norm and less in one value or the other. (Values that the 64-bit rotation, off by 2^-38 of the
+    norm, cannot place on a side of a border, and groups whose scale it cannot, are left out.)"""
+    n, H, P = 600, 4, D // 2
+    rng = np.random.default_rng(D)
+    pos = rng.integers(1, 40000, n)
+    ang = U.O.angles(np.stack([pos] * 3, 1).astype(np.float64), D, U.sections(D), 1e6, prcr.LAYOUT_SECTIONED)[:, None, :]
+    c, s = np.cos(ang), np.sin(ang)
+    p = rng.integers(128, 256, (n, H, P)) / 128.0 * rng.choice([-1, 1], (n, H, P))
+    which = rng.random((n, H, P)) < 0.5
+    with np.errstate(divide="ignore"):
+        q = np.clip(np.where(which, p * c / s, -p * s / c), -4, 4)
+    k = torch.from_numpy(np.concatenate([p, q], -1)).float().bfloat16().to(DEV)
+    codes, byte = append_keys(fmt, k, pos)
+    x = U.f64(k)
+    exact = U.rope64(x, np.stack([pos] * 3, 1), D)
+    pair = np.hypot(x[..., :P], x[..., P:])
+    e = 2.0 ** -36 * np.concatenate([pair, pair], -1)
+    low, high = (Q.quantize(fmt, np.abs(exact) + z * e) for z in (-1, 1))
+    sure = low[1] == high[1]
+    assert sure.mean() > 0.99 and np.array_equal(byte[sure], low[1][sure])
+    ok = sure[..., Q.groups(fmt, D)] & (low[0] == high[0])
+    mag = 127 if fmt == "e4m3" else 7
+    assert ok.mean() > 0.99 and np.array_equal((codes & mag)[ok], low[0][ok] & mag)
