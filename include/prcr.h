@@ -616,8 +616,12 @@ PRCR_API int prcr_dequantize_cache(const prcr_rope_cfg* cfg, const prcr_qcache_d
  *   out      device float32, the same shape, 16-byte aligned; must not overlap q
  *   q_pos, seq_len, max_len, status as in prcr_decode_attention; max_len at most the cache's
  *            capacity and PRCR_CACHE_MAX_LEN
- * The rotated query and the weights enter the tensor cores as two fp16 each (22 bits); codes are
- * exact there, sums, maxima and the output float32.
+ * The rotated query and the weights enter the tensor cores as two fp16 each (22 bits, but not
+ * below 2^-38 of the query's largest dim and, for each slot, 2^-36 of the head's largest weight times
+ * scale); codes are exact there, sums, maxima and the output float32. In E2M1 that holds for each
+ * group of dims by itself (2^-27 for 2^-36), except for groups whose scales are all 2^-112 or less beside
+ * larger ones. A unit (sequence, layer, KV head) with a group whose scale is 2^8 or more below its row's largest
+ * in any slot reads its slots again for each such group.
  * Limits: D in {64, 128, 256}, at most 8 query heads per KV head, n_q_heads * D <=
  * PRCR_DECODE_MAX_Q_ELEMS, and n_seqs * n_layers * n_q_heads below 2^31.
  * workspace: device, >= prcr_decode_quant_workspace_size(...) bytes, 16-byte aligned, not shared

@@ -32,7 +32,9 @@
 // for the sum, w = 2^(x + e - r + 11) for the accumulator, e the value's exponent. m and r follow the
 // largest x and x + e, but only when one is more than 2^4 past them, so that most tiles
 // rescale nothing and need no reduction over the lanes; w stays below 2^15, and what fp16 loses
-// of it is 2^-36 of the largest at most.
+// of it is 2^-36 of the largest at most. E2M1's groups of a row have one reference, so that this is of the row's largest group: a
+// group within 2^7 of that in every slot loses 2^-27 of its own largest at most. One that is not gets another pass over
+// the unit's tiles, in which its scales are the rows' (each such group as much time again; scales that differ so far are rare).
 //
 // Work is cut by what there is, not by sequence: all (sequence, layer, set of heads) units' tiles
 // in one row, one even share of it to each team of 1, 2 or 4 warps on the same slots of
@@ -63,6 +65,9 @@ constexpr float kNone = -3.0e38f;   // reference of no slot yet: below every log
 constexpr float kSlack = 4.0f;      // log2 of how far past its reference a weight may go
 constexpr float kWeightLog2 = 11.0f;
 constexpr int kCtaWarps = 4;
+// E2M1: a group is worked on once more, by itself, where its scale lies 2^8 or more below the row's largest in any slot (a difference of
+// bytes with one of these bits), unless none of its scales is above 2^-112 (no byte has one of these bits: groups of zeros).
+constexpr uint32_t kFarBelow = 0xf8, kLeastUsed = 0xf0;
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -519,25 +524,30 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
     };
 
     // the first tile is requested before the query is worked on
-    load_query(share.b, share.unit);
-    blocks();
-    places();
-    load_k();
-    load_scales();
-    load_v();
-    bool whole_tile = full;  // of the tile that is loaded
-    advance();
-    blocks();
-    if (EARLY) {
+    bool whole_tile;  // whether all slots of the tile that is loaded are there
+    auto load_first = [&]() {
+        blocks();
         places();
+        load_k();
+        load_scales();
+        load_v();
+        whole_tile = full;
         advance();
         blocks();
-    }
+        if (EARLY) {
+            places();
+            advance();
+            blocks();
+        }
+    };
+    load_query(share.b, share.unit);
+    load_first();
 
     // the unit that is attended to
     int ub = share.b, uu = share.unit, first = share.tile, un = share.tiles;
     int64_t todo = share.end - share.begin;
     bool step0 = true;  // the share's first unit
+    uint32_t again = 0;  // E2M1: groups of the unit's dims that are worked on once more, the lowest one now
     const int h0 = PAIR ? 2 * (t & 1) : 2 * t;  // this lane's heads are h0 and h0 + 1, in S^T's columns and in O^T's
     while (true) {
     const int layer = uu / a.head_sets, kh = (uu - layer * a.head_sets) * a.team + member;
@@ -552,7 +562,7 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 #pragma unroll
             for (int k = 0; k < 2; ++k)
                 if (has) sincos_turns(pos, a.turn_freq[2 * (lane + 32 * i) + k], &sn[i][k], &cs[i][k]);
-        if (!step0) load_query(ub, uu);
+        if (!step0 || (kFour && again)) load_query(ub, uu);
 #pragma unroll
         for (int h = 0; h < G; ++h) {
             if (h >= g) break;
@@ -610,6 +620,9 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
     // references: m of the sums; r, less kWeightLog2, of the accumulators
     float m[2] = {kNone, kNone}, r[2] = {kNone, kNone}, sum[2] = {0.0f, 0.0f};
     uint32_t nan_groups = 0;  // E2M1: groups of dims that a value makes NaN
+    uint32_t below[SW], used[SW];  // E2M1: bits of how far the groups' scales were below their rows' largest, and of the scales
+#pragma unroll
+    for (int i = 0; i < SW; ++i) below[i] = used[i] = 0;
 
     const int steps = int(min(int64_t(un - first), todo));
     for (int step = 0; step < steps; ++step) {
@@ -620,6 +633,12 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
 #pragma unroll
         for (int j = 0; j < OWN; ++j) {
             if constexpr (kFour) {
+                if (again) {  // all groups as if they had this one's scale
+                    const int only = __ffs(int(again)) - 1;
+                    const uint32_t byte = ((SW > 1 && only >= 4 ? vs[j][SW - 1] : vs[j][0]) >> (8 * (only & 3))) & 255;
+#pragma unroll
+                    for (int i = 0; i < SW; ++i) vs[j][i] = byte * 0x01010101u;
+                }
                 bool nan = false;
 #pragma unroll
                 for (int i = 0; i < SW; ++i) nan |= any_255(vs[j][i]);
@@ -634,6 +653,11 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
                 int top = 0;
 #pragma unroll
                 for (int i = 0; i < N; ++i) top = max(top, int((vs[j][i / 4] >> (8 * (i % 4))) & 255));
+#pragma unroll
+                for (int i = 0; i < SW; ++i) {
+                    below[i] |= uint32_t(top) * 0x01010101u - vs[j][i];
+                    used[i] |= vs[j][i];
+                }
                 // (a byte behind the bits of 2^23 is 2^23 + byte)
                 const float most = __uint_as_float(0x4b000000u + top);
                 vx[j] = most - 8388735.0f;
@@ -890,21 +914,46 @@ __global__ void __launch_bounds__(Shape<FMT, D>::kThreads, 1) decode_quant_kerne
     for (int z = 0; z < 2; ++z) {
         const int h = h0 + z;
         if (h >= g || kh >= H || (PAIR && t >= 2)) continue;
-        const float f = ex2(r[z] - m[z]) * (!whole ? 1.0f : sum[z] == 0.0f ? 0.0f : 1.0f / sum[z]);  // to the sums' reference
+        const float to_m = kFour && again && !whole ? dst[h * pitch + D] : m[z];  // (that of the part's sums, kept the first time)
+        const float f = ex2(r[z] - to_m) * (!whole ? 1.0f : sum[z] == 0.0f ? 0.0f : 1.0f / sum[z]);  // to the sums' reference
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
             const int d = kFour ? S::vdim(gid, j / 4) + 2 * (j % 4) : S::vdim(gid, j / 2) + 2 * (j % 2);
             const float to = kFour && (nan_groups >> (d / 4 % N) & 1) ? __uint_as_float(0x7fffffffu) : f;
             *reinterpret_cast<float2*>(mine + h * PITCH + d) = make_float2(o[j][z] * to, o[j][2 + z] * to);
         }
-        if (gid == 0 && !whole) *reinterpret_cast<float2*>(dst + h * pitch + D) = make_float2(m[z], sum[z]);
+        if (gid == 0 && !whole && !(kFour && again)) *reinterpret_cast<float2*>(dst + h * pitch + D) = make_float2(m[z], sum[z]);
     }
     __syncwarp();
     for (int e = lane; e < (kh < H ? g * P : 0); e += 32) {
         const int h = e / P, d = 2 * (e - h * P);
+        if (kFour && again && d / 4 % N != __ffs(int(again)) - 1) continue;
         *reinterpret_cast<float2*>(dst + h * pitch + d) = *reinterpret_cast<const float2*>(mine + h * PITCH + d);
     }
     __syncwarp();
+    if constexpr (kFour) {
+        if (again) {
+            again &= again - 1;
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint32_t low = __reduce_or_sync(kFull, below[i / 4] >> (8 * (i % 4)) & kFarBelow);
+                const uint32_t any = __reduce_or_sync(kFull, used[i / 4] >> (8 * (i % 4)) & kLeastUsed);
+                if (low && any && !(nan_groups >> i & 1)) again |= 1u << i;
+            }
+        }
+        if (again) {  // back to the unit's first tile
+            b = ub;
+            unit = uu;
+            at = first;
+            n = un;
+            left = todo;
+            tiles_of<TS>(a, b, s_end, err);
+            point();
+            load_first();
+            continue;
+        }
+    }
     todo -= steps;
     if (todo <= 0) break;
     step0 = false;

@@ -86,3 +86,87 @@ def test_append_of_pairs_that_cancel(fmt, D):
     ok = sure[..., Q.groups(fmt, D)] & (low[0] == high[0])
     mag = 127 if fmt == "e4m3" else 7
     assert ok.mean() > 0.99 and np.array_equal((codes & mag)[ok], low[0][ok] & mag)
+
+
+# ----------------------------------------------------------------------------
+# one new token: values' groups far apart
+# ----------------------------------------------------------------------------
+def decode_by_group(q, pos, K, V, byte):
+    """decode64's result and a bound that holds for each group of dims by itself: what fp16 loses of a slot's product weight, 2^-25 for each of its two
+    pieces' products and of itself, is 3 2^-29 of a group's largest one at most (groups lie less than 2^8 below their row's largest, or are
+    worked on apart; the largest of a row is 2^11 at least), of each of S slots, times a code's 6: S 2^-27 of the largest."""
+    Hq, D = q.shape
+    S, H, _ = K.shape
+    G, norm = Q.groups("e2m1", D), U.rope64(q[None], np.array([[pos] * 3]), D)[0]
+    out, bar = np.zeros((Hq, D)), np.zeros((Hq, D))
+    for j in range(D // 32):
+        ref, b = Q.decode64(q, pos, K, np.where(G == j, V, 0.0))
+        for h in range(Hq):
+            w = U.softmax64(K[:, h // (Hq // H)] @ norm[h] / np.sqrt(D))
+            b[h] += S * 2.0 ** -27 * 6 * (w * Q.scale64(byte[:, h // (Hq // H), j])).max()
+        out[:, G == j], bar[:, G == j] = ref[:, G == j], b[:, G == j]
+    return out, bar
+
+
+def spread_scales(kind, shape, rng):
+    """Bytes of values' scales, [..., groups of a row]: groups far apart in every slot, in any slot by chance, in few slots, by steps, zeros among them."""
+    n = shape[-1]
+    s = rng.integers(120, 126, shape)
+    if kind == "every slot":
+        s[..., 0] += 60
+    elif kind == "by chance":
+        s = rng.integers(20, 240, shape)
+    elif kind == "a few slots":  # in which the others' groups count for nothing beside the first, and as much as any slot's for themselves
+        s[rng.random(shape[:-1]) < 0.01, 0] += 45
+    elif kind == "steps":
+        s = s - 9 * np.arange(n)
+    elif kind == "zeros":
+        s[..., n - 1] = np.where(rng.random(shape[:-1]) < 0.5, 10, s[..., n - 1])
+        s[..., 0] = 10
+    return s.astype(np.uint8)
+
+
+@pytest.mark.parametrize("kind", ["every slot", "by chance", "a few slots", "steps", "zeros"])
+@pytest.mark.parametrize("D,H,g,block,lens,L", [(128, 2, 3, 16, [300, 0, 17], 2), (128, 3, 7, 7, [1, 140], 1), (64, 2, 8, 0, [200, 65], 2), (64, 1, 4, 5, [90], 1),
+                                               (256, 1, 8, 16, [250, 2], 1), (256, 2, 2, 4, [70], 1), (128, 4, 4, 32, [2500], 1), (128, 2, 6, 16, [40] * 700, 1)])
+def test_decode_of_groups_far_apart(D, H, g, block, lens, L, kind):
+    B, rng = len(lens), np.random.default_rng(len(lens) + D)
+    cache = Q.QCache("e2m1", L, H, D, [n + 1 for n in lens], block, seed=D + g)
+    cache.vs.copy_(torch.from_numpy(spread_scales(kind, tuple(cache.vs.shape), rng)).to(DEV))
+    if kind == "zeros":
+        cache.v[..., torch.from_numpy(Q.groups("e2m1", D)[::2] == 0).to(DEV)] = 0
+        last = torch.from_numpy(Q.groups("e2m1", D)[::2] == D // 32 - 1).to(DEV)
+        cache.v[:] = torch.where(last & (cache.vs[..., -1:] == 10), torch.zeros_like(cache.v), cache.v)
+    q, pos = normal((B, L, H * g, D), 7), rng.integers(0, 60000, B)
+    out, st = Q.run_decode(U.cfg_of(L, H, D), cache, 0, q, pos, lens, max(lens))
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    got = out.double().cpu().numpy()
+    for b in range(B) if B < 20 else (0, 1, 350, B - 1):
+        n = lens[b]
+        (K, V), byte = (cache.values(w, b, n) for w in "kv"), cache.held("v", b, np.arange(n))[1]
+        for l in range(L):
+            ref, bar = decode_by_group(U.f64(q[b, l]), int(pos[b]), K[l], V[l], byte[l]) if n else (0.0, 0.0)
+            off = np.abs(got[b, l] - ref)
+            assert (off <= bar).all(), (b, l, np.nanmax(off / (bar + 1e-300)))
+        if kind == "zeros":
+            assert (got[b][..., Q.groups("e2m1", D) == 0] == 0).all()
+
+
+def test_decode_of_groups_far_apart_and_nan():
+    """A group far below the others in a slot, another that reads as NaN: the second's dims are NaN, the first's as without it."""
+    H, g, D, n = 2, 4, 128, 100
+    cache = Q.QCache("e2m1", 1, H, D, [n], 0, seed=3)
+    cache.vs[..., 1] = 60
+    q = normal((1, 1, H * g, D), 1)
+    want, _ = Q.run_decode(U.cfg_of(1, H, D), cache, 0, q, [5], [n], n)
+    cache.vs[0, 0, 33, 1, 2] = Q.NAN
+    got, st = Q.run_decode(U.cfg_of(1, H, D), cache, 0, q, [5], [n], n)
+    hit = torch.zeros((H, g, D), dtype=torch.bool, device=DEV)
+    hit[1] = torch.from_numpy(Q.groups("e2m1", D) == 2).to(DEV)
+    hit = hit.view(H * g, D)
+    assert int(st.item()) == 0 and torch.equal(got[0, 0].isnan(), hit)
+    for j in range(4):  # the references differ, so the weights' and the sums' roundings: 2 (2^-21 + (n + 80) 2^-23) of the group's largest
+        dims = torch.from_numpy(Q.groups("e2m1", D) == j).to(DEV) & ~hit
+        off, most = (got[0, 0] - want[0, 0]).abs()[dims], want[0, 0].abs()[dims].max()
+        assert bool((off <= 5e-5 * most).all())
