@@ -261,7 +261,7 @@ __device__ __forceinline__ Share share_of(const DecodeQuantArgs& a, int team, ui
     int64_t sum = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
         n = b0 + lane < a.n_seqs ? tiles_of<TS>(a, b0 + lane, len, e) : 0;
-        // (below 2^31 together: 2^30 slots each, sixteen to a tile, 32 of them)
+        // (2^31 together at most: 2^30 slots each, sixteen to a tile, 32 of them)
         sum += __reduce_add_sync(kFull, unsigned(n));
     }
     err = __reduce_or_sync(kFull, e);
@@ -273,9 +273,9 @@ __device__ __forceinline__ Share share_of(const DecodeQuantArgs& a, int team, ui
     int64_t before = 0;  // tiles of a unit of the sequences passed
     for (int b0 = 0; b0 < a.n_seqs; b0 += 32) {
         if (a.n_seqs > 32) n = b0 + lane < a.n_seqs ? tiles_of<TS>(a, b0 + lane, len, e) : 0;
-        int upto = n;
+        uint32_t upto = uint32_t(n);  // (2^31 at most, as above)
         for (int k = 1; k < 32; k *= 2) {
-            const int x = __shfl_up_sync(kFull, upto, k);
+            const uint32_t x = __shfl_up_sync(kFull, upto, k);
             if (lane >= k) upto += x;
         }
         const uint32_t behind = __ballot_sync(kFull, (before + upto) * per_seq > s.begin);
@@ -284,7 +284,7 @@ __device__ __forceinline__ Share share_of(const DecodeQuantArgs& a, int team, ui
             s.b = b0 + at;
             s.tiles = __shfl_sync(kFull, n, at);
             s.len = __shfl_sync(kFull, len, at);
-            before += __shfl_sync(kFull, upto, at) - s.tiles;
+            before += int64_t(__shfl_sync(kFull, upto, at)) - s.tiles;
             break;
         }
         before += __shfl_sync(kFull, upto, 31);

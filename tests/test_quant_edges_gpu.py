@@ -170,3 +170,22 @@ def test_decode_of_groups_far_apart_and_nan():
         dims = torch.from_numpy(Q.groups("e2m1", D) == j).to(DEV) & ~hit
         off, most = (got[0, 0] - want[0, 0]).abs()[dims], want[0, 0].abs()[dims].max()
         assert bool((off <= 5e-5 * most).all())
+
+
+def test_decode_of_the_longest_sequences():
+    """32 sequences of 2^30 slots, 2^31 tiles together: blocks of their own that their tables repeat, all values of sequence b's 2^(b - 16). (Keys are
+    zeros, so that weights are one and the parts' sums exact up to 2^24 times their unit; joining 58 parts rounds twice 61 times: 2^-17.)"""
+    B, S, block, H, D = 32, 1 << 30, 4096, 1, 128
+    k = torch.zeros((1, B, block, H, D), dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn)
+    v = torch.full((1, B, block, H, D), 1.0, device=DEV).to(torch.float8_e4m3fn)
+    ks = torch.full((1, B, block, H, 1), 127, dtype=torch.uint8, device=DEV)
+    vs = (torch.arange(B, device=DEV) + 111).to(torch.uint8).view(1, B, 1, 1, 1).expand(1, B, block, H, 1).contiguous()
+    table = torch.arange(B, dtype=torch.int32, device=DEV).view(B, 1).expand(B, S // block).contiguous()
+    c, d, q = U.cfg_of(1, H, D), prcr.qcache_paged(k, v, ks, vs, table), normal((B, 1, 1, D), 1)
+    out, st = torch.full((B, 1, 1, D), float("nan"), device=DEV), status_word()
+    ws = torch.empty(prcr.decode_quant_workspace_size(c, d, B, 1, 1, S), dtype=torch.uint8, device=DEV)
+    prcr.decode_attention_quant(c, d, 0, q, torch.arange(B, device=DEV), i32([S] * B), S, out, st, ws)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    want = torch.exp2(torch.arange(B, device=DEV) - 16.0).view(B, 1, 1, 1)
+    assert bool(((out - want).abs() <= 2.0 ** -17 * want).all())
