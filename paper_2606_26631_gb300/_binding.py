@@ -252,6 +252,8 @@ def cache_contiguous(k: torch.Tensor, v: torch.Tensor) -> CacheDesc:
     _bf16(k, "cache k"); _bf16(v, "cache v")
     if k.stride() != v.stride() or k.shape != v.shape:
         raise ValueError("cache k and v must have the same shape and strides")
+    if k.device != v.device:
+        raise ValueError("cache k and v must be on one device")
     d = CacheDesc()
     d.kind, d.block_size = CACHE_CONTIGUOUS, 1
     d.k, d.v = k.data_ptr(), v.data_ptr()
@@ -262,13 +264,21 @@ def cache_contiguous(k: torch.Tensor, v: torch.Tensor) -> CacheDesc:
     return d
 
 
+def _block_table(block_table: torch.Tensor, k: torch.Tensor):
+    if block_table.dtype != torch.int32 or block_table.stride(-1) != 1:
+        raise ValueError("block_table must be int32 [B, max_blocks] with contiguous rows")
+    if block_table.device != k.device:
+        raise ValueError("block_table must be on the cache's device")
+
+
 def cache_paged(k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor) -> CacheDesc:
     """k, v: [n_L, n_blocks, block_size, H, D] bf16; block_table: [B, max_blocks] int32."""
     _bf16(k, "cache k"); _bf16(v, "cache v")
     if k.stride() != v.stride() or k.shape != v.shape:
         raise ValueError("cache k and v must have the same shape and strides")
-    if block_table.dtype != torch.int32 or block_table.stride(-1) != 1:
-        raise ValueError("block_table must be int32 [B, max_blocks] with contiguous rows")
+    if k.device != v.device:
+        raise ValueError("cache k and v must be on one device")
+    _block_table(block_table, k)
     d = CacheDesc()
     d.kind, d.block_size = CACHE_PAGED, k.shape[2]
     d.k, d.v = k.data_ptr(), v.data_ptr()
@@ -298,8 +308,7 @@ def _codes(k, v, k_scale, v_scale):
     for name, t in (("codes", k), ("scales", k_scale)):
         if (t.shape[4] > 1 and t.stride(4) != 1) or (heads > 1 and t.stride(3) != t.shape[4]):
             raise ValueError(f"{name}: a slot's heads must be contiguous")
-    index = k.get_device()
-    if any(t.get_device() != index for t in (v, k_scale, v_scale)):
+    if any(t.device != k.device for t in (v, k_scale, v_scale)):
         raise ValueError("codes and scales must be on one device")
     return fmt, dim, heads
 
@@ -331,8 +340,9 @@ def qcache_paged(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scal
                  block_table: torch.Tensor) -> QCacheDesc:
     """k, v: [n_L, n_blocks, block_size, H, D] float8_e4m3fn (or D/2 uint8), scales as for
     qcache_contiguous; block_table: [B, max_blocks] int32."""
-    if block_table.dtype != torch.int32 or block_table.stride(-1) != 1:
-        raise ValueError("block_table must be int32 [B, max_blocks] with contiguous rows")
+    _block_table(block_table, k)
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, max_blocks]")
     d = _qcache(k, v, k_scale, v_scale, 0)
     d.kind, d.block_size = CACHE_PAGED, k.shape[2]
     d.layer_stride, d.block_stride, d.slot_stride = _strides(k, 5, "k")[:3]
