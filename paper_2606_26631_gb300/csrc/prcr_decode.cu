@@ -139,8 +139,8 @@ __global__ void __launch_bounds__(TEAM ? kDecodeMaxTeam * 32 : DecodeShape<D>::k
             const int hq = e / P;
             const uint16_t* qx = qb + hq * D + (e - hq * P);
             if (q16) {
-                const uint4 x4 = __ldg(reinterpret_cast<const uint4*>(qx));
-                const uint4 y4 = __ldg(reinterpret_cast<const uint4*>(qx + P));
+                const uint4 x4 = *reinterpret_cast<const uint4*>(qx);
+                const uint4 y4 = *reinterpret_cast<const uint4*>(qx + P);
                 wx[r][0] = x4.x; wx[r][1] = x4.y; wx[r][2] = x4.z; wx[r][3] = x4.w;
                 wy[r][0] = y4.x; wy[r][1] = y4.y; wy[r][2] = y4.z; wy[r][3] = y4.w;
             } else {
@@ -659,8 +659,8 @@ __global__ void __launch_bounds__(kWideWarps * 32, 2)
     const uint16_t* qb = a.q + ((int64_t(b) * a.n_layers + l) * a.n_q_heads + kh * g) * D;
     for (int e = threadIdx.x; e < g * (P / 2); e += blockDim.x) {  // two pairs per thread (4-byte loads)
         const int h = e / (P / 2), i = 2 * (e - h * (P / 2));
-        const uint32_t wx = __ldg(reinterpret_cast<const unsigned int*>(qb + h * D + i));
-        const uint32_t wy = __ldg(reinterpret_cast<const unsigned int*>(qb + h * D + i + P));
+        const uint32_t wx = *reinterpret_cast<const uint32_t*>(qb + h * D + i);
+        const uint32_t wy = *reinterpret_cast<const uint32_t*>(qb + h * D + i + P);
         const float c0 = s_cos[i], s0 = s_sin[i], c1 = s_cos[i + 1], s1 = s_sin[i + 1];
         const float x0 = lo_f32(wx), x1 = hi_f32(wx), y0 = lo_f32(wy), y1 = hi_f32(wy);
         *reinterpret_cast<float2*>(q_s + h * kWideQPitch + i) =

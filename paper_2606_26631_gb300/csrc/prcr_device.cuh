@@ -11,9 +11,11 @@
 
 namespace prcr {
 
+// Eight bf16 that are read once. Not by the read-only path: most kernels are resident while the one before them in the
+// stream, the caller's own or one of these, still writes what they will read.
 __device__ __forceinline__ uint4 ld_stream(const uint16_t* p) {
     uint4 r;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
                  : "l"(p));
     return r;

@@ -455,13 +455,6 @@ __device__ __forceinline__ bool cast_rows(const CastArgs& a, int b, int tok0, Ca
     return __syncthreads_or(any);
 }
 
-// Of a cache: not by the read-only path, as this kernel may be resident while the one before it in the stream writes the rows.
-__device__ __forceinline__ uint4 ld_row(const uint16_t* p) {
-    uint4 r;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
-    return r;
-}
-
 template <int FMT>
 __global__ void __launch_bounds__(kCastThreads, 4) quantize_kernel(const __grid_constant__ CastArgs a) {
     __shared__ CastRow rows[kCastMaxTokens];
@@ -493,8 +486,8 @@ __global__ void __launch_bounds__(kCastThreads, 4) quantize_kernel(const __grid_
         }
         auto load = [&](int k) {
             if (act[k]) {
-                wk[k] = ld_row(a.wide.k + from[k]);
-                wv[k] = ld_row(a.wide.v + from[k]);
+                wk[k] = ld_stream(a.wide.k + from[k]);
+                wv[k] = ld_stream(a.wide.v + from[k]);
             }
             from[k] += a.wide.layer_stride;
         };

@@ -581,7 +581,7 @@ __device__ __forceinline__ void cta_logits(const SelectArgs& a, const FusedLayou
         // the query rows into shared memory, the cache rows of the CTA's tokens
         // (-1: none), and the query's turn
 #pragma unroll 4
-        for (int i = tid; i < H * g * P; i += NT) q_s[(i / P) * (QP / 2) + i % P] = __ldg(q_src + i);
+        for (int i = tid; i < H * g * P; i += NT) q_s[(i / P) * (QP / 2) + i % P] = q_src[i];
         const int64_t s0 = a.img_slot0[b];
         for (int t = tid; t < nt; t += NT) {
             const int64_t slot = s0 + m_beg + t;
@@ -636,7 +636,7 @@ __device__ __forceinline__ void cta_logits(const SelectArgs& a, const FusedLayou
         // pairs are neighbours: one word of each half
         each_fragment([&](int hq, int j, int t) {
             const uint32_t* q0 = q_src + hq * P + 16 * (j / 4) + 4 * t + j % 4;
-            const uint32_t w0 = __ldg(q0), w1 = __ldg(q0 + P / 2);
+            const uint32_t w0 = *q0, w1 = q0[P / 2];
             return make_uint4(w0 << 16, w1 << 16, w0 & 0xffff0000u, w1 & 0xffff0000u);
         });
         __syncthreads();
