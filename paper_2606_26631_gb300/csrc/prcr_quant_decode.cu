@@ -1110,8 +1110,9 @@ cudaError_t launch_fd(const DecodeQuantArgs& a, cudaStream_t stream) {
     const size_t smem = size_t(kCtaWarps) * S::warp_bytes(pair, a.group);
     auto k = pair ? (runs ? decode_quant_kernel<FMT, D, true, true> : decode_quant_kernel<FMT, D, true, false>)
                   : (runs ? decode_quant_kernel<FMT, D, false, true> : decode_quant_kernel<FMT, D, false, false>);
-    cudaError_t e = smem > 40 * 1024 ? raise_smem_limit(reinterpret_cast<const void*>(k), smem) : cudaSuccess;
-    if (e == cudaSuccess) e = launch_pdl(k, dim3(unsigned((a.teams * a.team + kCtaWarps - 1) / kCtaWarps)), dim3(kCtaWarps * 32), smem, stream, a);
+    static_assert(kCtaWarps * S::warp_bytes(false, 8) <= 48 * 1024 && kCtaWarps * S::warp_bytes(true, 4) <= 48 * 1024,
+                  "a launch takes up to 48 KB as it is");
+    const cudaError_t e = launch_pdl(k, dim3(unsigned((a.teams * a.team + kCtaWarps - 1) / kCtaWarps)), dim3(kCtaWarps * 32), smem, stream, a);
     if (e != cudaSuccess) return e;
     const int64_t units = int64_t(a.n_seqs) * a.n_layers * a.head_sets, rows = int64_t(a.n_seqs) * a.n_layers * a.n_kv_heads * a.group;
     const int64_t by_team = int64_t(a.teams) * a.team * a.group;
