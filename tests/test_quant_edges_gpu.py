@@ -189,3 +189,55 @@ def test_decode_of_the_longest_sequences():
     assert int(st.item()) == 0
     want = torch.exp2(torch.arange(B, device=DEV) - 16.0).view(B, 1, 1, 1)
     assert bool(((out - want).abs() <= 2.0 ** -17 * want).all())
+
+
+# ----------------------------------------------------------------------------
+# one new token: codes and logits that are not finite
+# ----------------------------------------------------------------------------
+@pytest.mark.parametrize("code", [0x7f, 0xff])
+@pytest.mark.parametrize("D,g", [(128, 4), (64, 7), (256, 8)])
+def test_decode_nan_codes(D, g, code):
+    """E4M3's codes for NaN: in a key all of its KV head's outputs are NaN, in a value that dim's; the others as without it."""
+    H, n, slot, c = 3, 90, 41, U.cfg_of(1, 3, D)
+    q, base = normal((1, 1, H * g, D), 3), Q.QCache("e4m3", 1, H, D, [n], 16, seed=8)
+    want, _ = Q.run_decode(c, base, 0, q, [5], [n], n)
+    for what in ("k", "v"):
+        cache = Q.QCache("e4m3", 1, H, D, [n], 16, seed=8)
+        x, w = cache.k if what == "k" else cache.v, cache.where(0, [slot])
+        rows = x[w]
+        rows[:, :, 1, 37] = code
+        x[w] = rows
+        got, st = Q.run_decode(c, cache, 0, q, [5], [n], n)
+        hit = torch.zeros((H, g, D), dtype=torch.bool, device=DEV)
+        if what == "k":
+            hit[1] = True
+        else:
+            hit[1, :, 37] = True
+        hit = hit.view(H * g, D)
+        assert int(st.item()) == 0 and torch.equal(got[0, 0].isnan(), hit)
+        assert torch.equal(got[0, 0][~hit], want[0, 0][~hit])
+
+
+@pytest.mark.parametrize("fmt,D,g,n", [("e4m3", 128, 1, 70), ("e4m3", 64, 8, 2000), ("e2m1", 128, 7, 70), ("e2m1", 64, 2, 2000), ("e2m1", 256, 1, 33)])
+def test_decode_logits_beyond_float32(fmt, D, g, n):
+    """A logit of minus infinity has no weight and the other slots have theirs; where all of a head's are, its outputs are zeros; one of plus
+    infinity makes them NaN. (Queries are ones at position 0, keys -1 or 1 in every dim times 2^127.)"""
+    H, c, minus, plus = 1, U.cfg_of(1, 1, D), 0xb8 if fmt == "e4m3" else 0xaa, 0x38 if fmt == "e4m3" else 0x22
+    q = torch.ones((1, 1, g, D), dtype=torch.bfloat16, device=DEV)
+    hit = [0, 3, n // 2, n - 1]
+
+    def run(at, code):
+        cache = Q.QCache(fmt, 1, H, D, [n], 16, seed=n)
+        w = cache.where(0, at)
+        cache.k[w], cache.ks[w] = code, 254
+        out, st = Q.run_decode(c, cache, 0, q, [0], [n], n)
+        assert int(st.item()) == 0
+        return cache, out[0, 0].double().cpu().numpy()
+
+    cache, got = run(hit, minus)
+    left = np.setdiff1d(np.arange(n), hit)
+    K, V = (Q.stand_for(fmt, *cache.held(w, 0, left))[0] for w in "kv")
+    ref, bar = Q.decode64(U.f64(q[0, 0]), 0, K, V)
+    assert (np.abs(got - ref) <= bar).all()
+    assert (run(np.arange(n), minus)[1] == 0).all()
+    assert np.isnan(run([hit[2]], plus)[1]).all()
