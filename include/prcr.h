@@ -589,7 +589,7 @@ PRCR_API int prcr_append_kv_quant(const prcr_rope_cfg* cfg, const prcr_qcache_de
  * count[b] and j < n_layers, keys and values alike.
  * prcr_dequantize_cache - the same slots back, as bf16, which holds them exactly (for
  * prcr_chunk_attention, prcr_select_topk_cached, prcr_accumulate_weights or prcr_evict). Scales
- * that no call here writes (below 10) may make values that bf16 does not hold: they are rounded.
+ * that no call here writes (below 10, above 247 in E4M3 or 253 in E2M1) may make values that bf16 does not hold: they are rounded.
  *   src_begin, dst_begin, count   device int32 [n_seqs]
  *   max_count                     >= every count: a host bound, at most PRCR_CACHE_MAX_LEN
  * Any head_dim that the format has; n_seqs at most 65535. A count that is negative or above
@@ -630,7 +630,8 @@ PRCR_API int prcr_dequantize_cache(const prcr_rope_cfg* cfg, const prcr_qcache_d
  * with less of them. The same call gives the same bits; calls with other sequences, layers or max_len
  * may sum in another order.
  * Status bits and what is left out are prcr_decode_attention's (slots past max_len are left
- * out); a sequence that reads no slot gets zeros, with max_len 0 all of them.       */
+ * out); a sequence that reads no slot gets zeros, with max_len 0 all of them. A logit that float32 does not hold (2^87 and
+ * more may count as such) has no weight if it is negative, as there, and makes its head NaN if it is positive. */
 PRCR_API size_t prcr_decode_quant_workspace_size(const prcr_rope_cfg* cfg, int32_t format,
                                                  int32_t n_seqs, int32_t n_layers,
                                                  int32_t n_q_heads, int64_t max_len);

@@ -75,8 +75,8 @@ int power_of_two(int n) {
 // Layers that a CTA walks: as few as make at most `ctas` CTAs, else `most`, evened out; as
 // many as the launch grid needs. Measured, us. Casts, 8 CTAs an SM, else 9 layers: E4M3, 36 layers of 16 sequences' up to 1024
 // slots written in 341, read in 343 (one layer 531, 412; 36 layers 355, 345); E2M1, one sequence's 933 slots 35, 35 (of 2 CTAs
-// an SM 37, 40; of 32 43, 42). Appends, 3 an SM, else 16: 28 layers of six prompts 156 (four layers 191, all 158); 24 layers
-// of two prompts' pieces 24.7 (of one CTA an SM 26.6, of 12 30.7).
+// an SM 37, 40; of 32 43, 42). Appends, 3 an SM, else 16: 28 layers of six prompts 158 (four layers 197, all 160); 24 layers
+// of two prompts' pieces 26.5 (of one CTA an SM the same, of 12 30.8).
 int layers_per_cta(int64_t tiles, int n_layers, int64_t ctas, int most) {
     int g = 1;
     while (g < most && tiles * ((n_layers + g - 1) / g) > ctas) ++g;

@@ -46,10 +46,11 @@
 // bytes go in tiles of 32 slots (E2M1 200 us; of 16 242, of 64 with 8 warps 207).
 //
 // Measured (us, and bytes read per time of the 6.8 TB/s that a copy makes): E4M3, 8 KV heads of 128, 36 layers:
-// 16 sequences of up to 4096 slots 452 (93 %), one of 933 22; one layer, 32 of up to 16,384 116 (84 %);
-// E2M1, 4 KV heads of seven queries, 28 layers, 8 of up to 8192 195 (47 %); E4M3, 4 KV heads of 256, one layer, 8 of up to
+// 16 sequences of up to 4096 slots 459 (92 %), one of 933 22; one layer, 32 of up to 16,384 116 (84 %);
+// E2M1, 4 KV heads of seven queries, 28 layers, 8 of up to 8192 197 (46 %); E4M3, 4 KV heads of 256, one layer, 8 of up to
 // 8000 33. E4M3 waits for memory; E2M1 for issue slots (61 % of them taken, the
-// tensor cores 33 % busy: some 470 instructions of a warp for 16 slots); what is short, for its launches.
+// tensor cores 32 % busy: some 470 instructions of a warp for 16 slots), so that it takes 0.86 of E4M3's time at the same
+// shape; head_dim 256 for latencies, at 8 warps an SM; what is short, for its launches.
 #include <algorithm>
 
 #include <cuda_fp16.h>

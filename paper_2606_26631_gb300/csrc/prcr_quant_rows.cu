@@ -11,7 +11,7 @@
 // (reading back: four tokens' requested together).
 //
 // Measured (us, and bytes moved per time of the 6.8 TB/s that a copy makes):
-//   append      E4M3, 4 KV heads of 128, 28 layers, prompts of 6 sequences, up to 2116 tokens each 156 (73 %);
+//   append      E4M3, 4 KV heads of 128, 28 layers, prompts of 6 sequences, up to 2116 tokens each 157 (72 %), E2M1 140 (68 %);
 //               one token of 16 sequences, 36 layers 7 (in a graph)
 //   quantise    E4M3, 8 KV heads of 128, 36 layers, up to 1024 tokens of 16 sequences 341 (95 %)
 //   dequantise  the same 344 (94 %); one layer, four prompts of up to 16,384 57 (75 %)
