@@ -211,6 +211,9 @@ __device__ __forceinline__ void sincos_pair(uint64_t f, float2& sine, float2& co
 // The exact a cos - b sin (second: b cos + a sin) in units of the scale, rounded to odd: any border between codes, of
 // few bits, lies on the same side of it.
 __device__ __noinline__ float settled(float a, float b, bool second, int32_t pos, uint64_t turn_freq, float unit) {
+    // At an angle of 0 (an image's first row, column or frame) a pair stays as it is, and one value in 16 of it lies on a border
+    // exactly (six prompts at t = 0, all of them computed: 3.9 ms for 0.31).
+    if (pos == 0) return (second ? b : a) * unit;
     double s, c;
     sincospi(double(int64_t(uint64_t(int64_t(pos)) * turn_freq)) * 0x1p-63, &s, &c);
     const double exact = (second ? double(b) * c + double(a) * s : double(a) * c - double(b) * s) * unit;
