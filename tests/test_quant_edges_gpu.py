@@ -132,7 +132,7 @@ def test_append_at_position_zero_takes_no_longer(fmt):
             torch.cuda.synchronize()
             ms.append(a.elapsed_time(b))
         took.append(min(ms))
-    assert took[1] < 4 * took[0], took
+    assert took[1] < 6 * took[0], took
 
 
 # ----------------------------------------------------------------------------
