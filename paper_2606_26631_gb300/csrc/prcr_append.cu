@@ -8,7 +8,7 @@
 // walks its layers with the next one's rows requested before the current
 // ones are written; the cos/sin of a token are computed once per CTA for all
 // heads and the CTA's layers. Measured: six prompts of up to 2116 tokens, 28 layers of
-// 4 heads of 128, 168 us, 6.1 TB/s (a CTA takes up to 8 layers; up to 2, 190 us: each
+// 4 heads of 128, 160 us, 6.4 TB/s (a CTA takes up to 8 layers; up to 2, 193 us: each
 // computes its tokens' angles again); one token each of 16 sequences, 36 layers of 8
 // heads, 4 us in a graph, 9 from Python, all latency.
 #include "prcr_cache.cuh"
